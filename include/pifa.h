@@ -58,7 +58,9 @@ typedef enum {
     PIFA_ERR_WRONG_DEVICE = -8, /* a handle used while another device is */
                                 /* current than the one it was created on*/
     PIFA_ERR_TOO_LARGE = -9     /* pifa_forward_noalloc: the call needs   */
-                                /* more workspace than its fixed scratch */
+                                /* more workspace than its fixed scratch; */
+                                /* q4_layer_norm_forward: than it has     */
+                                /* while its stream is being captured     */
 } pifa_status;
 
 /* Layer shape: W is d_out x d_in with rank r, 1 <= r <= min(d_in, d_out)
@@ -301,6 +303,140 @@ pifa_status lowrank_layer_forward(lowrank_handle h, const void* X, void* Y, int6
                                   void* stream);
 pifa_status lowrank_layer_reserve(lowrank_handle h, int64_t max_M);
 pifa_status lowrank_layer_destroy(lowrank_handle h);
+
+/*
+ * Root-mean-square norm of the rows a layer reads, with the residual's
+ * addition:
+ *   H = X + R,   rho_m = (mean_k H[m,k]^2 + eps)^-1/2,   Y[m,k] = H[m,k] rho_m gain[k]
+ *   X     device, M x d, dtype.
+ *   R     device, M x d, dtype, or NULL (H = X).
+ *   gain  device, d, dtype, or NULL (ones).
+ *   eps   positive and finite.
+ *   H     device, M x d, dtype, or NULL (not stored).
+ *   Y     device, M x d, dtype.
+ * Any d; no alignment is required.  Sums are fp32 (a row whose squares sum to
+ * more than 3.4e38 has rho = 0); H and Y are each rounded once, Y from the
+ * unrounded H.  H and Y may each be X or R themselves, not each other, and
+ * overlap nothing otherwise.  M = 0 returns PIFA_OK without launching.
+ * Asynchronous on `stream`; no workspace.
+ */
+pifa_status rms_norm_forward(const void* X, const void* R, const void* gain, float eps, void* H, void* Y,
+                             int64_t M, int64_t d, pifa_dtype dtype, void* stream);
+
+/*
+ * The same norm with rows in 8 bits, as q4_layer_forward_e4m3 reads them:
+ *   scale[m] = max(max_k |Y[m,k]| / 448, 2^-126),   Q[m,k] = e4m3(Y[m,k] / scale[m])
+ * (OCP e4m3, rounded to nearest even from fp32): Q stands for Q[m,k] scale[m].
+ *   Q      device, M x d bytes.   scale  device, M, fp32.
+ * X, R, gain, eps, H and dtype as for rms_norm_forward.  A NaN in a row, or
+ * an infinity in X + R, makes the row's scale NaN.  Q and scale overlap nothing.
+ */
+pifa_status rms_norm_forward_e4m3(const void* X, const void* R, const void* gain, float eps, void* H,
+                                  uint8_t* Q, float* scale, int64_t M, int64_t d, pifa_dtype dtype,
+                                  void* stream);
+
+/*
+ * Gradients of rms_norm_forward.  With u = gain dY (element by element) and
+ * rho as above, of the stored H:
+ *   dX[m,k] = rho u[m,k] - rho^3 H[m,k] mean_j(u[m,j] H[m,j]) + dR[m,k],
+ *   dgain[k] = sum_m dY[m,k] H[m,k] rho_m.
+ *   H     device, M x d, dtype: the forward's H (its X if it had no R).
+ *   gain  device, d, dtype, or NULL (ones).
+ *   dY    device, M x d, dtype.
+ *   dR    device, M x d, dtype, or NULL: the gradient that reaches H beside
+ *         the norm (through the residual stream).
+ *   dX    device, M x d, dtype, or NULL to skip: the gradient of X, and of R.
+ *         May be H, dY or dR itself.
+ *   dgain device, d, fp32 (overwritten), or NULL to skip.
+ *   work  device, at least rms_norm_backward_bytes(M, d) bytes, 4-byte
+ *         aligned (may be NULL where that is 0 or dgain is NULL); it keeps
+ *         nothing between calls, and calls that may overlap need one each.
+ * dgain's sums over the rows are fp32 in a fixed order (two calls give the same
+ * bits).  M = 0 zeroes dgain.  Asynchronous on `stream`.
+ */
+pifa_status rms_norm_backward(const void* H, const void* gain, const void* dY, const void* dR, float eps,
+                              void* dX, float* dgain, int64_t M, int64_t d, pifa_dtype dtype, void* work,
+                              size_t work_bytes, void* stream);
+
+/* Workspace of rms_norm_backward for M rows of d (partial sums of dgain); 0
+ * for sizes it does not take. */
+size_t rms_norm_backward_bytes(int64_t M, int64_t d);
+
+/*
+ * Layers with 4-bit weights, Y = X W^T with
+ *   W[n,k] = e2m1(code[n,k]) * 2^(scale[n, k / 32] - 127),
+ * the OCP microscaling format: a code is a sign bit above the index into
+ * {0, 0.5, 1, 1.5, 2, 3, 4, 6}, 32 consecutive weights of a row share an 8-bit
+ * power of two, and scale 255 makes them NaN.  17/32 of a byte per weight.
+ * d_in must be a multiple of 32 (PIFA_ERR_UNSUPPORTED) and at most 2^22.
+ *
+ * (A low-rank pair U V^T keeps its accuracy in this format as two such layers
+ * in a row.  PIFA's W_p and C do not: C rebuilds the non-pivot outputs with
+ * cancellation, which multiplies the weights' rounding.)
+ *
+ * q4_layer_create quantizes W (device, d_out x d_in, dtype).  A group's scale
+ * is the power of two that puts its largest magnitude at 4 to 8 units (values
+ * past 6 become 6) or the one that puts it at 2 to 4, whichever leaves the
+ * smaller squared error; codes are rounded to nearest, ties to even.  A group
+ * with an infinity or a NaN gets scale 255.
+ * q4_layer_create_mx takes weights in the format: codes (device, d_out x
+ * d_in / 2 bytes, the lower index in the lower half of a byte) and scales
+ * (device, d_out x d_in / 32 bytes).
+ * Both copy into memory the layer owns, in matrix-instruction operand order,
+ * and synchronise the device.
+ */
+typedef struct q4_layer* q4_handle;
+pifa_status q4_layer_create(const void* W, int64_t d_in, int64_t d_out, pifa_dtype dtype, q4_handle* out);
+pifa_status q4_layer_create_mx(const uint8_t* codes, const uint8_t* scales, int64_t d_in, int64_t d_out,
+                               q4_handle* out);
+pifa_status q4_layer_destroy(q4_handle h);
+
+/* Copy the layer's codes and scales, row-major as q4_layer_create_mx takes
+ * them, to device buffers (either may be NULL).  Asynchronous on `stream`. */
+pifa_status q4_layer_read(q4_handle h, uint8_t* codes, uint8_t* scales, void* stream);
+
+/* Bytes of codes and scales a forward must read: d_out (d_in / 2 + d_in / 32). */
+size_t q4_layer_weight_bytes(q4_handle h);
+
+/*
+ * Y = X W^T.
+ *   X  device, M x d_in, bf16, 16-byte aligned.
+ *   Y  device, M x d_out, bf16; every element is written.
+ * Weights are exact in the product up to bf16's range, sums are fp32, Y is
+ * rounded once.  M = 0 returns PIFA_OK without launching.  Asynchronous on
+ * `stream`; no workspace, so calls on one handle may overlap.
+ */
+pifa_status q4_layer_forward(q4_handle h, const void* X, void* Y, int64_t M, void* stream);
+
+/*
+ * Y[m,n] = scale[m] sum_k e4m3(Q[m,k]) W[n,k]: rows in 8 bits with a scale each,
+ * as rms_norm_forward_e4m3 writes them.  The matrix instruction that multiplies
+ * them cuts each product off at 2^-14 of the largest of its group of 32; sums
+ * are fp32 beyond the group.
+ *   Q      device, M x d_in bytes, 16-byte aligned.   scale  device, M, fp32.
+ *   Y      device, M x d_out, bf16.
+ */
+pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* scale, void* Y, int64_t M,
+                                  void* stream);
+
+/*
+ * rms_norm_forward and q4_layer_forward in one call:
+ *   H = X + R,   Y = (H rho gain) W^T.
+ * X, R, gain, eps and H as for rms_norm_forward with d = d_in and bf16, but X,
+ * R and gain 16-byte aligned, and H overlapping none of X, R, gain and Y
+ * (PIFA_ERR_INVALID_ARG).  For M <= 16 it is one launch: rho scales whole rows
+ * of the product, so it is applied to the sums.  More rows are normed into the
+ * layer's workspace (M x d_in bf16) first, and calls on one handle must not
+ * overlap.  The workspace grows on demand; memory it outgrows is kept until
+ * the layer is destroyed, so graphs captured with it stay valid.  A call
+ * whose stream is being captured does not grow it (PIFA_ERR_TOO_LARGE):
+ * reserve first.
+ */
+pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, const void* gain, float eps,
+                                  void* H, void* Y, int64_t M, void* stream);
+
+/* Pre-size the workspace for q4_layer_norm_forward of up to max_M rows. */
+pifa_status q4_layer_reserve(q4_handle h, int64_t max_M);
 
 /*
  * Online Error-Accumulation-Minimization reconstruction (Sec. 4; Part 1 of

@@ -1,0 +1,481 @@
+// Root-mean-square norm of the rows a layer reads, with the residual's
+// addition, and its gradients.
+//
+//   h = x + r,   rho = (mean_k h_k^2 + eps)^-1/2,   y_k = h_k rho g_k
+//   u = g dy,    dx = rho u - h rho^3 mean_k(u_k h_k) + dr,   dg = sum over rows of dy h rho
+//
+// Both are bound by memory: every operand is read once and every result
+// written once, in 16-byte pieces ("chunks"; rows of any length and alignment,
+// the hardware takes unaligned ones), and a row stays in registers between its
+// sums and its results.  TPR threads share a row, V chunks each, dealt so that
+// neighbouring threads hold neighbouring chunks.  Sums, rho and the quotient
+// are fp32; each result is rounded once, from the unrounded h.
+#pragma once
+
+#include "common.hpp"
+
+namespace pifa {
+
+constexpr int kNormThreads = 1024;     // of a workgroup in the wide forms
+constexpr float kE4m3Max = 448.f;      // largest e4m3 value
+constexpr float kE4m3Tiny = 0x1p-126f; // smallest row scale: its inverse is finite
+
+// The full chunks of a row; the d % N elements behind them are handled one
+// per thread (norm_tail), which costs rows of whole chunks a uniform branch.
+template <typename T>
+struct NormChunk {
+    static constexpr int N = 16 / (int)sizeof(T);
+    struct __attribute__((packed, aligned(sizeof(T)))) Any {
+        u32x4 v;
+    };
+    __device__ __forceinline__ static u32x4 load(const T* row, int64_t c, int64_t full) {
+        u32x4 v = zero16();
+        if (c < full) v = reinterpret_cast<const Any*>(row + c * N)->v;
+        return v;
+    }
+    __device__ __forceinline__ static float one(u32x4 raw, int e) {
+        const uint32_t w = raw[sizeof(T) == 4 ? e : e / 2];
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w);
+        else return bf16_bits_to_f32((uint16_t)(w >> (16 * (e & 1))));
+    }
+    __device__ __forceinline__ static void floats(u32x4 raw, float (&v)[N]) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = one(raw, e);
+    }
+    __device__ __forceinline__ static void store(T* row, int64_t c, int64_t full, const float (&v)[N]) {
+        T out[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) out[e] = (T)v[e];
+        if (c < full) reinterpret_cast<Any*>(row + c * N)->v = __builtin_bit_cast(u32x4, out);
+    }
+    // N e4m3 bytes
+    __device__ __forceinline__ static void store_e4m3(uint8_t* row, int64_t c, int64_t full, const float (&v)[N]) {
+        struct __attribute__((packed, aligned(1))) Bytes {
+            uint32_t w[N / 4];
+        };
+        Bytes b;
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            const int q = __builtin_amdgcn_cvt_pk_fp8_f32(v[e], v[e + 1], 0, false);
+            b.w[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[e + 2], v[e + 3], q, true);
+        }
+        if (c < full) *reinterpret_cast<Bytes*>(row + c * N) = b;
+    }
+};
+__device__ __forceinline__ uint8_t to_e4m3(float v) {
+    return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false);
+}
+
+// a > b or NaN: a maximum that a NaN survives
+__device__ __forceinline__ float max_or_nan(float a, float b) { return (a > b || a != a) ? a : b; }
+
+// Sum (or maximum) of one value over the TPR threads of each row, in a fixed
+// order.  `red` holds one float per wave; two calls in a row need two arrays.
+template <int TPR, bool MAX = false>
+__device__ __forceinline__ float row_reduce(float v, float* red) {
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) {
+        const float o = __shfl_xor(v, s);
+        v = MAX ? max_or_nan(v, o) : v + o;
+    }
+    if constexpr (TPR > kWave) {
+        constexpr int W = TPR / kWave;
+        const int wave = threadIdx.x / kWave;
+        if ((threadIdx.x & (kWave - 1)) == 0) red[wave] = v;
+        __syncthreads();
+        const int w0 = wave / W * W;
+        v = red[w0];
+#pragma unroll
+        for (int w = 1; w < W; ++w) v = MAX ? max_or_nan(v, red[w0 + w]) : v + red[w0 + w];
+    }
+    return v;
+}
+
+template <typename T>
+struct NormFwd {
+    const T* X;
+    const T* R;     // or null
+    const T* gain;  // or null: ones
+    T* H;           // or null; may be X or R
+    T* Y;           // bf16 / fp32 rows (may be X or R), or
+    uint8_t* Q;     // e4m3 rows with
+    float* scale;   // a scale each
+    int64_t M, d;
+    float eps;
+};
+
+// ROWS rows of at most TPR * V full chunks per workgroup.
+template <typename T, bool E4M3, int TPR, int V, int ROWS>
+__global__ __launch_bounds__(TPR* ROWS) void norm_fwd(NormFwd<T> p) {
+    using C = NormChunk<T>;
+    constexpr int N = C::N;
+    __shared__ float red[2][TPR * ROWS / kWave];
+    const int t = threadIdx.x % TPR;
+    const int64_t m = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+    const bool live = m < p.M;
+    const int64_t row = (live ? m : 0) * p.d;
+    const int64_t full = live ? p.d / N : 0;  // rows past M: nothing is loaded or stored
+    const int64_t kt = p.d / N * N + t;       // this thread's element behind the full chunks
+    const bool tail = live && t < N && kt < p.d;
+
+    float h[V][N], ht = 0.f, gt = 1.f;
+    u32x4 x[V], r[V], g[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = C::load(p.X + row, t + i * TPR, full);
+    if (p.R) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) r[i] = C::load(p.R + row, t + i * TPR, full);
+    }
+    if (p.gain) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] = C::load(p.gain, t + i * TPR, full);
+    }
+    if (tail) {
+        ht = (float)p.X[row + kt];
+        if (p.R) ht += (float)p.R[row + kt];
+        if (p.gain) gt = (float)p.gain[kt];
+    }
+    float ss = ht * ht;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        C::floats(x[i], h[i]);
+        if (p.R) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) h[i][e] += C::one(r[i], e);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) ss += h[i][e] * h[i][e];
+    }
+    if (p.H) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) C::store(p.H + row, t + i * TPR, full, h[i]);
+        if (tail) p.H[row + kt] = (T)ht;
+    }
+    const float rho = rsqrtf(row_reduce<TPR>(ss, red[0]) / (float)p.d + p.eps);
+    ht *= rho * gt;
+    float amax = fabsf(ht);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            h[i][e] *= rho;
+            if (p.gain) h[i][e] *= C::one(g[i], e);
+            if constexpr (E4M3) amax = max_or_nan(fabsf(h[i][e]), amax);
+        }
+        if constexpr (!E4M3) C::store(p.Y + row, t + i * TPR, full, h[i]);
+    }
+    if constexpr (!E4M3) {
+        if (tail) p.Y[row + kt] = (T)ht;
+    } else {
+        const float s = max_or_nan(row_reduce<TPR, true>(amax, red[1]) / kE4m3Max, kE4m3Tiny);
+        const float inv = 1.f / s;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) h[i][e] *= inv;
+            C::store_e4m3(p.Q + row, t + i * TPR, full, h[i]);
+        }
+        if (tail) p.Q[row + kt] = to_e4m3(ht * inv);
+        if (live && t == 0) p.scale[m] = s;
+    }
+}
+
+// Rows too long for a workgroup's registers are read again for the results
+// (and for the maximum of 8-bit rows).  H or Y may be X or R: a thread stores
+// only elements that it alone reads, after its last read of them.
+template <typename T, bool E4M3>
+__global__ __launch_bounds__(kNormThreads) void norm_fwd_long(NormFwd<T> p) {
+    using C = NormChunk<T>;
+    constexpr int N = C::N;
+    __shared__ float red[2][kNormThreads / kWave];
+    const int64_t row = (int64_t)blockIdx.x * p.d;
+    const int64_t full = p.d / N, kt = full * N + threadIdx.x;
+    const bool tail = threadIdx.x < N && kt < p.d;
+    auto sum = [&](int64_t c, float(&h)[N]) {
+        C::floats(C::load(p.X + row, c, full), h);
+        if (p.R) {
+            const u32x4 r = C::load(p.R + row, c, full);
+#pragma unroll
+            for (int e = 0; e < N; ++e) h[e] += C::one(r, e);
+        }
+    };
+    float ht = 0.f;
+    if (tail) ht = (float)p.X[row + kt] + (p.R ? (float)p.R[row + kt] : 0.f);
+    float ss = ht * ht;
+    for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
+        float h[N];
+        sum(c, h);
+#pragma unroll
+        for (int e = 0; e < N; ++e) ss += h[e] * h[e];
+    }
+    const float rho = rsqrtf(row_reduce<kNormThreads>(ss, red[0]) / (float)p.d + p.eps);
+    if (tail && p.H) p.H[row + kt] = (T)ht;
+    ht *= rho * (tail && p.gain ? (float)p.gain[kt] : 1.f);
+    auto norm = [&](int64_t c, const float(&h)[N], float(&y)[N]) {
+        u32x4 g = zero16();
+        if (p.gain) g = C::load(p.gain, c, full);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            y[e] = h[e] * rho;
+            if (p.gain) y[e] *= C::one(g, e);
+        }
+    };
+    float inv = 1.f;
+    if constexpr (E4M3) {
+        float amax = fabsf(ht);
+        for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
+            float h[N], y[N];
+            sum(c, h);
+            norm(c, h, y);
+#pragma unroll
+            for (int e = 0; e < N; ++e) amax = max_or_nan(fabsf(y[e]), amax);
+        }
+        const float s = max_or_nan(row_reduce<kNormThreads, true>(amax, red[1]) / kE4m3Max, kE4m3Tiny);
+        inv = 1.f / s;
+        if (threadIdx.x == 0) p.scale[blockIdx.x] = s;
+        if (tail) p.Q[row + kt] = to_e4m3(ht * inv);
+    } else {
+        if (tail) p.Y[row + kt] = (T)ht;
+    }
+    for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
+        float h[N], y[N];
+        sum(c, h);
+        norm(c, h, y);
+        if (p.H) C::store(p.H + row, c, full, h);
+        if constexpr (E4M3) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] *= inv;
+            C::store_e4m3(p.Q + row, c, full, y);
+        } else {
+            C::store(p.Y + row, c, full, y);
+        }
+    }
+}
+
+template <typename T>
+struct NormBwd {
+    const T* H;
+    const T* gain;  // or null: ones
+    const T* dY;
+    const T* dR;    // or null: nothing flows in beside the norm
+    T* dX;          // or null; may be dY or dR
+    float* dgain;   // or null: per workgroup partial sums at dgain + blockIdx.x * d
+    int64_t M, d;
+    float eps;
+};
+
+// A workgroup takes ROWS rows at a time, rows ROWS * blockIdx.x + i * ROWS *
+// gridDim.x, and keeps the gain's gradient of the columns its threads hold in
+// registers over all of them; at the end the ROWS sums of a column are added
+// in LDS, so that only gridDim.x partial sums per column go to memory.  The
+// next rows' operands are loaded before the current ones' sums are reduced.
+template <typename T, int TPR, int V>
+__global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
+    using C = NormChunk<T>;
+    constexpr int N = C::N;
+    constexpr int ROWS = kNormThreads / TPR;
+    __shared__ float red[2][2][kNormThreads / kWave];
+    __shared__ float cols[ROWS > 1 ? kNormThreads * (V * N + 1) : 1];
+    const int t = threadIdx.x % TPR, rg = threadIdx.x / TPR;
+    const int64_t step = (int64_t)gridDim.x * ROWS, nfull = p.d / N, kt = nfull * N + t;
+    const bool has_tail = t < N && kt < p.d, add = p.dR && p.dX;
+
+    float dg[V][N], dgt = 0.f;
+    u32x4 g[V];
+    float gt = 1.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        g[i] = zero16();
+        if (p.gain) g[i] = C::load(p.gain, t + i * TPR, nfull);
+#pragma unroll
+        for (int e = 0; e < N; ++e) dg[i][e] = 0.f;
+    }
+    if (p.gain && has_tail) gt = (float)p.gain[kt];
+    auto gain = [&](int i, int e) { return p.gain ? C::one(g[i], e) : 1.f; };
+
+    struct Rows {
+        u32x4 h[V], y[V], r[V];
+        float ht, yt, rt;
+    };
+    auto fetch = [&](int64_t m, Rows& f) {
+        const bool live = m < p.M;
+        const int64_t row = live ? m * p.d : 0, full = live ? nfull : 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            f.h[i] = C::load(p.H + row, t + i * TPR, full);
+            f.y[i] = C::load(p.dY + row, t + i * TPR, full);
+            if (add) f.r[i] = C::load(p.dR + row, t + i * TPR, full);
+        }
+        f.ht = f.yt = f.rt = 0.f;
+        if (live && has_tail) {
+            f.ht = (float)p.H[row + kt];
+            f.yt = (float)p.dY[row + kt];
+            if (add) f.rt = (float)p.dR[row + kt];
+        }
+    };
+    const int64_t first = (int64_t)blockIdx.x * ROWS;
+    Rows cur, nxt;
+    fetch(first + rg, cur);
+    int par = 0;
+    for (int64_t m0 = first; m0 < p.M; m0 += step) {  // uniform over the workgroup
+        const int64_t m = m0 + rg;
+        const bool more = m0 + step < p.M;
+        if (more) fetch(m + step, nxt);
+        float ss = cur.ht * cur.ht, uh = gt * cur.yt * cur.ht;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float h = C::one(cur.h[i], e);
+                ss += h * h;
+                uh += gain(i, e) * C::one(cur.y[i], e) * h;
+            }
+        ss = row_reduce<TPR>(ss, red[par][0]);
+        uh = row_reduce<TPR>(uh, red[par][1]);
+        par ^= 1;
+        const float rho = rsqrtf(ss / (float)p.d + p.eps);
+        const float back = rho * rho * (uh / (float)p.d);
+        const bool live = m < p.M;
+        const int64_t row = live ? m * p.d : 0, full = live ? nfull : 0;
+        // the second reading of the row's registers converts them again: kept
+        // from the first one, the fp32 values do not fit 128 registers
+#pragma unroll
+        for (int i = 0; i < V; ++i) asm volatile("" : "+v"(cur.h[i]), "+v"(cur.y[i]), "+v"(g[i]));
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            float dx[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float h = C::one(cur.h[i], e), y = C::one(cur.y[i], e);
+                dg[i][e] += y * h * rho;
+                dx[e] = rho * (gain(i, e) * y - h * back);
+                if (add) dx[e] += C::one(cur.r[i], e);
+            }
+            if (p.dX) C::store(p.dX + row, t + i * TPR, full, dx);
+        }
+        dgt += cur.yt * cur.ht * rho;
+        if (live && has_tail && p.dX) p.dX[row + kt] = (T)(rho * (gt * cur.yt - cur.ht * back) + cur.rt);
+        if (more) cur = nxt;
+    }
+    if (!p.dgain) return;
+    float* out = p.dgain + (int64_t)blockIdx.x * p.d;
+    if constexpr (ROWS > 1) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) cols[(i * N + e) * kNormThreads + threadIdx.x] = dg[i][e];
+        cols[V * N * kNormThreads + threadIdx.x] = dgt;
+        __syncthreads();
+        // column j: element j % N of chunk j / N, or a tail element
+        for (int j = threadIdx.x; j < p.d; j += kNormThreads) {
+            const int c = j / N;
+            const float* from = c < nfull ? cols + ((c / TPR) * N + j % N) * kNormThreads + c % TPR
+                                          : cols + V * N * kNormThreads + j % N;
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < ROWS; ++w) s += from[w * TPR];
+            out[j] = s;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int64_t c = t + i * TPR;
+                if (c < nfull) out[c * N + e] = dg[i][e];
+            }
+        if (has_tail) out[kt] = dgt;
+    }
+}
+
+// Rows too long for registers: a second pass over each row, and the partial
+// sums of the gain's gradient kept in memory (each thread reads and writes
+// its own columns only).
+template <typename T>
+__global__ __launch_bounds__(kNormThreads) void norm_bwd_long(NormBwd<T> p) {
+    using C = NormChunk<T>;
+    constexpr int N = C::N;
+    __shared__ float red[2][2][kNormThreads / kWave];
+    const int64_t full = p.d / N, kt = full * N + threadIdx.x;
+    const bool tail = threadIdx.x < N && kt < p.d;
+    float* out = p.dgain ? p.dgain + (int64_t)blockIdx.x * p.d : nullptr;
+    const float gt = tail && p.gain ? (float)p.gain[kt] : 1.f;
+    auto load = [&](int64_t row, int64_t c, float(&h)[N], float(&y)[N], float(&g)[N]) {
+        C::floats(C::load(p.H + row, c, full), h);
+        C::floats(C::load(p.dY + row, c, full), y);
+        if (p.gain) C::floats(C::load(p.gain, c, full), g);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (!p.gain) g[e] = 1.f;
+    };
+    int par = 0;
+    for (int64_t m = blockIdx.x; m < p.M; m += gridDim.x, par ^= 1) {
+        const int64_t row = m * p.d;
+        const float ht = tail ? (float)p.H[row + kt] : 0.f, yt = tail ? (float)p.dY[row + kt] : 0.f;
+        float ss = ht * ht, uh = gt * yt * ht;
+        for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
+            float h[N], y[N], g[N];
+            load(row, c, h, y, g);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                ss += h[e] * h[e];
+                uh += g[e] * y[e] * h[e];
+            }
+        }
+        ss = row_reduce<kNormThreads>(ss, red[par][0]);
+        uh = row_reduce<kNormThreads>(uh, red[par][1]);
+        const float rho = rsqrtf(ss / (float)p.d + p.eps);
+        const float back = rho * rho * (uh / (float)p.d);
+        const bool begun = m != blockIdx.x;
+        for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
+            float h[N], y[N], g[N], dx[N];
+            load(row, c, h, y, g);
+            if (out) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float v = y[e] * h[e] * rho;
+                    out[c * N + e] = begun ? out[c * N + e] + v : v;
+                }
+            }
+            if (p.dX) {
+                u32x4 r = zero16();
+                if (p.dR) r = C::load(p.dR + row, c, full);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    dx[e] = rho * (g[e] * y[e] - h[e] * back);
+                    if (p.dR) dx[e] += C::one(r, e);
+                }
+                C::store(p.dX + row, c, full, dx);
+            }
+        }
+        if (tail) {
+            if (out) out[kt] = begun ? out[kt] + yt * ht * rho : yt * ht * rho;
+            if (p.dX) p.dX[row + kt] = (T)(rho * (gt * yt - ht * back) + (p.dR ? (float)p.dR[row + kt] : 0.f));
+        }
+    }
+}
+
+// dgain = the sum of P partial rows of d, in a fixed order: a workgroup of
+// 16 x 64 threads takes 64 columns.
+__global__ __launch_bounds__(kNormThreads) void norm_dgain(const float* __restrict__ part, int64_t P, int64_t d,
+                                                          float* __restrict__ dgain) {
+    __shared__ float red[kNormThreads];
+    const int64_t k = (int64_t)blockIdx.x * kWave + (threadIdx.x & (kWave - 1));
+    float s = 0.f;
+    if (k < d)
+        for (int64_t q = threadIdx.x / kWave; q < P; q += kNormThreads / kWave) s += part[q * d + k];
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x < kWave && k < d) {
+#pragma unroll
+        for (int w = 1; w < kNormThreads / kWave; ++w) s += red[w * kWave + threadIdx.x];
+        dgain[k] = s;
+    }
+}
+
+// dgain of no rows (a fill kernel: a captured graph may hold it)
+__global__ void norm_zero(float* p, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) p[i] = 0.f;
+}
+
+}  // namespace pifa

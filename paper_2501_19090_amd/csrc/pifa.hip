@@ -28,8 +28,10 @@
 #include "gemv_skinny.hpp"
 #include "layout.hpp"
 #include "linalg64.hpp"
+#include "norm.hpp"
 #include "prepack.hpp"
 #include "probe.hpp"
+#include "q4.hpp"
 
 using namespace pifa;
 
@@ -121,6 +123,11 @@ enum Site {
     kSiteCalibGather,
     kSiteCalibGram,
     kSiteCalibSolve,
+    kSiteNorm,
+    kSiteNormBwd,
+    kSiteNormDgain,
+    kSiteQ4,
+    kSiteQ4Norm,
     kSiteCount
 };
 
@@ -131,7 +138,9 @@ const char* const kSiteNames[kSiteCount] = {
     "lowrank_gemv2_tu",    "lowrank_f32",         "pifa_group_gemm1",    "pifa_group_gemm2",
     "pifa_group_gemv1",    "pifa_group_gemv2",    "pifa_bwd_gather",     "pifa_bwd_gp",
     "pifa_bwd_dx",         "pifa_bwd_dwp",        "pifa_bwd_dc",         "pifa_bwd_rows_f16",
-    "pifa_calib_gather",   "pifa_calib_gram",     "pifa_calib_solve"};
+    "pifa_calib_gather",   "pifa_calib_gram",     "pifa_calib_solve",
+    "rms_norm",            "rms_norm_bwd",        "rms_norm_dgain",      "q4_product",
+    "q4_norm_product"};
 
 struct Profiler {
     std::mutex mu;
@@ -2210,6 +2219,366 @@ pifa_status pifa_build_f64(const double* W, pifa_dims dims, double* W_p, double*
     PIFA_HIP(hipGetLastError());
     PIFA_HIP(hipStreamSynchronize(st));
     return PIFA_OK;
+}
+
+}  // extern "C"
+
+// ===================================================================== norms
+namespace {
+
+pifa_status check_norm(int64_t M, int64_t d, pifa_dtype dtype, float eps) {
+    if (!valid_dtype(dtype) || M < 0 || d < 1 || !(eps > 0.f) || std::isinf(eps)) return PIFA_ERR_INVALID_ARG;
+    if (d > INT32_MAX || M > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
+    return PIFA_OK;
+}
+
+template <typename T, bool E4M3, int TPR, int V, int ROWS>
+void norm_fwd_launch(const NormFwd<T>& p, hipStream_t st) {
+    hipLaunchKernelGGL((norm_fwd<T, E4M3, TPR, V, ROWS>), dim3((unsigned)ceil_div(p.M, ROWS)), dim3(TPR * ROWS), 0, st,
+                       p);
+}
+
+template <typename T, bool E4M3>
+hipError_t launch_norm(const NormFwd<T>& p, hipStream_t st) {
+    TimedLaunch timed(kSiteNorm, st);
+    const int64_t chunks = p.d / NormChunk<T>::N;  // full ones
+    if (chunks <= 64) norm_fwd_launch<T, E4M3, 64, 1, 4>(p, st);
+    else if (chunks <= 256) norm_fwd_launch<T, E4M3, 256, 1, 1>(p, st);
+    else if (chunks <= 512 && p.M > kCus) norm_fwd_launch<T, E4M3, 256, 2, 1>(p, st);
+    else if (chunks <= 1024 && p.M > kCus) norm_fwd_launch<T, E4M3, 256, 4, 1>(p, st);
+    else if (chunks <= 1024) norm_fwd_launch<T, E4M3, 1024, 1, 1>(p, st);
+    else if (chunks <= 2048) norm_fwd_launch<T, E4M3, 1024, 2, 1>(p, st);
+    else if (chunks <= 4096) norm_fwd_launch<T, E4M3, 1024, 4, 1>(p, st);
+    else hipLaunchKernelGGL((norm_fwd_long<T, E4M3>), dim3((unsigned)p.M), dim3(kNormThreads), 0, st, p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t norm_forward_run(const void* X, const void* R, const void* gain, float eps, void* H, void* Y, uint8_t* Q,
+                            float* scale, int64_t M, int64_t d, hipStream_t st) {
+    const NormFwd<T> p{(const T*)X, (const T*)R, (const T*)gain, (T*)H, (T*)Y, Q, scale, M, d, eps};
+    return Q ? launch_norm<T, true>(p, st) : launch_norm<T, false>(p, st);
+}
+
+// Backward: rows a workgroup takes at a time (of its 1024 threads, a row gets
+// one per full chunk); at most one workgroup per CU, so that there are few
+// partial sums of dgain.
+int64_t norm_bwd_rows(int64_t d, int64_t n) {
+    const int64_t chunks = d / n;
+    return chunks <= 64 ? 16 : chunks <= 128 ? 8 : chunks <= 256 ? 4 : chunks <= 512 ? 2 : 1;
+}
+int64_t norm_bwd_groups(int64_t M, int64_t d, int64_t n) {
+    return std::min<int64_t>(kCus, ceil_div(M, norm_bwd_rows(d, n)));
+}
+
+template <typename T>
+pifa_status norm_backward_run(const void* H, const void* gain, const void* dY, const void* dR, float eps, void* dX,
+                              float* dgain, int64_t M, int64_t d, float* work, hipStream_t st) {
+    constexpr int64_t N = NormChunk<T>::N;
+    const int64_t chunks = d / N, groups = norm_bwd_groups(M, d, N);
+    const NormBwd<T> p{(const T*)H, (const T*)gain, (const T*)dY, (const T*)dR, (T*)dX,
+                       dgain && groups > 1 ? work : dgain, M, d, eps};
+    {
+        TimedLaunch timed(kSiteNormBwd, st);
+        const dim3 grid((unsigned)groups), block(kNormThreads);
+        if (chunks <= 64) hipLaunchKernelGGL((norm_bwd<T, 64, 1>), grid, block, 0, st, p);
+        else if (chunks <= 128) hipLaunchKernelGGL((norm_bwd<T, 128, 1>), grid, block, 0, st, p);
+        else if (chunks <= 256) hipLaunchKernelGGL((norm_bwd<T, 256, 1>), grid, block, 0, st, p);
+        else if (chunks <= 512) hipLaunchKernelGGL((norm_bwd<T, 512, 1>), grid, block, 0, st, p);
+        else if (chunks <= 1024) hipLaunchKernelGGL((norm_bwd<T, 1024, 1>), grid, block, 0, st, p);
+        else if (chunks <= 2048) hipLaunchKernelGGL((norm_bwd<T, 1024, 2>), grid, block, 0, st, p);
+        else hipLaunchKernelGGL((norm_bwd_long<T>), grid, block, 0, st, p);
+        if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
+    }
+    if (dgain && groups > 1) {
+        TimedLaunch timed(kSiteNormDgain, st);
+        hipLaunchKernelGGL(norm_dgain, dim3((unsigned)ceil_div(d, kWave)), dim3(kNormThreads), 0, st, work, groups, d,
+                           dgain);
+        if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
+    }
+    return PIFA_OK;
+}
+
+}  // namespace
+
+// ===================================================================== 4-bit layers
+struct q4_layer {
+    int device = 0;
+    int64_t d_in = 0, d_out = 0;
+    uint8_t* W = nullptr;  // packed (q4.hpp)
+    // Normed rows.  Graphs captured with an outgrown buffer still point to it,
+    // so all are kept; each is at least twice the one before.
+    static constexpr int kMaxBufs = 48;
+    void* ws[kMaxBufs] = {};
+    int n_ws = 0;
+    size_t ws_bytes = 0;
+};
+
+namespace {
+
+constexpr int64_t kQ4MaxIn = 1ll << 22;  // a row's 64-row tile of X stays inside 31-bit offsets
+
+void free_q4(q4_layer* h) {
+    if (!h) return;
+    if (h->W) (void)hipFree(h->W);
+    for (int i = 0; i < h->n_ws; ++i) (void)hipFree(h->ws[i]);
+    delete h;
+}
+
+pifa_status q4_ensure(q4_layer* h, size_t need, hipStream_t st) {
+    if (need <= h->ws_bytes) return PIFA_OK;
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    PIFA_HIP(hipStreamIsCapturing(st, &cap));
+    if (cap != hipStreamCaptureStatusNone) return PIFA_ERR_TOO_LARGE;
+    if (h->n_ws == q4_layer::kMaxBufs) return PIFA_ERR_OOM;
+    need = std::max(need, 2 * h->ws_bytes);
+    void* p = nullptr;
+    if (hipMalloc(&p, need) != hipSuccess) {
+        (void)hipGetLastError();
+        return PIFA_ERR_OOM;
+    }
+    h->ws[h->n_ws++] = p;
+    h->ws_bytes = need;
+    return PIFA_OK;
+}
+
+// Allocates a layer for W of d_out x d_in; `fill` writes its packed weights.
+template <typename Fill>
+pifa_status q4_create(int64_t d_in, int64_t d_out, q4_handle* out, Fill fill) {
+    if (!out) return PIFA_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (d_in < 1 || d_out < 1) return PIFA_ERR_INVALID_ARG;
+    if (d_in % kQ4Group != 0 || d_in > kQ4MaxIn || d_out > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
+    q4_layer* h = new (std::nothrow) q4_layer();
+    if (!h) return PIFA_ERR_OOM;
+    h->d_in = d_in;
+    h->d_out = d_out;
+    pifa_status s = PIFA_OK;
+    if (hipGetDevice(&h->device) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
+        s = PIFA_ERR_HIP;
+    } else if (hipMalloc(&h->W, (size_t)q4_packed_bytes(d_out, d_in)) != hipSuccess) {
+        (void)hipGetLastError();
+        s = PIFA_ERR_OOM;
+    } else {
+        fill(h, dim3(grid_for(packed_groups(d_out) * 16 * packed_kblocks(d_in) * 4)));
+        if (hipGetLastError() != hipSuccess || hipDeviceSynchronize() != hipSuccess) s = PIFA_ERR_HIP;
+    }
+    if (s != PIFA_OK) {
+        free_q4(h);
+        return s;
+    }
+    *out = h;
+    return PIFA_OK;
+}
+
+template <int ACT, bool NORM, int MT, int NG, int WAVES, int U>
+void q4_few_launch(const Q4Args& p, hipStream_t st) {
+    hipLaunchKernelGGL((q4_few<ACT, NORM, MT, NG, WAVES, U>),
+                       dim3((unsigned)ceil_div(packed_groups(p.N), NG), (unsigned)ceil_div(p.M, 16 * MT)),
+                       dim3(WAVES * kWave), 0, st, p);
+}
+
+// Rows of one launch: grid.y counts tiles of at least 16 rows.
+constexpr int64_t kQ4MaxRows = 1 << 19;
+
+template <int ACT>
+hipError_t launch_q4(Q4Args p, hipStream_t st) {
+    const int64_t M = p.M;
+    for (int64_t m = 0; m < M; m += kQ4MaxRows) {
+        TimedLaunch timed(kSiteQ4, st);
+        Q4Args q = p;
+        q.M = std::min(kQ4MaxRows, M - m);
+        q.X = (const char*)p.X + m * p.K * (ACT == kQ4Bf16 ? 2 : 1);
+        if (p.x_scale) q.x_scale = p.x_scale + m;
+        q.Y = p.Y + m * p.N;
+        if (q.M <= 16) q4_few_launch<ACT, false, 1, 1, 8, 2>(q, st);
+        else if (q.M <= 32) q4_few_launch<ACT, false, 2, 2, 8, 1>(q, st);
+        else q4_few_launch<ACT, false, 4, 4, 8, 1>(q, st);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && x < y + nb && y < x + na;
+}
+
+}  // namespace
+
+extern "C" {
+
+pifa_status rms_norm_forward(const void* X, const void* R, const void* gain, float eps, void* H, void* Y, int64_t M,
+                             int64_t d, pifa_dtype dtype, void* stream) {
+    const pifa_status s = check_norm(M, d, dtype, eps);
+    if (s != PIFA_OK) return s;
+    if (M == 0) return PIFA_OK;
+    if (!X || !Y || H == Y) return PIFA_ERR_INVALID_ARG;
+    const hipStream_t st = as_stream(stream);
+    const hipError_t e = dtype == PIFA_BF16 ? norm_forward_run<bf16>(X, R, gain, eps, H, Y, nullptr, nullptr, M, d, st)
+                                            : norm_forward_run<float>(X, R, gain, eps, H, Y, nullptr, nullptr, M, d, st);
+    return e == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+}
+
+pifa_status rms_norm_forward_e4m3(const void* X, const void* R, const void* gain, float eps, void* H, uint8_t* Q,
+                                  float* scale, int64_t M, int64_t d, pifa_dtype dtype, void* stream) {
+    const pifa_status s = check_norm(M, d, dtype, eps);
+    if (s != PIFA_OK) return s;
+    if (M == 0) return PIFA_OK;
+    if (!X || !Q || !scale) return PIFA_ERR_INVALID_ARG;
+    const hipStream_t st = as_stream(stream);
+    const hipError_t e = dtype == PIFA_BF16 ? norm_forward_run<bf16>(X, R, gain, eps, H, nullptr, Q, scale, M, d, st)
+                                            : norm_forward_run<float>(X, R, gain, eps, H, nullptr, Q, scale, M, d, st);
+    return e == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+}
+
+size_t rms_norm_backward_bytes(int64_t M, int64_t d) {
+    if (M < 1 || d < 1 || d > INT32_MAX || M > INT32_MAX) return 0;
+    const int64_t groups = std::max(norm_bwd_groups(M, d, NormChunk<bf16>::N), norm_bwd_groups(M, d, NormChunk<float>::N));
+    return groups > 1 ? (size_t)groups * (size_t)d * sizeof(float) : 0;
+}
+
+pifa_status rms_norm_backward(const void* H, const void* gain, const void* dY, const void* dR, float eps, void* dX,
+                              float* dgain, int64_t M, int64_t d, pifa_dtype dtype, void* work, size_t work_bytes,
+                              void* stream) {
+    const pifa_status s = check_norm(M, d, dtype, eps);
+    if (s != PIFA_OK) return s;
+    const hipStream_t st = as_stream(stream);
+    if (M == 0) {
+        if (!dgain) return PIFA_OK;
+        hipLaunchKernelGGL(norm_zero, dim3(grid_for(d)), dim3(256), 0, st, dgain, d);
+        return hipGetLastError() == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+    }
+    if (!H || !dY) return PIFA_ERR_INVALID_ARG;
+    if (!dX && !dgain) return PIFA_OK;
+    if (dgain) {
+        const size_t need = rms_norm_backward_bytes(M, d);
+        if (need > 0 && (!work || work_bytes < need)) return PIFA_ERR_INVALID_ARG;
+    }
+    return dtype == PIFA_BF16 ? norm_backward_run<bf16>(H, gain, dY, dR, eps, dX, dgain, M, d, (float*)work, st)
+                              : norm_backward_run<float>(H, gain, dY, dR, eps, dX, dgain, M, d, (float*)work, st);
+}
+
+pifa_status q4_layer_create(const void* W, int64_t d_in, int64_t d_out, pifa_dtype dtype, q4_handle* out) {
+    if (out) *out = nullptr;
+    if (!W || !valid_dtype(dtype)) return PIFA_ERR_INVALID_ARG;
+    return q4_create(d_in, d_out, out, [&](q4_layer* h, dim3 grid) {
+        if (dtype == PIFA_BF16)
+            hipLaunchKernelGGL((q4_quantize<bf16>), grid, dim3(256), 0, 0, (const bf16*)W, d_out, d_in, h->W);
+        else
+            hipLaunchKernelGGL((q4_quantize<float>), grid, dim3(256), 0, 0, (const float*)W, d_out, d_in, h->W);
+    });
+}
+
+pifa_status q4_layer_create_mx(const uint8_t* codes, const uint8_t* scales, int64_t d_in, int64_t d_out,
+                               q4_handle* out) {
+    if (out) *out = nullptr;
+    if (!codes || !scales) return PIFA_ERR_INVALID_ARG;
+    return q4_create(d_in, d_out, out, [&](q4_layer* h, dim3 grid) {
+        hipLaunchKernelGGL((q4_convert<true>), grid, dim3(256), 0, 0, const_cast<uint8_t*>(codes),
+                           const_cast<uint8_t*>(scales), d_out, d_in, h->W);
+    });
+}
+
+pifa_status q4_layer_destroy(q4_handle h) {
+    if (!h) return PIFA_OK;
+    (void)hipDeviceSynchronize();
+    free_q4(h);
+    return PIFA_OK;
+}
+
+pifa_status q4_layer_read(q4_handle h, uint8_t* codes, uint8_t* scales, void* stream) {
+    if (!h) return PIFA_ERR_INVALID_ARG;
+    if (!codes && !scales) return PIFA_OK;
+    PIFA_ON_DEVICE(h->device);
+    hipLaunchKernelGGL((q4_convert<false>), dim3(grid_for(packed_groups(h->d_out) * 16 * packed_kblocks(h->d_in) * 4)),
+                       dim3(256), 0, as_stream(stream), codes, scales, h->d_out, h->d_in, h->W);
+    return hipGetLastError() == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+}
+
+size_t q4_layer_weight_bytes(q4_handle h) {
+    return h ? (size_t)h->d_out * (size_t)(h->d_in / 2 + h->d_in / kQ4Group) : 0;
+}
+
+pifa_status q4_layer_forward(q4_handle h, const void* X, void* Y, int64_t M, void* stream) {
+    if (!h || M < 0) return PIFA_ERR_INVALID_ARG;
+    if (M == 0) return PIFA_OK;
+    if (!X || !Y) return PIFA_ERR_INVALID_ARG;
+    if (M > INT32_MAX || !aligned16(X)) return PIFA_ERR_UNSUPPORTED;
+    PIFA_ON_DEVICE(h->device);
+    Q4Args p{};
+    p.W = h->W;
+    p.X = X;
+    p.Y = (bf16*)Y;
+    p.M = M;
+    p.N = h->d_out;
+    p.K = h->d_in;
+    return launch_q4<kQ4Bf16>(p, as_stream(stream)) == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+}
+
+pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* scale, void* Y, int64_t M,
+                                  void* stream) {
+    if (!h || M < 0) return PIFA_ERR_INVALID_ARG;
+    if (M == 0) return PIFA_OK;
+    if (!Q || !scale || !Y) return PIFA_ERR_INVALID_ARG;
+    if (M > INT32_MAX || !aligned16(Q)) return PIFA_ERR_UNSUPPORTED;
+    PIFA_ON_DEVICE(h->device);
+    Q4Args p{};
+    p.W = h->W;
+    p.X = Q;
+    p.x_scale = scale;
+    p.Y = (bf16*)Y;
+    p.M = M;
+    p.N = h->d_out;
+    p.K = h->d_in;
+    return launch_q4<kQ4E4m3>(p, as_stream(stream)) == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+}
+
+pifa_status q4_layer_reserve(q4_handle h, int64_t max_M) {
+    if (!h || max_M < 0) return PIFA_ERR_INVALID_ARG;
+    if (max_M > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
+    PIFA_ON_DEVICE(h->device);
+    return max_M <= kDecodeMaxM ? PIFA_OK : q4_ensure(h, (size_t)max_M * (size_t)h->d_in * 2, 0);
+}
+
+pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, const void* gain, float eps, void* H,
+                                  void* Y, int64_t M, void* stream) {
+    if (!h) return PIFA_ERR_INVALID_ARG;
+    pifa_status s = check_norm(M, h->d_in, PIFA_BF16, eps);
+    if (s != PIFA_OK) return s;
+    if (M == 0) return PIFA_OK;
+    if (!X || !Y) return PIFA_ERR_INVALID_ARG;
+    const size_t in = (size_t)M * (size_t)h->d_in * 2, out = (size_t)M * (size_t)h->d_out * 2;
+    if (overlap(H, in, X, in) || overlap(H, in, R, in) || overlap(H, in, gain, (size_t)h->d_in * 2) ||
+        overlap(H, in, Y, out))
+        return PIFA_ERR_INVALID_ARG;
+    if (!aligned16(X) || !aligned16(R) || !aligned16(gain)) return PIFA_ERR_UNSUPPORTED;
+    PIFA_ON_DEVICE(h->device);
+    const hipStream_t st = as_stream(stream);
+    Q4Args p{};
+    p.W = h->W;
+    p.X = X;
+    p.Y = (bf16*)Y;
+    p.M = M;
+    p.N = h->d_out;
+    p.K = h->d_in;
+    if (M <= kDecodeMaxM) {
+        p.R = (const bf16*)R;
+        p.gain = (const bf16*)gain;
+        p.H = (bf16*)H;
+        p.eps = eps;
+        TimedLaunch timed(kSiteQ4Norm, st);
+        q4_few_launch<kQ4Bf16, true, 1, 1, 8, 1>(p, st);
+        return hipGetLastError() == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+    }
+    s = q4_ensure(h, in, st);
+    if (s != PIFA_OK) return s;
+    void* rows = h->ws[h->n_ws - 1];
+    if (norm_forward_run<bf16>(X, R, gain, eps, H, rows, nullptr, nullptr, M, h->d_in, st) != hipSuccess)
+        return PIFA_ERR_HIP;
+    p.X = rows;
+    return launch_q4<kQ4Bf16>(p, st) == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
 }
 
 pifa_status pifa_profile_enable(int on) {

@@ -49,6 +49,7 @@ _lib = None
 _vp = ctypes.c_void_p
 _i64 = ctypes.c_int64
 _i32p = ctypes.POINTER(ctypes.c_int32)
+_f32 = ctypes.c_float
 _st = ctypes.c_int
 
 _SIGNATURES = {
@@ -91,6 +92,20 @@ _SIGNATURES = {
     "pifa_calib_read": (_st, [_vp, _vp, _vp, _vp]),
     "pifa_calib_reconstruct": (_st, [_vp, _vp, _i64, _vp, _i64, ctypes.c_double, ctypes.c_double, _vp, _vp, _vp]),
     "pifa_build_f64": (_st, [_vp, pifa_dims, _vp, _vp, _i32p, _i32p, ctypes.POINTER(ctypes.c_double), _vp]),
+    "rms_norm_forward": (_st, [_vp, _vp, _vp, _f32, _vp, _vp, _i64, _i64, ctypes.c_int, _vp]),
+    "rms_norm_forward_e4m3": (_st, [_vp, _vp, _vp, _f32, _vp, _vp, _vp, _i64, _i64, ctypes.c_int, _vp]),
+    "rms_norm_backward": (_st, [_vp, _vp, _vp, _vp, _f32, _vp, _vp, _i64, _i64, ctypes.c_int, _vp, ctypes.c_size_t,
+                                _vp]),
+    "rms_norm_backward_bytes": (ctypes.c_size_t, [_i64, _i64]),
+    "q4_layer_create": (_st, [_vp, _i64, _i64, ctypes.c_int, ctypes.POINTER(_vp)]),
+    "q4_layer_create_mx": (_st, [_vp, _vp, _i64, _i64, ctypes.POINTER(_vp)]),
+    "q4_layer_destroy": (_st, [_vp]),
+    "q4_layer_read": (_st, [_vp, _vp, _vp, _vp]),
+    "q4_layer_weight_bytes": (ctypes.c_size_t, [_vp]),
+    "q4_layer_forward": (_st, [_vp, _vp, _vp, _i64, _vp]),
+    "q4_layer_forward_e4m3": (_st, [_vp, _vp, _vp, _vp, _i64, _vp]),
+    "q4_layer_norm_forward": (_st, [_vp, _vp, _vp, _vp, _f32, _vp, _vp, _i64, _vp]),
+    "q4_layer_reserve": (_st, [_vp, _i64]),
     "pifa_probe_mfma": (_st, [_i64, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
     "pifa_probe_mfma_random": (_st, [_i64, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
     "pifa_probe_hbm_read": (_st, [_vp, _i64, ctypes.c_int, ctypes.POINTER(ctypes.c_double), _vp]),
@@ -567,6 +582,177 @@ def pifa_build_f64(W, r: int, stream=None):
     return piv, npiv, Wp, C, np.array(list(report))
 
 
+# Buffers of the norms and 4-bit layers: every tensor given has the element
+# type, lives on the device that is current (the kernels run there), is
+# contiguous and holds what the call reads or writes.
+def _ptr_of(t, name: str, dtype, count: int, dev: int) -> int | None:
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError("%s is %s, the call expects %s" % (name, t.dtype, dtype))
+    if t.get_device() != dev:
+        raise ValueError("%s is on %s, the call runs on cuda:%d" % (name, t.device, dev))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    if t.numel() < count:
+        raise ValueError("%s holds %d values, the call needs %d" % (name, t.numel(), count))
+    return t.data_ptr()
+
+
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+def _rows_of(t, M, d):
+    """(M, d) of a call on the rows of t: its own, where not given."""
+    return (t.numel() // max(int(t.shape[-1]), 1) if M is None else int(M), int(t.shape[-1]) if d is None else int(d))
+
+
+def rms_norm_forward(X, gain, eps: float, R=None, H=None, Y=None, M: int | None = None, d: int | None = None,
+                     stream=None):
+    """The norm of the rows of X + R (R may be None), times gain (may be None).
+    Returns Y (allocated when not given); H, where given, takes X + R.  The
+    rows are X's last dimension unless M and d say otherwise."""
+    import torch
+    M, d = _rows_of(X, M, d)
+    if Y is None:
+        Y = torch.empty_like(X)
+    dt, dev, n = X.dtype, _current_device(), M * d
+    code = _dtype_code(X)
+    _check("rms_norm_forward", lib().rms_norm_forward(
+        _ptr_of(X, "X", dt, n, dev), _ptr_of(R, "R", dt, n, dev), _ptr_of(gain, "gain", dt, d, dev), eps,
+        _ptr_of(H, "H", dt, n, dev), _ptr_of(Y, "Y", dt, n, dev), M, d, code, _stream(stream)))
+    return Y
+
+
+def rms_norm_forward_e4m3(X, gain, eps: float, R=None, H=None, Q=None, scale=None, M: int | None = None,
+                          d: int | None = None, stream=None):
+    """The same norm in 8 bits.  Returns (Q, scale): float8_e4m3fn rows and one
+    fp32 scale a row, which stand for Q * scale (allocated when not given)."""
+    import torch
+    M, d = _rows_of(X, M, d)
+    if Q is None:
+        Q = torch.empty(X.shape, dtype=torch.float8_e4m3fn, device=X.device)
+    if scale is None:
+        scale = torch.empty(M, dtype=torch.float32, device=X.device)
+    dt, dev, n = X.dtype, _current_device(), M * d
+    code = _dtype_code(X)
+    _check("rms_norm_forward_e4m3", lib().rms_norm_forward_e4m3(
+        _ptr_of(X, "X", dt, n, dev), _ptr_of(R, "R", dt, n, dev), _ptr_of(gain, "gain", dt, d, dev), eps,
+        _ptr_of(H, "H", dt, n, dev), _ptr_of(Q, "Q", torch.float8_e4m3fn, n, dev),
+        _ptr_of(scale, "scale", torch.float32, M, dev), M, d, code, _stream(stream)))
+    return Q, scale
+
+
+def rms_norm_backward_bytes(M: int, d: int) -> int:
+    return int(lib().rms_norm_backward_bytes(int(M), int(d)))
+
+
+def rms_norm_backward(H, gain, dY, eps: float, dR=None, dX=None, dgain=None, work=None, M: int | None = None,
+                      d: int | None = None, stream=None, need_dX: bool = True, need_dgain: bool = True):
+    """Gradients of rms_norm_forward: (dX, dgain), dX plus dR where given.
+    Outputs and workspace are allocated when not given; need_dX / need_dgain
+    False skip one (None in its place)."""
+    import torch
+    M, d = _rows_of(H, M, d)
+    if dX is None and need_dX:
+        dX = torch.empty_like(H)
+    if dgain is None and need_dgain:
+        dgain = torch.empty(d, dtype=torch.float32, device=H.device)
+    if work is None and dgain is not None:
+        work = torch.empty(rms_norm_backward_bytes(M, d), dtype=torch.uint8, device=H.device)
+    dt, dev, n = H.dtype, _current_device(), M * d
+    code = _dtype_code(H)
+    nwork = 0 if work is None else work.numel() * work.element_size()
+    _check("rms_norm_backward", lib().rms_norm_backward(
+        _ptr_of(H, "H", dt, n, dev), _ptr_of(gain, "gain", dt, d, dev), _ptr_of(dY, "dY", dt, n, dev),
+        _ptr_of(dR, "dR", dt, n, dev), eps, _ptr_of(dX, "dX", dt, n, dev),
+        _ptr_of(dgain, "dgain", torch.float32, d, dev), M, d, code,
+        None if work is None else _ptr_of(work, "work", work.dtype, 0, dev), nwork, _stream(stream)))
+    return dX, dgain
+
+
+def q4_layer_create(W, d_in: int | None = None, d_out: int | None = None, dtype: int | None = None) -> int:
+    """Quantizes W (d_out x d_in) to 4 bits; returns an opaque handle."""
+    d_in = W.shape[1] if d_in is None else int(d_in)
+    d_out = W.shape[0] if d_out is None else int(d_out)
+    dt = _dtype_code(W) if dtype is None else int(dtype)
+    dev = _current_device()
+    out = _vp()
+    _check("q4_layer_create", lib().q4_layer_create(_ptr_of(W, "W", _torch_dtype(dt), d_out * d_in, dev), d_in, d_out,
+                                                    dt, ctypes.byref(out)))
+    return _remember(out.value, d_in=d_in, d_out=d_out, dt=PIFA_BF16, dev=dev)
+
+
+def q4_layer_create_mx(codes, scales, d_in: int | None = None, d_out: int | None = None) -> int:
+    """codes: uint8 d_out x d_in / 2 (the lower index in the lower half of a
+    byte), scales: uint8 d_out x d_in / 32 (powers of two, biased by 127)."""
+    import torch
+    d_in = 2 * codes.shape[1] if d_in is None else int(d_in)
+    d_out = codes.shape[0] if d_out is None else int(d_out)
+    dev = _current_device()
+    out = _vp()
+    _check("q4_layer_create_mx", lib().q4_layer_create_mx(
+        _ptr_of(codes, "codes", torch.uint8, d_out * (d_in // 2), dev),
+        _ptr_of(scales, "scales", torch.uint8, d_out * (d_in // 32), dev), d_in, d_out, ctypes.byref(out)))
+    return _remember(out.value, d_in=d_in, d_out=d_out, dt=PIFA_BF16, dev=dev)
+
+
+def q4_layer_destroy(handle: int) -> None:
+    _forget(handle)
+    _check("q4_layer_destroy", lib().q4_layer_destroy(handle))
+
+
+def q4_layer_read(handle: int, codes=None, scales=None, stream=None) -> None:
+    """Copies the layer's codes and scales (either may be None)."""
+    import torch
+    d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    dev = _current_device()
+    _check("q4_layer_read", lib().q4_layer_read(
+        handle, _ptr_of(codes, "codes", torch.uint8, d["d_out"] * d["d_in"] // 2, dev),
+        _ptr_of(scales, "scales", torch.uint8, d["d_out"] * d["d_in"] // 32, dev), _stream(stream)))
+
+
+def q4_layer_weight_bytes(handle: int) -> int:
+    return int(lib().q4_layer_weight_bytes(handle))
+
+
+def q4_layer_reserve(handle: int, max_M: int) -> None:
+    _check("q4_layer_reserve", lib().q4_layer_reserve(handle, int(max_M)))
+
+
+def q4_layer_forward(handle: int, X, Y, M: int | None = None, stream=None) -> None:
+    import torch
+    M = X.shape[0] if M is None else int(M)
+    d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    dev = _current_device()
+    _check("q4_layer_forward", lib().q4_layer_forward(
+        handle, _ptr_of(X, "X", torch.bfloat16, M * d["d_in"], dev), _ptr_of(Y, "Y", torch.bfloat16, M * d["d_out"], dev),
+        M, _stream(stream)))
+
+
+def q4_layer_forward_e4m3(handle: int, Q, scale, Y, M: int | None = None, stream=None) -> None:
+    import torch
+    M = Q.shape[0] if M is None else int(M)
+    d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    dev = _current_device()
+    _check("q4_layer_forward_e4m3", lib().q4_layer_forward_e4m3(
+        handle, _ptr_of(Q, "Q", torch.float8_e4m3fn, M * d["d_in"], dev), _ptr_of(scale, "scale", torch.float32, M, dev),
+        _ptr_of(Y, "Y", torch.bfloat16, M * d["d_out"], dev), M, _stream(stream)))
+
+
+def q4_layer_norm_forward(handle: int, X, gain, eps: float, R=None, H=None, Y=None, M: int | None = None,
+                          stream=None) -> None:
+    import torch
+    M = X.shape[0] if M is None else int(M)
+    d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    dev, bf, n = _current_device(), torch.bfloat16, M * d["d_in"]
+    _check("q4_layer_norm_forward", lib().q4_layer_norm_forward(
+        handle, _ptr_of(X, "X", bf, n, dev), _ptr_of(R, "R", bf, n, dev), _ptr_of(gain, "gain", bf, d["d_in"], dev), eps,
+        _ptr_of(H, "H", bf, n, dev), _ptr_of(Y, "Y", bf, M * d["d_out"], dev), M, _stream(stream)))
+
+
 def pifa_probe_mfma(iters: int = 20000, stream=None):
     """(dense bf16 MFMA TFLOP/s, shader clock in MHz) of an MFMA-only kernel."""
     tf, mhz = ctypes.c_double(), ctypes.c_double()
@@ -632,6 +818,70 @@ class PifaLayer:
     def close(self):
         if self.handle:
             pifa_layer_destroy(self.handle)
+            self.handle = 0
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Q4Layer:
+    """Owns a 4-bit layer: ``layer(X)`` allocates Y and runs q4_layer_forward."""
+
+    def __init__(self, W=None, handle: int = 0, d_in: int = 0, d_out: int = 0):
+        self.handle = q4_layer_create(W) if W is not None else handle
+        self.d_in = int(W.shape[1]) if W is not None else int(d_in)
+        self.d_out = int(W.shape[0]) if W is not None else int(d_out)
+
+    @classmethod
+    def from_mx(cls, codes, scales):
+        """A layer of weights already in the format (see q4_layer_create_mx)."""
+        return cls(None, q4_layer_create_mx(codes, scales), 2 * codes.shape[1], codes.shape[0])
+
+    def _out(self, Y, M: int, X):
+        import torch
+        return torch.empty((M, self.d_out), dtype=torch.bfloat16, device=X.device) if Y is None else Y
+
+    def __call__(self, X, Y=None, stream=None):
+        Y = self._out(Y, X.shape[0], X)
+        q4_layer_forward(self.handle, X, Y, X.shape[0], stream)
+        return Y
+
+    def forward_e4m3(self, Q, scale, Y=None, stream=None):
+        """Rows in 8 bits with a scale each, as rms_norm_forward_e4m3 returns them."""
+        Y = self._out(Y, Q.shape[0], Q)
+        q4_layer_forward_e4m3(self.handle, Q, scale, Y, Q.shape[0], stream)
+        return Y
+
+    def norm_forward(self, X, gain, eps: float, R=None, H=None, Y=None, stream=None):
+        """The product of the norm of X + R; H, where given, takes X + R."""
+        Y = self._out(Y, X.shape[0], X)
+        q4_layer_norm_forward(self.handle, X, gain, eps, R, H, Y, X.shape[0], stream)
+        return Y
+
+    def reserve(self, max_M: int):
+        q4_layer_reserve(self.handle, max_M)
+
+    def read(self):
+        """(codes, scales) as from_mx takes them."""
+        import torch
+        dev = "cuda:%d" % _current_device()
+        codes = torch.empty((self.d_out, self.d_in // 2), dtype=torch.uint8, device=dev)
+        scales = torch.empty((self.d_out, self.d_in // 32), dtype=torch.uint8, device=dev)
+        q4_layer_read(self.handle, codes, scales)
+        return codes, scales
+
+    def close(self):
+        if self.handle:
+            q4_layer_destroy(self.handle)
             self.handle = 0
 
     def __enter__(self):

@@ -1,0 +1,299 @@
+"""Norms (rms_norm_forward, _e4m3, _backward) against their fp64 forms.
+
+Tolerances, element by element.  A result is rounded once, by at most half a
+step: 2^-8 of it in bf16, 2^-24 in fp32, and in e4m3 2^-4 of it or 2^-10 of the
+row's scale.  Behind it stand fp32 sums of at most 128 additions on the way of
+one element (a thread's own, then a tree), so the sum of squares is good to 128
+* 2^-24 = 2^-17, rho to half of that plus a few roundings: 2^-17 altogether.
+"""
+import numpy as np
+import pytest
+
+from oracle import norm_q4 as o
+from paper_2501_19090_amd import inputs
+
+from gpu_util import from_dev, to_dev, torch_mod
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-5
+FP = 2.0 ** -17
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+WIDTHS = [1, 3, 8, 64, 127, 512, 1000, 2048, 2867, 4096, 8192, 8200, 16391, 33000]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch_mod().cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _pifa():
+    from paper_2501_19090_amd import pifa
+    return pifa
+
+
+def _rows(M, d, dtype, seed, scale=1.0, outliers=True):
+    rng = np.random.default_rng([seed, M, d])
+    x = rng.standard_normal((M, d)) * scale
+    if outliers and d > 4:
+        x[:, rng.integers(0, d, 2)] *= 50.0
+    st, x64 = inputs.round_to(x, dtype)
+    return to_dev(st), x64
+
+
+def _gain(d, dtype, seed):
+    st, g = inputs.round_to(1.0 + 0.3 * np.random.default_rng(seed).standard_normal((1, d)), dtype)
+    return to_dev(st).reshape(d), g[0]
+
+
+def _tiny(dtype):
+    """Below the normal range a rounding is a fixed step."""
+    return 2.0 ** -126
+
+
+def _close(got, want, tol, what):
+    off = np.abs(got - want) - tol
+    assert np.isfinite(got).all(), what
+    assert (off <= 0).all(), (what, float(off.max()), np.unravel_index(off.argmax(), off.shape))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("M", [1, 5, 300])
+def test_forward(M, d, dtype):
+    pifa, torch = _pifa(), torch_mod()
+    x_dev, x = _rows(M, d, dtype, 1)
+    r_dev, r = _rows(M, d, dtype, 2)
+    g_dev, g = _gain(d, dtype, 3)
+    H, Y = torch.full_like(x_dev, float("nan")), torch.full_like(x_dev, float("nan"))
+    pifa.rms_norm_forward(x_dev, g_dev, EPS, R=r_dev, H=H, Y=Y)
+    torch.cuda.synchronize()
+    h, y = o.rms_norm(x, g, EPS, r)
+    # h = x + r is one fp32 addition ahead of its rounding
+    _close(from_dev(H), h, np.abs(h) * (HALF[dtype] + 2.0 ** -24) + _tiny(dtype), "H")
+    _close(from_dev(Y), y, np.abs(y) * (HALF[dtype] + FP) + _tiny(dtype), "Y")
+    # neither residual nor gain
+    y2 = pifa.rms_norm_forward(x_dev, None, EPS)
+    torch.cuda.synchronize()
+    _, y = o.rms_norm(x, None, EPS)
+    _close(from_dev(y2), y, np.abs(y) * (HALF[dtype] + FP) + _tiny(dtype), "Y alone")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("M", [1, 300])
+def test_forward_e4m3(M, d, dtype):
+    pifa, torch = _pifa(), torch_mod()
+    x_dev, x = _rows(M, d, dtype, 4)
+    r_dev, r = _rows(M, d, dtype, 5)
+    g_dev, g = _gain(d, dtype, 6)
+    H = torch.full_like(x_dev, float("nan"))
+    Q, s = pifa.rms_norm_forward_e4m3(x_dev, g_dev, EPS, R=r_dev, H=H)
+    torch.cuda.synchronize()
+    h, y = o.rms_norm(x, g, EPS, r)
+    want = o.e4m3_scale(y)
+    s = from_dev(s)
+    _close(s, want, want * FP, "scale")
+    v = o.e4m3_value(Q.view(torch.uint8).cpu().numpy()) * s[:, None]
+    _close(v, y, np.maximum(np.abs(y) * 2.0 ** -4, s[:, None] * 2.0 ** -10) + np.abs(y) * FP, "Q scale")
+    _close(from_dev(H), h, np.abs(h) * (HALF[dtype] + 2.0 ** -24) + _tiny(dtype), "H")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("M", [1, 7, 1100])
+def test_backward(M, d, dtype):
+    pifa, torch = _pifa(), torch_mod()
+    if M * d > 4e6:
+        M = 270  # more rows than workgroups all the same
+    h_dev, h = _rows(M, d, dtype, 7)
+    dy_dev, dy = _rows(M, d, dtype, 8, scale=1e-2, outliers=False)
+    dr_dev, dr = _rows(M, d, dtype, 9, scale=1e-2, outliers=False)
+    g_dev, g = _gain(d, dtype, 10)
+    dX, dg = pifa.rms_norm_backward(h_dev, g_dev, dy_dev, EPS, dR=dr_dev)
+    dX2, dg2 = pifa.rms_norm_backward(h_dev, g_dev, dy_dev, EPS, dR=dr_dev)
+    torch.cuda.synchronize()
+    assert torch.equal(dX, dX2) and torch.equal(dg, dg2)  # a fixed order of sums
+    want, dgain = o.rms_norm_backward(h, g, dy, EPS, dr)
+    p = o.rho(h, EPS)
+    # each term is good to 2^-17 of it, the mean to 2^-17 of its terms' magnitudes, rho^3 to three times that
+    terms = p * np.abs(g * dy) + p ** 3 * np.abs(h) * np.abs(g * dy * h).mean(1, keepdims=True) + np.abs(dr)
+    _close(from_dev(dX), want, np.abs(want) * HALF[dtype] + terms * 4 * FP + _tiny(dtype), "dX")
+    # a column's terms are good to 2^-16, their sum takes at most 128 additions on the way of one
+    _close(from_dev(dg), dgain, np.abs(dy * h * p).sum(0) * (2 * FP + FP) + 1e-30, "dgain")
+    # without gain, residual gradient, or one of the outputs
+    only, none = pifa.rms_norm_backward(h_dev, None, dy_dev, EPS, need_dgain=False)
+    none2, dg3 = pifa.rms_norm_backward(h_dev, g_dev, dy_dev, EPS, need_dX=False)
+    torch.cuda.synchronize()
+    assert none is None and none2 is None and torch.equal(dg3, dg)
+    want, _ = o.rms_norm_backward(h, None, dy, EPS)
+    _close(from_dev(only), want, np.abs(want) * HALF[dtype] + terms * 8 * FP + _tiny(dtype), "dX alone")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_backward_against_differences(dtype):
+    """The gradient of sum(Y * dY) by central differences of the forward itself,
+    in fp32 sums of its outputs: a random direction, step 2^-6."""
+    pifa, torch = _pifa(), torch_mod()
+    M, d = 4, 257
+    rng = np.random.default_rng(11)
+    h = rng.standard_normal((M, d)).astype(np.float32)
+    g = (1 + 0.3 * rng.standard_normal(d)).astype(np.float32)
+    dy = rng.standard_normal((M, d)).astype(np.float32)
+    t = lambda a: torch.from_numpy(a).cuda().to(torch.float32)
+    if dtype == "bf16":
+        h, g, dy = (torch.from_numpy(a).to(torch.bfloat16).float().numpy() for a in (h, g, dy))
+    cast = (lambda a: t(a).to(torch.bfloat16)) if dtype == "bf16" else t
+    dX, dg = pifa.rms_norm_backward(cast(h), cast(g), cast(dy), EPS)
+    dX, dg = from_dev(dX), from_dev(dg)
+    v, w = rng.standard_normal((M, d)).astype(np.float32), rng.standard_normal(d).astype(np.float32)
+    step = np.float32(2.0 ** -6)
+
+    def loss(hh, gg):
+        return float((pifa.rms_norm_forward(t(hh), t(gg), EPS).double() * t(dy).double()).sum())
+
+    # the second-order remainder of a step of 2^-6 in each element: at most step^2
+    # times a few times the size of the terms; fp32 outputs add 2^-24 / step of them
+    size = float(np.abs(dy).sum())
+    num = (loss(h + step * v, g) - loss(h - step * v, g)) / (2 * step)
+    half = 2.0 ** -8 if dtype == "bf16" else 0.0
+    assert abs(num - float((dX * v).sum())) <= size * (8 * step ** 2 + 2.0 ** -16) + half * float(np.abs(dX * v).sum())
+    num = (loss(h, g + step * w) - loss(h, g - step * w)) / (2 * step)
+    assert abs(num - float((dg * w).sum())) <= size * 2.0 ** -14  # linear in the gain
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_unaligned_rows_and_outputs_in_place(dtype):
+    """Buffers that start anywhere, H over R, Y over X, dX over dY."""
+    pifa, torch = _pifa(), torch_mod()
+    M, d = 19, 1003
+    x_dev, x = _rows(M, d, dtype, 20)
+    r_dev, r = _rows(M, d, dtype, 21)
+    g_dev, g = _gain(d, dtype, 22)
+    h, y = o.rms_norm(x, g, EPS, r)
+
+    def at(t, off):
+        """t's values at an element offset of `off` in a larger buffer of guard values."""
+        big = torch.full((t.numel() + 32,), 7.0, dtype=t.dtype, device=t.device)
+        big[off:off + t.numel()] = t.reshape(-1)
+        return big, big[off:off + t.numel()].view(t.shape)
+
+    for off in (1, 3, 8):
+        bx, xv = at(x_dev, off)
+        br, rv = at(r_dev, off + 2)
+        bg, gv = at(g_dev, off + 1)
+        assert pifa.rms_norm_forward(xv, gv, EPS, R=rv, H=rv, Y=xv) is xv
+        torch.cuda.synchronize()
+        _close(from_dev(rv), h, np.abs(h) * (HALF[dtype] + 2.0 ** -24) + _tiny(dtype), "H over R")
+        _close(from_dev(xv), y, np.abs(y) * (HALF[dtype] + FP) + _tiny(dtype), "Y over X")
+        for big, o_, n in ((bx, off, M * d), (br, off + 2, M * d)):
+            assert (big[:o_] == 7).all() and (big[o_ + n:] == 7).all()
+        # 8-bit rows and a gradient at odd places
+        qbig = torch.zeros(M * d + 32, dtype=torch.uint8, device="cuda")
+        Q = qbig[off:off + M * d].view(M, d).view(torch.float8_e4m3fn)
+        q0, s0 = pifa.rms_norm_forward_e4m3(x_dev, g_dev, EPS, R=r_dev)
+        q1, s1 = pifa.rms_norm_forward_e4m3(x_dev, gv, EPS, R=r_dev, Q=Q)
+        assert torch.equal(q0.view(torch.uint8), q1.view(torch.uint8)) and torch.equal(s0, s1)
+        assert (qbig[:off] == 0).all() and (qbig[off + M * d:] == 0).all()
+        d0, g0 = pifa.rms_norm_backward(x_dev, g_dev, r_dev, EPS, dR=r_dev)
+        by, yv = at(r_dev, off)
+        d1, g1 = pifa.rms_norm_backward(x_dev, gv, yv, EPS, dR=yv, dX=yv)
+        assert d1 is yv and torch.equal(d0, d1) and torch.equal(g0, g1)
+        assert (by[:off] == 7).all() and (by[off + M * d:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_special_values_stay_in_their_rows(dtype):
+    pifa, torch = _pifa(), torch_mod()
+    M, d = 6, 515
+    x_dev, x = _rows(M, d, dtype, 30)
+    x_dev[1] = 0.0
+    x_dev[2, 100] = float("nan")
+    x_dev[3, 514] = float("inf")
+    x_dev[4] = 1e-30  # squares vanish beside eps
+    clean = torch.tensor([0, 5])
+    y = pifa.rms_norm_forward(x_dev, None, EPS)
+    q, s = pifa.rms_norm_forward_e4m3(x_dev, None, EPS)
+    dx, dg = pifa.rms_norm_backward(x_dev, None, x_dev, EPS)
+    torch.cuda.synchronize()
+    assert (y[1] == 0).all() and (q[1].float() == 0).all() and float(s[1]) == o.TINY
+    assert torch.isnan(y[2]).all() and torch.isnan(s[2])
+    assert torch.isnan(y[3, 514]) and (y[3, :514] == 0).all() and torch.isnan(s[3])
+    assert torch.isfinite(y[clean]).all() and torch.isfinite(dx[clean]).all()
+    _close(from_dev(y)[4], o.rms_norm(from_dev(x_dev)[4:5], None, EPS)[1][0], np.full(d, 1e-27 * 0.01), "tiny row")
+    assert torch.isnan(dg[100])
+    # rows whose largest value needs a scale below the smallest one: it is held at 2^-126
+    t = torch.full((1, 64), 1e-38, dtype=x_dev.dtype, device="cuda")
+    q, s = pifa.rms_norm_forward_e4m3(t, None, 1.0)
+    assert float(s[0]) == o.TINY and abs(float(q[0, 0]) * o.TINY - 1e-38) <= 1e-38 * 2.0 ** -4 + 2.0 ** -8 * 1e-38
+
+
+def test_no_rows_and_refused_calls():
+    pifa, torch = _pifa(), torch_mod()
+    x = torch.randn(4, 16, device="cuda", dtype=torch.bfloat16)
+    empty = torch.empty(0, 16, device="cuda", dtype=torch.bfloat16)
+    assert pifa.rms_norm_forward(empty, None, EPS).shape == (0, 16)
+    q, s = pifa.rms_norm_forward_e4m3(empty, None, EPS)
+    assert q.shape == (0, 16) and s.numel() == 0
+    dX, dg = pifa.rms_norm_backward(empty, None, empty, EPS)
+    torch.cuda.synchronize()
+    assert dX.numel() == 0 and (dg == 0).all()
+    for eps in (0.0, -1.0, float("nan"), float("inf")):
+        with pytest.raises(pifa.PifaError):
+            pifa.rms_norm_forward(x, None, eps)
+    with pytest.raises(pifa.PifaError):
+        pifa.rms_norm_forward(x, None, EPS, H=(y := torch.empty_like(x)), Y=y)
+    with pytest.raises(TypeError):
+        pifa.rms_norm_forward(x, torch.ones(16, device="cuda"), EPS)  # gain of another type
+    with pytest.raises(TypeError):
+        pifa.rms_norm_forward(x.half(), None, EPS)
+    with pytest.raises(ValueError):
+        pifa.rms_norm_forward(x.t(), None, EPS)
+    with pytest.raises(ValueError):
+        pifa.rms_norm_forward(x, None, EPS, R=x[:3])
+    with pytest.raises(ValueError):
+        pifa.rms_norm_forward(x, None, EPS, R=x.cpu())
+    with pytest.raises(ValueError):
+        pifa.rms_norm_backward(x, None, x, EPS, dgain=torch.empty(15, device="cuda"))
+    big = torch.randn(40, 16, device="cuda", dtype=torch.bfloat16)
+    with pytest.raises(pifa.PifaError):
+        pifa.rms_norm_backward(big, None, big, EPS, work=torch.empty(8, dtype=torch.uint8, device="cuda"))
+
+
+def test_captured_and_replayed_beside_eager_work():
+    """A graph of norm, 8-bit norm and gradients, replayed on new inputs with
+    eager calls between, on a stream of its own."""
+    pifa, torch = _pifa(), torch_mod()
+    M, d = 70, 1024
+    x, r, dy = (torch.randn(M, d, device="cuda").to(torch.bfloat16) for _ in range(3))
+    g = torch.randn(d, device="cuda").to(torch.bfloat16)
+    H, Y, dX = (torch.empty_like(x) for _ in range(3))
+    Q, s = torch.empty(M, d, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(M, device="cuda")
+    dg, work = torch.empty(d, device="cuda"), torch.empty(pifa.rms_norm_backward_bytes(M, d), dtype=torch.uint8, device="cuda")
+
+    def calls(H, Y, Q, s, dX, dg, work):
+        pifa.rms_norm_forward(x, g, EPS, R=r, H=H, Y=Y)
+        pifa.rms_norm_forward_e4m3(x, g, EPS, R=r, Q=Q, scale=s)
+        pifa.rms_norm_backward(H, g, dy, EPS, dR=r, dX=dX, dgain=dg, work=work)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        calls(H, Y, Q, s, dX, dg, work)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            calls(H, Y, Q, s, dX, dg, work)
+    for i in range(4):
+        for t in (x, r, dy):
+            t.copy_(torch.randn(M, d, device="cuda"))
+        for t in (H, Y, dX):
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        other = [torch.empty_like(t) for t in (H, Y, Q, s, dX, dg, work)]
+        calls(*other)
+        torch.cuda.synchronize()
+        for a, b in zip((H, Y, Q, s, dX, dg), other):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i

@@ -1,0 +1,415 @@
+"""4-bit layers against the fp64 product of the weights their codes stand for.
+
+Tolerances, element by element.  An output is rounded once to bf16: 2^-8 of it.
+fp32 sums: K / 32 additions of at most 2^-23 of the terms' magnitudes so far on
+the way of one term (fewer: the K range is split over waves), 2^-15 of the sum of
+magnitudes at K = 8192.  A 16x16x128 step of 8-bit rows cuts the 32 products
+of a group off at 2^-14 of the largest: 32 * 2^-14 = 2^-9 of the product of the
+group's largest value in the row and in the weights.  The norm's form rounds its rows to bf16 first: 2^-8 of every term,
+which adds up to at most 2^-8 of the sum of magnitudes.
+"""
+import numpy as np
+import pytest
+
+from oracle import norm_q4 as o
+from paper_2501_19090_amd import inputs
+
+from gpu_util import from_dev, rel_fro, to_dev, torch_mod
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-5
+SUMS = 2.0 ** -15
+SHAPES = [(32, 1), (32, 16), (64, 17), (96, 40), (128, 63), (160, 64), (256, 1000), (512, 130), (1024, 333), (2048, 256),
+          (4096, 97), (11008, 48)]
+ROWS = [1, 2, 7, 16, 17, 33, 64, 65, 130, 257, 500]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch_mod().cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def _pifa():
+    from paper_2501_19090_amd import pifa
+    return pifa
+
+
+def _codes(d_in, d_out, seed, spread=4):
+    """Random codes and scales 2^-spread .. 2^spread around 1 / sqrt(d_in), and the weights they stand for."""
+    rng = np.random.default_rng([seed, d_in, d_out])
+    codes = rng.integers(0, 256, (d_out, d_in // 2), dtype=np.uint8)
+    mid = 127 - int(np.log2(d_in) / 2)
+    scales = rng.integers(mid - spread, mid + spread + 1, (d_out, d_in // 32)).astype(np.uint8)
+    return codes, scales, o.mx_weights(codes, scales)
+
+
+def _dev(a):
+    return torch_mod().from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _layer(d_in, d_out, seed, spread=4):
+    codes, scales, w = _codes(d_in, d_out, seed, spread)
+    return _pifa().Q4Layer.from_mx(_dev(codes), _dev(scales)), w
+
+
+def _x(M, d_in, seed):
+    st, x = inputs.round_to(np.random.default_rng([seed, M, d_in]).standard_normal((M, d_in)), "bf16")
+    return to_dev(st), x
+
+
+def _check(got, want, mags, frac, what):
+    got = from_dev(got)
+    assert np.isfinite(got).all(), what
+    off = np.abs(got - want) - (np.abs(want) * 2.0 ** -8 + mags * frac)
+    assert (off <= 0).all(), (what, float(off.max()), np.unravel_index(off.argmax(), off.shape))
+
+
+def _guarded(M, N):
+    torch = torch_mod()
+    big = torch.full((M * N + 64,), -17.0, dtype=torch.bfloat16, device="cuda")
+    return big, big[:M * N].view(M, N)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward(shape):
+    torch = torch_mod()
+    d_in, d_out = shape
+    layer, w = _layer(d_in, d_out, 1)
+    with layer:
+        for M in ROWS:
+            x_dev, x = _x(M, d_in, 2)
+            big, Y = _guarded(M, d_out)
+            layer(x_dev, Y)
+            torch.cuda.synchronize()
+            _check(Y, x @ w.T, np.abs(x) @ np.abs(w).T, SUMS, (shape, M))
+            assert (big[M * d_out:] == -17).all()
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward_e4m3(shape):
+    torch = torch_mod()
+    d_in, d_out = shape
+    layer, w = _layer(d_in, d_out, 3)
+    with layer:
+        for M in ROWS:
+            rng = np.random.default_rng([4, M, d_in])
+            q = rng.integers(0, 256, (M, d_in)).astype(np.uint8)
+            q[(q & 127) == 127] = 0
+            s = (2.0 ** rng.uniform(-12, 4, M)).astype(np.float32)
+            x = o.e4m3_value(q)
+            big, Y = _guarded(M, d_out)
+            layer.forward_e4m3(_dev(q).view(torch.float8_e4m3fn), _dev(s), Y)
+            torch.cuda.synchronize()
+            f = s.astype(np.float64)[:, None]
+            top = lambda a: np.abs(a).reshape(a.shape[0], -1, 32).max(axis=2)
+            cut = 2.0 ** -9 * (top(x) @ top(w).T) + SUMS * (np.abs(x) @ np.abs(w).T)
+            _check(Y, f * (x @ w.T), f * cut, 1.0, (shape, M))
+            assert (big[M * d_out:] == -17).all()
+
+
+@pytest.mark.parametrize("with_r,with_gain,with_h", [(True, True, True), (False, True, False), (True, False, True),
+                                                     (False, False, True)])
+@pytest.mark.parametrize("shape", [(32, 5), (96, 40), (1024, 333), (4096, 97)])
+def test_norm_forward(shape, with_r, with_gain, with_h):
+    torch = torch_mod()
+    d_in, d_out = shape
+    layer, w = _layer(d_in, d_out, 5)
+    g_st, g = inputs.round_to(1.0 + 0.3 * np.random.default_rng(6).standard_normal((1, d_in)), "bf16")
+    g_dev = to_dev(g_st).reshape(-1) if with_gain else None
+    with layer:
+        for M in (1, 3, 16, 17, 90):
+            x_dev, x = _x(M, d_in, 7)
+            r_dev, r = _x(M, d_in, 8) if with_r else (None, None)
+            h, y = o.rms_norm(x, g[0] if with_gain else None, EPS, r)
+            big, Y = _guarded(M, d_out)
+            hbig, H = _guarded(M, d_in) if with_h else (None, None)
+            layer.norm_forward(x_dev, g_dev, EPS, R=r_dev, H=H, Y=Y)
+            torch.cuda.synchronize()
+            mags = np.abs(y) @ np.abs(w).T
+            _check(Y, y @ w.T, mags, 2.0 ** -8 + 2 * SUMS, (shape, M))
+            assert rel_fro(from_dev(Y), y @ w.T) < 5e-3  # both roundings are 1.7e-3 rms
+            assert (big[M * d_out:] == -17).all()
+            if with_h:
+                off = np.abs(from_dev(H) - h) - np.abs(h) * (2.0 ** -8 + 2.0 ** -24)
+                assert (off <= 2.0 ** -126).all() and (hbig[M * d_in:] == -17).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(32, 1), (96, 40), (1024, 77)])
+def test_quantized_weights(shape, dtype):
+    """q4_layer_create against both candidates of every group: the weights are
+    one candidate's, to the bit, and the better one's unless their errors are
+    nearly the same (fp32 sums of 32 squares: 2^-18)."""
+    pifa, torch = _pifa(), torch_mod()
+    d_in, d_out = shape
+    rng = np.random.default_rng([9, d_in])
+    w = rng.standard_normal((d_out, d_in)) * 2.0 ** rng.integers(-20, 20, (d_out, d_in // 32)).repeat(32, axis=1)
+    w[0, :32] = 0.0
+    st, w = inputs.round_to(w, dtype)
+    with pifa.Q4Layer(to_dev(st)) as layer:
+        codes, scales = (t.cpu().numpy() for t in layer.read())
+        # read, made again from what was read, and read again: the same bytes
+        with pifa.Q4Layer.from_mx(_dev(codes), _dev(scales)) as again:
+            c2, s2 = (t.cpu().numpy() for t in again.read())
+        x_dev, x = _x(3, d_in, 10)
+        Y = layer(x_dev)
+        torch.cuda.synchronize()
+    assert np.array_equal(codes, c2) and np.array_equal(scales, s2)
+    got = o.mx_weights(codes, scales)
+    _check(Y, x @ got.T, np.abs(x) @ np.abs(got).T, SUMS, "product")
+    cand, pick = o.mx_candidates(w)
+    for c in range(2):
+        took = scales == cand[c][0]
+        rows = np.repeat(took, 32, axis=1)
+        assert np.array_equal(got[rows], cand[c][1][rows])
+        worse = took & (pick != c) & (cand[0][0] != cand[1][0])
+        assert (np.abs(cand[0][2] - cand[1][2])[worse] <= 2.0 ** -18 * cand[0][2][worse]).all()
+    assert ((scales == cand[0][0]) | (scales == cand[1][0])).all()
+    assert scales[0, 0] == 127 and (codes[0, :16] & 0x77 == 0).all()
+
+
+def test_quantizing_ends_of_the_range():
+    pifa, torch = _pifa(), torch_mod()
+    w = np.zeros((6, 32), np.float32)
+    w[0, 0], w[1, 1], w[2, 2] = np.inf, np.nan, 3.4e38
+    w[3, 3] = 2.0 ** -126
+    w[4, 4] = 2.0 ** -149
+    w[5] = 2.0 ** -120
+    with pifa.Q4Layer(_dev(w)) as layer:
+        codes, scales = (t.cpu().numpy() for t in layer.read())
+        x = torch.ones(1, 32, dtype=torch.bfloat16, device="cuda")
+        y = from_dev(layer(x))[0]
+        q = torch.ones(1, 32, device="cuda").to(torch.float8_e4m3fn)
+        y8 = from_dev(layer.forward_e4m3(q, torch.ones(1, device="cuda")))[0]
+    v = o.mx_weights(codes, scales)
+    assert scales[0, 0] == 255 and scales[1, 0] == 255 and np.isnan(v[:2]).all()
+    assert abs(v[2, 2] / 3.4e38 - 1) <= 0.25 and np.count_nonzero(v[2]) == 1
+    assert abs(v[3, 3] * 2.0 ** 126 - 1) <= 0.25 and (v[4] == 0).all()
+    assert np.array_equal(v[5], w[5].astype(np.float64))
+    for got in (y, y8):
+        assert np.isnan(got[:2]).all() and got[4] == 0
+        assert abs(got[5] / 2.0 ** -115 - 1) <= 2.0 ** -8
+
+
+def test_nan_and_infinite_rows_stay_in_their_rows():
+    torch = torch_mod()
+    d_in, d_out = 224, 50
+    layer, w = _layer(d_in, d_out, 11)
+    with layer:
+        for M in (5, 16, 40, 80, 300):
+            x_dev, x = _x(M, d_in, 12)
+            bad = x_dev.clone()
+            bad[1, 3], bad[M - 1, 223] = float("nan"), float("inf")
+            good, got = from_dev(layer(x_dev)), from_dev(layer(bad))
+            keep = [m for m in range(M) if m not in (1, M - 1)]
+            assert np.array_equal(good[keep], got[keep])
+            assert np.isnan(got[1]).all() and not np.isfinite(got[M - 1][w[:, 223] != 0]).any()
+            q = x_dev.float().to(torch.float8_e4m3fn)
+            s = torch.ones(M, device="cuda")
+            ref = from_dev(layer.forward_e4m3(q, s))
+            qb = q.view(torch.uint8).clone()
+            qb[1, 100] = 0x7F
+            got = from_dev(layer.forward_e4m3(qb.view(torch.float8_e4m3fn), s))
+            keep = [m for m in range(M) if m != 1]
+            assert np.isnan(got[1]).all() and np.array_equal(ref[keep], got[keep])
+
+
+def test_last_rows_of_a_batch_are_all_that_is_read():
+    """Rows behind the last one are neither read nor written: the buffers end there."""
+    torch = torch_mod()
+    d_in, d_out = 352, 30
+    layer, w = _layer(d_in, d_out, 13)
+    with layer:
+        for M in (1, 15, 31, 63, 200):
+            big = torch.full(((M + 300) * d_in,), float("nan"), dtype=torch.bfloat16, device="cuda")
+            x_dev, x = _x(M, d_in, 14)
+            big[:M * d_in] = x_dev.reshape(-1)
+            Ybig, Y = _guarded(M, d_out)
+            layer(big[:M * d_in].view(M, d_in), Y)
+            torch.cuda.synchronize()
+            _check(Y, x @ w.T, np.abs(x) @ np.abs(w).T, SUMS, M)
+            assert (Ybig[M * d_out:] == -17).all()
+
+
+def test_a_block_end_to_end():
+    """Residual, norm and layer as a block runs them: apart, in one call, and
+    with 8-bit rows; the three agree within their roundings."""
+    pifa, torch = _pifa(), torch_mod()
+    d, ff = 1024, 2752
+    w = np.random.default_rng(15).standard_normal((ff, d)) / 32
+    g_dev = (1 + 0.2 * torch.randn(d, device="cuda")).to(torch.bfloat16)
+    with pifa.Q4Layer(to_dev(inputs.round_to(w, "bf16")[0])) as layer:
+        wq = o.mx_weights(*(t.cpu().numpy() for t in layer.read()))
+        # 4-bit weights of a normal matrix: 11.7% off; its product as much
+        assert rel_fro(wq, w) < 0.13
+        for M in (1, 12, 40, 300):
+            x_dev, x = _x(M, d, 16)
+            r_dev, r = _x(M, d, 17)
+            H, H2, H3 = (torch.empty_like(x_dev) for _ in range(3))
+            apart = layer(pifa.rms_norm_forward(x_dev, g_dev, EPS, R=r_dev, H=H))
+            one = layer.norm_forward(x_dev, g_dev, EPS, R=r_dev, H=H2)
+            q, s = pifa.rms_norm_forward_e4m3(x_dev, g_dev, EPS, R=r_dev, H=H3)
+            eight = layer.forward_e4m3(q, s)
+            torch.cuda.synchronize()
+            assert torch.equal(H, H2) and torch.equal(H, H3)
+            _, y = o.rms_norm(x, from_dev(g_dev), EPS, r)
+            want = y @ wq.T
+            assert rel_fro(from_dev(apart), want) < 5e-3 and rel_fro(from_dev(one), want) < 5e-3
+            assert rel_fro(from_dev(eight), want) < 2.0 ** -4  # half a step of e4m3, at most
+            if M > 16:
+                assert torch.equal(apart, one)
+
+
+def test_trained_pifa_block():
+    """norm -> PIFA layer and back: the norm's gradient takes the layer's dX."""
+    import oracle
+    pifa, torch = _pifa(), torch_mod()
+    d_in, d_out, r, M = 256, 320, 96, 40
+    U, V = inputs.lowrank_factors(d_out, d_in, r, seed=7)
+    lay = oracle.build_pifa(U @ V, r)
+    wp_st, wp = inputs.round_to(lay["Wp"], "bf16")
+    c_st, c = inputs.round_to(lay["C"], "bf16")
+    x_dev, x = _x(M, d_in, 18)
+    r_dev, res = _x(M, d_in, 19)
+    g_st, g = inputs.round_to(1.0 + 0.3 * np.random.default_rng(20).standard_normal((1, d_in)), "bf16")
+    g_dev = to_dev(g_st).reshape(-1)
+    dy_st, dy = inputs.round_to(0.1 * np.random.default_rng(21).standard_normal((M, d_out)), "bf16")
+    with pifa.PifaLayer(to_dev(wp_st), to_dev(c_st), lay["pivot_idx"], lay["nonpivot_idx"], d_out) as layer:
+        H = torch.empty_like(x_dev)
+        N = pifa.rms_norm_forward(x_dev, g_dev, EPS, R=r_dev, H=H)
+        Y = layer(N)
+        dN, dH = torch.empty_like(N), torch.empty_like(N)
+        pifa.pifa_layer_backward(layer.handle, N, Y, to_dev(dy_st), dX=dN)
+        _, dg = pifa.rms_norm_backward(H, g_dev, dN, EPS, dR=r_dev, dX=dH)
+        torch.cuda.synchronize()
+    W = np.zeros((d_out, d_in))
+    W[lay["pivot_idx"]], W[lay["nonpivot_idx"]] = wp, c @ wp
+    h, n = o.rms_norm(x, g[0], EPS, res)
+    want, dgain = o.rms_norm_backward(h, g[0], dy @ W, EPS, res)
+    assert rel_fro(from_dev(Y), n @ W.T) < 1e-2   # the layer's bar, its input rounded as well
+    assert rel_fro(from_dev(dH), want) < 1e-2 and rel_fro(from_dev(dg), dgain) < 1e-2
+
+
+def test_no_rows_and_refused_calls():
+    pifa, torch = _pifa(), torch_mod()
+    layer, _ = _layer(64, 24, 22)
+    bf = torch.bfloat16
+    with layer:
+        assert layer(torch.empty(0, 64, dtype=bf, device="cuda")).shape == (0, 24)
+        x, y = torch.zeros(40, 64, dtype=bf, device="cuda"), torch.zeros(40, 24, dtype=bf, device="cuda")
+        assert layer.norm_forward(x[:0], None, EPS).shape == (0, 24)
+        with pytest.raises(ValueError):
+            layer(x[:, :32].contiguous(), y)  # too short
+        with pytest.raises(ValueError):
+            layer(x, y[:39])
+        with pytest.raises(TypeError):
+            layer(x.float(), y)
+        with pytest.raises(ValueError):
+            layer(x.cpu(), y)
+        flat = torch.zeros(40 * 64 + 8, dtype=bf, device="cuda")
+        with pytest.raises(pifa.PifaError) as e:
+            layer(flat[1:40 * 64 + 1].view(40, 64), y)  # not on 16 bytes
+        assert e.value.status == pifa.PIFA_ERR_UNSUPPORTED
+        for H in (x, y.view(-1)[:24 * 40]):
+            with pytest.raises((pifa.PifaError, ValueError)):
+                layer.norm_forward(x, None, EPS, H=H, Y=y)
+        with pytest.raises(pifa.PifaError):
+            layer.norm_forward(x, None, 0.0)
+        assert pifa.q4_layer_weight_bytes(layer.handle) == 24 * (32 + 2)
+    codes, scales = torch.zeros(4, 20, dtype=torch.uint8, device="cuda"), torch.zeros(4, 2, dtype=torch.uint8, device="cuda")
+    with pytest.raises(pifa.PifaError) as e:
+        pifa.Q4Layer.from_mx(codes, scales)  # d_in 40
+    assert e.value.status == pifa.PIFA_ERR_UNSUPPORTED
+    with pytest.raises(ValueError):
+        pifa.Q4Layer.from_mx(torch.zeros(4, 32, dtype=torch.uint8, device="cuda"), scales[:2])
+
+
+def test_captured_and_replayed_beside_eager_work():
+    """Graphs of every form, for few and many rows, replayed on new inputs with
+    eager calls and a growing workspace between."""
+    pifa, torch = _pifa(), torch_mod()
+    d_in, d_out = 512, 200
+    layer, w = _layer(d_in, d_out, 23)
+    g = (1 + 0.2 * torch.randn(d_in, device="cuda")).to(torch.bfloat16)
+    with layer:
+        fresh, _ = _layer(d_in, d_out, 23)
+        for M in (3, 50, 300):
+            x, r = (torch.randn(M, d_in, device="cuda").to(torch.bfloat16) for _ in range(2))
+            q, s = torch.empty(M, d_in, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(M, device="cuda")
+            outs = [torch.empty(M, d_out, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+            H = torch.empty_like(x)
+            layer.reserve(M)
+
+            def calls(lay, outs, H, q, s):
+                lay(x, outs[0])
+                pifa.rms_norm_forward_e4m3(x, g, EPS, R=r, Q=q, scale=s)
+                lay.forward_e4m3(q, s, outs[1])
+                lay.norm_forward(x, g, EPS, R=r, H=H, Y=outs[2])
+
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.stream(side):
+                calls(layer, outs, H, q, s)
+                side.synchronize()
+                with torch.cuda.graph(graph, stream=side):
+                    calls(layer, outs, H, q, s)
+            # the workspace grows behind the graph's back: what it captured stays valid
+            layer.reserve(4 * M + 100)
+            for i in range(3):
+                for t in (x, r):
+                    t.copy_(torch.randn(M, d_in, device="cuda"))
+                for t in outs:
+                    t.fill_(float("nan"))
+                graph.replay()
+                torch.cuda.synchronize()
+                o2, H2 = [torch.empty_like(t) for t in outs], torch.empty_like(H)
+                calls(fresh, o2, H2, torch.empty_like(q), torch.empty_like(s))
+                torch.cuda.synchronize()
+                assert torch.equal(H, H2), (M, i)
+                for a, b in zip(outs, o2):
+                    assert torch.equal(a, b), (M, i)
+        fresh.close()
+
+
+def test_capture_does_not_grow_the_workspace():
+    pifa, torch = _pifa(), torch_mod()
+    layer, _ = _layer(64, 24, 24)
+    with layer:
+        x, y = torch.zeros(40, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(40, 24, dtype=torch.bfloat16, device="cuda")
+        side = torch.cuda.Stream()
+        graph = torch.cuda.CUDAGraph()
+        status = None
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graph, stream=side):
+                y.add_(1)
+                try:
+                    layer.norm_forward(x, None, EPS, Y=y)
+                except pifa.PifaError as e:
+                    status = e.status
+        assert status == pifa.PIFA_ERR_TOO_LARGE
+        layer.reserve(40)
+        layer.norm_forward(x, None, EPS, Y=y)
+        torch.cuda.synchronize()
+        assert (y == 0).all()
+
+
+def test_two_streams_at_once():
+    """Products of one layer need no workspace: calls on two streams may overlap."""
+    torch = torch_mod()
+    layer, w = _layer(1024, 512, 25)
+    with layer:
+        xs = [_x(M, 1024, 26 + M) for M in (4, 100)]
+        want = [layer(x) for x, _ in xs]
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in xs]
+        outs = [torch.empty_like(t) for t in want]
+        for _ in range(10):
+            for st, (x, _), y in zip(streams, xs, outs):
+                with torch.cuda.stream(st):
+                    layer(x, y)
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
