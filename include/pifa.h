@@ -368,7 +368,7 @@ size_t rms_norm_backward_bytes(int64_t M, int64_t d);
  * the OCP microscaling format: a code is a sign bit above the index into
  * {0, 0.5, 1, 1.5, 2, 3, 4, 6}, 32 consecutive weights of a row share an 8-bit
  * power of two, and scale 255 makes them NaN.  17/32 of a byte per weight.
- * d_in must be a multiple of 32 (PIFA_ERR_UNSUPPORTED) and at most 2^22.
+ * d_in must be a multiple of 32 (PIFA_ERR_UNSUPPORTED) and at most 2^21.
  *
  * (A low-rank pair U V^T keeps its accuracy in this format as two such layers
  * in a row.  PIFA's W_p and C do not: C rebuilds the non-pivot outputs with

@@ -32,6 +32,7 @@
 #include "prepack.hpp"
 #include "probe.hpp"
 #include "q4.hpp"
+#include "q4_gemm.hpp"
 
 using namespace pifa;
 
@@ -2316,7 +2317,7 @@ struct q4_layer {
 
 namespace {
 
-constexpr int64_t kQ4MaxIn = 1ll << 22;  // a row's 64-row tile of X stays inside 31-bit offsets
+constexpr int64_t kQ4MaxIn = 1ll << 21;  // 256 rows of X stay inside 31-bit offsets
 
 void free_q4(q4_layer* h) {
     if (!h) return;
@@ -2378,6 +2379,12 @@ void q4_few_launch(const Q4Args& p, hipStream_t st) {
                        dim3(WAVES * kWave), 0, st, p);
 }
 
+template <int ACT, int BM, int BN, int WM, int WN, int S, int OCC>
+void q4_tiles_launch(const Q4Args& p, hipStream_t st) {
+    hipLaunchKernelGGL((q4_tiles<ACT, BM, BN, WM, WN, S, OCC>),
+                       dim3((unsigned)(ceil_div(p.M, BM) * ceil_div(p.N, BN))), dim3(8 * kWave), 0, st, p);
+}
+
 // Rows of one launch: grid.y counts tiles of at least 16 rows.
 constexpr int64_t kQ4MaxRows = 1 << 19;
 
@@ -2393,7 +2400,9 @@ hipError_t launch_q4(Q4Args p, hipStream_t st) {
         q.Y = p.Y + m * p.N;
         if (q.M <= 16) q4_few_launch<ACT, false, 1, 1, 8, 2>(q, st);
         else if (q.M <= 32) q4_few_launch<ACT, false, 2, 2, 8, 1>(q, st);
-        else q4_few_launch<ACT, false, 4, 4, 8, 1>(q, st);
+        else if (q.M <= 64) q4_few_launch<ACT, false, 4, 4, 8, 1>(q, st);
+        else if (ceil_div(q.M, 256) * ceil_div(q.N, 256) >= kCus) q4_tiles_launch<ACT, 256, 256, 2, 4, 3, 2>(q, st);
+        else q4_tiles_launch<ACT, 128, 128, 2, 4, 3, 4>(q, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

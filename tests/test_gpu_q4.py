@@ -109,6 +109,31 @@ def test_forward_e4m3(shape):
             assert (big[M * d_out:] == -17).all()
 
 
+@pytest.mark.parametrize("M,d_in,d_out", [(2050, 96, 8100), (4100, 352, 4096), (300, 64, 60000)])
+def test_many_tiles(M, d_in, d_out):
+    """Products of more than 256 tiles of 256 x 256, in both forms (fp64 on the
+    GPU: the product is large)."""
+    torch = torch_mod()
+    layer, w = _layer(d_in, d_out, 31)
+    with layer:
+        x_dev, _ = _x(M, d_in, 32)
+        q = x_dev.float().to(torch.float8_e4m3fn)
+        s = torch.rand(M, device="cuda") + 0.5
+        wd = _dev(w)
+        top = lambda a: a.abs().view(a.shape[0], -1, 32).amax(2)
+        for x, f, run in ((x_dev.double(), 1.0, lambda Y: layer(x_dev, Y)),
+                          (q.double(), s.double()[:, None], lambda Y: layer.forward_e4m3(q, s, Y))):
+            big, Y = _guarded(M, d_out)
+            run(Y)
+            want = f * (x @ wd.t().contiguous())
+            mags = SUMS * (x.abs() @ wd.abs().t().contiguous())
+            if torch.is_tensor(f):
+                mags = f * (mags + 2.0 ** -9 * (top(x) @ top(wd).t().contiguous()))
+            off = (Y.double() - want).abs() - want.abs() * 2.0 ** -8 - mags
+            assert torch.isfinite(Y).all() and float(off.max()) <= 0, (M, d_in, d_out, float(off.max()))
+            assert (big[M * d_out:] == -17).all()
+
+
 @pytest.mark.parametrize("with_r,with_gain,with_h", [(True, True, True), (False, True, False), (True, False, True),
                                                      (False, False, True)])
 @pytest.mark.parametrize("shape", [(32, 5), (96, 40), (1024, 333), (4096, 97)])
