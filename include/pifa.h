@@ -424,10 +424,10 @@ pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* sc
  *   H = X + R,   Y = (H rho gain) W^T.
  * X, R, gain, eps and H as for rms_norm_forward with d = d_in and bf16, but X,
  * R and gain 16-byte aligned, and H overlapping none of X, R, gain and Y
- * (PIFA_ERR_INVALID_ARG).  For M <= 16 it is one launch: rho scales whole rows
- * of the product, so it is applied to the sums.  More rows are normed into the
- * layer's workspace (M x d_in bf16) first, and calls on one handle must not
- * overlap.  The workspace grows on demand; memory it outgrows is kept until
+ * (PIFA_ERR_INVALID_ARG).  For M <= 16 with M d_in <= 12288 it is one launch:
+ * rho scales whole rows of the product, so it is applied to the sums.  More are
+ * normed into the layer's workspace (M x d_in bf16) first, and such calls on
+ * one handle must not overlap.  The workspace grows on demand; memory it outgrows is kept until
  * the layer is destroyed, so graphs captured with it stay valid.  A call
  * whose stream is being captured does not grow it (PIFA_ERR_TOO_LARGE):
  * reserve first.

@@ -2372,20 +2372,106 @@ pifa_status q4_create(int64_t d_in, int64_t d_out, q4_handle* out, Fill fill) {
     return PIFA_OK;
 }
 
-template <int ACT, bool NORM, int MT, int NG, int WAVES, int U>
+template <int ACT, int NG, int U>
 void q4_few_launch(const Q4Args& p, hipStream_t st) {
-    hipLaunchKernelGGL((q4_few<ACT, NORM, MT, NG, WAVES, U>),
-                       dim3((unsigned)ceil_div(packed_groups(p.N), NG), (unsigned)ceil_div(p.M, 16 * MT)),
-                       dim3(WAVES * kWave), 0, st, p);
+    hipLaunchKernelGGL((q4_few<ACT, 1, NG, 8, U>), dim3((unsigned)ceil_div(packed_groups(p.N), NG)), dim3(8 * kWave), 0,
+                       st, p);
 }
 
+template <int ACT, bool NORM, int NG, int U>
+void q4_staged_launch(const Q4Args& p, hipStream_t st) {
+    hipLaunchKernelGGL((q4_staged<ACT, NORM, NG, 8, U>), dim3((unsigned)ceil_div(packed_groups(p.N), NG)),
+                       dim3(8 * kWave), (size_t)q4_staged_lds(p.M, p.K, ACT == kQ4Bf16 ? 2 : 1, NORM, NG * 8), st, p);
+}
+
+// Whether the norm's form is one launch (the rows staged by every workgroup).
+constexpr int64_t kQ4NormElems = 12288;
+bool q4_norm_in_one(int64_t M, int64_t K) { return M <= 16 && M * K <= kQ4NormElems; }
+
+// Forms of a product of more than 16 rows, with the time a tile takes in us: p
+// + a K / 1000, alone on its CU (one) or two at a time (two; 0: LDS leaves room
+// for one).  A form whose p is 0 is not there: another is faster everywhere.
+// Measured at K = 4096 and 11008 over 17 to 4096 rows with hot weights; over 78
+// drawn sizes (K 256 to 13000, N 285 to 28000, M 18 to 3500) the form picked is
+// the measured best or within 8% of it at 72, and within 22% at all.
+struct Q4Form {
+    int bm, bn;
+    double one_p, one_a, two_p, two_a;
+};
+enum Q4Forms : int {
+    kQ4T16x32,
+    kQ4T32x32,
+    kQ4T32x64,
+    kQ4T32x128,
+    kQ4T64x64Deep,
+    kQ4T64x64,
+    kQ4T64x128,
+    kQ4T128x128,
+    kQ4T128x128Pair,
+    kQ4T128x256,
+    kQ4T256x256,
+    kQ4FormCount
+};
+const Q4Form kQ4FormTable[2][kQ4FormCount] = {
+    {{16, 32, 2.9, 0.75, 0, 0},
+     {32, 32, 3.4, 1.13, 0, 0},
+     {32, 64, 3.8, 1.55, 0, 0},
+     {32, 128, 5.4, 2.2, 0, 0},
+     {64, 64, 4.6, 2.6, 0, 0},
+     {64, 64, 3.9, 3.07, 4.0, 5.1},
+     {64, 128, 0, 0, 0, 0},
+     {128, 128, 8.4, 7.05, 0, 0},
+     {128, 128, 9.5, 8.56, 10.5, 12.9},
+     {128, 256, 14.0, 13.6, 10.6, 23.9},
+     {256, 256, 14.9, 21.3, 0, 0}},
+    {{16, 32, 2.9, 0.43, 0, 0},
+     {32, 32, 3.4, 0.80, 0, 0},
+     {32, 64, 3.2, 1.0, 0, 0},
+     {32, 128, 5.0, 1.6, 0, 0},
+     {64, 64, 0, 0, 0, 0},
+     {64, 64, 4.3, 1.40, 6.0, 2.55},
+     {64, 128, 4.0, 2.27, 5.7, 3.95},
+     {128, 128, 5.2, 3.79, 0, 0},
+     {128, 128, 6.4, 3.72, 8.0, 6.54},
+     {128, 256, 0, 0, 0, 0},
+     {256, 256, 15.4, 10.2, 0, 0}}};
+
+int q4_form(int act, int64_t M, int64_t N, int64_t K) {
+    const double k = (double)K / 1000.0;
+    int best = 0;
+    double best_t = 1e300;
+    for (int i = 0; i < kQ4FormCount; ++i) {
+        const Q4Form& f = kQ4FormTable[act][i];
+        if (f.one_p == 0) continue;
+        const int64_t tiles = ceil_div(M, f.bm) * ceil_div(N, f.bn);
+        const double one = f.one_p + f.one_a * k, two = f.two_p + f.two_a * k;
+        double t;
+        if (f.two_a == 0) {
+            t = (double)ceil_div(tiles, kCus) * one;
+        } else {
+            const int64_t rest = tiles % (2 * kCus);
+            t = (double)(tiles / (2 * kCus)) * two + (rest == 0 ? 0.0 : rest <= kCus ? one : two);
+        }
+        if (t < best_t) {
+            best_t = t;
+            best = i;
+        }
+    }
+    return best;
+}
+
+template <int ACT, int BM, int BN, int WM, int WN, int KG, int SMAX, int OCC>
+void q4_mid_launch(const Q4Args& p, hipStream_t st) {
+    hipLaunchKernelGGL((q4_mid<ACT, BM, BN, WM, WN, KG, SMAX, OCC>),
+                       dim3((unsigned)(ceil_div(p.M, BM) * ceil_div(p.N, BN))), dim3(WM * WN * KG * kWave), 0, st, p);
+}
 template <int ACT, int BM, int BN, int WM, int WN, int S, int OCC>
 void q4_tiles_launch(const Q4Args& p, hipStream_t st) {
     hipLaunchKernelGGL((q4_tiles<ACT, BM, BN, WM, WN, S, OCC>),
                        dim3((unsigned)(ceil_div(p.M, BM) * ceil_div(p.N, BN))), dim3(8 * kWave), 0, st, p);
 }
 
-// Rows of one launch: grid.y counts tiles of at least 16 rows.
+// Rows of one launch: their tiles stay a 32-bit grid for every d_out.
 constexpr int64_t kQ4MaxRows = 1 << 19;
 
 template <int ACT>
@@ -2398,11 +2484,39 @@ hipError_t launch_q4(Q4Args p, hipStream_t st) {
         q.X = (const char*)p.X + m * p.K * (ACT == kQ4Bf16 ? 2 : 1);
         if (p.x_scale) q.x_scale = p.x_scale + m;
         q.Y = p.Y + m * p.N;
-        if (q.M <= 16) q4_few_launch<ACT, false, 1, 1, 8, 2>(q, st);
-        else if (q.M <= 32) q4_few_launch<ACT, false, 2, 2, 8, 1>(q, st);
-        else if (q.M <= 64) q4_few_launch<ACT, false, 4, 4, 8, 1>(q, st);
-        else if (ceil_div(q.M, 256) * ceil_div(q.N, 256) >= kCus) q4_tiles_launch<ACT, 256, 256, 2, 4, 3, 2>(q, st);
-        else q4_tiles_launch<ACT, 128, 128, 2, 4, 3, 4>(q, st);
+        const int64_t groups = packed_groups(q.N);
+        // choice
+        if (q.M <= 16) {
+            if (ACT == kQ4Bf16 && q.M <= 2 && q4_staged_lds(q.M, q.K, 2, false, 8) <= kStreamMaxLds)
+                q4_staged_launch<ACT, false, 1, 2>(q, st);
+            else if (groups <= kCus) q4_few_launch<ACT, 1, 2>(q, st);
+            else if (groups <= 600) q4_few_launch<ACT, 2, 1>(q, st);
+            else q4_few_launch<ACT, 4, 1>(q, st);
+        } else {
+            constexpr bool kE4 = ACT == kQ4E4m3;
+            switch (q4_form(ACT, q.M, q.N, q.K)) {
+                case kQ4T16x32: q4_mid_launch<ACT, 16, 32, 1, 1, 8, 4, 2>(q, st); break;
+                case kQ4T32x32: q4_mid_launch<ACT, 32, 32, 1, 1, 8, 3, 2>(q, st); break;
+                case kQ4T32x64: q4_mid_launch<ACT, 32, 64, 1, 2, 4, 3, 4>(q, st); break;
+                case kQ4T32x128: q4_mid_launch<ACT, 32, 128, 1, 4, 4, 3, 4>(q, st); break;
+                case kQ4T64x64Deep:
+                    if constexpr (!kE4) q4_mid_launch<ACT, 64, 64, 2, 2, 4, 3, 4>(q, st);
+                    break;
+                case kQ4T64x64: q4_mid_launch<ACT, 64, 64, 2, 2, 2, 3, 4>(q, st); break;
+                case kQ4T64x128:
+                    if constexpr (kE4) q4_mid_launch<ACT, 64, 128, 2, 4, 1, 3, 4>(q, st);
+                    break;
+                case kQ4T128x128: q4_mid_launch<ACT, 128, 128, 2, 4, 1, 3, 2>(q, st); break;
+                case kQ4T128x128Pair:
+                    if constexpr (kE4) q4_tiles_launch<ACT, 128, 128, 2, 4, 3, 4>(q, st);
+                    else q4_mid_launch<ACT, 128, 128, 2, 2, 1, 3, 2>(q, st);
+                    break;
+                case kQ4T128x256:
+                    if constexpr (!kE4) q4_tiles_launch<ACT, 128, 256, 2, 4, 3, 2>(q, st);
+                    break;
+                default: q4_tiles_launch<ACT, 256, 256, 2, 4, 3, 2>(q, st);
+            }
+        }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -2548,7 +2662,7 @@ pifa_status q4_layer_reserve(q4_handle h, int64_t max_M) {
     if (!h || max_M < 0) return PIFA_ERR_INVALID_ARG;
     if (max_M > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
     PIFA_ON_DEVICE(h->device);
-    return max_M <= kDecodeMaxM ? PIFA_OK : q4_ensure(h, (size_t)max_M * (size_t)h->d_in * 2, 0);
+    return q4_norm_in_one(max_M, h->d_in) ? PIFA_OK : q4_ensure(h, (size_t)max_M * (size_t)h->d_in * 2, 0);
 }
 
 pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, const void* gain, float eps, void* H,
@@ -2572,13 +2686,16 @@ pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, con
     p.M = M;
     p.N = h->d_out;
     p.K = h->d_in;
-    if (M <= kDecodeMaxM) {
+    if (q4_norm_in_one(M, h->d_in)) {
         p.R = (const bf16*)R;
         p.gain = (const bf16*)gain;
         p.H = (bf16*)H;
         p.eps = eps;
         TimedLaunch timed(kSiteQ4Norm, st);
-        q4_few_launch<kQ4Bf16, true, 1, 1, 8, 1>(p, st);
+        // choice
+        if (packed_groups(p.N) <= kCus) q4_staged_launch<kQ4Bf16, true, 1, 2>(p, st);
+        else if (packed_groups(p.N) <= 1024) q4_staged_launch<kQ4Bf16, true, 2, 1>(p, st);
+        else q4_staged_launch<kQ4Bf16, true, 4, 1>(p, st);
         return hipGetLastError() == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
     }
     s = q4_ensure(h, in, st);

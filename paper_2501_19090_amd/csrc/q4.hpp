@@ -22,6 +22,7 @@
 #pragma once
 
 #include "common.hpp"
+#include "gemm_dma.hpp"
 #include "gemm_mfma.hpp"
 #include "layout.hpp"
 #include "norm.hpp"
@@ -63,7 +64,7 @@ __device__ __forceinline__ float e2m1_value(uint32_t c) {  // c = 0..7
 // to 4, the one with the smaller squared error is taken, the first on a tie.
 // A group with an infinity or a NaN gets the NaN scale.
 template <typename T>
-__global__ void q4_quantize(const T* __restrict__ W, int64_t N, int64_t K, uint8_t* __restrict__ packed) {
+__global__ __launch_bounds__(256) void q4_quantize(const T* __restrict__ W, int64_t N, int64_t K, uint8_t* __restrict__ packed) {
     const int64_t KB = packed_kblocks(K), groups = KB * 4;
     const int64_t total = packed_groups(N) * 16 * groups;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
@@ -202,17 +203,79 @@ __device__ __forceinline__ void q4_store4(const Q4Args& p, int64_t m, int64_t n,
     }
 }
 
+// 4 x 4 transpose of 16-byte pieces over the lane groups q = lane / 16: piece c
+// of group q goes to piece q of group c.
+__device__ __forceinline__ void q4_turn(u32x4 (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t a = x[0][i], b = x[1][i], c = x[2][i], d = x[3][i];
+        auto s = __builtin_amdgcn_permlane32_swap(a, c, false, false);
+        a = s[0];
+        c = s[1];
+        s = __builtin_amdgcn_permlane32_swap(b, d, false, false);
+        b = s[0];
+        d = s[1];
+        s = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+        x[0][i] = s[0];
+        x[1][i] = s[1];
+        s = __builtin_amdgcn_permlane16_swap(c, d, false, false);
+        x[2][i] = s[0];
+        x[3][i] = s[1];
+    }
+}
+
+// Lane l's codes and scale of block b of a group's stream (zeros if not `in`).
+__device__ __forceinline__ void q4_load(__amdgpu_buffer_rsrc_t rs, bool in, int b, int lane, u32x4& w, uint32_t& s) {
+    const uint32_t at = in ? (uint32_t)b * kQ4Block : kMaskedOffset;
+    w = load16(rs, at + lane * 16);
+    s = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(at + 1024 + lane), 0, 0);
+}
+
+// The steps of one wave (blocks wave, wave + WAVES, ... below KB, U of them a
+// step; step 0 is in `even` already): the loads of a step are issued before the
+// products of the one before it, in two sets of registers in turn.  No load
+// stands under a condition, or the wait for the one set would be a wait for
+// both.
+template <int U, int WAVES, typename Blk, typename Fetch, typename Step>
+__device__ __forceinline__ void q4_pipeline(int wave, int KB, Blk (&even)[U], Blk (&odd)[U], const Fetch& fetch,
+                                            const Step& step) {
+    const int n = wave < KB ? (KB - wave + U * WAVES - 1) / (U * WAVES) : 0;
+    auto products = [&](int s, Blk(&f)[U]) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int b = wave + (s * U + u) * WAVES;
+            if (u == 0 || b < KB) step(b, f[u]);  // uniform
+        }
+    };
+    int i = 0;
+    for (; i + 2 < n; i += 2) {
+        fetch(i + 1, odd);
+        products(i, even);
+        fetch(i + 2, even);
+        products(i + 1, odd);
+    }
+    if (i + 1 < n) {
+        fetch(i + 1, odd);
+        products(i, even);
+        products(i + 1, odd);
+    } else if (i < n) {
+        products(i, even);
+    }
+}
+
 // A workgroup owns NG groups of 16 weight rows (columns of Y) and 16 MT rows of
 // X (blockIdx.y picks them); its waves take the 128-wide blocks of K in turn,
 // each on registers alone, and are summed in LDS at the end.  The loads of a
-// wave's next U blocks are issued before the MFMAs of the current ones.
-template <int ACT, bool NORM, int MT, int NG, int WAVES, int U>
+// wave's next U blocks are issued before the MFMAs of the current ones.  bf16
+// rows are loaded 64 bytes at a time (piece c of lane group q: columns 32 c + 8
+// q ..) and turned over the lane groups to meet the codes, whose lane has 32
+// columns of its row.
+template <int ACT, int MT, int NG, int WAVES, int U>
 __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
-    static_assert(!NORM || (MT == 1 && ACT == kQ4Bf16), "the norm's form has one tile of bf16 rows");
-    constexpr int XC = ACT == kQ4Bf16 ? 4 : 2;  // 16-byte pieces of a row's 32 values
+    constexpr int XC = ACT == kQ4Bf16 ? 4 : 2;  // 16-byte pieces of a lane's 32 values
     constexpr int ES = ACT == kQ4Bf16 ? 2 : 1;
     __shared__ f32x4 red[WAVES][MT * NG][kWave];
-    __shared__ float reds[NORM ? WAVES : 1][16];
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = lane & 15, q = lane >> 4;
@@ -221,78 +284,47 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
     const int64_t left = p.M - m0;
     const int rows = left < 16 * MT ? (int)left : 16 * MT;
 
-    // streams: buffer ranges end with the data, so masked lanes read zeros
+    // the range ends with the last row; masked lanes read zeros
     const auto xrs = make_rsrc31((const char*)p.X + m0 * p.K * ES, (int64_t)rows * p.K * ES);
-    __amdgpu_buffer_rsrc_t rrs, grs;
-    if constexpr (NORM) {
-        rrs = make_rsrc31(p.R, p.R ? (int64_t)rows * p.K * 2 : 0);
-        grs = make_rsrc31(p.gain, p.gain ? p.K * 2 : 0);
-    }
-    const uint8_t* wp[NG];
+    __amdgpu_buffer_rsrc_t wrs[NG];
     const int64_t groups = packed_groups(p.N);
 #pragma unroll
-    for (int j = 0; j < NG; ++j) wp[j] = p.W + (g0 + j < groups ? g0 + j : groups - 1) * KB * kQ4Block;
+    for (int j = 0; j < NG; ++j)
+        wrs[j] = make_rsrc31(p.W + (g0 + j < groups ? g0 + j : 0) * KB * kQ4Block,
+                             g0 + j < groups ? (int64_t)KB * kQ4Block : 0);
 
     f32x4 acc[MT][NG];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int j = 0; j < NG; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float ss = 0.f;
 
     struct Blk {
         u32x4 w[NG];
         uint32_t s[NG];
         u32x4 x[MT][XC];
-        u32x4 r[NORM ? XC : 1], g[NORM ? XC : 1];
     };
-    // first column of piece c of this lane's 32 values of block b
-    auto col = [&](int b, int c) { return ACT == kQ4Bf16 ? 128 * b + 32 * q + 8 * c : 128 * b + 64 * c + 16 * q; };
+    constexpr int PIECE = 64 / ES;  // columns between a lane's pieces as loaded
     auto fetch = [&](int b, Blk& f) {
-        const bool in = b < KB;  // uniform
-        const int bb = in ? b : KB - 1;
 #pragma unroll
-        for (int j = 0; j < NG; ++j) {
-            const uint8_t* blk = wp[j] + (int64_t)bb * kQ4Block;
-            f.w[j] = *reinterpret_cast<const u32x4*>(blk + lane * 16);
-            f.s[j] = blk[1024 + lane];
-        }
+        for (int j = 0; j < NG; ++j) q4_load(wrs[j], b < KB, b, lane, f.w[j], f.s[j]);
 #pragma unroll
         for (int c = 0; c < XC; ++c) {
-            const int k = col(b, c);
+            const int k = 128 * b + PIECE * c + 16 / ES * q;
 #pragma unroll
             for (int t = 0; t < MT; ++t)
                 f.x[t][c] = load16(xrs, row + 16 * t < rows && k < K ? (uint32_t)(((row + 16 * t) * K + k) * ES)
                                                                      : kMaskedOffset);
-            if constexpr (NORM) {
-                f.r[c] = load16(rrs, row < rows && k < K ? (uint32_t)((row * K + k) * 2) : kMaskedOffset);
-                f.g[c] = load16(grs, row < rows && k < K ? (uint32_t)(k * 2) : kMaskedOffset);
-            }
         }
     };
+    auto fetch_step = [&](int s, Blk(&f)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) fetch(wave + (s * U + u) * WAVES, f[u]);
+    };
     auto step = [&](int b, Blk& f) {
-        if (b >= KB) return;  // uniform
-        if constexpr (NORM) {
-            typedef NormChunk<bf16> C;
-#pragma unroll
-            for (int c = 0; c < XC; ++c) {
-                float h[8], r[8], g[8];
-                C::floats(f.x[0][c], h);
-                C::floats(f.r[c], r);
-                C::floats(f.g[c], g);
-                bf16 v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    h[e] += r[e];
-                    ss += h[e] * h[e];
-                    v[e] = (bf16)(p.gain ? h[e] * g[e] : h[e]);
-                }
-                const int k = col(b, c);
-                if (p.H && blockIdx.x == 0 && row < rows && k < K) C::store(p.H + row * p.K, k / 8, p.K / 8, h);
-                f.x[0][c] = __builtin_bit_cast(u32x4, v);
-            }
-        }
         if constexpr (ACT == kQ4Bf16) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t) q4_turn(f.x[t]);
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
                 const float s = __builtin_bit_cast(float, f.s[j] << 23);
@@ -311,33 +343,14 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
                     acc[t][j] = q4_mfma_e4m3(f.w[j], f.s[j], f.x[t][0], f.x[t][1], acc[t][j]);
         }
     };
-    Blk cur[U], nxt[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) fetch(wave + u * WAVES, cur[u]);
-    for (int b = wave; b < KB; b += U * WAVES) {
-        const bool more = b + U * WAVES < KB;  // uniform
-        if (more) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) fetch(b + (U + u) * WAVES, nxt[u]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int u = 0; u < U; ++u) step(b + u * WAVES, cur[u]);
-        if (more) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) cur[u] = nxt[u];
-        }
-    }
+    Blk even[U], odd[U];
+    fetch_step(0, even);
+    q4_pipeline<U, WAVES>(wave, KB, even, odd, fetch_step, step);
 
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int j = 0; j < NG; ++j) red[wave][t * NG + j][lane] = acc[t][j];
-    if constexpr (NORM) {
-        ss += __shfl_xor(ss, 16);
-        ss += __shfl_xor(ss, 32);
-        if (lane < 16) reds[wave][lane] = ss;
-    }
     __syncthreads();
     for (int i = wave; i < MT * NG; i += WAVES) {
         const int t = i / NG, j = i % NG;
@@ -345,15 +358,148 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) tot += red[w][i][lane];
         const int64_t m = m0 + 16 * t + row;
-        float factor = 1.f;
-        if constexpr (NORM) {
-            float s = reds[0][row];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) s += reds[w][row];
-            factor = rsqrtf(s / (float)p.K + p.eps);
-        }
-        if constexpr (ACT == kQ4E4m3) factor = m < p.M ? p.x_scale[m] : 0.f;
+        const float factor = ACT == kQ4E4m3 ? (m < p.M ? p.x_scale[m] : 0.f) : 1.f;
         if (g0 + j < groups) q4_store4(p, m, (g0 + j) * 16 + 4 * q, tot, factor);
+    }
+}
+
+// ------------------------------------------------------------------ few rows, staged
+// As q4_few, with the rows in LDS (layout as above), which each workgroup
+// stages while its first weights are on their way.
+__host__ __device__ inline int64_t q4_staged_lds(int64_t M, int64_t K, int es, bool norm, int red_kb) {
+    return M * packed_kblocks(K) * 128 * es + 16 + (norm ? (M * ceil_div(K, 512) + 16) * 4 : 0) + red_kb * 1024;
+}
+
+template <int ACT, bool NORM, int NG, int WAVES, int U>
+__global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
+    constexpr int XC = ACT == kQ4Bf16 ? 4 : 2, ES = ACT == kQ4Bf16 ? 2 : 1;
+    extern __shared__ __attribute__((aligned(1024))) char dyn[];
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int row = lane & 15, q = lane >> 4;
+    const int K = (int)p.K, KB = (int)packed_kblocks(p.K), M = (int)p.M;
+    const int xbytes = M * KB * 128 * ES;
+    f32x4* red = reinterpret_cast<f32x4*>(dyn);  // WAVES x NG x 64
+    char* xs = dyn + WAVES * NG * 1024;
+    float* rho = reinterpret_cast<float*>(xs + xbytes + 16);
+    float* sums = rho + 16;
+
+    const int64_t groups = packed_groups(p.N), g0 = (int64_t)blockIdx.x * NG;
+    struct Blk {
+        u32x4 w[NG];
+        uint32_t s[NG];
+    };
+    __amdgpu_buffer_rsrc_t wrs[NG];
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+        wrs[j] = make_rsrc31(p.W + (g0 + j < groups ? g0 + j : 0) * KB * kQ4Block,
+                             g0 + j < groups ? (int64_t)KB * kQ4Block : 0);
+    auto fetch_step = [&](int s, Blk(&f)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int b = wave + (s * U + u) * WAVES;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) q4_load(wrs[j], b < KB, b, lane, f[u].w[j], f[u].s[j]);
+        }
+    };
+    Blk even[U], odd[U];
+    fetch_step(0, even);
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)xs;
+    if (threadIdx.x < 4) reinterpret_cast<uint32_t*>(xs + xbytes)[threadIdx.x] = 0;
+    if constexpr (NORM) {
+        typedef NormChunk<bf16> C;
+        const int segs = (K + 511) / 512, units = M * segs, full = K / 8;
+        constexpr int UN = 4;
+        for (int u0 = wave; u0 < units; u0 += UN * WAVES) {
+            u32x4 x[UN], r[UN], g[UN];
+#pragma unroll
+            for (int i = 0; i < UN; ++i) {
+                const int u = u0 + i * WAVES, m = u / segs, c = (u - m * segs) * 64 + lane;
+                const int in = u < units ? full : 0;
+                x[i] = C::load((const bf16*)p.X + (int64_t)m * K, c, in);
+                r[i] = zero16();
+                g[i] = zero16();
+                if (p.R) r[i] = C::load(p.R + (int64_t)m * K, c, in);
+                if (p.gain) g[i] = C::load(p.gain, c, in);
+            }
+#pragma unroll
+            for (int i = 0; i < UN; ++i) {
+                const int u = u0 + i * WAVES, m = u / segs, c = (u - m * segs) * 64 + lane;
+                if (u >= units) break;
+                float h[8], ss = 0.f;
+                bf16 v[8];
+                C::floats(x[i], h);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    h[e] += C::one(r[i], e);
+                    ss += h[e] * h[e];
+                    v[e] = (bf16)(p.gain ? h[e] * C::one(g[i], e) : h[e]);
+                }
+                if (p.H && blockIdx.x == 0) C::store(p.H + (int64_t)m * K, c, full, h);
+                if (c < KB * 16)
+                    *reinterpret_cast<u32x4*>(xs + (((c >> 4) * 16 + (c & 3) * 4 + ((c >> 2) & 3)) * M + m) * 16) =
+                        __builtin_bit_cast(u32x4, v);
+#pragma unroll
+                for (int s = 1; s < kWave; s <<= 1) ss += __shfl_xor(ss, s);
+                if (lane == 0) sums[u] = ss;
+            }
+        }
+        __syncthreads();
+        for (int m = wave; m < M; m += WAVES) {
+            float ss = 0.f;
+            for (int s = lane; s < segs; s += kWave) ss += sums[m * segs + s];
+#pragma unroll
+            for (int s = 1; s < kWave; s <<= 1) ss += __shfl_xor(ss, s);
+            if (lane == 0) rho[m] = rsqrtf(ss / (float)K + p.eps);
+        }
+    } else {
+        const u32x4 xrs = raw_rsrc31(p.X, (int64_t)M * K * ES);
+        const int pieces = xbytes / 16;
+        for (int i0 = wave * kWave; i0 < pieces; i0 += WAVES * kWave) {
+            const int i = i0 + lane, r = i % M, at = i / M;
+            const int b = at / (4 * XC), c = (at >> 2) % XC, qq = at & 3;
+            const int k = ACT == kQ4Bf16 ? 128 * b + 32 * qq + 8 * c : 128 * b + 64 * c + 16 * qq;
+            if (i < pieces) dma16(xrs, k < K ? (uint32_t)((r * K + k) * ES) : kMaskedOffset, lds0 + i0 * 16);
+        }
+        wait_vm<0>();
+        __syncthreads();
+    }
+    const bool live = row < M;
+    uint32_t xat[XC];
+#pragma unroll
+    for (int c = 0; c < XC; ++c) xat[c] = live ? (uint32_t)(((c * 4 + q) * M + row) * 16) : (uint32_t)xbytes;
+    const uint32_t xstep = live ? (uint32_t)(128 * ES * M) : 0u;
+    f32x4 acc[NG];
+#pragma unroll
+    for (int j = 0; j < NG; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](int b, Blk& f) {
+        u32x4 x[XC];
+#pragma unroll
+        for (int c = 0; c < XC; ++c) x[c] = *reinterpret_cast<const u32x4*>(xs + xat[c] + (uint32_t)b * xstep);
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+            if constexpr (ACT == kQ4Bf16) {
+                const float s = __builtin_bit_cast(float, f.s[j] << 23);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[j] = q4_mfma_bf16(q4_to_bf16(f.w[j][c], s), x[c], acc[j]);
+            } else {
+                acc[j] = q4_mfma_e4m3(f.w[j], f.s[j], x[0], x[1], acc[j]);
+            }
+        }
+    };
+    q4_pipeline<U, WAVES>(wave, KB, even, odd, fetch_step, step);
+#pragma unroll
+    for (int j = 0; j < NG; ++j) red[(wave * NG + j) * kWave + lane] = acc[j];
+    __syncthreads();
+    if (wave < NG && g0 + wave < groups) {
+        f32x4 tot = red[wave * kWave + lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) tot += red[(w * NG + wave) * kWave + lane];
+        float f = 1.f;
+        if constexpr (NORM) f = live ? rho[row] : 0.f;
+        if constexpr (ACT == kQ4E4m3) f = live ? p.x_scale[row] : 0.f;
+        q4_store4(p, row, (g0 + wave) * 16 + 4 * q, tot, f);
     }
 }
 

@@ -34,122 +34,194 @@
 
 namespace pifa {
 
+// A lane's 4 TN consecutive columns n .. of its rows m, m + 16, ...
+template <bool E4, int TM, int TN>
+__device__ __forceinline__ void q4_store_rows(const Q4Args& p, const f32x4 (&acc)[TM][TN], int64_t m, int64_t n) {
+    constexpr int W = 4 * TN, C = W < 8 ? W : 8;  // columns of a store
+    struct __attribute__((packed, aligned(2))) Run {
+        uint16_t h[C];
+    };
+#pragma unroll
+    for (int i = 0; i < TM; ++i, m += 16) {
+        if (m >= p.M) continue;
+        const float f = E4 ? p.x_scale[m] : 1.f;
+        uint16_t* y = reinterpret_cast<uint16_t*>(p.Y) + m * p.N + n;
+#pragma unroll
+        for (int x = 0; x < W; x += C) {
+            Run r;
+#pragma unroll
+            for (int e = 0; e < C; ++e) {
+                const float v = acc[i][(x + e) / 4][(x + e) & 3];
+                r.h[e] = f32_to_bf16_bits(E4 ? v * f : v);
+            }
+            if (n + x + C <= p.N) {
+                *reinterpret_cast<Run*>(y + x) = r;
+            } else {
+#pragma unroll
+                for (int e = 0; e < C; ++e)
+                    if (n + x + e < p.N) y[x + e] = r.h[e];
+            }
+        }
+    }
+}
+
+// The K tiles of one group of NW waves, WN of them along N, and what a lane
+// reads of them.  X rows lie in 16-byte slots, slot = chunk ^ ((row / 2) % 8),
+// so that the 16 rows a fragment read covers fall on different banks; the rows
+// of weight group gl have their slots swapped (row ^ swap(gl)) for the same
+// reason.  The scales are a piece of their own, 64 bytes a group.  A wave loads
+// pieces w, w + NW, ...: first the XPIECES of X, then those of the codes, then
+// the scales; which of them its j-th is does not change, so its buffer, its
+// step along K and its place are chosen once (and where it is the same for all
+// waves, known to the compiler).  Waves without a last piece of their own load
+// the scales again, so that all wait for the same number of loads.
+template <int ACT, int BM, int BN, int NW, int WN, int TN>
+struct Q4Stage {
+    static constexpr bool E4 = ACT == kQ4E4m3;
+    static constexpr int ES = E4 ? 1 : 2, BK = E4 ? 128 : 64;
+    static constexpr int GB = E4 ? 1024 : 512;  // bytes of codes of a 16-row group per K tile
+    static constexpr int XPIECES = BM / 8, WPIECES = BN / 16 * GB / 1024, PIECES = XPIECES + WPIECES + 1;
+    static constexpr int kBytes = PIECES * 1024;
+    static constexpr int kLoads = (PIECES + NW - 1) / NW;
+    static_assert(BM % 16 == 0 && BN % 32 == 0 && BN <= 256, "pieces");
+    static_assert(TN == 1 || TN == 2 || TN == 4, "fragments of a wave");
+
+    // 0 X, 1 codes, 2 scales
+    __device__ __forceinline__ static constexpr int kind_of(int piece) {
+        return piece < XPIECES ? 0 : piece < XPIECES + WPIECES ? 1 : 2;
+    }
+    __device__ __forceinline__ static constexpr bool same_kind(int j) { return kind_of(NW * j) == kind_of(NW * j + NW - 1); }
+    __device__ __forceinline__ int kind(int j) const { return same_kind(j) ? kind_of(NW * j) : kinds[j]; }
+
+    int nk, w;
+    const char *xbase, *wbase;
+    int xbytes, wbytes;  // of the buffers behind them
+    int kinds[kLoads];
+    uint32_t off[kLoads], last[kLoads], place[kLoads];
+    uint32_t rx[2], rw[TN], rs;  // a lane's places in a stage
+
+    __device__ __forceinline__ static int swap(int gl) { return TN == 4 ? 4 * (gl & 3) : TN == 2 ? 4 * (gl & 1) : 0; }
+    __device__ __forceinline__ static int clip(int64_t n) { return n > 0x7FFFFFFF ? 0x7FFFFFFF : (int)n; }
+
+    // wrow: the wave's first row of the tile, wn: its place along N
+    __device__ __forceinline__ void init(const Q4Args& p, int64_t m0, int64_t n0, int wave, int wrow, int wn, int lane) {
+        const int64_t KB = packed_kblocks(p.K);
+        const int K = (int)p.K, li = lane & 15, lg = lane >> 4;
+        w = wave;
+        nk = (K + BK - 1) / BK;
+        xbase = (const char*)p.X + m0 * p.K * ES;
+        wbase = (const char*)p.W + n0 / 16 * KB * kQ4Block;
+        xbytes = clip((p.M - m0) * p.K * ES);
+        wbytes = clip((packed_groups(p.N) - n0 / 16) * KB * kQ4Block);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            int piece = w + NW * j;
+            if (piece >= PIECES) piece = PIECES - 1;
+            place[j] = (uint32_t)__builtin_amdgcn_readfirstlane(piece * 1024);
+            kinds[j] = __builtin_amdgcn_readfirstlane(kind_of(piece));
+            if (kind(j) == 0) {  // 8 rows x 128 bytes
+                const int row = 8 * piece + (lane >> 3), c = (lane & 7) ^ ((row >> 1) & 7);
+                off[j] = (uint32_t)(row * K * ES + 16 * c);
+                last[j] = (nk - 1) * BK + (16 / ES) * c < K ? off[j] : kMaskedOffset;
+            } else {
+                if (kind(j) == 1) {  // e4m3: a group's 128 columns; bf16: 64 columns of two groups
+                    const int q = piece - XPIECES, gl = E4 ? q : 2 * q + (lane >> 5);
+                    off[j] = (uint32_t)(gl * KB * kQ4Block + ((li ^ swap(gl)) + 16 * (E4 ? lg : lg & 1)) * 16);
+                } else {  // 64 bytes of each group
+                    const int gl = lane >> 2;
+                    off[j] = gl < BN / 16 ? (uint32_t)(gl * KB * kQ4Block + 1024 + (lane & 3) * 16) : kMaskedOffset;
+                }
+                last[j] = off[j];
+            }
+        }
+        const int row = wrow + li;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) rx[h] = (uint32_t)(row * 128 + (((4 * h + lg) ^ ((row >> 1) & 7)) << 4));
+        const int n = (li >> 2) * 4 * TN + (li & 3), gw = n >> 4, gl = wn * TN + gw;  // n + 4 j: same group
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+            rw[j] = (uint32_t)(XPIECES * 1024 + gl * GB + ((((n & 15) + 4 * j) ^ swap(gl)) << 4) +
+                               (E4 ? lg * 256 : lg * 4));
+        rs = (uint32_t)((XPIECES + WPIECES) * 1024 + gl * 64 + (n & 15) + (E4 ? 16 * lg : 0));
+    }
+    // the wave's j-th load of K tile t into the stage at lds.  A tile past the
+    // last is not multiplied; its loads stay inside the buffers.
+    __device__ __forceinline__ void issue(int t, uint32_t lds, int j) const {
+        const int blk = (E4 ? t : t >> 1) * kQ4Block, k = kind(j);
+        const int at = k == 0 ? t * 128 : k == 1 && !E4 ? blk + (t & 1) * 512 : blk;
+        const uint64_t b = reinterpret_cast<uint64_t>(k == 0 ? xbase : wbase) + (uint32_t)at;
+        const int n = (k == 0 ? xbytes : wbytes) - at;
+        const u32x4 rs = {(uint32_t)b, (uint32_t)(b >> 32), (uint32_t)(n > 0 ? n : 0), 0x00020000u};
+        const bool ends = same_kind(j) && k != 0;  // no tail of their own: padded
+        dma16(rs, !ends && t == nk - 1 ? last[j] : off[j], lds + place[j]);
+    }
+    __device__ __forceinline__ u32x4 x(const char* st, int h, int i) const {
+        return *reinterpret_cast<const u32x4*>(st + rx[h] + i * 2048);
+    }
+    __device__ __forceinline__ u32x4 codes(const char* st, int j) const {  // e4m3
+        return *reinterpret_cast<const u32x4*>(st + rw[j]);
+    }
+    __device__ __forceinline__ uint32_t codes(const char* st, int j, int h) const {  // bf16, step h
+        return *reinterpret_cast<const uint32_t*>(st + rw[j] + h * 256);
+    }
+    // e4m3: the scale of fragment j; bf16: of step `sub` (0..3) of the block
+    __device__ __forceinline__ uint32_t scale(const char* st, int j, int sub) const {
+        return *reinterpret_cast<const uint8_t*>(st + rs + 4 * j + 16 * sub);
+    }
+};
+
 template <int ACT, int BM, int BN, int WM, int WN, int S, int OCC>
 __global__ __launch_bounds__(8 * kWave, OCC) void q4_tiles(Q4Args p) {
     constexpr bool E4 = ACT == kQ4E4m3;
     constexpr int NW = 8;
     static_assert(WM * WN == NW, "eight waves");
     constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
-    static_assert(TM % 2 == 0 && (TN == 2 || TN == 4), "fragments of a wave");
-    constexpr int BK = E4 ? 128 : 64;
-    constexpr int GB = E4 ? 1024 : 512;  // bytes of codes of a 16-row group per K tile
-    constexpr int XB = BM * 128, WB = BN / 16 * GB, SB = NW * 256;
-    constexpr int STAGE = XB + WB + SB;
+    static_assert(TM % 2 == 0, "fragments of a wave");
+    using Stage = Q4Stage<ACT, BM, BN, NW, WN, TN>;
+    constexpr int STAGE = Stage::kBytes, DPW = Stage::kLoads;
     static_assert(S >= 2 && S * STAGE <= 163840, "160 KB of LDS");
-    constexpr int XP = BM / 8 / NW;                              // 1 KB pieces of X a wave loads per K tile
-    constexpr int WPIECES = WB / 1024, WP = (WPIECES + NW - 1) / NW;  // with fewer pieces than waves, some load one twice
-    static_assert(BM % 64 == 0 && (WPIECES % NW == 0 || NW % WPIECES == 0), "pieces do not split over the waves");
-    constexpr int DPW = XP + WP + 1;
     __shared__ __attribute__((aligned(1024))) char smem[S * STAGE];
 
-    const int64_t K = p.K, KB = packed_kblocks(K), nk = ceil_div(K, BK);
     int64_t tm, tn;
     tile_coords<BM, BN>(blockIdx.x, ceil_div(p.M, BM), ceil_div(p.N, BN), tm, tn);
     const int64_t m0 = tm * BM, n0 = tn * BN;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave / WN, wn = wave % WN, grp = wave >= NW / 2 ? 1 : 0;
-    const int li = lane & 15, lg = lane >> 4;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-
-    // ---- loads.  X rows in 16-byte slots, slot = chunk ^ ((row / 2) % 8), so
-    // that the 16 rows a fragment read covers fall on different banks; weight
-    // groups with their rows' slots swapped by 4 (gl % 4), for the same reason.
-    constexpr int ES = E4 ? 1 : 2;
-    const u32x4 xrs = raw_rsrc31((const char*)p.X + m0 * K * ES, (p.M - m0) * K * ES);
-    const u32x4 wrs = raw_rsrc31(p.W + n0 / 16 * KB * kQ4Block, (packed_groups(p.N) - n0 / 16) * KB * kQ4Block);
-    auto w_swap = [](int gl) { return TN == 4 ? 4 * (gl & 3) : 4 * (gl & 1); };
-    uint32_t xoff[XP], woff[WP], soff;
-    int xc[XP];
-#pragma unroll
-    for (int j = 0; j < XP; ++j) {  // piece: 8 rows x 128 bytes
-        const int row = 8 * (wave + NW * j) + (lane >> 3);
-        xc[j] = (lane & 7) ^ ((row >> 1) & 7);
-        xoff[j] = (uint32_t)(row * K * ES + 16 * xc[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < WP; ++j) {
-        const int piece = (wave + NW * j) % WPIECES;
-        if constexpr (E4) {  // a group's 128 columns
-            woff[j] = (uint32_t)(piece * KB * kQ4Block + ((li ^ w_swap(piece)) + 16 * lg) * 16);
-        } else {  // 64 columns of two groups
-            const int gl = 2 * piece + (lane >> 5);
-            woff[j] = (uint32_t)(gl * KB * kQ4Block + ((li ^ w_swap(gl)) + 16 * (lg & 1)) * 16);
-        }
-    }
-    // the scales of the wave's own TN groups, 64 bytes each
-    soff = lg < TN ? (uint32_t)((wn * TN + lg) * KB * kQ4Block + 1024 + 4 * li) : kMaskedOffset;
-    auto issue1 = [&](int64_t t, int d) {
-        const uint32_t st = lds0 + (uint32_t)(t % S) * STAGE;
-        const int64_t k0 = t * BK;
-        if (d < XP) {
-            const int j = d < XP ? d : 0;
-            dma16(xrs, k0 + (16 / ES) * xc[j] < K ? xoff[j] + (uint32_t)(t * 128) : kMaskedOffset,
-                  st + (wave + NW * j) * 1024);
-        } else if (d < XP + WP) {
-            const int j = d < XP + WP && d >= XP ? d - XP : 0;
-            const uint32_t add = E4 ? (uint32_t)(t * kQ4Block) : (uint32_t)((t >> 1) * kQ4Block + (t & 1) * 512);
-            dma16(wrs, k0 < K ? woff[j] + add : kMaskedOffset, st + XB + (wave + NW * j) % WPIECES * 1024);
-        } else {
-            const uint32_t add = (uint32_t)((E4 ? t : t >> 1) * kQ4Block);
-            dma4(wrs, k0 < K ? soff + add : kMaskedOffset, st + XB + WB + wave * 256);
-        }
-    };
-    auto issue = [&](int64_t t) {
-#pragma unroll
-        for (int d = 0; d < DPW; ++d) issue1(t, d);
-    };
+    Stage sg;
+    sg.init(p, m0, n0, wave, wm * WTM, wn, lane);
+    const int nk = sg.nk;
 
     // ---- operands of a segment
     constexpr int FA = E4 ? TM / 2 : TM;  // row fragments
     u32x4 fa[E4 ? 2 : 1][FA], fb[TN];
     uint32_t fs[TN];
-    auto frags = [&](int64_t t, int seg) {
-        const char* st = smem + (t % S) * STAGE;
-        auto x_at = [&](int i, int step) {
-            const int row = wm * WTM + 16 * i + li;
-            return *reinterpret_cast<const u32x4*>(st + row * 128 + (((4 * step + lg) ^ ((row >> 1) & 7)) << 4));
-        };
-        const char* wst = st + XB;
-        const uint8_t* sst = reinterpret_cast<const uint8_t*>(st) + XB + WB + wave * 256;
-        if (!E4 || seg == 0) {
+    auto frags = [&](int t, const char* st, int seg) {
+        if constexpr (E4) {
+            if (seg == 0) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    fb[j] = sg.codes(st, j);
+                    fs[j] = sg.scale(st, j, 0);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < FA; ++i) {
+                fa[0][i] = sg.x(st, 0, seg * FA + i);
+                fa[1][i] = sg.x(st, 1, seg * FA + i);
+            }
+        } else {
             uint32_t codes[TN];
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
-                const int n = (li >> 2) * 4 * TN + 4 * j + (li & 3);  // column within the wave's
-                const int gw = n >> 4, gl = wn * TN + gw, row = n & 15;
-                const char* at = wst + gl * GB + ((row ^ w_swap(gl)) << 4);
-                if constexpr (E4) {
-                    fb[j] = *reinterpret_cast<const u32x4*>(at + lg * 256);
-                    fs[j] = sst[gw * 64 + 16 * lg + row];
-                } else {
-                    codes[j] = *reinterpret_cast<const uint32_t*>(at + seg * 256 + 4 * lg);
-                    fs[j] = sst[gw * 64 + 16 * (2 * (int)(t & 1) + seg) + row];
-                }
+                codes[j] = sg.codes(st, j, seg);
+                fs[j] = sg.scale(st, j, 2 * (t & 1) + seg);
             }
-            if constexpr (!E4) {
 #pragma unroll
-                for (int i = 0; i < FA; ++i) fa[0][i] = x_at(i, seg);
+            for (int i = 0; i < FA; ++i) fa[0][i] = sg.x(st, seg, i);
 #pragma unroll
-                for (int j = 0; j < TN; ++j) fb[j] = q4_to_bf16(codes[j], __builtin_bit_cast(float, fs[j] << 23));
-            }
-        }
-        if constexpr (E4) {
-#pragma unroll
-            for (int i = 0; i < FA; ++i) {
-                fa[0][i] = x_at(seg * FA + i, 0);
-                fa[1][i] = x_at(seg * FA + i, 1);
-            }
+            for (int j = 0; j < TN; ++j) fb[j] = q4_to_bf16(codes[j], __builtin_bit_cast(float, fs[j] << 23));
         }
     };
     f32x4 acc[TM][TN];
@@ -158,7 +230,7 @@ __global__ __launch_bounds__(8 * kWave, OCC) void q4_tiles(Q4Args p) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     // a segment's MFMAs, with tile t's loads between them (ISSUE)
-    auto mma = [&](auto with, auto which, int64_t t) {
+    auto mma = [&](auto with, auto which, int t, uint32_t lds) {
         constexpr bool ISSUE = decltype(with)::value;
         constexpr int seg = decltype(which)::value;
         constexpr int GAP = FA * TN / DPW > 0 ? FA * TN / DPW : 1;
@@ -173,7 +245,7 @@ __global__ __launch_bounds__(8 * kWave, OCC) void q4_tiles(Q4Args p) {
                 if constexpr (ISSUE) {
                     if (n % GAP == GAP / 2 && d < DPW) {
                         __builtin_amdgcn_sched_barrier(0);
-                        issue1(t, d++);
+                        sg.issue(t, lds, d++);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
@@ -181,37 +253,43 @@ __global__ __launch_bounds__(8 * kWave, OCC) void q4_tiles(Q4Args p) {
             }
         if constexpr (ISSUE) {
 #pragma unroll
-            for (; d < DPW; ++d) issue1(t, d);
+            for (; d < DPW; ++d) sg.issue(t, lds, d);
         }
     };
 
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s) issue(s);
-    if (grp) {
-        issue(S - 1);
-        wait_vm<(S - 1) * DPW>();
-    } else {
-        wait_vm<(S - 2) * DPW>();
+    for (int s = 0; s < S; ++s) {
+        if (s < S - 1 || grp) {
+#pragma unroll
+            for (int d = 0; d < DPW; ++d) sg.issue(s, lds0 + s * STAGE, d);
+        }
     }
+    if (grp) wait_vm<(S - 1) * DPW>();
+    else wait_vm<(S - 2) * DPW>();
     slot_barrier();
     auto loop = [&](auto second) {
         constexpr bool G1 = decltype(second)::value;
-        auto segment = [&](auto which, int64_t t) {
-            constexpr int seg = decltype(which)::value;
-            frags(t, seg);
-            wait_lgkm0();
-            if (G1 && seg == 1) wait_vm<(S - 2) * DPW>();
-            slot_barrier();
-            __builtin_amdgcn_s_setprio(1);
-            if constexpr (seg == (G1 ? 1 : 0)) mma(std::true_type{}, which, t + (G1 ? S : S - 1));
-            else mma(std::false_type{}, which, 0);
-            __builtin_amdgcn_s_setprio(0);
-            if (!G1 && seg == 1) wait_vm<(S - 2) * DPW>();
-            slot_barrier();
-        };
-        for (int64_t t = 0; t < nk; ++t) {
-            segment(std::integral_constant<int, 0>{}, t);
-            segment(std::integral_constant<int, 1>{}, t);
+        int at = 0;  // tile t's stage
+        for (int t = 0; t < nk; ++t) {
+            const char* st = smem + at * STAGE;
+            const int next = at + 1 == S ? 0 : at + 1, prev = at == 0 ? S - 1 : at - 1;
+            auto segment = [&](auto which) {
+                constexpr int seg = decltype(which)::value;
+                frags(t, st, seg);
+                wait_lgkm0();
+                if (G1 && seg == 1) wait_vm<(S - 2) * DPW>();
+                slot_barrier();
+                __builtin_amdgcn_s_setprio(1);
+                if constexpr (seg == (G1 ? 1 : 0))
+                    mma(std::true_type{}, which, t + (G1 ? S : S - 1), lds0 + (G1 ? at : prev) * STAGE);
+                else mma(std::false_type{}, which, 0, 0);
+                __builtin_amdgcn_s_setprio(0);
+                if (!G1 && seg == 1) wait_vm<(S - 2) * DPW>();
+                slot_barrier();
+            };
+            segment(std::integral_constant<int, 0>{});
+            segment(std::integral_constant<int, 1>{});
+            at = next;
         }
     };
     if (grp) {
@@ -223,35 +301,144 @@ __global__ __launch_bounds__(8 * kWave, OCC) void q4_tiles(Q4Args p) {
         wait_vm<0>();
         slot_barrier();
     }
+    q4_store_rows<E4, TM, TN>(p, acc, m0 + wm * WTM + (lane & 15), n0 + wn * WTN + (lane >> 4) * 4 * TN);
+}
 
-    // ---- a lane's 4 TN consecutive columns of each of its TM rows
-    const int64_t n = n0 + wn * WTN + lg * 4 * TN;
-    struct __attribute__((packed, aligned(2))) Any16 {
-        u32x4 v;
+// Middling numbers of rows.  A slot of the form above costs a barrier and an
+// LDS round trip, which the few MFMAs of a small tile do not cover, so here a
+// wave reads the operands of its next K tile while it multiplies the current
+// one, and a K tile costs one barrier.  KG groups of WM x WN waves take every
+// KG-th K tile each (their sums meet in LDS at the end), so a long K is a
+// short loop also where there are few tiles.
+// Step s's stage is read (into registers) before the barrier of step s, and
+// loaded again with step s + S after it.
+// S: stages of each group's ring, as many as fit LDS up to SMAX.
+template <int ACT, int BM, int BN, int WM, int WN, int KG, int SMAX, int OCC>
+__global__ __launch_bounds__(WM* WN* KG* kWave, OCC) void q4_mid(Q4Args p) {
+    constexpr bool E4 = ACT == kQ4E4m3;
+    constexpr int NW = WM * WN;
+    constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
+    using Stage = Q4Stage<ACT, BM, BN, NW, WN, TN>;
+    constexpr int STAGE = Stage::kBytes, DPW = Stage::kLoads;
+    constexpr int FIT = 163840 / (KG * STAGE), S = FIT < SMAX ? FIT : SMAX;
+    constexpr int LOOP = KG * S * STAGE, RED = (KG - 1) * BM * BN * 4;
+    static_assert(S >= 2 && LOOP <= 163840 && RED <= 163840, "160 KB of LDS");
+    __shared__ __attribute__((aligned(1024))) char smem[LOOP > RED ? LOOP : RED];
+
+    int64_t tm, tn;
+    tile_coords<BM, BN>(blockIdx.x, ceil_div(p.M, BM), ceil_div(p.N, BN), tm, tn);
+    const int64_t m0 = tm * BM, n0 = tn * BN;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int kg = wave / NW, w = wave % NW, wm = w / WN, wn = w % WN;
+    char* ring = smem + kg * S * STAGE;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring;
+    Stage sg;
+    sg.init(p, m0, n0, w, wm * WTM, wn, lane);
+    const int steps = (sg.nk + KG - 1) / KG;
+
+    auto issue = [&](int s, int at) {
+#pragma unroll
+        for (int d = 0; d < DPW; ++d) sg.issue(s * KG + kg, lds0 + at * STAGE, d);
     };
+    struct Ops {
+        u32x4 x[2][TM];
+        u32x4 w[E4 ? TN : 1];        // e4m3: codes of a K tile
+        uint32_t c[E4 ? 1 : 2][TN];  // bf16: codes of its two steps
+        uint32_t s[E4 ? 1 : 2][TN];
+    };
+    auto read = [&](int s, int at, Ops& o) {
+        const char* st = ring + at * STAGE;
+        const int t = s * KG + kg;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + wm * WTM + 16 * i + li;
-        if (m >= p.M) continue;
-        const float f = E4 ? p.x_scale[m] : 1.f;
-        uint16_t h[4 * TN];
-#pragma unroll
-        for (int x = 0; x < 4 * TN; ++x) h[x] = f32_to_bf16_bits(E4 ? acc[i][x / 4][x & 3] * f : acc[i][x / 4][x & 3]);
-        uint16_t* y = reinterpret_cast<uint16_t*>(p.Y) + m * p.N + n;
-#pragma unroll
-        for (int x = 0; x < 4 * TN; x += 8) {
-            if (n + x + 8 <= p.N) {
-                uint16_t c[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) c[e] = h[x + e];
-                reinterpret_cast<Any16*>(y + x)->v = __builtin_bit_cast(u32x4, c);
+        for (int j = 0; j < TN; ++j) {
+            if constexpr (E4) {
+                o.w[j] = sg.codes(st, j);
+                o.s[0][j] = sg.scale(st, j, 0);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (n + x + e < p.N) y[x + e] = h[x + e];
+                for (int h = 0; h < 2; ++h) {
+                    o.c[h][j] = sg.codes(st, j, h);
+                    o.s[h][j] = sg.scale(st, j, 2 * (t & 1) + h);
+                }
             }
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < TM; ++i) o.x[h][i] = sg.x(st, h, i);
+    };
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto mma = [&](const Ops& o) {
+        if constexpr (E4) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = q4_mfma_e4m3(o.w[j], o.s[0][j], o.x[0][i], o.x[1][i], acc[i][j]);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 wj[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) wj[j] = q4_to_bf16(o.c[h][j], __builtin_bit_cast(float, o.s[h][j] << 23));
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = q4_mfma_bf16(wj[j], o.x[h][i], acc[i][j]);
+            }
+        }
+    };
+
+#pragma unroll
+    for (int s = 0; s < S; ++s) issue(s, s);
+    wait_vm<(S - 1) * DPW>();
+    slot_barrier();
+    Ops even, odd;
+    read(0, 0, even);
+    int at = 0;  // step s's stage
+    auto step = [&](int s, const Ops& cur, Ops& nxt) {
+        const int next = at + 1 == S ? 0 : at + 1;
+        wait_lgkm0();
+        wait_vm<(S - 2) * DPW>();  // step s + 1's loads
+        slot_barrier();
+        issue(s + S, at);
+        read(s + 1, next, nxt);
+        __builtin_amdgcn_sched_barrier(0);
+        if (KG == 1 || s * KG + kg < sg.nk) mma(cur);  // uniform
+        __builtin_amdgcn_sched_barrier(0);
+        at = next;
+    };
+    int s = 0;
+    for (; s + 1 < steps; s += 2) {
+        step(s, even, odd);
+        step(s + 1, odd, even);
     }
+    if (s * KG + kg < sg.nk) mma(even);  // the last of an odd number: its operands are read
+    wait_vm<0>();
+    if constexpr (KG > 1) {
+        wait_lgkm0();
+        slot_barrier();  // the ring's memory takes the sums
+        f32x4* red = reinterpret_cast<f32x4*>(smem);
+        if (kg > 0) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) red[(((kg - 1) * NW + w) * TM * TN + i * TN + j) * kWave + lane] = acc[i][j];
+        }
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int g = 0; g < KG - 1; ++g)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] += red[((g * NW + w) * TM * TN + i * TN + j) * kWave + lane];
+    }
+    q4_store_rows<E4, TM, TN>(p, acc, m0 + wm * WTM + (lane & 15), n0 + wn * WTN + (lane >> 4) * 4 * TN);
 }
 
 }  // namespace pifa

@@ -599,9 +599,39 @@ def _ptr_of(t, name: str, dtype, count: int, dev: int) -> int | None:
     return t.data_ptr()
 
 
-def _current_device() -> int:
-    import torch
-    return torch.cuda.current_device()
+class _Torch:
+    """What the calls below need of torch, looked up once: a decode step's calls
+    are short, and torch.cuda.current_stream() alone takes longer than a launch."""
+
+    def __init__(self):
+        import torch
+        self.empty, self.empty_like = torch.empty, torch.empty_like
+        self.bf16, self.f32, self.u8, self.e4m3 = torch.bfloat16, torch.float32, torch.uint8, torch.float8_e4m3fn
+        self.codes = {torch.bfloat16: PIFA_BF16, torch.float32: PIFA_F32}
+        self.device = torch.cuda.current_device
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+    def stream(self, stream, dev: int) -> int:
+        """The given stream, or the device's current one."""
+        if stream is None and self.raw_stream is not None:
+            return self.raw_stream(dev)
+        return _stream(stream)
+
+    def code(self, dtype) -> int:
+        c = self.codes.get(dtype)
+        if c is None:
+            raise TypeError("unsupported dtype %s (bf16 or fp32)" % dtype)
+        return c
+
+
+_torch = None
+
+
+def _rt() -> _Torch:
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch
 
 
 def _rows_of(t, M, d):
@@ -614,15 +644,15 @@ def rms_norm_forward(X, gain, eps: float, R=None, H=None, Y=None, M: int | None 
     """The norm of the rows of X + R (R may be None), times gain (may be None).
     Returns Y (allocated when not given); H, where given, takes X + R.  The
     rows are X's last dimension unless M and d say otherwise."""
-    import torch
+    rt = _rt()
     M, d = _rows_of(X, M, d)
     if Y is None:
-        Y = torch.empty_like(X)
-    dt, dev, n = X.dtype, _current_device(), M * d
-    code = _dtype_code(X)
+        Y = rt.empty_like(X)
+    dt, dev, n = X.dtype, rt.device(), M * d
+    code = rt.code(dt)
     _check("rms_norm_forward", lib().rms_norm_forward(
         _ptr_of(X, "X", dt, n, dev), _ptr_of(R, "R", dt, n, dev), _ptr_of(gain, "gain", dt, d, dev), eps,
-        _ptr_of(H, "H", dt, n, dev), _ptr_of(Y, "Y", dt, n, dev), M, d, code, _stream(stream)))
+        _ptr_of(H, "H", dt, n, dev), _ptr_of(Y, "Y", dt, n, dev), M, d, code, rt.stream(stream, dev)))
     return Y
 
 
@@ -630,18 +660,18 @@ def rms_norm_forward_e4m3(X, gain, eps: float, R=None, H=None, Q=None, scale=Non
                           d: int | None = None, stream=None):
     """The same norm in 8 bits.  Returns (Q, scale): float8_e4m3fn rows and one
     fp32 scale a row, which stand for Q * scale (allocated when not given)."""
-    import torch
+    rt = _rt()
     M, d = _rows_of(X, M, d)
     if Q is None:
-        Q = torch.empty(X.shape, dtype=torch.float8_e4m3fn, device=X.device)
+        Q = rt.empty(X.shape, dtype=rt.e4m3, device=X.device)
     if scale is None:
-        scale = torch.empty(M, dtype=torch.float32, device=X.device)
-    dt, dev, n = X.dtype, _current_device(), M * d
-    code = _dtype_code(X)
+        scale = rt.empty(M, dtype=rt.f32, device=X.device)
+    dt, dev, n = X.dtype, rt.device(), M * d
+    code = rt.code(dt)
     _check("rms_norm_forward_e4m3", lib().rms_norm_forward_e4m3(
         _ptr_of(X, "X", dt, n, dev), _ptr_of(R, "R", dt, n, dev), _ptr_of(gain, "gain", dt, d, dev), eps,
-        _ptr_of(H, "H", dt, n, dev), _ptr_of(Q, "Q", torch.float8_e4m3fn, n, dev),
-        _ptr_of(scale, "scale", torch.float32, M, dev), M, d, code, _stream(stream)))
+        _ptr_of(H, "H", dt, n, dev), _ptr_of(Q, "Q", rt.e4m3, n, dev),
+        _ptr_of(scale, "scale", rt.f32, M, dev), M, d, code, rt.stream(stream, dev)))
     return Q, scale
 
 
@@ -654,31 +684,32 @@ def rms_norm_backward(H, gain, dY, eps: float, dR=None, dX=None, dgain=None, wor
     """Gradients of rms_norm_forward: (dX, dgain), dX plus dR where given.
     Outputs and workspace are allocated when not given; need_dX / need_dgain
     False skip one (None in its place)."""
-    import torch
+    rt = _rt()
     M, d = _rows_of(H, M, d)
     if dX is None and need_dX:
-        dX = torch.empty_like(H)
+        dX = rt.empty_like(H)
     if dgain is None and need_dgain:
-        dgain = torch.empty(d, dtype=torch.float32, device=H.device)
+        dgain = rt.empty(d, dtype=rt.f32, device=H.device)
     if work is None and dgain is not None:
-        work = torch.empty(rms_norm_backward_bytes(M, d), dtype=torch.uint8, device=H.device)
-    dt, dev, n = H.dtype, _current_device(), M * d
-    code = _dtype_code(H)
+        work = rt.empty(rms_norm_backward_bytes(M, d), dtype=rt.u8, device=H.device)
+    dt, dev, n = H.dtype, rt.device(), M * d
+    code = rt.code(dt)
     nwork = 0 if work is None else work.numel() * work.element_size()
     _check("rms_norm_backward", lib().rms_norm_backward(
         _ptr_of(H, "H", dt, n, dev), _ptr_of(gain, "gain", dt, d, dev), _ptr_of(dY, "dY", dt, n, dev),
         _ptr_of(dR, "dR", dt, n, dev), eps, _ptr_of(dX, "dX", dt, n, dev),
-        _ptr_of(dgain, "dgain", torch.float32, d, dev), M, d, code,
-        None if work is None else _ptr_of(work, "work", work.dtype, 0, dev), nwork, _stream(stream)))
+        _ptr_of(dgain, "dgain", rt.f32, d, dev), M, d, code,
+        None if work is None else _ptr_of(work, "work", work.dtype, 0, dev), nwork, rt.stream(stream, dev)))
     return dX, dgain
 
 
 def q4_layer_create(W, d_in: int | None = None, d_out: int | None = None, dtype: int | None = None) -> int:
     """Quantizes W (d_out x d_in) to 4 bits; returns an opaque handle."""
+    rt = _rt()
     d_in = W.shape[1] if d_in is None else int(d_in)
     d_out = W.shape[0] if d_out is None else int(d_out)
     dt = _dtype_code(W) if dtype is None else int(dtype)
-    dev = _current_device()
+    dev = rt.device()
     out = _vp()
     _check("q4_layer_create", lib().q4_layer_create(_ptr_of(W, "W", _torch_dtype(dt), d_out * d_in, dev), d_in, d_out,
                                                     dt, ctypes.byref(out)))
@@ -688,14 +719,14 @@ def q4_layer_create(W, d_in: int | None = None, d_out: int | None = None, dtype:
 def q4_layer_create_mx(codes, scales, d_in: int | None = None, d_out: int | None = None) -> int:
     """codes: uint8 d_out x d_in / 2 (the lower index in the lower half of a
     byte), scales: uint8 d_out x d_in / 32 (powers of two, biased by 127)."""
-    import torch
+    rt = _rt()
     d_in = 2 * codes.shape[1] if d_in is None else int(d_in)
     d_out = codes.shape[0] if d_out is None else int(d_out)
-    dev = _current_device()
+    dev = rt.device()
     out = _vp()
     _check("q4_layer_create_mx", lib().q4_layer_create_mx(
-        _ptr_of(codes, "codes", torch.uint8, d_out * (d_in // 2), dev),
-        _ptr_of(scales, "scales", torch.uint8, d_out * (d_in // 32), dev), d_in, d_out, ctypes.byref(out)))
+        _ptr_of(codes, "codes", rt.u8, d_out * (d_in // 2), dev),
+        _ptr_of(scales, "scales", rt.u8, d_out * (d_in // 32), dev), d_in, d_out, ctypes.byref(out)))
     return _remember(out.value, d_in=d_in, d_out=d_out, dt=PIFA_BF16, dev=dev)
 
 
@@ -706,12 +737,12 @@ def q4_layer_destroy(handle: int) -> None:
 
 def q4_layer_read(handle: int, codes=None, scales=None, stream=None) -> None:
     """Copies the layer's codes and scales (either may be None)."""
-    import torch
+    rt = _rt()
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
-    dev = _current_device()
+    dev = rt.device()
     _check("q4_layer_read", lib().q4_layer_read(
-        handle, _ptr_of(codes, "codes", torch.uint8, d["d_out"] * d["d_in"] // 2, dev),
-        _ptr_of(scales, "scales", torch.uint8, d["d_out"] * d["d_in"] // 32, dev), _stream(stream)))
+        handle, _ptr_of(codes, "codes", rt.u8, d["d_out"] * d["d_in"] // 2, dev),
+        _ptr_of(scales, "scales", rt.u8, d["d_out"] * d["d_in"] // 32, dev), rt.stream(stream, dev)))
 
 
 def q4_layer_weight_bytes(handle: int) -> int:
@@ -723,34 +754,34 @@ def q4_layer_reserve(handle: int, max_M: int) -> None:
 
 
 def q4_layer_forward(handle: int, X, Y, M: int | None = None, stream=None) -> None:
-    import torch
+    rt = _rt()
     M = X.shape[0] if M is None else int(M)
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
-    dev = _current_device()
+    dev = rt.device()
     _check("q4_layer_forward", lib().q4_layer_forward(
-        handle, _ptr_of(X, "X", torch.bfloat16, M * d["d_in"], dev), _ptr_of(Y, "Y", torch.bfloat16, M * d["d_out"], dev),
-        M, _stream(stream)))
+        handle, _ptr_of(X, "X", rt.bf16, M * d["d_in"], dev), _ptr_of(Y, "Y", rt.bf16, M * d["d_out"], dev),
+        M, rt.stream(stream, dev)))
 
 
 def q4_layer_forward_e4m3(handle: int, Q, scale, Y, M: int | None = None, stream=None) -> None:
-    import torch
+    rt = _rt()
     M = Q.shape[0] if M is None else int(M)
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
-    dev = _current_device()
+    dev = rt.device()
     _check("q4_layer_forward_e4m3", lib().q4_layer_forward_e4m3(
-        handle, _ptr_of(Q, "Q", torch.float8_e4m3fn, M * d["d_in"], dev), _ptr_of(scale, "scale", torch.float32, M, dev),
-        _ptr_of(Y, "Y", torch.bfloat16, M * d["d_out"], dev), M, _stream(stream)))
+        handle, _ptr_of(Q, "Q", rt.e4m3, M * d["d_in"], dev), _ptr_of(scale, "scale", rt.f32, M, dev),
+        _ptr_of(Y, "Y", rt.bf16, M * d["d_out"], dev), M, rt.stream(stream, dev)))
 
 
 def q4_layer_norm_forward(handle: int, X, gain, eps: float, R=None, H=None, Y=None, M: int | None = None,
                           stream=None) -> None:
-    import torch
+    rt = _rt()
     M = X.shape[0] if M is None else int(M)
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
-    dev, bf, n = _current_device(), torch.bfloat16, M * d["d_in"]
+    dev, bf, n = rt.device(), rt.bf16, M * d["d_in"]
     _check("q4_layer_norm_forward", lib().q4_layer_norm_forward(
         handle, _ptr_of(X, "X", bf, n, dev), _ptr_of(R, "R", bf, n, dev), _ptr_of(gain, "gain", bf, d["d_in"], dev), eps,
-        _ptr_of(H, "H", bf, n, dev), _ptr_of(Y, "Y", bf, M * d["d_out"], dev), M, _stream(stream)))
+        _ptr_of(H, "H", bf, n, dev), _ptr_of(Y, "Y", bf, M * d["d_out"], dev), M, rt.stream(stream, dev)))
 
 
 def pifa_probe_mfma(iters: int = 20000, stream=None):
@@ -873,7 +904,7 @@ class Q4Layer:
     def read(self):
         """(codes, scales) as from_mx takes them."""
         import torch
-        dev = "cuda:%d" % _current_device()
+        dev = "cuda:%d" % _rt().device()
         codes = torch.empty((self.d_out, self.d_in // 2), dtype=torch.uint8, device=dev)
         scales = torch.empty((self.d_out, self.d_in // 32), dtype=torch.uint8, device=dev)
         q4_layer_read(self.handle, codes, scales)

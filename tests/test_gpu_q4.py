@@ -144,7 +144,7 @@ def test_norm_forward(shape, with_r, with_gain, with_h):
     g_st, g = inputs.round_to(1.0 + 0.3 * np.random.default_rng(6).standard_normal((1, d_in)), "bf16")
     g_dev = to_dev(g_st).reshape(-1) if with_gain else None
     with layer:
-        for M in (1, 3, 16, 17, 90):
+        for M in (1, 3, 7, 16, 17, 90):
             x_dev, x = _x(M, d_in, 7)
             r_dev, r = _x(M, d_in, 8) if with_r else (None, None)
             h, y = o.rms_norm(x, g[0] if with_gain else None, EPS, r)
