@@ -109,10 +109,15 @@ def test_forward_e4m3(shape):
             assert (big[M * d_out:] == -17).all()
 
 
-@pytest.mark.parametrize("M,d_in,d_out", [(2050, 96, 8100), (4100, 352, 4096), (300, 64, 60000)])
-def test_many_tiles(M, d_in, d_out):
-    """Products of more than 256 tiles of 256 x 256, in both forms (fp64 on the
-    GPU: the product is large)."""
+@pytest.mark.parametrize("M,d_in,d_out", [
+    (18, 96, 20), (2054, 96, 33), (2080, 1120, 33), (34, 96, 4114), (65, 544, 8310), (65, 2080, 8308), (2090, 2080, 386),
+    (33, 96, 8200), (33, 352, 8576), (196, 224, 12524), (129, 96, 10963), (259, 96, 13206), (267, 32, 13064),
+    (521, 96, 13453), (778, 96, 14177), (708, 2080, 10990), (2050, 96, 8100), (300, 64, 60000)])
+def test_every_tile(M, d_in, d_out):
+    """Sizes at which each of the tiles is the one picked, in bf16, e4m3 or both:
+    16 x 32, 32 x 32, 32 x 64, 32 x 128, 64 x 64 (both depths), 64 x 128, 128 x
+    128 (both forms), 128 x 256 and 256 x 256, all with ragged ends (fp64 on the
+    GPU: the products are large)."""
     torch = torch_mod()
     layer, w = _layer(d_in, d_out, 31)
     with layer:
