@@ -12,6 +12,8 @@
 // are fp32; each result is rounded once, from the unrounded h.
 #pragma once
 
+#include <type_traits>
+
 #include "common.hpp"
 
 namespace pifa {
@@ -264,21 +266,50 @@ struct NormBwd {
     float eps;
 };
 
+// Sums of two values over the TPR threads of each row, one barrier for both.
+template <int TPR>
+__device__ __forceinline__ float2 row_sum2(float a, float b, float2* red) {
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) {
+        a += __shfl_xor(a, s);
+        b += __shfl_xor(b, s);
+    }
+    if constexpr (TPR > kWave) {
+        constexpr int W = TPR / kWave;
+        const int wave = threadIdx.x / kWave;
+        if ((threadIdx.x & (kWave - 1)) == 0) red[wave] = float2{a, b};
+        __syncthreads();
+        const int w0 = wave / W * W;
+        a = red[w0].x;
+        b = red[w0].y;
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+            a += red[w0 + w].x;
+            b += red[w0 + w].y;
+        }
+    }
+    return float2{a, b};
+}
+
 // A workgroup takes ROWS rows at a time, rows ROWS * blockIdx.x + i * ROWS *
 // gridDim.x, and keeps the gain's gradient of the columns its threads hold in
 // registers over all of them; at the end the ROWS sums of a column are added
 // in LDS, so that only gridDim.x partial sums per column go to memory.  The
-// next rows' operands are loaded before the current ones' sums are reduced.
-template <typename T, int TPR, int V>
+// next rows' operands are loaded before the current ones' sums are reduced, in
+// two sets of registers in turn.
+// EXACT: rows are TPR * V full chunks and have a residual gradient and a dX, so
+// that no load or store stands under a condition (behind one, the wait for a
+// row's operands would be a wait for its successor's too).
+template <typename T, int TPR, int V, bool EXACT>
 __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
     using C = NormChunk<T>;
     constexpr int N = C::N;
     constexpr int ROWS = kNormThreads / TPR;
-    __shared__ float red[2][2][kNormThreads / kWave];
+    __shared__ float2 red[2][kNormThreads / kWave];
     __shared__ float cols[ROWS > 1 ? kNormThreads * (V * N + 1) : 1];
-    const int t = threadIdx.x % TPR, rg = threadIdx.x / TPR;
-    const int64_t step = (int64_t)gridDim.x * ROWS, nfull = p.d / N, kt = nfull * N + t;
-    const bool has_tail = t < N && kt < p.d, add = p.dR && p.dX;
+    const int t = threadIdx.x % TPR, rg = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+    const int64_t step = (int64_t)gridDim.x * ROWS, nfull = EXACT ? TPR * V : p.d / N, kt = nfull * N + t;
+    const bool has_tail = !EXACT && t < N && kt < p.d, add = EXACT || (p.dR && p.dX);
 
     float dg[V][N], dgt = 0.f;
     u32x4 g[V];
@@ -299,12 +330,19 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
     };
     auto fetch = [&](int64_t m, Rows& f) {
         const bool live = m < p.M;
-        const int64_t row = live ? m * p.d : 0, full = live ? nfull : 0;
+        const int64_t row = (EXACT && !live ? p.M - 1 : live ? m : 0) * p.d, full = live ? nfull : 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            f.h[i] = C::load(p.H + row, t + i * TPR, full);
-            f.y[i] = C::load(p.dY + row, t + i * TPR, full);
-            if (add) f.r[i] = C::load(p.dR + row, t + i * TPR, full);
+            const int64_t c = t + i * TPR, n = EXACT ? nfull : full;  // EXACT: c < nfull is known
+            if constexpr (EXACT) {
+                f.h[i] = reinterpret_cast<const typename C::Any*>(p.H + row + c * N)->v;
+                f.y[i] = reinterpret_cast<const typename C::Any*>(p.dY + row + c * N)->v;
+                f.r[i] = reinterpret_cast<const typename C::Any*>(p.dR + row + c * N)->v;
+            } else {
+                f.h[i] = C::load(p.H + row, c, n);
+                f.y[i] = C::load(p.dY + row, c, n);
+                if (add) f.r[i] = C::load(p.dR + row, c, n);
+            }
         }
         f.ht = f.yt = f.rt = 0.f;
         if (live && has_tail) {
@@ -313,29 +351,25 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
             if (add) f.rt = (float)p.dR[row + kt];
         }
     };
-    const int64_t first = (int64_t)blockIdx.x * ROWS;
-    Rows cur, nxt;
-    fetch(first + rg, cur);
     int par = 0;
-    for (int64_t m0 = first; m0 < p.M; m0 += step) {  // uniform over the workgroup
-        const int64_t m = m0 + rg;
-        const bool more = m0 + step < p.M;
-        if (more) fetch(m + step, nxt);
+    // LAST: rows past M may be among them
+    auto rows = [&](auto last, int64_t m, Rows& cur) {
+        constexpr bool LAST = decltype(last)::value || !EXACT;
+        const bool live = !LAST || m < p.M;
         float ss = cur.ht * cur.ht, uh = gt * cur.yt * cur.ht;
 #pragma unroll
         for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int e = 0; e < N; ++e) {
+                // written-out fused steps: every form of this kernel gives the same bits
                 const float h = C::one(cur.h[i], e);
-                ss += h * h;
-                uh += gain(i, e) * C::one(cur.y[i], e) * h;
+                ss = __builtin_fmaf(h, h, ss);
+                uh = __builtin_fmaf(gain(i, e) * C::one(cur.y[i], e), h, uh);
             }
-        ss = row_reduce<TPR>(ss, red[par][0]);
-        uh = row_reduce<TPR>(uh, red[par][1]);
+        const float2 sums = row_sum2<TPR>(ss, uh, red[par]);
         par ^= 1;
-        const float rho = rsqrtf(ss / (float)p.d + p.eps);
-        const float back = rho * rho * (uh / (float)p.d);
-        const bool live = m < p.M;
+        const float rho = rsqrtf(sums.x / (float)p.d + p.eps);
+        const float back = rho * rho * (sums.y / (float)p.d);
         const int64_t row = live ? m * p.d : 0, full = live ? nfull : 0;
         // the second reading of the row's registers converts them again: kept
         // from the first one, the fp32 values do not fit 128 registers
@@ -347,15 +381,33 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float h = C::one(cur.h[i], e), y = C::one(cur.y[i], e);
-                dg[i][e] += y * h * rho;
+                dg[i][e] = __builtin_fmaf(LAST && EXACT && !live ? 0.f : y * h, rho, dg[i][e]);
                 dx[e] = rho * (gain(i, e) * y - h * back);
                 if (add) dx[e] += C::one(cur.r[i], e);
             }
-            if (p.dX) C::store(p.dX + row, t + i * TPR, full, dx);
+            if constexpr (EXACT && !LAST) C::store(p.dX + row, t + i * TPR, TPR * V, dx);
+            else if (p.dX) C::store(p.dX + row, t + i * TPR, full, dx);
         }
-        dgt += cur.yt * cur.ht * rho;
+        dgt = __builtin_fmaf(cur.yt * cur.ht, rho, dgt);
         if (live && has_tail && p.dX) p.dX[row + kt] = (T)(rho * (gt * cur.yt - cur.ht * back) + cur.rt);
-        if (more) cur = nxt;
+    };
+    const int64_t first = (int64_t)blockIdx.x * ROWS;
+    Rows even, odd;
+    fetch(first + rg, even);
+    int64_t m0 = first;  // uniform over the workgroup
+    for (; EXACT && m0 + 2 * step + ROWS <= p.M; m0 += 2 * step) {
+        fetch(m0 + step + rg, odd);
+        __builtin_amdgcn_sched_barrier(0);
+        rows(std::false_type{}, m0 + rg, even);
+        fetch(m0 + 2 * step + rg, even);
+        __builtin_amdgcn_sched_barrier(0);
+        rows(std::false_type{}, m0 + step + rg, odd);
+    }
+    for (; m0 < p.M; m0 += step) {  // EXACT: at most three, the last of them perhaps cut
+        const bool more = m0 + step < p.M;
+        if (more) fetch(m0 + step + rg, odd);
+        rows(std::true_type{}, m0 + rg, even);
+        if (more) even = odd;
     }
     if (!p.dgain) return;
     float* out = p.dgain + (int64_t)blockIdx.x * p.d;
@@ -455,20 +507,28 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_long(NormBwd<T> p) {
     }
 }
 
-// dgain = the sum of P partial rows of d, in a fixed order: a workgroup of
-// 16 x 64 threads takes 64 columns.
-__global__ __launch_bounds__(kNormThreads) void norm_dgain(const float* __restrict__ part, int64_t P, int64_t d,
+// dgain = the sum of P <= 256 partial rows of d, in a fixed order: a workgroup
+// of 16 x 64 threads takes 64 columns; a thread's loads are all in flight.
+constexpr int kNormMaxGroups = 256;
+__global__ __launch_bounds__(kNormThreads) void norm_dgain(const float* __restrict__ part, int P, int64_t d,
                                                           float* __restrict__ dgain) {
+    constexpr int SLICES = kNormThreads / kWave, EACH = kNormMaxGroups / SLICES;
     __shared__ float red[kNormThreads];
     const int64_t k = (int64_t)blockIdx.x * kWave + (threadIdx.x & (kWave - 1));
-    float s = 0.f;
-    if (k < d)
-        for (int64_t q = threadIdx.x / kWave; q < P; q += kNormThreads / kWave) s += part[q * d + k];
+    const int slice = threadIdx.x / kWave;
+    float v[EACH], s = 0.f;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int q = slice + i * SLICES;
+        v[i] = part[(int64_t)(q < P ? q : 0) * d + (k < d ? k : 0)];
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) s += slice + i * SLICES < P ? v[i] : 0.f;
     red[threadIdx.x] = s;
     __syncthreads();
     if (threadIdx.x < kWave && k < d) {
 #pragma unroll
-        for (int w = 1; w < kNormThreads / kWave; ++w) s += red[w * kWave + threadIdx.x];
+        for (int w = 1; w < SLICES; ++w) s += red[w * kWave + threadIdx.x];
         dgain[k] = s;
     }
 }

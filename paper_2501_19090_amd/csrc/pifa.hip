@@ -2269,7 +2269,7 @@ int64_t norm_bwd_rows(int64_t d, int64_t n) {
     return chunks <= 64 ? 16 : chunks <= 128 ? 8 : chunks <= 256 ? 4 : chunks <= 512 ? 2 : 1;
 }
 int64_t norm_bwd_groups(int64_t M, int64_t d, int64_t n) {
-    return std::min<int64_t>(kCus, ceil_div(M, norm_bwd_rows(d, n)));
+    return std::min<int64_t>({kCus, kNormMaxGroups, ceil_div(M, norm_bwd_rows(d, n))});
 }
 
 template <typename T>
@@ -2282,19 +2282,26 @@ pifa_status norm_backward_run(const void* H, const void* gain, const void* dY, c
     {
         TimedLaunch timed(kSiteNormBwd, st);
         const dim3 grid((unsigned)groups), block(kNormThreads);
-        if (chunks <= 64) hipLaunchKernelGGL((norm_bwd<T, 64, 1>), grid, block, 0, st, p);
-        else if (chunks <= 128) hipLaunchKernelGGL((norm_bwd<T, 128, 1>), grid, block, 0, st, p);
-        else if (chunks <= 256) hipLaunchKernelGGL((norm_bwd<T, 256, 1>), grid, block, 0, st, p);
-        else if (chunks <= 512) hipLaunchKernelGGL((norm_bwd<T, 512, 1>), grid, block, 0, st, p);
-        else if (chunks <= 1024) hipLaunchKernelGGL((norm_bwd<T, 1024, 1>), grid, block, 0, st, p);
-        else if (chunks <= 2048) hipLaunchKernelGGL((norm_bwd<T, 1024, 2>), grid, block, 0, st, p);
+        const bool whole = d % N == 0 && dR && dX;
+        auto launch = [&](auto tpr, auto v) {
+            constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value;
+            if (whole && chunks == TPR * V) hipLaunchKernelGGL((norm_bwd<T, TPR, V, true>), grid, block, 0, st, p);
+            else hipLaunchKernelGGL((norm_bwd<T, TPR, V, false>), grid, block, 0, st, p);
+        };
+        using std::integral_constant;
+        if (chunks <= 64) launch(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+        else if (chunks <= 128) launch(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+        else if (chunks <= 256) launch(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+        else if (chunks <= 512) launch(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+        else if (chunks <= 1024) launch(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+        else if (chunks <= 2048) launch(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
         else hipLaunchKernelGGL((norm_bwd_long<T>), grid, block, 0, st, p);
         if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
     }
     if (dgain && groups > 1) {
         TimedLaunch timed(kSiteNormDgain, st);
-        hipLaunchKernelGGL(norm_dgain, dim3((unsigned)ceil_div(d, kWave)), dim3(kNormThreads), 0, st, work, groups, d,
-                           dgain);
+        hipLaunchKernelGGL(norm_dgain, dim3((unsigned)ceil_div(d, kWave)), dim3(kNormThreads), 0, st, work, (int)groups,
+                           d, dgain);
         if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
     }
     return PIFA_OK;
