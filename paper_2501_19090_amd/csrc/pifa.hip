@@ -2381,7 +2381,7 @@ pifa_status q4_create(int64_t d_in, int64_t d_out, q4_handle* out, Fill fill) {
 
 template <int ACT, int NG, int U>
 void q4_few_launch(const Q4Args& p, hipStream_t st) {
-    hipLaunchKernelGGL((q4_few<ACT, 1, NG, 8, U>), dim3((unsigned)ceil_div(packed_groups(p.N), NG)), dim3(8 * kWave), 0,
+    hipLaunchKernelGGL((q4_few<ACT, NG, 8, U>), dim3((unsigned)ceil_div(packed_groups(p.N), NG)), dim3(8 * kWave), 0,
                        st, p);
 }
 
@@ -2391,7 +2391,11 @@ void q4_staged_launch(const Q4Args& p, hipStream_t st) {
                        dim3(8 * kWave), (size_t)q4_staged_lds(p.M, p.K, ACT == kQ4Bf16 ? 2 : 1, NORM, NG * 8), st, p);
 }
 
-// Whether the norm's form is one launch (the rows staged by every workgroup).
+// Whether the norm's form is one launch.  Every workgroup norms the rows again,
+// so it pays while they are few (one launch / norm, then product, us): 4096^2
+// one row 4.8 / 6.0, three 5.8 / 6.7, four 6.4 / 6.9, five 7.7 / 7.0; 4096 ->
+// 12288 one row 7.5 / 8.7, five 10.6 / 9.9; 2048 -> 6000 six rows 6.1 / 6.3,
+// eight 7.2 / 6.5; 8192 -> 28672 one row 24.8 / 26.1, two 29.4 / 27.0.
 constexpr int64_t kQ4NormElems = 12288;
 bool q4_norm_in_one(int64_t M, int64_t K) { return M <= 16 && M * K <= kQ4NormElems; }
 
@@ -2492,10 +2496,20 @@ hipError_t launch_q4(Q4Args p, hipStream_t st) {
         if (p.x_scale) q.x_scale = p.x_scale + m;
         q.Y = p.Y + m * p.N;
         const int64_t groups = packed_groups(q.N);
-        // choice
         if (q.M <= 16) {
+            // Staged or not (us): one row of 4096^2 3.5 / 4.1, 4096 -> 11008 6.2 / 7.0,
+            // 8192 -> 28672 23.0 / 24.9; three rows of 4096^2 4.0 / 4.3, of 2048 ->
+            // 6000 3.9 / 3.6, of 8192 -> 28672 28.0 / 25.1.
+            // 1 / 2 / 4 groups a workgroup, eight bf16 rows: 4096^2 5.0 / 5.4 / 6.5,
+            // 2048 -> 6000 5.1 / 3.9 / 4.4, 4096 -> 11008 10.2 / 9.0 / 7.4.
+            // Tiles, which read the rows once for 128 columns, against 4 groups: 16
+            // rows of 8192 -> 16640 19.7 / 23.8, -> 28672 28.0 / 33.0, of 4096 -> 16640
+            // 12.4 / 14.3; 9 rows of 4096 -> 28672 14.3 / 12.8, 16 of 2048 -> 28672
+            // 10.0 / 9.6, of 8192 -> 14336 (896 groups) 19.7 / 14.1.
             if (ACT == kQ4Bf16 && q.M <= 2 && q4_staged_lds(q.M, q.K, 2, false, 8) <= kStreamMaxLds)
                 q4_staged_launch<ACT, false, 1, 2>(q, st);
+            else if (ACT == kQ4Bf16 && groups > 1024 && q.M * q.K > 49152)
+                q4_mid_launch<kQ4Bf16, 16, 128, 1, 2, 4, 4, 2>(q, st);
             else if (groups <= kCus) q4_few_launch<ACT, 1, 2>(q, st);
             else if (groups <= 600) q4_few_launch<ACT, 2, 1>(q, st);
             else q4_few_launch<ACT, 4, 1>(q, st);
@@ -2699,7 +2713,8 @@ pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, con
         p.H = (bf16*)H;
         p.eps = eps;
         TimedLaunch timed(kSiteQ4Norm, st);
-        // choice
+        // 1 / 2 / 4 groups a workgroup, one row (us): 4096^2 4.8 / 5.1 / 6.2, 4096 ->
+        // 12288 9.8 / 7.5 / 7.8, 8192 -> 28672 30.6 / 26.2 / 24.8
         if (packed_groups(p.N) <= kCus) q4_staged_launch<kQ4Bf16, true, 1, 2>(p, st);
         else if (packed_groups(p.N) <= 1024) q4_staged_launch<kQ4Bf16, true, 2, 1>(p, st);
         else q4_staged_launch<kQ4Bf16, true, 4, 1>(p, st);

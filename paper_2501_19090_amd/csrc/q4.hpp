@@ -210,17 +210,13 @@ __device__ __forceinline__ void q4_turn(u32x4 (&x)[4]) {
     for (int i = 0; i < 4; ++i) {
         uint32_t a = x[0][i], b = x[1][i], c = x[2][i], d = x[3][i];
         auto s = __builtin_amdgcn_permlane32_swap(a, c, false, false);
-        a = s[0];
-        c = s[1];
+        a = s[0]; c = s[1];
         s = __builtin_amdgcn_permlane32_swap(b, d, false, false);
-        b = s[0];
-        d = s[1];
+        b = s[0]; d = s[1];
         s = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-        x[0][i] = s[0];
-        x[1][i] = s[1];
+        x[0][i] = s[0]; x[1][i] = s[1];
         s = __builtin_amdgcn_permlane16_swap(c, d, false, false);
-        x[2][i] = s[0];
-        x[3][i] = s[1];
+        x[2][i] = s[0]; x[3][i] = s[1];
     }
 }
 
@@ -264,83 +260,66 @@ __device__ __forceinline__ void q4_pipeline(int wave, int KB, Blk (&even)[U], Bl
     }
 }
 
-// A workgroup owns NG groups of 16 weight rows (columns of Y) and 16 MT rows of
-// X (blockIdx.y picks them); its waves take the 128-wide blocks of K in turn,
-// each on registers alone, and are summed in LDS at the end.  The loads of a
-// wave's next U blocks are issued before the MFMAs of the current ones.  bf16
-// rows are loaded 64 bytes at a time (piece c of lane group q: columns 32 c + 8
-// q ..) and turned over the lane groups to meet the codes, whose lane has 32
-// columns of its row.
-template <int ACT, int MT, int NG, int WAVES, int U>
+// At most 16 rows.  A workgroup owns NG groups of 16 weight rows (columns of Y);
+// its waves take the 128-wide blocks of K in turn, each on registers alone, and
+// are summed in LDS at the end.  The rows come from the caches again for every
+// workgroup: NG grows with the number of groups (see the dispatch).  A bf16
+// lane multiplies 64 consecutive bytes of a row; the four lanes of a row load
+// them as 64 bytes side by side per instruction and turn them (16 rows of 8192
+// -> 28672 33 us, loaded as they are multiplied 38 us).
+template <int ACT, int NG, int WAVES, int U>
 __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
     constexpr int XC = ACT == kQ4Bf16 ? 4 : 2;  // 16-byte pieces of a lane's 32 values
     constexpr int ES = ACT == kQ4Bf16 ? 2 : 1;
-    __shared__ f32x4 red[WAVES][MT * NG][kWave];
+    static_assert(NG <= WAVES, "a wave adds up a group");
+    __shared__ f32x4 red[WAVES][NG][kWave];
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = lane & 15, q = lane >> 4;
-    const int KB = (int)packed_kblocks(p.K), K = (int)p.K;
-    const int64_t g0 = (int64_t)blockIdx.x * NG, m0 = (int64_t)blockIdx.y * (16 * MT);
-    const int64_t left = p.M - m0;
-    const int rows = left < 16 * MT ? (int)left : 16 * MT;
+    const int KB = (int)packed_kblocks(p.K), K = (int)p.K, rows = (int)p.M;
+    const int64_t groups = packed_groups(p.N), g0 = (int64_t)blockIdx.x * NG;
 
     // the range ends with the last row; masked lanes read zeros
-    const auto xrs = make_rsrc31((const char*)p.X + m0 * p.K * ES, (int64_t)rows * p.K * ES);
+    const auto xrs = make_rsrc31(p.X, (int64_t)rows * K * ES);
     __amdgpu_buffer_rsrc_t wrs[NG];
-    const int64_t groups = packed_groups(p.N);
 #pragma unroll
     for (int j = 0; j < NG; ++j)
         wrs[j] = make_rsrc31(p.W + (g0 + j < groups ? g0 + j : 0) * KB * kQ4Block,
                              g0 + j < groups ? (int64_t)KB * kQ4Block : 0);
-
-    f32x4 acc[MT][NG];
+    f32x4 acc[NG];
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int j = 0; j < NG; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NG; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     struct Blk {
         u32x4 w[NG];
         uint32_t s[NG];
-        u32x4 x[MT][XC];
-    };
-    constexpr int PIECE = 64 / ES;  // columns between a lane's pieces as loaded
-    auto fetch = [&](int b, Blk& f) {
-#pragma unroll
-        for (int j = 0; j < NG; ++j) q4_load(wrs[j], b < KB, b, lane, f.w[j], f.s[j]);
-#pragma unroll
-        for (int c = 0; c < XC; ++c) {
-            const int k = 128 * b + PIECE * c + 16 / ES * q;
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-                f.x[t][c] = load16(xrs, row + 16 * t < rows && k < K ? (uint32_t)(((row + 16 * t) * K + k) * ES)
-                                                                     : kMaskedOffset);
-        }
+        u32x4 x[XC];
     };
     auto fetch_step = [&](int s, Blk(&f)[U]) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) fetch(wave + (s * U + u) * WAVES, f[u]);
+        for (int u = 0; u < U; ++u) {
+            const int b = wave + (s * U + u) * WAVES;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) q4_load(wrs[j], b < KB, b, lane, f[u].w[j], f[u].s[j]);
+#pragma unroll
+            for (int c = 0; c < XC; ++c) {
+                // 64 bytes in a row of the four lane groups; bf16 is turned in step()
+                const int k = 128 * b + (64 / ES) * c + (16 / ES) * q;
+                f[u].x[c] = load16(xrs, row < rows && k < K ? (uint32_t)((row * K + k) * ES) : kMaskedOffset);
+            }
+        }
     };
-    auto step = [&](int b, Blk& f) {
-        if constexpr (ACT == kQ4Bf16) {
+    auto step = [&](int, Blk& f) {
+        if constexpr (ACT == kQ4Bf16) q4_turn(f.x);
 #pragma unroll
-            for (int t = 0; t < MT; ++t) q4_turn(f.x[t]);
-#pragma unroll
-            for (int j = 0; j < NG; ++j) {
+        for (int j = 0; j < NG; ++j) {
+            if constexpr (ACT == kQ4Bf16) {
                 const float s = __builtin_bit_cast(float, f.s[j] << 23);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const u32x4 w = q4_to_bf16(f.w[j][c], s);
-#pragma unroll
-                    for (int t = 0; t < MT; ++t) acc[t][j] = q4_mfma_bf16(w, f.x[t][c], acc[t][j]);
-                }
+                for (int c = 0; c < 4; ++c) acc[j] = q4_mfma_bf16(q4_to_bf16(f.w[j][c], s), f.x[c], acc[j]);
+            } else {
+                acc[j] = q4_mfma_e4m3(f.w[j], f.s[j], f.x[0], f.x[1], acc[j]);
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < NG; ++j)
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-                    acc[t][j] = q4_mfma_e4m3(f.w[j], f.s[j], f.x[t][0], f.x[t][1], acc[t][j]);
         }
     };
     Blk even[U], odd[U];
@@ -348,24 +327,28 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
     q4_pipeline<U, WAVES>(wave, KB, even, odd, fetch_step, step);
 
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int j = 0; j < NG; ++j) red[wave][t * NG + j][lane] = acc[t][j];
+    for (int j = 0; j < NG; ++j) red[wave][j][lane] = acc[j];
     __syncthreads();
-    for (int i = wave; i < MT * NG; i += WAVES) {
-        const int t = i / NG, j = i % NG;
-        f32x4 tot = red[0][i][lane];
+    if (wave < NG && g0 + wave < groups) {
+        f32x4 tot = red[0][wave][lane];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) tot += red[w][i][lane];
-        const int64_t m = m0 + 16 * t + row;
-        const float factor = ACT == kQ4E4m3 ? (m < p.M ? p.x_scale[m] : 0.f) : 1.f;
-        if (g0 + j < groups) q4_store4(p, m, (g0 + j) * 16 + 4 * q, tot, factor);
+        for (int w = 1; w < WAVES; ++w) tot += red[w][wave][lane];
+        const float factor = ACT == kQ4E4m3 ? (row < rows ? p.x_scale[row] : 0.f) : 1.f;
+        q4_store4(p, row, (g0 + wave) * 16 + 4 * q, tot, factor);
     }
 }
 
 // ------------------------------------------------------------------ few rows, staged
-// As q4_few, with the rows in LDS (layout as above), which each workgroup
-// stages while its first weights are on their way.
+// As q4_few, with the rows in LDS, which each workgroup stages while its first
+// weights are on their way; the norm's form norms them on the way there: the
+// product is of (X + R) gain, rounded to bf16, and rho, a factor of the row,
+// is applied to the sums.  The staged rows leave the loop nothing to load but
+// weights.
+//
+// LDS: the sums of the waves; then, for each block of K, its pieces (column
+// chunk c, lane group q, row r) at ((c * 4 + q) * M + r) * 16 bytes; 16 zero
+// bytes, which the lanes of rows past M read; rho and the partial sums of
+// squares (512 columns each).
 __host__ __device__ inline int64_t q4_staged_lds(int64_t M, int64_t K, int es, bool norm, int red_kb) {
     return M * packed_kblocks(K) * 128 * es + 16 + (norm ? (M * ceil_div(K, 512) + 16) * 4 : 0) + red_kb * 1024;
 }
@@ -409,6 +392,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
     if (threadIdx.x < 4) reinterpret_cast<uint32_t*>(xs + xbytes)[threadIdx.x] = 0;
     if constexpr (NORM) {
         typedef NormChunk<bf16> C;
+        // a wave takes 512 columns of a row at a time, four such units in flight
         const int segs = (K + 511) / 512, units = M * segs, full = K / 8;
         constexpr int UN = 4;
         for (int u0 = wave; u0 < units; u0 += UN * WAVES) {
@@ -426,7 +410,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
 #pragma unroll
             for (int i = 0; i < UN; ++i) {
                 const int u = u0 + i * WAVES, m = u / segs, c = (u - m * segs) * 64 + lane;
-                if (u >= units) break;
+                if (u >= units) break;  // uniform
                 float h[8], ss = 0.f;
                 bf16 v[8];
                 C::floats(x[i], h);
@@ -437,6 +421,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
                     v[e] = (bf16)(p.gain ? h[e] * C::one(g[i], e) : h[e]);
                 }
                 if (p.H && blockIdx.x == 0) C::store(p.H + (int64_t)m * K, c, full, h);
+                // columns 8c .. 8c + 7: block c / 16, lane group (c / 4) % 4, piece c % 4
                 if (c < KB * 16)
                     *reinterpret_cast<u32x4*>(xs + (((c >> 4) * 16 + (c & 3) * 4 + ((c >> 2) & 3)) * M + m) * 16) =
                         __builtin_bit_cast(u32x4, v);
@@ -446,7 +431,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
             }
         }
         __syncthreads();
-        for (int m = wave; m < M; m += WAVES) {
+        for (int m = wave; m < M; m += WAVES) {  // read after the barrier behind the products
             float ss = 0.f;
             for (int s = lane; s < segs; s += kWave) ss += sums[m * segs + s];
 #pragma unroll

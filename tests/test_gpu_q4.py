@@ -443,3 +443,22 @@ def test_two_streams_at_once():
         torch.cuda.synchronize()
         for a, b in zip(outs, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("M,d_in,d_out", [(16, 4096, 16400), (13, 8192, 16387), (9, 8160, 20000), (12, 4096, 16400)])
+def test_wide_outputs_of_few_rows(M, d_in, d_out):
+    """More than 1024 groups of 16 columns: tiles of 16 x 128 above 49152 elements
+    of X, the form of few rows at just as many, ragged in every direction."""
+    torch = torch_mod()
+    layer, w = _layer(d_in, d_out, 41)
+    with layer:
+        x, _ = _x(M, d_in, 42)
+        wd = _dev(w)
+        big, Y = _guarded(M, d_out)
+        layer(x, Y)
+        want = x.double() @ wd.t().contiguous()
+        mags = SUMS * (x.double().abs() @ wd.abs().t().contiguous())
+        off = (Y.double() - want).abs() - want.abs() * 2.0 ** -8 - mags
+        assert torch.isfinite(Y).all() and float(off.max()) <= 0, float(off.max())
+        torch.cuda.synchronize()
+        assert bool((big[M * d_out:] == -17).all())
