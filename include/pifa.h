@@ -401,7 +401,8 @@ size_t q4_layer_weight_bytes(q4_handle h);
 /*
  * Y = X W^T.
  *   X  device, M x d_in, bf16, 16-byte aligned.
- *   Y  device, M x d_out, bf16; every element is written.
+ *   Y  device, M x d_out, bf16; every element is written.  It must not overlap
+ *      X (PIFA_ERR_INVALID_ARG).
  * Weights are exact in the product up to bf16's range, sums are fp32, Y is
  * rounded once.  M = 0 returns PIFA_OK without launching.  Asynchronous on
  * `stream`; no workspace, so calls on one handle may overlap.
@@ -414,7 +415,7 @@ pifa_status q4_layer_forward(q4_handle h, const void* X, void* Y, int64_t M, voi
  * them cuts each product off at 2^-14 of the largest of its group of 32; sums
  * are fp32 beyond the group.
  *   Q      device, M x d_in bytes, 16-byte aligned.   scale  device, M, fp32.
- *   Y      device, M x d_out, bf16.
+ *   Y      device, M x d_out, bf16, overlapping neither (PIFA_ERR_INVALID_ARG).
  */
 pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* scale, void* Y, int64_t M,
                                   void* stream);
@@ -423,8 +424,9 @@ pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* sc
  * rms_norm_forward and q4_layer_forward in one call:
  *   H = X + R,   Y = (H rho gain) W^T.
  * X, R, gain, eps and H as for rms_norm_forward with d = d_in and bf16, but X,
- * R and gain 16-byte aligned, and H overlapping none of X, R, gain and Y
- * (PIFA_ERR_INVALID_ARG).  For M <= 16 with M d_in <= 12288 it is one launch:
+ * R and gain 16-byte aligned, and H and Y overlapping neither each other nor X,
+ * R and gain (PIFA_ERR_INVALID_ARG): workgroups that still read them follow
+ * those that write.  For M <= 16 with M d_in <= 12288 it is one launch:
  * rho scales whole rows of the product, so it is applied to the sums.  More are
  * normed into the layer's workspace (M x d_in bf16) first, and such calls on
  * one handle must not overlap.  The workspace grows on demand; memory it outgrows is kept until

@@ -2649,7 +2649,9 @@ pifa_status q4_layer_forward(q4_handle h, const void* X, void* Y, int64_t M, voi
     if (!h || M < 0) return PIFA_ERR_INVALID_ARG;
     if (M == 0) return PIFA_OK;
     if (!X || !Y) return PIFA_ERR_INVALID_ARG;
-    if (M > INT32_MAX || !aligned16(X)) return PIFA_ERR_UNSUPPORTED;
+    if (M > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
+    if (overlap(Y, (size_t)M * (size_t)h->d_out * 2, X, (size_t)M * (size_t)h->d_in * 2)) return PIFA_ERR_INVALID_ARG;
+    if (!aligned16(X)) return PIFA_ERR_UNSUPPORTED;
     PIFA_ON_DEVICE(h->device);
     Q4Args p{};
     p.W = h->W;
@@ -2666,7 +2668,11 @@ pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* sc
     if (!h || M < 0) return PIFA_ERR_INVALID_ARG;
     if (M == 0) return PIFA_OK;
     if (!Q || !scale || !Y) return PIFA_ERR_INVALID_ARG;
-    if (M > INT32_MAX || !aligned16(Q)) return PIFA_ERR_UNSUPPORTED;
+    if (M > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
+    const size_t out = (size_t)M * (size_t)h->d_out * 2;
+    if (overlap(Y, out, Q, (size_t)M * (size_t)h->d_in) || overlap(Y, out, scale, (size_t)M * 4))
+        return PIFA_ERR_INVALID_ARG;
+    if (!aligned16(Q)) return PIFA_ERR_UNSUPPORTED;
     PIFA_ON_DEVICE(h->device);
     Q4Args p{};
     p.W = h->W;
@@ -2695,7 +2701,8 @@ pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, con
     if (!X || !Y) return PIFA_ERR_INVALID_ARG;
     const size_t in = (size_t)M * (size_t)h->d_in * 2, out = (size_t)M * (size_t)h->d_out * 2;
     if (overlap(H, in, X, in) || overlap(H, in, R, in) || overlap(H, in, gain, (size_t)h->d_in * 2) ||
-        overlap(H, in, Y, out))
+        overlap(H, in, Y, out) || overlap(Y, out, X, in) || overlap(Y, out, R, in) ||
+        overlap(Y, out, gain, (size_t)h->d_in * 2))
         return PIFA_ERR_INVALID_ARG;
     if (!aligned16(X) || !aligned16(R) || !aligned16(gain)) return PIFA_ERR_UNSUPPORTED;
     PIFA_ON_DEVICE(h->device);

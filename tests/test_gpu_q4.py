@@ -462,3 +462,29 @@ def test_wide_outputs_of_few_rows(M, d_in, d_out):
         assert torch.isfinite(Y).all() and float(off.max()) <= 0, float(off.max())
         torch.cuda.synchronize()
         assert bool((big[M * d_out:] == -17).all())
+
+
+@pytest.mark.parametrize("M", [1, 40])
+def test_outputs_over_inputs_are_refused(M):
+    """Y over an input (each by one element at its end) is refused, next to it is not."""
+    torch, pifa = torch_mod(), _pifa()
+    d = 256
+    layer, _ = _layer(d, d, 51)
+    n = M * d
+    with layer:
+        layer.reserve(M)
+        buf = torch.zeros(4 * n + d, dtype=torch.bfloat16, device="cuda")
+        lib, h, at = pifa.lib(), layer.handle, lambda i: buf.data_ptr() + 2 * i
+        inval = pifa.PIFA_ERR_INVALID_ARG
+        norm = lambda X, R, g, Y: lib.q4_layer_norm_forward(h, at(X), R and at(R), g and at(g), EPS, None, at(Y), M, None)
+        assert lib.q4_layer_forward(h, at(0), at(n - 1), M, None) == inval
+        assert lib.q4_layer_forward(h, at(n), at(1), M, None) == inval
+        assert lib.q4_layer_forward(h, at(0), at(n), M, None) == pifa.PIFA_OK
+        scale = torch.ones(M, device="cuda")
+        assert lib.q4_layer_forward_e4m3(h, at(0), scale.data_ptr(), at(n // 2 - 1), M, None) == inval
+        assert lib.q4_layer_forward_e4m3(h, at(2 * n), at(n - 2), at(0), M, None) == inval
+        assert lib.q4_layer_forward_e4m3(h, at(0), scale.data_ptr(), at(n // 2), M, None) == pifa.PIFA_OK
+        assert norm(0, None, None, 0) == inval and norm(0, None, None, n - 1) == inval
+        assert norm(0, n, None, 2 * n - 1) == inval and norm(0, n, 3 * n, 3 * n + d - 1) == inval
+        assert norm(0, n, 3 * n, 2 * n) == pifa.PIFA_OK
+        torch.cuda.synchronize()
