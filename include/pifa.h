@@ -314,7 +314,8 @@ pifa_status lowrank_layer_destroy(lowrank_handle h);
  *   eps   positive and finite.
  *   H     device, M x d, dtype, or NULL (not stored).
  *   Y     device, M x d, dtype.
- * Any d; no alignment is required.  Sums are fp32 (a row whose squares sum to
+ * d is at most 2^27 (PIFA_ERR_UNSUPPORTED), here and below; no alignment is
+ * required.  Sums are fp32 (a row whose squares sum to
  * more than 3.4e38 has rho = 0); H and Y are each rounded once, Y from the
  * unrounded H.  H and Y may each be X or R themselves, not each other, and
  * overlap nothing otherwise.  M = 0 returns PIFA_OK without launching.
@@ -368,7 +369,8 @@ size_t rms_norm_backward_bytes(int64_t M, int64_t d);
  * the OCP microscaling format: a code is a sign bit above the index into
  * {0, 0.5, 1, 1.5, 2, 3, 4, 6}, 32 consecutive weights of a row share an 8-bit
  * power of two, and scale 255 makes them NaN.  17/32 of a byte per weight.
- * d_in must be a multiple of 32 (PIFA_ERR_UNSUPPORTED) and at most 2^21.
+ * d_in must be a multiple of 32 and at most 2^21, d_out at most 2^27
+ * (PIFA_ERR_UNSUPPORTED).
  *
  * (A low-rank pair U V^T keeps its accuracy in this format as two such layers
  * in a row.  PIFA's W_p and C do not: C rebuilds the non-pivot outputs with

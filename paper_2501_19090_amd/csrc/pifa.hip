@@ -2227,9 +2227,13 @@ pifa_status pifa_build_f64(const double* W, pifa_dims dims, double* W_p, double*
 // ===================================================================== norms
 namespace {
 
+// A launch may not pass 2^32 threads: columns of a row in one launch (64 columns
+// of dgain take 1024 threads), rows of one launch (1024 threads at most each).
+constexpr int64_t kNormMaxD = 1ll << 27, kNormMaxRows = 1ll << 21;
+
 pifa_status check_norm(int64_t M, int64_t d, pifa_dtype dtype, float eps) {
     if (!valid_dtype(dtype) || M < 0 || d < 1 || !(eps > 0.f) || std::isinf(eps)) return PIFA_ERR_INVALID_ARG;
-    if (d > INT32_MAX || M > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
+    if (d > kNormMaxD || M > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
     return PIFA_OK;
 }
 
@@ -2257,8 +2261,15 @@ hipError_t launch_norm(const NormFwd<T>& p, hipStream_t st) {
 template <typename T>
 hipError_t norm_forward_run(const void* X, const void* R, const void* gain, float eps, void* H, void* Y, uint8_t* Q,
                             float* scale, int64_t M, int64_t d, hipStream_t st) {
-    const NormFwd<T> p{(const T*)X, (const T*)R, (const T*)gain, (T*)H, (T*)Y, Q, scale, M, d, eps};
-    return Q ? launch_norm<T, true>(p, st) : launch_norm<T, false>(p, st);
+    for (int64_t m = 0; m < M; m += kNormMaxRows) {
+        const int64_t at = m * d;
+        auto from = [&](auto* p) { return p ? p + at : p; };
+        const NormFwd<T> p{from((const T*)X), from((const T*)R), (const T*)gain, from((T*)H), from((T*)Y), from(Q),
+                           scale ? scale + m : nullptr, std::min(kNormMaxRows, M - m), d, eps};
+        const hipError_t e = Q ? launch_norm<T, true>(p, st) : launch_norm<T, false>(p, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // Backward: rows a workgroup takes at a time (of its 1024 threads, a row gets
@@ -2324,7 +2335,8 @@ struct q4_layer {
 
 namespace {
 
-constexpr int64_t kQ4MaxIn = 1ll << 21;  // 256 rows of X stay inside 31-bit offsets
+constexpr int64_t kQ4MaxIn = 1ll << 21;   // 256 rows of X stay inside 31-bit offsets
+constexpr int64_t kQ4MaxOut = 1ll << 27;  // 16 rows are one launch
 
 void free_q4(q4_layer* h) {
     if (!h) return;
@@ -2356,7 +2368,7 @@ pifa_status q4_create(int64_t d_in, int64_t d_out, q4_handle* out, Fill fill) {
     if (!out) return PIFA_ERR_INVALID_ARG;
     *out = nullptr;
     if (d_in < 1 || d_out < 1) return PIFA_ERR_INVALID_ARG;
-    if (d_in % kQ4Group != 0 || d_in > kQ4MaxIn || d_out > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
+    if (d_in % kQ4Group != 0 || d_in > kQ4MaxIn || d_out > kQ4MaxOut) return PIFA_ERR_UNSUPPORTED;
     q4_layer* h = new (std::nothrow) q4_layer();
     if (!h) return PIFA_ERR_OOM;
     h->d_in = d_in;
@@ -2482,16 +2494,20 @@ void q4_tiles_launch(const Q4Args& p, hipStream_t st) {
                        dim3((unsigned)(ceil_div(p.M, BM) * ceil_div(p.N, BN))), dim3(8 * kWave), 0, st, p);
 }
 
-// Rows of one launch: their tiles stay a 32-bit grid for every d_out.
-constexpr int64_t kQ4MaxRows = 1 << 19;
+// Rows of one launch: at most 2^31 outputs, a thread for each in the smallest
+// tile, since a launch may not pass 2^32 threads.
+int64_t q4_rows_of_launch(int64_t N) {
+    return std::min<int64_t>(1 << 19, std::max<int64_t>(16, ((1ll << 31) / N) & ~15ll));
+}
 
 template <int ACT>
 hipError_t launch_q4(Q4Args p, hipStream_t st) {
     const int64_t M = p.M;
-    for (int64_t m = 0; m < M; m += kQ4MaxRows) {
+    const int64_t slice = q4_rows_of_launch(p.N);
+    for (int64_t m = 0; m < M; m += slice) {
         TimedLaunch timed(kSiteQ4, st);
         Q4Args q = p;
-        q.M = std::min(kQ4MaxRows, M - m);
+        q.M = std::min(slice, M - m);
         q.X = (const char*)p.X + m * p.K * (ACT == kQ4Bf16 ? 2 : 1);
         if (p.x_scale) q.x_scale = p.x_scale + m;
         q.Y = p.Y + m * p.N;
@@ -2578,7 +2594,7 @@ pifa_status rms_norm_forward_e4m3(const void* X, const void* R, const void* gain
 }
 
 size_t rms_norm_backward_bytes(int64_t M, int64_t d) {
-    if (M < 1 || d < 1 || d > INT32_MAX || M > INT32_MAX) return 0;
+    if (M < 1 || d < 1 || d > kNormMaxD || M > INT32_MAX) return 0;
     const int64_t groups = std::max(norm_bwd_groups(M, d, NormChunk<bf16>::N), norm_bwd_groups(M, d, NormChunk<float>::N));
     return groups > 1 ? (size_t)groups * (size_t)d * sizeof(float) : 0;
 }

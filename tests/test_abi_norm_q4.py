@@ -93,3 +93,18 @@ def test_binding_checks_tensors():
                                     (x, torch.bfloat16, 256, 0, ValueError), (x.t(), torch.bfloat16, 256, -1, ValueError)):
         with pytest.raises(err):
             check(bad, "X", dtype, n, dev)
+
+
+def test_sizes_past_a_launch_are_refused():
+    """Rows and outputs whose launch would pass 2^32 threads."""
+    lib, ref = pifa.lib(), ctypes.byref(ctypes.c_void_p())
+    d = (1 << 27) + 1
+    assert lib.rms_norm_forward(FAKE, None, None, 1e-5, None, FAKE2, 2, d, BF16, None) == UNSUP
+    assert lib.rms_norm_forward_e4m3(FAKE, None, None, 1e-5, None, FAKE2, FAKE, 2, d, BF16, None) == UNSUP
+    assert lib.rms_norm_backward(FAKE, None, FAKE, None, 1e-5, FAKE, FAKE, 2, d, BF16, FAKE, 1 << 62, None) == UNSUP
+    assert pifa.rms_norm_backward_bytes(2, d) == 0 and pifa.rms_norm_backward_bytes(2, d - 1) == 2 * 4 * (d - 1)
+    assert lib.q4_layer_create(FAKE, 32, d, BF16, ref) == UNSUP
+    assert lib.q4_layer_create_mx(FAKE, FAKE, 32, d, ref) == UNSUP
+
+
+FAKE2 = ctypes.c_void_p(0x2000)

@@ -297,3 +297,22 @@ def test_captured_and_replayed_beside_eager_work():
         torch.cuda.synchronize()
         for a, b in zip((H, Y, Q, s, dX, dg), other):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
+
+
+@pytest.mark.parametrize("d,M", [(1, (1 << 26) + 5), (520, (1 << 21) + 3)])
+def test_more_rows_than_one_launch(d, M):
+    """The rows behind the first 2^21 of a call: the same values as in a call of their own."""
+    pifa, torch = _pifa(), torch_mod()
+    x = torch.empty(M, d, dtype=torch.bfloat16, device="cuda")
+    x[:, :] = (torch.arange(M, device="cuda") % 251 + 1).to(torch.bfloat16)[:, None]
+    x[:, 0] += 1
+    g, _ = _gain(d, "bf16", 21)
+    Y = pifa.rms_norm_forward(x, g, EPS)
+    Q, s = pifa.rms_norm_forward_e4m3(x, g, EPS)
+    for m in (0, (1 << 21) - 2, (1 << 21) + 1, M - 2):
+        rows = x[m:m + 2].contiguous()
+        assert torch.equal(Y[m:m + 2], pifa.rms_norm_forward(rows, g, EPS)), m
+        q2, s2 = pifa.rms_norm_forward_e4m3(rows, g, EPS)
+        assert torch.equal(Q[m:m + 2].view(torch.uint8), q2.view(torch.uint8)) and torch.equal(s[m:m + 2], s2), m
+    # every row of one value of the period is the same row
+    assert torch.equal(Y[:M // 251 * 251].view(-1, 251, d)[-1], Y[:251])

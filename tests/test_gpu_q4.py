@@ -488,3 +488,28 @@ def test_outputs_over_inputs_are_refused(M):
         assert norm(0, n, None, 2 * n - 1) == inval and norm(0, n, 3 * n, 3 * n + d - 1) == inval
         assert norm(0, n, 3 * n, 2 * n) == pifa.PIFA_OK
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("M,d_in,d_out", [((1 << 19) + 21, 32, 3), (65, 32, (1 << 26) + 5)])
+def test_more_than_one_launch(M, d_in, d_out):
+    """Rows behind the first slice of a call, and slices of few rows of many outputs."""
+    torch, pifa = torch_mod(), _pifa()
+    rng = torch.Generator(device="cuda").manual_seed(5)
+    codes = torch.randint(0, 256, (d_out, d_in // 2), dtype=torch.uint8, device="cuda", generator=rng)
+    scales = torch.full((d_out, d_in // 32), 125, dtype=torch.uint8, device="cuda")
+    x = torch.randn(M, d_in, device="cuda", generator=rng).bfloat16()
+    q, s = x.float().to(torch.float8_e4m3fn), torch.rand(M, device="cuda", generator=rng) + 0.5
+    grid = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, -0., -.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device="cuda")
+    with pifa.Q4Layer.from_mx(codes, scales) as layer:
+        for out, X, f in ((layer(x), x, None), (layer.forward_e4m3(q, s), q, s)):
+            assert out.shape == (M, d_out)
+            n0 = max(0, d_out - 40)
+            c = codes[n0:].int()
+            w = torch.stack((grid[c & 15], grid[c >> 4]), 2).view(d_out - n0, d_in) / 4
+            a = X.double() * (1 if f is None else f.double()[:, None])
+            got, want = out[:, n0:].double(), a @ w.t().contiguous()
+            mags = a.abs() @ w.abs().t().contiguous()
+            cut = 0 if f is None else 2.0 ** -9 * a.abs().amax(1)[:, None] * w.abs().amax(1)[None, :]
+            off = (got - want).abs() - want.abs() * 2.0 ** -8 - SUMS * mags - cut
+            assert torch.isfinite(got).all() and float(off.max()) <= 0, float(off.max())
+            del out
