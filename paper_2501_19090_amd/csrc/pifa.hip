@@ -2243,13 +2243,22 @@ void norm_fwd_launch(const NormFwd<T>& p, hipStream_t st) {
                        p);
 }
 
+// Threads of a row x its chunks each, by the row's full chunks (bf16, us): the
+// fewest threads while there are rows for every CU (4096 rows of 512: 64 x 1 4.2,
+// 256 x 1 6.2, 1024 x 1 14.8; of 2048: 256 x 1 12.7, 1024 x 1 15.7; of 8192: 256 x
+// 4 47.8, 1024 x 1 47.0, 1024 x 2 47.3, in 8 bits 45.8, 45.6, 49.8), the most
+// where few rows wait for their loads (one row of 4096: 1024 x 1 2.65, 256 x 2
+// 2.78; of 8192: 2.9, 256 x 4 3.4).  8-bit rows reduce twice, which 1024 threads
+// pay for at 512 chunks (one row of 4096: 3.67, 256 x 2 3.38; 64 rows 4.01, 3.74),
+// not at 1024 (one row of 8192: 3.86, 256 x 4 4.30).  Rows past 4096 chunks are
+// read again (one row of 32768, which registers hold: 4.9, read again 6.5).
 template <typename T, bool E4M3>
 hipError_t launch_norm(const NormFwd<T>& p, hipStream_t st) {
     TimedLaunch timed(kSiteNorm, st);
     const int64_t chunks = p.d / NormChunk<T>::N;  // full ones
     if (chunks <= 64) norm_fwd_launch<T, E4M3, 64, 1, 4>(p, st);
     else if (chunks <= 256) norm_fwd_launch<T, E4M3, 256, 1, 1>(p, st);
-    else if (chunks <= 512 && p.M > kCus) norm_fwd_launch<T, E4M3, 256, 2, 1>(p, st);
+    else if (chunks <= 512 && (E4M3 || p.M > kCus)) norm_fwd_launch<T, E4M3, 256, 2, 1>(p, st);
     else if (chunks <= 1024 && p.M > kCus) norm_fwd_launch<T, E4M3, 256, 4, 1>(p, st);
     else if (chunks <= 1024) norm_fwd_launch<T, E4M3, 1024, 1, 1>(p, st);
     else if (chunks <= 2048) norm_fwd_launch<T, E4M3, 1024, 2, 1>(p, st);
@@ -2274,7 +2283,10 @@ hipError_t norm_forward_run(const void* X, const void* R, const void* gain, floa
 
 // Backward: rows a workgroup takes at a time (of its 1024 threads, a row gets
 // one per full chunk); at most one workgroup per CU, so that there are few
-// partial sums of dgain.
+// partial sums of dgain.  More threads a row than chunks, or two chunks each
+// where one fits, lose (4096 rows, us): 512: 64 threads 8.7, 128 10.6; 2048: 256
+// 17.6, 512 22.0; 4096: 512 31.0, 1024 39.8, 256 x 2 40.4; 8192: 1024 55.6, 512 x
+// 2 66.7; 16384: 1024 x 2 122.7, read twice 343.
 int64_t norm_bwd_rows(int64_t d, int64_t n) {
     const int64_t chunks = d / n;
     return chunks <= 64 ? 16 : chunks <= 128 ? 8 : chunks <= 256 ? 4 : chunks <= 512 ? 2 : 1;
@@ -2412,14 +2424,18 @@ constexpr int64_t kQ4NormElems = 12288;
 bool q4_norm_in_one(int64_t M, int64_t K) { return M <= 16 && M * K <= kQ4NormElems; }
 
 // Forms of a product of more than 16 rows, with the time a tile takes in us: p
-// + a K / 1000, alone on its CU (one) or two at a time (two; 0: LDS leaves room
-// for one).  A form whose p is 0 is not there: another is faster everywhere.
-// Measured at K = 4096 and 11008 over 17 to 4096 rows with hot weights; over 78
-// drawn sizes (K 256 to 13000, N 285 to 28000, M 18 to 3500) the form picked is
-// the measured best or within 8% of it at 72, and within 22% at all.
+// + a K / 1000, alone on its CU (one), or two or three at a time (0: LDS leaves no
+// room).  A form whose p is 0 is not there: another is faster everywhere.
+// Measured at K = 4096 and 11008 over 17 to 4096 rows with hot weights.  bf16,
+// 118 drawn sizes (K 288 to 12736, N 270 to 22327, M 20 to 3859): the form picked
+// is the measured best or within 8% of it at 112, and within 32% at all.
+// The codes of bf16 products are converted once for every wave along the rows:
+// tiles of 64 x 128 and 128 x 128 with one (us, against the best of the others):
+// 64 rows of 8192 -> 28672 43 / 54, 128 rows 65 / 79; 203 rows of 4096 -> 22016
+// 47 / 53; 512 rows of 11008 -> 4096 51 / 58.
 struct Q4Form {
     int bm, bn;
-    double one_p, one_a, two_p, two_a;
+    double one_p, one_a, two_p, two_a, three_p, three_a;
 };
 enum Q4Forms : int {
     kQ4T16x32,
@@ -2428,7 +2444,9 @@ enum Q4Forms : int {
     kQ4T32x128,
     kQ4T64x64Deep,
     kQ4T64x64,
+    kQ4T64x128Deep,
     kQ4T64x128,
+    kQ4T128x128Deep,
     kQ4T128x128,
     kQ4T128x128Pair,
     kQ4T128x256,
@@ -2442,8 +2460,10 @@ const Q4Form kQ4FormTable[2][kQ4FormCount] = {
      {32, 128, 5.4, 2.2, 0, 0},
      {64, 64, 4.6, 2.6, 0, 0},
      {64, 64, 3.9, 3.07, 4.0, 5.1},
-     {64, 128, 0, 0, 0, 0},
-     {128, 128, 8.4, 7.05, 0, 0},
+     {64, 128, 7.6, 3.8, 0, 0},
+     {64, 128, 6.6, 5.16, 6.9, 7.1, 5.8, 11.3},
+     {128, 128, 8.1, 6.8, 0, 0},
+     {128, 128, 0, 0, 0, 0},
      {128, 128, 9.5, 8.56, 10.5, 12.9},
      {128, 256, 14.0, 13.6, 10.6, 23.9},
      {256, 256, 14.9, 21.3, 0, 0}},
@@ -2453,7 +2473,9 @@ const Q4Form kQ4FormTable[2][kQ4FormCount] = {
      {32, 128, 5.0, 1.6, 0, 0},
      {64, 64, 0, 0, 0, 0},
      {64, 64, 4.3, 1.40, 6.0, 2.55},
+     {64, 128, 0, 0, 0, 0},
      {64, 128, 4.0, 2.27, 5.7, 3.95},
+     {128, 128, 0, 0, 0, 0},
      {128, 128, 5.2, 3.79, 0, 0},
      {128, 128, 6.4, 3.72, 8.0, 6.54},
      {128, 256, 0, 0, 0, 0},
@@ -2467,14 +2489,10 @@ int q4_form(int act, int64_t M, int64_t N, int64_t K) {
         const Q4Form& f = kQ4FormTable[act][i];
         if (f.one_p == 0) continue;
         const int64_t tiles = ceil_div(M, f.bm) * ceil_div(N, f.bn);
-        const double one = f.one_p + f.one_a * k, two = f.two_p + f.two_a * k;
-        double t;
-        if (f.two_a == 0) {
-            t = (double)ceil_div(tiles, kCus) * one;
-        } else {
-            const int64_t rest = tiles % (2 * kCus);
-            t = (double)(tiles / (2 * kCus)) * two + (rest == 0 ? 0.0 : rest <= kCus ? one : two);
-        }
+        const double at_once[3] = {f.one_p + f.one_a * k, f.two_p + f.two_a * k, f.three_p + f.three_a * k};
+        const int most = f.three_a > 0 ? 3 : f.two_a > 0 ? 2 : 1;
+        const int64_t slots = most * kCus, rest = tiles % slots;
+        const double t = (double)(tiles / slots) * at_once[most - 1] + (rest ? at_once[(rest - 1) / kCus] : 0.0);
         if (t < best_t) {
             best_t = t;
             best = i;
@@ -2540,10 +2558,19 @@ hipError_t launch_q4(Q4Args p, hipStream_t st) {
                     if constexpr (!kE4) q4_mid_launch<ACT, 64, 64, 2, 2, 4, 3, 4>(q, st);
                     break;
                 case kQ4T64x64: q4_mid_launch<ACT, 64, 64, 2, 2, 2, 3, 4>(q, st); break;
+                case kQ4T64x128Deep:
+                    if constexpr (!kE4) q4_mid_launch<ACT, 64, 128, 1, 4, 2, 4, 2>(q, st);
+                    break;
                 case kQ4T64x128:
                     if constexpr (kE4) q4_mid_launch<ACT, 64, 128, 2, 4, 1, 3, 4>(q, st);
+                    else q4_mid_launch<ACT, 64, 128, 1, 4, 1, 4, 2>(q, st);
                     break;
-                case kQ4T128x128: q4_mid_launch<ACT, 128, 128, 2, 4, 1, 3, 2>(q, st); break;
+                case kQ4T128x128Deep:
+                    if constexpr (!kE4) q4_mid_launch<ACT, 128, 128, 1, 4, 2, 3, 2>(q, st);
+                    break;
+                case kQ4T128x128:
+                    if constexpr (kE4) q4_mid_launch<ACT, 128, 128, 2, 4, 1, 3, 2>(q, st);
+                    break;
                 case kQ4T128x128Pair:
                     if constexpr (kE4) q4_tiles_launch<ACT, 128, 128, 2, 4, 3, 4>(q, st);
                     else q4_mid_launch<ACT, 128, 128, 2, 2, 1, 3, 2>(q, st);

@@ -513,3 +513,10 @@ def test_more_than_one_launch(M, d_in, d_out):
             off = (got - want).abs() - want.abs() * 2.0 ** -8 - SUMS * mags - cut
             assert torch.isfinite(got).all() and float(off.max()) <= 0, float(off.max())
             del out
+
+
+@pytest.mark.parametrize("M,d_in,d_out", [(773, 576, 1242), (895, 2880, 1172), (797, 32, 2706), (898, 4032, 2263),
+                                          (843, 32, 6922), (899, 1728, 13164)])
+def test_tiles_with_one_wave_along_the_rows(M, d_in, d_out):
+    """Sizes at which bf16 rows take 64 x 128 (both depths) and 128 x 128 tiles, and those next to them."""
+    test_every_tile(M, d_in, d_out)
