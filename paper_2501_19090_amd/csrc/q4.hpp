@@ -19,6 +19,10 @@
 // l of a wave feeds as an MFMA operand.  Rows past N and columns past K hold
 // zero codes under scale 127 (1.0), so a block is a kilobyte and 64 bytes of
 // one stream.
+//
+// Few rows are bound by that stream: one row of 8192 -> 28672 (125 MB) 22.9 us,
+// 5.4 TB/s, where plain reads of 1 GiB reach 6.6; of 4096 -> 11008 (24 MB) 6.2
+// us, of which reading at that rate is 3.7 and a launch about 2.
 #pragma once
 
 #include "common.hpp"

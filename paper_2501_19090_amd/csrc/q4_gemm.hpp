@@ -24,6 +24,10 @@
 // The weights are the first MFMA operand and their rows are dealt over the TN
 // fragments so that a lane's accumulators are 4 TN consecutive columns of a
 // row of Y: row i of fragment j is column (i / 4) * 4 TN + 4 j + i % 4.
+//
+// Measured: 4096 rows of 4096 -> 11008 in bf16 279 us, 1.32 PFLOP/s (a library
+// product of 8192^3: 1.40), matrix cores busy in 65% of the cycles CUs work; 1999
+// rows of 11008 -> 4096 in e4m3 79 us, 2.29 PFLOP/s (library: 2.64), 56%.
 #pragma once
 
 #include "common.hpp"
@@ -313,6 +317,8 @@ __global__ __launch_bounds__(8 * kWave, OCC) void q4_tiles(Q4Args p) {
 // Step s's stage is read (into registers) before the barrier of step s, and
 // loaded again with step s + S after it.
 // S: stages of each group's ring, as many as fit LDS up to SMAX.
+// Bound by those steps, not by memory: 57 rows of 4096 -> 11008 14.1 us, of which
+// reading 26 MB takes 4; deeper rings (4 to 7 stages) gained nothing.
 template <int ACT, int BM, int BN, int WM, int WN, int KG, int SMAX, int OCC>
 __global__ __launch_bounds__(WM* WN* KG* kWave, OCC) void q4_mid(Q4Args p) {
     constexpr bool E4 = ACT == kQ4E4m3;
