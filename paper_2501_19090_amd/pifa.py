@@ -753,10 +753,19 @@ def q4_layer_reserve(handle: int, max_M: int) -> None:
     _check("q4_layer_reserve", lib().q4_layer_reserve(handle, int(max_M)))
 
 
+def _q4_rows(X, name: str, d_in: int, M):
+    """Rows of a 4-bit layer's call: X's last dimension, where M is not given."""
+    if M is not None:
+        return int(M)
+    if X.dim() == 0 or (d_in and X.shape[-1] != d_in):
+        raise ValueError("%s is %s, its rows (last dimension) should hold %d values" % (name, tuple(X.shape), d_in))
+    return X.numel() // d_in if d_in else X.shape[0]
+
+
 def q4_layer_forward(handle: int, X, Y, M: int | None = None, stream=None) -> None:
     rt = _rt()
-    M = X.shape[0] if M is None else int(M)
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    M = _q4_rows(X, "X", d["d_in"], M)
     dev = rt.device()
     _check("q4_layer_forward", lib().q4_layer_forward(
         handle, _ptr_of(X, "X", rt.bf16, M * d["d_in"], dev), _ptr_of(Y, "Y", rt.bf16, M * d["d_out"], dev),
@@ -765,8 +774,8 @@ def q4_layer_forward(handle: int, X, Y, M: int | None = None, stream=None) -> No
 
 def q4_layer_forward_e4m3(handle: int, Q, scale, Y, M: int | None = None, stream=None) -> None:
     rt = _rt()
-    M = Q.shape[0] if M is None else int(M)
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    M = _q4_rows(Q, "Q", d["d_in"], M)
     dev = rt.device()
     _check("q4_layer_forward_e4m3", lib().q4_layer_forward_e4m3(
         handle, _ptr_of(Q, "Q", rt.e4m3, M * d["d_in"], dev), _ptr_of(scale, "scale", rt.f32, M, dev),
@@ -776,8 +785,8 @@ def q4_layer_forward_e4m3(handle: int, Q, scale, Y, M: int | None = None, stream
 def q4_layer_norm_forward(handle: int, X, gain, eps: float, R=None, H=None, Y=None, M: int | None = None,
                           stream=None) -> None:
     rt = _rt()
-    M = X.shape[0] if M is None else int(M)
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    M = _q4_rows(X, "X", d["d_in"], M)
     dev, bf, n = rt.device(), rt.bf16, M * d["d_in"]
     _check("q4_layer_norm_forward", lib().q4_layer_norm_forward(
         handle, _ptr_of(X, "X", bf, n, dev), _ptr_of(R, "R", bf, n, dev), _ptr_of(gain, "gain", bf, d["d_in"], dev), eps,
@@ -865,7 +874,8 @@ class PifaLayer:
 
 
 class Q4Layer:
-    """Owns a 4-bit layer: ``layer(X)`` allocates Y and runs q4_layer_forward."""
+    """Owns a 4-bit layer: ``layer(X)`` allocates Y and runs q4_layer_forward.
+    Rows are the last dimension of X (d_in values each) and of Y (d_out)."""
 
     def __init__(self, W=None, handle: int = 0, d_in: int = 0, d_out: int = 0):
         self.handle = q4_layer_create(W) if W is not None else handle
@@ -877,25 +887,25 @@ class Q4Layer:
         """A layer of weights already in the format (see q4_layer_create_mx)."""
         return cls(None, q4_layer_create_mx(codes, scales), 2 * codes.shape[1], codes.shape[0])
 
-    def _out(self, Y, M: int, X):
-        import torch
-        return torch.empty((M, self.d_out), dtype=torch.bfloat16, device=X.device) if Y is None else Y
+    def _out(self, Y, X):
+        rt = _rt()
+        return rt.empty((*X.shape[:-1], self.d_out), dtype=rt.bf16, device=X.device) if Y is None else Y
 
     def __call__(self, X, Y=None, stream=None):
-        Y = self._out(Y, X.shape[0], X)
-        q4_layer_forward(self.handle, X, Y, X.shape[0], stream)
+        Y = self._out(Y, X)
+        q4_layer_forward(self.handle, X, Y, None, stream)
         return Y
 
     def forward_e4m3(self, Q, scale, Y=None, stream=None):
         """Rows in 8 bits with a scale each, as rms_norm_forward_e4m3 returns them."""
-        Y = self._out(Y, Q.shape[0], Q)
-        q4_layer_forward_e4m3(self.handle, Q, scale, Y, Q.shape[0], stream)
+        Y = self._out(Y, Q)
+        q4_layer_forward_e4m3(self.handle, Q, scale, Y, None, stream)
         return Y
 
     def norm_forward(self, X, gain, eps: float, R=None, H=None, Y=None, stream=None):
         """The product of the norm of X + R; H, where given, takes X + R."""
-        Y = self._out(Y, X.shape[0], X)
-        q4_layer_norm_forward(self.handle, X, gain, eps, R, H, Y, X.shape[0], stream)
+        Y = self._out(Y, X)
+        q4_layer_norm_forward(self.handle, X, gain, eps, R, H, Y, None, stream)
         return Y
 
     def reserve(self, max_M: int):

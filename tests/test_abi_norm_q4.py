@@ -108,3 +108,13 @@ def test_sizes_past_a_launch_are_refused():
 
 
 FAKE2 = ctypes.c_void_p(0x2000)
+
+
+def test_rows_of_a_4_bit_call():
+    torch = pytest.importorskip("torch")
+    rows = pifa._q4_rows
+    assert rows(torch.zeros(2, 3, 64), "X", 64, None) == 6 and rows(torch.zeros(64), "X", 64, None) == 1
+    assert rows(torch.zeros(0, 64), "X", 64, None) == 0 and rows(torch.zeros(7, 5), "X", 64, 2) == 2
+    for shape in ((4, 96), (64, 4), (4, 32), ()):
+        with pytest.raises(ValueError):
+            rows(torch.zeros(shape), "X", 64, None)

@@ -520,3 +520,22 @@ def test_more_than_one_launch(M, d_in, d_out):
 def test_tiles_with_one_wave_along_the_rows(M, d_in, d_out):
     """Sizes at which bf16 rows take 64 x 128 (both depths) and 128 x 128 tiles, and those next to them."""
     test_every_tile(M, d_in, d_out)
+
+
+def test_batches_of_sequences():
+    """X of more than two dimensions: every row is multiplied, Y keeps the leading ones."""
+    torch, pifa = torch_mod(), _pifa()
+    layer, _ = _layer(128, 48, 61)
+    with layer:
+        x, _ = _x(15, 128, 62)
+        gain = torch.ones(128, dtype=torch.bfloat16, device="cuda")
+        q, s = pifa.rms_norm_forward_e4m3(x.view(3, 5, 128), gain, EPS)
+        for lead in ((3, 5), (15, 1), (1, 3, 5)):
+            b = x.view(*lead, 128)
+            assert torch.equal(layer(b), layer(x).view(*lead, 48))
+            assert torch.equal(layer.norm_forward(b, gain, EPS), layer.norm_forward(x, gain, EPS).view(*lead, 48))
+            assert torch.equal(layer.forward_e4m3(q.view(*lead, 128), s), layer.forward_e4m3(q.view(15, 128), s).view(*lead, 48))
+        assert layer(x[4]).shape == (48,) and torch.equal(layer(x[4]), layer(x[4:5])[0])
+        for bad in (x.view(30, 64), x.view(5, 384)):
+            with pytest.raises(ValueError):
+                layer(bad)
