@@ -428,7 +428,7 @@ pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* sc
  * X, R, gain, eps and H as for rms_norm_forward with d = d_in and bf16, but X,
  * R and gain 16-byte aligned, and H and Y overlapping neither each other nor X,
  * R and gain (PIFA_ERR_INVALID_ARG): workgroups that still read them follow
- * those that write.  For M <= 16 with M d_in <= 12288 it is one launch:
+ * those that write.  For M <= 8 with M d_in <= 12288 it is one launch:
  * rho scales whole rows of the product, so it is applied to the sums.  More are
  * normed into the layer's workspace (M x d_in bf16) first, and such calls on
  * one handle must not overlap.  The workspace grows on demand; memory it outgrows is kept until

@@ -2417,11 +2417,12 @@ void q4_staged_launch(const Q4Args& p, hipStream_t st) {
 
 // Whether the norm's form is one launch.  Every workgroup norms the rows again,
 // so it pays while they are few (one launch / norm, then product, us): 4096^2
-// one row 4.8 / 6.0, three 5.8 / 6.7, four 6.4 / 6.9, five 7.7 / 7.0; 4096 ->
-// 12288 one row 7.5 / 8.7, five 10.6 / 9.9; 2048 -> 6000 six rows 6.1 / 6.3,
-// eight 7.2 / 6.5; 8192 -> 28672 one row 24.8 / 26.1, two 29.4 / 27.0.
+// one row 5.2 / 6.2, three 6.7 / 6.8; 4096 -> 12288 one row 7.8 / 8.9, three 9.5 /
+// 9.8; 8192 -> 4096 one row 7.1 / 8.4; 8192 -> 28672 one row 25.4 / 26.3; 2048 ->
+// 6000 four rows 6.2 / 6.3, six 7.0 / 6.2; 1024 -> 3000 eight rows 5.9 / 5.8.  Where
+// the two are level the one launch also keeps the rows' precision.
 constexpr int64_t kQ4NormElems = 12288;
-bool q4_norm_in_one(int64_t M, int64_t K) { return M <= 16 && M * K <= kQ4NormElems; }
+bool q4_norm_in_one(int64_t M, int64_t K) { return M <= kQ4NormRows && M * K <= kQ4NormElems; }
 
 // Forms of a product of more than 16 rows, with the time a tile takes in us: p
 // + a K / 1000, alone on its CU (one), or two or three at a time (0: LDS leaves no
@@ -2763,8 +2764,8 @@ pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, con
         p.H = (bf16*)H;
         p.eps = eps;
         TimedLaunch timed(kSiteQ4Norm, st);
-        // 1 / 2 / 4 groups a workgroup, one row (us): 4096^2 4.8 / 5.1 / 6.2, 4096 ->
-        // 12288 9.8 / 7.5 / 7.8, 8192 -> 28672 30.6 / 26.2 / 24.8
+        // 1 / 2 / 4 groups a workgroup, one row (us): 4096^2 5.2 / 5.6 / 6.6, 4096 ->
+        // 12288 10.8 / 7.8 / 8.2, 8192 -> 28672 32.8 / 27.3 / 25.4
         if (packed_groups(p.N) <= kCus) q4_staged_launch<kQ4Bf16, true, 1, 2>(p, st);
         else if (packed_groups(p.N) <= 1024) q4_staged_launch<kQ4Bf16, true, 2, 1>(p, st);
         else q4_staged_launch<kQ4Bf16, true, 4, 1>(p, st);

@@ -345,16 +345,24 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
 // ------------------------------------------------------------------ few rows, staged
 // As q4_few, with the rows in LDS, which each workgroup stages while its first
 // weights are on their way; the norm's form norms them on the way there: the
-// product is of (X + R) gain, rounded to bf16, and rho, a factor of the row,
-// is applied to the sums.  The staged rows leave the loop nothing to load but
-// weights.
+// product is of (X + R) gain, and rho, a factor of the row, is applied to the
+// sums.  Rounded to bf16 alone, (X + R) gain would add as much error as the
+// output's rounding (more where a few columns carry a row), so at most 8 rows
+// take the MFMA's 16: row m is the rounded values, row 8 + m what the rounding
+// left, and their sums are added at the end.  The staged rows leave the loop
+// nothing to load but weights.
 //
-// LDS: the sums of the waves; then, for each block of K, its pieces (column
-// chunk c, lane group q, row r) at ((c * 4 + q) * M + r) * 16 bytes; 16 zero
-// bytes, which the lanes of rows past M read; rho and the partial sums of
-// squares (512 columns each).
+// LDS: for each block of K, its pieces (column chunk c, lane group q, row slot r
+// of S) at ((c * 4 + q) * S + r) * 16 bytes (S = M, the norm's form 2 M); 16 zero
+// bytes, which the lanes of rows past M read; over both, after the loop, the
+// sums of the waves.  Then rho and the partial sums of squares (512 columns each).
+constexpr int kQ4NormRows = 8;
+__host__ __device__ inline int64_t q4_staged_rows_lds(int64_t M, int64_t K, int es, bool norm, int red_kb) {
+    const int64_t x = (norm ? 2 : 1) * M * packed_kblocks(K) * 128 * es + 16;
+    return x > red_kb * 1024 ? x : red_kb * 1024;
+}
 __host__ __device__ inline int64_t q4_staged_lds(int64_t M, int64_t K, int es, bool norm, int red_kb) {
-    return M * packed_kblocks(K) * 128 * es + 16 + (norm ? (M * ceil_div(K, 512) + 16) * 4 : 0) + red_kb * 1024;
+    return q4_staged_rows_lds(M, K, es, norm, red_kb) + (norm ? (M * ceil_div(K, 512) + 16) * 4 : 0);
 }
 
 template <int ACT, bool NORM, int NG, int WAVES, int U>
@@ -365,10 +373,10 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = lane & 15, q = lane >> 4;
     const int K = (int)p.K, KB = (int)packed_kblocks(p.K), M = (int)p.M;
-    const int xbytes = M * KB * 128 * ES;
-    f32x4* red = reinterpret_cast<f32x4*>(dyn);  // WAVES x NG x 64
-    char* xs = dyn + WAVES * NG * 1024;
-    float* rho = reinterpret_cast<float*>(xs + xbytes + 16);
+    const int S = NORM ? 2 * M : M, xbytes = S * KB * 128 * ES;
+    f32x4* red = reinterpret_cast<f32x4*>(dyn);  // WAVES x NG x 64, after the loop
+    char* xs = dyn;
+    float* rho = reinterpret_cast<float*>(dyn + q4_staged_rows_lds(M, K, ES, NORM, WAVES * NG));
     float* sums = rho + 16;
 
     const int64_t groups = packed_groups(p.N), g0 = (int64_t)blockIdx.x * NG;
@@ -416,19 +424,24 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
                 const int u = u0 + i * WAVES, m = u / segs, c = (u - m * segs) * 64 + lane;
                 if (u >= units) break;  // uniform
                 float h[8], ss = 0.f;
-                bf16 v[8];
+                bf16 v[8], left[8];
                 C::floats(x[i], h);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     h[e] += C::one(r[i], e);
                     ss += h[e] * h[e];
-                    v[e] = (bf16)(p.gain ? h[e] * C::one(g[i], e) : h[e]);
+                    const float y = p.gain ? h[e] * C::one(g[i], e) : h[e];
+                    v[e] = (bf16)y;
+                    const float rest = y - (float)v[e];
+                    left[e] = (bf16)(rest == rest ? rest : 0.f);  // an infinity leaves nothing
                 }
                 if (p.H && blockIdx.x == 0) C::store(p.H + (int64_t)m * K, c, full, h);
                 // columns 8c .. 8c + 7: block c / 16, lane group (c / 4) % 4, piece c % 4
-                if (c < KB * 16)
-                    *reinterpret_cast<u32x4*>(xs + (((c >> 4) * 16 + (c & 3) * 4 + ((c >> 2) & 3)) * M + m) * 16) =
-                        __builtin_bit_cast(u32x4, v);
+                if (c < KB * 16) {
+                    char* at = xs + (((c >> 4) * 16 + (c & 3) * 4 + ((c >> 2) & 3)) * S + m) * 16;
+                    *reinterpret_cast<u32x4*>(at) = __builtin_bit_cast(u32x4, v);
+                    *reinterpret_cast<u32x4*>(at + M * 16) = __builtin_bit_cast(u32x4, left);
+                }
 #pragma unroll
                 for (int s = 1; s < kWave; s <<= 1) ss += __shfl_xor(ss, s);
                 if (lane == 0) sums[u] = ss;
@@ -455,10 +468,12 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
         __syncthreads();
     }
     const bool live = row < M;
+    const int slot = NORM && row >= kQ4NormRows ? row - kQ4NormRows + M : row;
+    const bool held = NORM && row >= kQ4NormRows ? row - kQ4NormRows < M : live;
     uint32_t xat[XC];
 #pragma unroll
-    for (int c = 0; c < XC; ++c) xat[c] = live ? (uint32_t)(((c * 4 + q) * M + row) * 16) : (uint32_t)xbytes;
-    const uint32_t xstep = live ? (uint32_t)(128 * ES * M) : 0u;
+    for (int c = 0; c < XC; ++c) xat[c] = held ? (uint32_t)(((c * 4 + q) * S + slot) * 16) : (uint32_t)xbytes;
+    const uint32_t xstep = held ? (uint32_t)(128 * ES * S) : 0u;
     f32x4 acc[NG];
 #pragma unroll
     for (int j = 0; j < NG; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -478,6 +493,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
         }
     };
     q4_pipeline<U, WAVES>(wave, KB, even, odd, fetch_step, step);
+    __syncthreads();  // the sums take the rows' place
 #pragma unroll
     for (int j = 0; j < NG; ++j) red[(wave * NG + j) * kWave + lane] = acc[j];
     __syncthreads();
@@ -486,7 +502,11 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) tot += red[(w * NG + wave) * kWave + lane];
         float f = 1.f;
-        if constexpr (NORM) f = live ? rho[row] : 0.f;
+        if constexpr (NORM) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tot[i] += __shfl(tot[i], lane ^ kQ4NormRows);
+            f = live ? rho[row] : 0.f;
+        }
         if constexpr (ACT == kQ4E4m3) f = live ? p.x_scale[row] : 0.f;
         q4_store4(p, row, (g0 + wave) * 16 + 4 * q, tot, f);
     }

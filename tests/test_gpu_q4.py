@@ -539,3 +539,30 @@ def test_batches_of_sequences():
         for bad in (x.view(30, 64), x.view(5, 384)):
             with pytest.raises(ValueError):
                 layer(bad)
+
+
+@pytest.mark.parametrize("M,d_in,d_out", [(1, 4096, 1000), (1, 12288, 40), (2, 2080, 16400), (3, 4096, 257), (8, 1536, 5000),
+                                          (8, 32, 17), (5, 96, 16500), (7, 1728, 33)])
+def test_norm_of_few_rows_keeps_its_rows(M, d_in, d_out):
+    """Few rows are multiplied as two bf16 values each, 2^-8 2^-8 = 2^-16 from the
+    row; rho and the products' inputs add fp32 roundings (2^-17), the sums 2^-15.
+    Beside those only the output's rounding is left, also where a few columns
+    carry the row."""
+    torch = torch_mod()
+    layer, w = _layer(d_in, d_out, 71)
+    with layer:
+        for seed in (72, 73):
+            rng = np.random.default_rng([seed, M, d_in])
+            spikes = np.ones(d_in)
+            spikes[rng.integers(0, d_in, 3)] = 60.0
+            st, x = inputs.round_to(rng.standard_normal((M, d_in)) * spikes, "bf16")
+            rst, r = inputs.round_to(rng.standard_normal((M, d_in)), "bf16")
+            gst, g = inputs.round_to(rng.uniform(0.5, 1.5, d_in), "bf16")
+            big, Y = _guarded(M, d_out)
+            H = torch.empty(M, d_in, dtype=torch.bfloat16, device="cuda")
+            layer.norm_forward(to_dev(st), to_dev(gst), EPS, R=to_dev(rst), H=H, Y=Y)
+            rows = (x + r) * o.rho(x + r, EPS) * g
+            _check(Y, rows @ w.T, np.abs(rows) @ np.abs(w).T, 2.0 ** -16 + 2.0 ** -17 + SUMS, (M, d_in, d_out, seed))
+            assert bool((big[M * d_out:] == -17).all())
+            off = np.abs(from_dev(H) - (x + r)) - np.abs(x + r) * 2.0 ** -8
+            assert (off <= 0).all()
