@@ -430,8 +430,9 @@ pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* sc
  * R and gain (PIFA_ERR_INVALID_ARG): workgroups that still read them follow
  * those that write.  For M <= 8 with M d_in <= 12288 it is one launch:
  * rho scales whole rows of the product, so it is applied to the sums.  More are
- * normed into the layer's workspace (M x d_in bf16) first, and such calls on
- * one handle must not overlap.  The workspace grows on demand; memory it outgrows is kept until
+ * normed into the layer's workspace first (M x d_in bf16; up to 8 rows twice
+ * that, with what the rounding left, so that only more rows are rounded
+ * between norm and product), and such calls on one handle must not overlap.  The workspace grows on demand; memory it outgrows is kept until
  * the layer is destroyed, so graphs captured with it stay valid.  A call
  * whose stream is being captured does not grow it (PIFA_ERR_TOO_LARGE):
  * reserve first.

@@ -97,6 +97,11 @@ __device__ __forceinline__ float row_reduce(float v, float* red) {
     return v;
 }
 
+// What the forward writes: rows of T, e4m3 rows with scales, or rows of T with
+// what their rounding left in rows of their own (a product that adds both
+// loses nothing).
+enum NormOut : int { kNormSame = 0, kNormE4m3 = 1, kNormSplit = 2 };
+
 template <typename T>
 struct NormFwd {
     const T* X;
@@ -106,15 +111,24 @@ struct NormFwd {
     T* Y;           // bf16 / fp32 rows (may be X or R), or
     uint8_t* Q;     // e4m3 rows with
     float* scale;   // a scale each
+    T* left;        // kNormSplit: Y less its rounded values
     int64_t M, d;
     float eps;
 };
 
+// y - (T)y, 0 for what is not finite
+template <typename T>
+__device__ __forceinline__ float norm_rest(float y) {
+    const float r = y - (float)(T)y;
+    return r == r ? r : 0.f;
+}
+
 // ROWS rows of at most TPR * V full chunks per workgroup.
-template <typename T, bool E4M3, int TPR, int V, int ROWS>
+template <typename T, int OUT, int TPR, int V, int ROWS>
 __global__ __launch_bounds__(TPR* ROWS) void norm_fwd(NormFwd<T> p) {
     using C = NormChunk<T>;
     constexpr int N = C::N;
+    constexpr bool E4M3 = OUT == kNormE4m3;
     __shared__ float red[2][TPR * ROWS / kWave];
     const int t = threadIdx.x % TPR;
     const int64_t m = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
@@ -169,9 +183,17 @@ __global__ __launch_bounds__(TPR* ROWS) void norm_fwd(NormFwd<T> p) {
             if constexpr (E4M3) amax = max_or_nan(fabsf(h[i][e]), amax);
         }
         if constexpr (!E4M3) C::store(p.Y + row, t + i * TPR, full, h[i]);
+        if constexpr (OUT == kNormSplit) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) h[i][e] = norm_rest<T>(h[i][e]);
+            C::store(p.left + row, t + i * TPR, full, h[i]);
+        }
     }
     if constexpr (!E4M3) {
         if (tail) p.Y[row + kt] = (T)ht;
+        if constexpr (OUT == kNormSplit) {
+            if (tail) p.left[row + kt] = (T)norm_rest<T>(ht);
+        }
     } else {
         const float s = max_or_nan(row_reduce<TPR, true>(amax, red[1]) / kE4m3Max, kE4m3Tiny);
         const float inv = 1.f / s;
@@ -189,10 +211,11 @@ __global__ __launch_bounds__(TPR* ROWS) void norm_fwd(NormFwd<T> p) {
 // Rows too long for a workgroup's registers are read again for the results
 // (and for the maximum of 8-bit rows).  H or Y may be X or R: a thread stores
 // only elements that it alone reads, after its last read of them.
-template <typename T, bool E4M3>
+template <typename T, int OUT>
 __global__ __launch_bounds__(kNormThreads) void norm_fwd_long(NormFwd<T> p) {
     using C = NormChunk<T>;
     constexpr int N = C::N;
+    constexpr bool E4M3 = OUT == kNormE4m3;
     __shared__ float red[2][kNormThreads / kWave];
     const int64_t row = (int64_t)blockIdx.x * p.d;
     const int64_t full = p.d / N, kt = full * N + threadIdx.x;
@@ -242,6 +265,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_long(NormFwd<T> p) {
         if (tail) p.Q[row + kt] = to_e4m3(ht * inv);
     } else {
         if (tail) p.Y[row + kt] = (T)ht;
+        if constexpr (OUT == kNormSplit) {
+            if (tail) p.left[row + kt] = (T)norm_rest<T>(ht);
+        }
     }
     for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
         float h[N], y[N];
@@ -254,6 +280,11 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_long(NormFwd<T> p) {
             C::store_e4m3(p.Q + row, c, full, y);
         } else {
             C::store(p.Y + row, c, full, y);
+            if constexpr (OUT == kNormSplit) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) y[e] = norm_rest<T>(y[e]);
+                C::store(p.left + row, c, full, y);
+            }
         }
     }
 }

@@ -2237,9 +2237,9 @@ pifa_status check_norm(int64_t M, int64_t d, pifa_dtype dtype, float eps) {
     return PIFA_OK;
 }
 
-template <typename T, bool E4M3, int TPR, int V, int ROWS>
+template <typename T, int OUT, int TPR, int V, int ROWS>
 void norm_fwd_launch(const NormFwd<T>& p, hipStream_t st) {
-    hipLaunchKernelGGL((norm_fwd<T, E4M3, TPR, V, ROWS>), dim3((unsigned)ceil_div(p.M, ROWS)), dim3(TPR * ROWS), 0, st,
+    hipLaunchKernelGGL((norm_fwd<T, OUT, TPR, V, ROWS>), dim3((unsigned)ceil_div(p.M, ROWS)), dim3(TPR * ROWS), 0, st,
                        p);
 }
 
@@ -2252,30 +2252,36 @@ void norm_fwd_launch(const NormFwd<T>& p, hipStream_t st) {
 // pay for at 512 chunks (one row of 4096: 3.67, 256 x 2 3.38; 64 rows 4.01, 3.74),
 // not at 1024 (one row of 8192: 3.86, 256 x 4 4.30).  Rows past 4096 chunks are
 // read again (one row of 32768, which registers hold: 4.9, read again 6.5).
-template <typename T, bool E4M3>
+template <typename T, int OUT>
 hipError_t launch_norm(const NormFwd<T>& p, hipStream_t st) {
     TimedLaunch timed(kSiteNorm, st);
     const int64_t chunks = p.d / NormChunk<T>::N;  // full ones
-    if (chunks <= 64) norm_fwd_launch<T, E4M3, 64, 1, 4>(p, st);
-    else if (chunks <= 256) norm_fwd_launch<T, E4M3, 256, 1, 1>(p, st);
-    else if (chunks <= 512 && (E4M3 || p.M > kCus)) norm_fwd_launch<T, E4M3, 256, 2, 1>(p, st);
-    else if (chunks <= 1024 && p.M > kCus) norm_fwd_launch<T, E4M3, 256, 4, 1>(p, st);
-    else if (chunks <= 1024) norm_fwd_launch<T, E4M3, 1024, 1, 1>(p, st);
-    else if (chunks <= 2048) norm_fwd_launch<T, E4M3, 1024, 2, 1>(p, st);
-    else if (chunks <= 4096) norm_fwd_launch<T, E4M3, 1024, 4, 1>(p, st);
-    else hipLaunchKernelGGL((norm_fwd_long<T, E4M3>), dim3((unsigned)p.M), dim3(kNormThreads), 0, st, p);
+    if (chunks <= 64) norm_fwd_launch<T, OUT, 64, 1, 4>(p, st);
+    else if (chunks <= 256) norm_fwd_launch<T, OUT, 256, 1, 1>(p, st);
+    else if (chunks <= 512 && (OUT == kNormE4m3 || p.M > kCus)) norm_fwd_launch<T, OUT, 256, 2, 1>(p, st);
+    else if (chunks <= 1024 && p.M > kCus) norm_fwd_launch<T, OUT, 256, 4, 1>(p, st);
+    else if (chunks <= 1024) norm_fwd_launch<T, OUT, 1024, 1, 1>(p, st);
+    else if (chunks <= 2048) norm_fwd_launch<T, OUT, 1024, 2, 1>(p, st);
+    else if (chunks <= 4096) norm_fwd_launch<T, OUT, 1024, 4, 1>(p, st);
+    else hipLaunchKernelGGL((norm_fwd_long<T, OUT>), dim3((unsigned)p.M), dim3(kNormThreads), 0, st, p);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t norm_forward_run(const void* X, const void* R, const void* gain, float eps, void* H, void* Y, uint8_t* Q,
-                            float* scale, int64_t M, int64_t d, hipStream_t st) {
+                            float* scale, int64_t M, int64_t d, hipStream_t st, void* left = nullptr) {
     for (int64_t m = 0; m < M; m += kNormMaxRows) {
         const int64_t at = m * d;
         auto from = [&](auto* p) { return p ? p + at : p; };
         const NormFwd<T> p{from((const T*)X), from((const T*)R), (const T*)gain, from((T*)H), from((T*)Y), from(Q),
-                           scale ? scale + m : nullptr, std::min(kNormMaxRows, M - m), d, eps};
-        const hipError_t e = Q ? launch_norm<T, true>(p, st) : launch_norm<T, false>(p, st);
+                           scale ? scale + m : nullptr, from((T*)left), std::min(kNormMaxRows, M - m), d, eps};
+        hipError_t e;
+        if constexpr (sizeof(T) == 2) {
+            if (left) e = launch_norm<T, kNormSplit>(p, st);
+            else e = Q ? launch_norm<T, kNormE4m3>(p, st) : launch_norm<T, kNormSame>(p, st);
+        } else {
+            e = Q ? launch_norm<T, kNormE4m3>(p, st) : launch_norm<T, kNormSame>(p, st);
+        }
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -2403,9 +2409,9 @@ pifa_status q4_create(int64_t d_in, int64_t d_out, q4_handle* out, Fill fill) {
     return PIFA_OK;
 }
 
-template <int ACT, int NG, int U>
+template <int ACT, int NG, int U, bool SPLIT = false>
 void q4_few_launch(const Q4Args& p, hipStream_t st) {
-    hipLaunchKernelGGL((q4_few<ACT, NG, 8, U>), dim3((unsigned)ceil_div(packed_groups(p.N), NG)), dim3(8 * kWave), 0,
+    hipLaunchKernelGGL((q4_few<ACT, NG, 8, U, SPLIT>), dim3((unsigned)ceil_div(packed_groups(p.N), NG)), dim3(8 * kWave), 0,
                        st, p);
 }
 
@@ -2417,11 +2423,18 @@ void q4_staged_launch(const Q4Args& p, hipStream_t st) {
 
 // Whether the norm's form is one launch.  Every workgroup norms the rows again,
 // so it pays while they are few (one launch / norm, then product, us): 4096^2
-// one row 5.2 / 6.2, three 6.7 / 6.8; 4096 -> 12288 one row 7.8 / 8.9, three 9.5 /
-// 9.8; 8192 -> 4096 one row 7.1 / 8.4; 8192 -> 28672 one row 25.4 / 26.3; 2048 ->
-// 6000 four rows 6.2 / 6.3, six 7.0 / 6.2; 1024 -> 3000 eight rows 5.9 / 5.8.  Where
-// the two are level the one launch also keeps the rows' precision.
+// one row 5.2 / 6.8, three 6.7 / 7.5; 4096 -> 12288 one row 7.9 / 9.9, three 9.9 /
+// 10.2; 8192 -> 4096 one row 7.2 / 9.1; 8192 -> 28672 one row 25.3 / 28.6; 2048 ->
+// 6000 four rows 6.2 / 6.6, six 7.0 / 6.8, seven 7.2 / 7.1; 1024 -> 3000 eight rows
+// 5.9 / 6.2.
 constexpr int64_t kQ4NormElems = 12288;
+// Rows of the workspace for up to M: at most 8 rows come with what their
+// rounding to bf16 left, which the product adds.  Without it the error against
+// 64 bits is 1.4 times that of fp32 rows, and up to 1.6 where few columns carry
+// few rows; with it two rows of 8192 -> 28672 take 28.8 us (27.0), eight of 4096 ->
+// 12288 11.5 (10.4).  More rows would need twice the products, and their rows
+// even the error out (1.4 times).
+int64_t q4_norm_rows(int64_t M) { return std::max(M, 2 * std::min<int64_t>(M, kQ4NormRows)); }
 bool q4_norm_in_one(int64_t M, int64_t K) { return M <= kQ4NormRows && M * K <= kQ4NormElems; }
 
 // Forms of a product of more than 16 rows, with the time a tile takes in us: p
@@ -2733,7 +2746,7 @@ pifa_status q4_layer_reserve(q4_handle h, int64_t max_M) {
     if (!h || max_M < 0) return PIFA_ERR_INVALID_ARG;
     if (max_M > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
     PIFA_ON_DEVICE(h->device);
-    return q4_norm_in_one(max_M, h->d_in) ? PIFA_OK : q4_ensure(h, (size_t)max_M * (size_t)h->d_in * 2, 0);
+    return q4_norm_in_one(max_M, h->d_in) ? PIFA_OK : q4_ensure(h, (size_t)q4_norm_rows(max_M) * (size_t)h->d_in * 2, 0);
 }
 
 pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, const void* gain, float eps, void* H,
@@ -2771,12 +2784,21 @@ pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, con
         else q4_staged_launch<kQ4Bf16, true, 4, 1>(p, st);
         return hipGetLastError() == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
     }
-    s = q4_ensure(h, in, st);
+    s = q4_ensure(h, (size_t)q4_norm_rows(M) * (size_t)h->d_in * 2, st);
     if (s != PIFA_OK) return s;
-    void* rows = h->ws[h->n_ws - 1];
-    if (norm_forward_run<bf16>(X, R, gain, eps, H, rows, nullptr, nullptr, M, h->d_in, st) != hipSuccess)
+    bf16* rows = (bf16*)h->ws[h->n_ws - 1];
+    bf16* left = M <= kQ4NormRows ? rows + M * h->d_in : nullptr;
+    if (norm_forward_run<bf16>(X, R, gain, eps, H, rows, nullptr, nullptr, M, h->d_in, st, left) != hipSuccess)
         return PIFA_ERR_HIP;
     p.X = rows;
+    if (left) {
+        TimedLaunch timed(kSiteQ4, st);
+        const int64_t groups = packed_groups(p.N);
+        if (groups <= kCus) q4_few_launch<kQ4Bf16, 1, 2, true>(p, st);
+        else if (groups <= 600) q4_few_launch<kQ4Bf16, 2, 1, true>(p, st);
+        else q4_few_launch<kQ4Bf16, 4, 1, true>(p, st);
+        return hipGetLastError() == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+    }
     return launch_q4<kQ4Bf16>(p, st) == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
 }
 

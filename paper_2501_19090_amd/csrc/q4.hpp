@@ -264,6 +264,8 @@ __device__ __forceinline__ void q4_pipeline(int wave, int KB, Blk (&even)[U], Bl
     }
 }
 
+constexpr int kQ4NormRows = 8;  // rows that come as two bf16 values each
+
 // At most 16 rows.  A workgroup owns NG groups of 16 weight rows (columns of Y);
 // its waves take the 128-wide blocks of K in turn, each on registers alone, and
 // are summed in LDS at the end.  The rows come from the caches again for every
@@ -271,7 +273,9 @@ __device__ __forceinline__ void q4_pipeline(int wave, int KB, Blk (&even)[U], Bl
 // lane multiplies 64 consecutive bytes of a row; the four lanes of a row load
 // them as 64 bytes side by side per instruction and turn them (16 rows of 8192
 // -> 28672 33 us, loaded as they are multiplied 38 us).
-template <int ACT, int NG, int WAVES, int U>
+// SPLIT: X is at most 8 rows and behind them what their rounding left, which
+// take rows 8 + m of the MFMA; both sums are added at the end.
+template <int ACT, int NG, int WAVES, int U, bool SPLIT>
 __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
     constexpr int XC = ACT == kQ4Bf16 ? 4 : 2;  // 16-byte pieces of a lane's 32 values
     constexpr int ES = ACT == kQ4Bf16 ? 2 : 1;
@@ -284,7 +288,10 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
     const int64_t groups = packed_groups(p.N), g0 = (int64_t)blockIdx.x * NG;
 
     // the range ends with the last row; masked lanes read zeros
-    const auto xrs = make_rsrc31(p.X, (int64_t)rows * K * ES);
+    const auto xrs = make_rsrc31(p.X, (int64_t)rows * (SPLIT ? 2 : 1) * K * ES);
+    const bool second = SPLIT && row >= kQ4NormRows;
+    const bool held = second ? row - kQ4NormRows < rows : row < rows;
+    const int slot = second ? row - kQ4NormRows + rows : row;
     __amdgpu_buffer_rsrc_t wrs[NG];
 #pragma unroll
     for (int j = 0; j < NG; ++j)
@@ -309,7 +316,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
             for (int c = 0; c < XC; ++c) {
                 // 64 bytes in a row of the four lane groups; bf16 is turned in step()
                 const int k = 128 * b + (64 / ES) * c + (16 / ES) * q;
-                f[u].x[c] = load16(xrs, row < rows && k < K ? (uint32_t)((row * K + k) * ES) : kMaskedOffset);
+                f[u].x[c] = load16(xrs, held && k < K ? (uint32_t)((slot * K + k) * ES) : kMaskedOffset);
             }
         }
     };
@@ -337,6 +344,10 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
         f32x4 tot = red[0][wave][lane];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) tot += red[w][wave][lane];
+        if constexpr (SPLIT) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tot[i] += __shfl(tot[i], lane ^ kQ4NormRows);
+        }
         const float factor = ACT == kQ4E4m3 ? (row < rows ? p.x_scale[row] : 0.f) : 1.f;
         q4_store4(p, row, (g0 + wave) * 16 + 4 * q, tot, factor);
     }
@@ -356,7 +367,6 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
 // of S) at ((c * 4 + q) * S + r) * 16 bytes (S = M, the norm's form 2 M); 16 zero
 // bytes, which the lanes of rows past M read; over both, after the loop, the
 // sums of the waves.  Then rho and the partial sums of squares (512 columns each).
-constexpr int kQ4NormRows = 8;
 __host__ __device__ inline int64_t q4_staged_rows_lds(int64_t M, int64_t K, int es, bool norm, int red_kb) {
     const int64_t x = (norm ? 2 : 1) * M * packed_kblocks(K) * 128 * es + 16;
     return x > red_kb * 1024 ? x : red_kb * 1024;

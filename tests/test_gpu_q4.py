@@ -566,3 +566,8 @@ def test_norm_of_few_rows_keeps_its_rows(M, d_in, d_out):
             assert bool((big[M * d_out:] == -17).all())
             off = np.abs(from_dev(H) - (x + r)) - np.abs(x + r) * 2.0 ** -8
             assert (off <= 0).all()
+
+
+@pytest.mark.parametrize("M,d_in,d_out", [(2, 8192, 700), (4, 4096, 5000), (8, 2048, 16400), (3, 33024, 40), (1, 12320, 97), (8, 1568, 15)])
+def test_norm_in_its_own_launch_keeps_few_rows(M, d_in, d_out):
+    test_norm_of_few_rows_keeps_its_rows(M, d_in, d_out)
