@@ -7,6 +7,7 @@ runs in the HIP library; if it is missing, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
@@ -617,6 +618,18 @@ class _Torch:
             return self.raw_stream(dev)
         return _stream(stream)
 
+    def under(self, stream):
+        """Context in which a call's outputs and workspaces are allocated: the
+        caching allocator hands a freed block out again on the stream it was
+        allocated under at once, so that has to be the stream that uses it."""
+        if stream is None:
+            return contextlib.nullcontext()
+        import torch
+        if not isinstance(stream, torch.cuda.Stream):
+            raw = _stream(stream)
+            stream = torch.cuda.ExternalStream(raw) if raw else torch.cuda.default_stream()
+        return torch.cuda.stream(stream)
+
     def code(self, dtype) -> int:
         c = self.codes.get(dtype)
         if c is None:
@@ -647,7 +660,8 @@ def rms_norm_forward(X, gain, eps: float, R=None, H=None, Y=None, M: int | None 
     rt = _rt()
     M, d = _rows_of(X, M, d)
     if Y is None:
-        Y = rt.empty_like(X)
+        with rt.under(stream):
+            Y = rt.empty_like(X)
     dt, dev, n = X.dtype, rt.device(), M * d
     code = rt.code(dt)
     _check("rms_norm_forward", lib().rms_norm_forward(
@@ -662,10 +676,11 @@ def rms_norm_forward_e4m3(X, gain, eps: float, R=None, H=None, Q=None, scale=Non
     fp32 scale a row, which stand for Q * scale (allocated when not given)."""
     rt = _rt()
     M, d = _rows_of(X, M, d)
-    if Q is None:
-        Q = rt.empty(X.shape, dtype=rt.e4m3, device=X.device)
-    if scale is None:
-        scale = rt.empty(M, dtype=rt.f32, device=X.device)
+    with rt.under(stream):
+        if Q is None:
+            Q = rt.empty(X.shape, dtype=rt.e4m3, device=X.device)
+        if scale is None:
+            scale = rt.empty(M, dtype=rt.f32, device=X.device)
     dt, dev, n = X.dtype, rt.device(), M * d
     code = rt.code(dt)
     _check("rms_norm_forward_e4m3", lib().rms_norm_forward_e4m3(
@@ -682,16 +697,17 @@ def rms_norm_backward_bytes(M: int, d: int) -> int:
 def rms_norm_backward(H, gain, dY, eps: float, dR=None, dX=None, dgain=None, work=None, M: int | None = None,
                       d: int | None = None, stream=None, need_dX: bool = True, need_dgain: bool = True):
     """Gradients of rms_norm_forward: (dX, dgain), dX plus dR where given.
-    Outputs and workspace are allocated when not given; need_dX / need_dgain
+    Outputs and workspace are allocated when not given, under the call's stream; need_dX / need_dgain
     False skip one (None in its place)."""
     rt = _rt()
     M, d = _rows_of(H, M, d)
-    if dX is None and need_dX:
-        dX = rt.empty_like(H)
-    if dgain is None and need_dgain:
-        dgain = rt.empty(d, dtype=rt.f32, device=H.device)
-    if work is None and dgain is not None:
-        work = rt.empty(rms_norm_backward_bytes(M, d), dtype=rt.u8, device=H.device)
+    with rt.under(stream):
+        if dX is None and need_dX:
+            dX = rt.empty_like(H)
+        if dgain is None and need_dgain:
+            dgain = rt.empty(d, dtype=rt.f32, device=H.device)
+        if work is None and dgain is not None:
+            work = rt.empty(rms_norm_backward_bytes(M, d), dtype=rt.u8, device=H.device)
     dt, dev, n = H.dtype, rt.device(), M * d
     code = rt.code(dt)
     nwork = 0 if work is None else work.numel() * work.element_size()
@@ -887,24 +903,27 @@ class Q4Layer:
         """A layer of weights already in the format (see q4_layer_create_mx)."""
         return cls(None, q4_layer_create_mx(codes, scales), 2 * codes.shape[1], codes.shape[0])
 
-    def _out(self, Y, X):
+    def _out(self, Y, X, stream):
+        if Y is not None:
+            return Y
         rt = _rt()
-        return rt.empty((*X.shape[:-1], self.d_out), dtype=rt.bf16, device=X.device) if Y is None else Y
+        with rt.under(stream):
+            return rt.empty((*X.shape[:-1], self.d_out), dtype=rt.bf16, device=X.device)
 
     def __call__(self, X, Y=None, stream=None):
-        Y = self._out(Y, X)
+        Y = self._out(Y, X, stream)
         q4_layer_forward(self.handle, X, Y, None, stream)
         return Y
 
     def forward_e4m3(self, Q, scale, Y=None, stream=None):
         """Rows in 8 bits with a scale each, as rms_norm_forward_e4m3 returns them."""
-        Y = self._out(Y, Q)
+        Y = self._out(Y, Q, stream)
         q4_layer_forward_e4m3(self.handle, Q, scale, Y, None, stream)
         return Y
 
     def norm_forward(self, X, gain, eps: float, R=None, H=None, Y=None, stream=None):
         """The product of the norm of X + R; H, where given, takes X + R."""
-        Y = self._out(Y, X)
+        Y = self._out(Y, X, stream)
         q4_layer_norm_forward(self.handle, X, gain, eps, R, H, Y, None, stream)
         return Y
 

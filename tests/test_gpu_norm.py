@@ -316,3 +316,50 @@ def test_more_rows_than_one_launch(d, M):
         assert torch.equal(Q[m:m + 2].view(torch.uint8), q2.view(torch.uint8)) and torch.equal(s[m:m + 2], s2), m
     # every row of one value of the period is the same row
     assert torch.equal(Y[:M // 251 * 251].view(-1, 251, d)[-1], Y[:251])
+
+
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_workspace_of_a_call_on_another_stream(as_handle):
+    """Gradients on a stream of their own, behind work that holds it up: memory
+    that is allocated and filled on the current stream meanwhile is not the
+    call's workspace."""
+    pifa, torch = _pifa(), torch_mod()
+    M, d = 1100, 1003
+    h_dev, _ = _rows(M, d, "f32", 40)
+    dy_dev, _ = _rows(M, d, "f32", 41)
+    want_x, want_g = pifa.rms_norm_backward(h_dev, None, dy_dev, EPS)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    n = pifa.rms_norm_backward_bytes(M, d)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)
+    dX, dg = pifa.rms_norm_backward(h_dev, None, dy_dev, EPS, stream=side.cuda_stream if as_handle else side)
+    held_up = not side.query()
+    others = [torch.full((n // 4,), 7.0, device="cuda") for _ in range(4)]
+    torch.cuda.current_stream().synchronize()
+    assert held_up
+    side.synchronize()
+    assert torch.equal(dg, want_g) and torch.equal(dX, want_x)
+    assert all(bool((t == 7).all()) for t in others)
+
+
+def test_outputs_of_calls_on_another_stream():
+    """Outputs a call allocates belong to its stream: a block that the current
+    stream still reads is not taken."""
+    pifa, torch = _pifa(), torch_mod()
+    x_dev, _ = _rows(300, 512, "bf16", 42)
+    g_dev, _ = _gain(512, "bf16", 43)
+    want = pifa.rms_norm_forward(x_dev, g_dev, EPS)
+    wq, ws = pifa.rms_norm_forward_e4m3(x_dev, g_dev, EPS)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream, 0, torch.cuda.default_stream()):
+        busy = torch.full_like(x_dev, 3.0)
+        torch.cuda._sleep(20_000_000)
+        kept = busy.clone()  # reads `busy` behind the sleep
+        del busy
+        y = pifa.rms_norm_forward(x_dev, g_dev, EPS, stream=stream)
+        q, s = pifa.rms_norm_forward_e4m3(x_dev, g_dev, EPS, stream=stream)
+        torch.cuda.synchronize()
+        assert bool((kept == 3).all())
+        assert torch.equal(y, want) and torch.equal(q.view(torch.uint8), wq.view(torch.uint8)) and torch.equal(s, ws)

@@ -571,3 +571,26 @@ def test_norm_of_few_rows_keeps_its_rows(M, d_in, d_out):
 @pytest.mark.parametrize("M,d_in,d_out", [(2, 8192, 700), (4, 4096, 5000), (8, 2048, 16400), (3, 33024, 40), (1, 12320, 97), (8, 1568, 15)])
 def test_norm_in_its_own_launch_keeps_few_rows(M, d_in, d_out):
     test_norm_of_few_rows_keeps_its_rows(M, d_in, d_out)
+
+
+def test_outputs_of_calls_on_another_stream():
+    """Y of a call on a stream of its own is not memory that the current stream still reads."""
+    torch, pifa = torch_mod(), _pifa()
+    layer, _ = _layer(512, 256, 81)
+    with layer:
+        x, _ = _x(40, 512, 82)
+        q, s = pifa.rms_norm_forward_e4m3(x, None, EPS)
+        layer.reserve(40)
+        calls = (lambda **kw: layer(x, **kw), lambda **kw: layer.forward_e4m3(q, s, **kw),
+                 lambda **kw: layer.norm_forward(x, None, EPS, **kw))
+        side = torch.cuda.Stream()
+        for call in calls:
+            want = call()
+            torch.cuda.synchronize()
+            busy = torch.full_like(want, 3.0)
+            torch.cuda._sleep(20_000_000)
+            kept = busy.clone()
+            del busy
+            got = call(stream=side)
+            torch.cuda.synchronize()
+            assert bool((kept == 3).all()) and torch.equal(got, want)
