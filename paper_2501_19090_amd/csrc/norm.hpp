@@ -295,7 +295,7 @@ struct NormBwd {
     const T* gain;  // or null: ones
     const T* dY;
     const T* dR;    // or null: nothing flows in beside the norm
-    T* dX;          // or null; may be dY or dR
+    T* dX;          // or null; may be H, dY or dR
     float* dgain;   // or null: per workgroup partial sums at dgain + blockIdx.x * d
     int64_t M, d;
     float eps;
@@ -363,20 +363,24 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
         u32x4 h[V], y[V], r[V];
         float ht, yt, rt;
     };
-    auto fetch = [&](int64_t m, Rows& f) {
-        const bool live = m < p.M;
-        const int64_t row = (EXACT && !live ? p.M - 1 : live ? m : 0) * p.d, full = live ? nfull : 0;
+    // ALL: no row past M is among them (where a workgroup takes one row at a
+    // time, none ever is).  A row past M is zeros and reads nothing: the rows
+    // before it may be other waves', which store dX over them meanwhile.
+    auto fetch = [&](auto all, int64_t m, Rows& f) {
+        constexpr bool ALL = EXACT && (ROWS == 1 || decltype(all)::value);
+        const bool live = ALL || m < p.M;
+        const int64_t row = (live ? m : 0) * p.d, full = live ? nfull : 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int64_t c = t + i * TPR, n = EXACT ? nfull : full;  // EXACT: c < nfull is known
-            if constexpr (EXACT) {
+            const int64_t c = t + i * TPR;
+            if constexpr (ALL) {  // c < nfull is known
                 f.h[i] = reinterpret_cast<const typename C::Any*>(p.H + row + c * N)->v;
                 f.y[i] = reinterpret_cast<const typename C::Any*>(p.dY + row + c * N)->v;
                 f.r[i] = reinterpret_cast<const typename C::Any*>(p.dR + row + c * N)->v;
             } else {
-                f.h[i] = C::load(p.H + row, c, n);
-                f.y[i] = C::load(p.dY + row, c, n);
-                if (add) f.r[i] = C::load(p.dR + row, c, n);
+                f.h[i] = C::load(p.H + row, c, full);
+                f.y[i] = C::load(p.dY + row, c, full);
+                if (add) f.r[i] = C::load(p.dR + row, c, full);
             }
         }
         f.ht = f.yt = f.rt = 0.f;
@@ -416,7 +420,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float h = C::one(cur.h[i], e), y = C::one(cur.y[i], e);
-                dg[i][e] = __builtin_fmaf(LAST && EXACT && !live ? 0.f : y * h, rho, dg[i][e]);
+                dg[i][e] = __builtin_fmaf(y * h, rho, dg[i][e]);
                 dx[e] = rho * (gain(i, e) * y - h * back);
                 if (add) dx[e] += C::one(cur.r[i], e);
             }
@@ -428,19 +432,19 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
     };
     const int64_t first = (int64_t)blockIdx.x * ROWS;
     Rows even, odd;
-    fetch(first + rg, even);
+    fetch(std::false_type{}, first + rg, even);
     int64_t m0 = first;  // uniform over the workgroup
     for (; EXACT && m0 + 2 * step + ROWS <= p.M; m0 += 2 * step) {
-        fetch(m0 + step + rg, odd);
+        fetch(std::true_type{}, m0 + step + rg, odd);
         __builtin_amdgcn_sched_barrier(0);
         rows(std::false_type{}, m0 + rg, even);
-        fetch(m0 + 2 * step + rg, even);
+        fetch(std::true_type{}, m0 + 2 * step + rg, even);
         __builtin_amdgcn_sched_barrier(0);
         rows(std::false_type{}, m0 + step + rg, odd);
     }
     for (; m0 < p.M; m0 += step) {  // EXACT: at most three, the last of them perhaps cut
         const bool more = m0 + step < p.M;
-        if (more) fetch(m0 + step + rg, odd);
+        if (more) fetch(std::false_type{}, m0 + step + rg, odd);
         rows(std::true_type{}, m0 + rg, even);
         if (more) even = odd;
     }

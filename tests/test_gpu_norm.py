@@ -363,3 +363,30 @@ def test_outputs_of_calls_on_another_stream():
         torch.cuda.synchronize()
         assert bool((kept == 3).all())
         assert torch.equal(y, want) and torch.equal(q.view(torch.uint8), wq.view(torch.uint8)) and torch.equal(s, ws)
+
+
+@pytest.mark.parametrize("d,M", [(512, 17), (512, 16 * 256 + 1), (1024, 9), (2048, 5), (4096, 3), (4096, 517), (8192, 2)])
+def test_backward_over_its_rows_keeps_a_bad_value_in_its_column(d, M):
+    """dX over H, rows of whole chunks and a last group of rows that is cut: a
+    NaN in the last row's dR is that element's of dX, one in its dY that row's of
+    dX and that column's of dgain; neither is another column's."""
+    pifa, torch = _pifa(), torch_mod()
+    h_dev, h = _rows(M, d, "bf16", 50)
+    dy_dev, dy = _rows(M, d, "bf16", 51, scale=1e-2, outliers=False)
+    dr_dev, dr = _rows(M, d, "bf16", 52, scale=1e-2, outliers=False)
+    g_dev, g = _gain(d, "bf16", 53)
+    ref_x, ref_g = pifa.rms_norm_backward(h_dev, g_dev, dy_dev, EPS, dR=dr_dev)
+    bad_r, bad_y = dr_dev.clone(), dy_dev.clone()
+    bad_r[M - 1, 7], bad_y[M - 1, 9] = float("nan"), float("nan")
+    torch.cuda.synchronize()
+    for _ in range(5):
+        over = h_dev.clone()
+        dX, dg = pifa.rms_norm_backward(over, g_dev, dy_dev, EPS, dR=bad_r, dX=over)
+        assert dX is over and torch.equal(dg, ref_g) and torch.equal(dX[:M - 1], ref_x[:M - 1])
+        assert torch.isnan(dX[M - 1, 7]) and int(torch.isnan(dX).sum()) == 1
+        over = h_dev.clone()
+        dX, dg = pifa.rms_norm_backward(over, g_dev, bad_y, EPS, dR=dr_dev, dX=over)
+        assert torch.equal(dX[:M - 1], ref_x[:M - 1]) and torch.isnan(dX[M - 1]).all()
+        assert torch.isnan(dg[9]) and int(torch.isnan(dg).sum()) == 1
+        dg[9] = ref_g[9]
+        assert torch.equal(dg, ref_g)
