@@ -116,11 +116,28 @@ struct NormFwd {
     float eps;
 };
 
-// y - (T)y, 0 for what is not finite
+// y as two bf16 values: hi next to it (at most the largest bf16, so that a y that
+// would round to infinity is not one), lo next to what that leaves: an infinity
+// or a NaN is in lo.
+struct NormPair {
+    bf16 hi, lo;
+    __device__ __forceinline__ explicit NormPair(float y)
+        : hi((bf16)__builtin_amdgcn_fmed3f(y, -0x1.FEp127f, 0x1.FEp127f)), lo((bf16)(y - (float)hi)) {}
+};
+
+// A chunk of both rows of kNormSplit.
 template <typename T>
-__device__ __forceinline__ float norm_rest(float y) {
-    const float r = y - (float)(T)y;
-    return r == r ? r : 0.f;
+__device__ __forceinline__ void norm_store_pairs(const NormFwd<T>& p, int64_t row, int64_t c, int64_t full,
+                                                 float (&y)[NormChunk<T>::N]) {
+    float lo[NormChunk<T>::N];
+#pragma unroll
+    for (int e = 0; e < NormChunk<T>::N; ++e) {
+        const NormPair v(y[e]);
+        y[e] = (float)v.hi;
+        lo[e] = (float)v.lo;
+    }
+    NormChunk<T>::store(p.Y + row, c, full, y);
+    NormChunk<T>::store(p.left + row, c, full, lo);
 }
 
 // ROWS rows of at most TPR * V full chunks per workgroup.
@@ -182,17 +199,16 @@ __global__ __launch_bounds__(TPR* ROWS) void norm_fwd(NormFwd<T> p) {
             if (p.gain) h[i][e] *= C::one(g[i], e);
             if constexpr (E4M3) amax = max_or_nan(fabsf(h[i][e]), amax);
         }
-        if constexpr (!E4M3) C::store(p.Y + row, t + i * TPR, full, h[i]);
-        if constexpr (OUT == kNormSplit) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) h[i][e] = norm_rest<T>(h[i][e]);
-            C::store(p.left + row, t + i * TPR, full, h[i]);
-        }
+        if constexpr (OUT == kNormSame) C::store(p.Y + row, t + i * TPR, full, h[i]);
+        if constexpr (OUT == kNormSplit) norm_store_pairs<T>(p, row, t + i * TPR, full, h[i]);
     }
-    if constexpr (!E4M3) {
+    if constexpr (OUT == kNormSame) {
         if (tail) p.Y[row + kt] = (T)ht;
-        if constexpr (OUT == kNormSplit) {
-            if (tail) p.left[row + kt] = (T)norm_rest<T>(ht);
+    } else if constexpr (OUT == kNormSplit) {
+        if (tail) {
+            const NormPair y(ht);
+            p.Y[row + kt] = y.hi;
+            p.left[row + kt] = y.lo;
         }
     } else {
         const float s = max_or_nan(row_reduce<TPR, true>(amax, red[1]) / kE4m3Max, kE4m3Tiny);
@@ -264,9 +280,14 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_long(NormFwd<T> p) {
         if (threadIdx.x == 0) p.scale[blockIdx.x] = s;
         if (tail) p.Q[row + kt] = to_e4m3(ht * inv);
     } else {
-        if (tail) p.Y[row + kt] = (T)ht;
         if constexpr (OUT == kNormSplit) {
-            if (tail) p.left[row + kt] = (T)norm_rest<T>(ht);
+            if (tail) {
+                const NormPair y(ht);
+                p.Y[row + kt] = y.hi;
+                p.left[row + kt] = y.lo;
+            }
+        } else if (tail) {
+            p.Y[row + kt] = (T)ht;
         }
     }
     for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
@@ -279,12 +300,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_long(NormFwd<T> p) {
             for (int e = 0; e < N; ++e) y[e] *= inv;
             C::store_e4m3(p.Q + row, c, full, y);
         } else {
-            C::store(p.Y + row, c, full, y);
-            if constexpr (OUT == kNormSplit) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) y[e] = norm_rest<T>(y[e]);
-                C::store(p.left + row, c, full, y);
-            }
+            if constexpr (OUT == kNormSplit) norm_store_pairs<T>(p, row, c, full, y);
+            else C::store(p.Y + row, c, full, y);
         }
     }
 }

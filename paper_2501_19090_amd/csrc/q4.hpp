@@ -441,9 +441,9 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
                     h[e] += C::one(r[i], e);
                     ss += h[e] * h[e];
                     const float y = p.gain ? h[e] * C::one(g[i], e) : h[e];
-                    v[e] = (bf16)y;
-                    const float rest = y - (float)v[e];
-                    left[e] = (bf16)(rest == rest ? rest : 0.f);  // an infinity leaves nothing
+                    const NormPair pair(y);
+                    v[e] = pair.hi;
+                    left[e] = pair.lo;
                 }
                 if (p.H && blockIdx.x == 0) C::store(p.H + (int64_t)m * K, c, full, h);
                 // columns 8c .. 8c + 7: block c / 16, lane group (c / 4) % 4, piece c % 4

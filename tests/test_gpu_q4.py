@@ -594,3 +594,29 @@ def test_outputs_of_calls_on_another_stream():
             got = call(stream=side)
             torch.cuda.synchronize()
             assert bool((kept == 3).all()) and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("M,d_in", [(2, 4096), (4, 4096), (3, 33024)])
+def test_norm_of_few_rows_next_to_the_end_of_the_range(M, d_in):
+    """A value past the largest bf16 that fp32 still holds is two finite bf16
+    values, not an infinity and its opposite.  One weight a row, so the product is
+    that value's (one launch, two launches, rows read twice)."""
+    torch, pifa = torch_mod(), _pifa()
+    d_out = 40
+    codes, scales = np.zeros((d_out, d_in // 2), np.uint8), np.full((d_out, d_in // 32), 27, np.uint8)
+    codes[:, 2] = 1 + np.arange(d_out) % 7  # column 4, 2^-100 times 0.5 .. 6
+    w = o.mx_weights(codes, scales)
+    x = np.ones((M, d_in))
+    x[:, : d_in * 3 // 5] = 1 + 2.0 ** -7
+    gain = np.zeros(d_in)
+    gain[4] = 1.9921875 * 2.0 ** 127  # the largest bf16
+    r = np.zeros((M, d_in))
+    # one launch holds X + R times the gain, two launches the normed row
+    r[:, 4] = 2.0 ** -8 - 2.0 ** -7 if M * d_in <= 12288 else 0.0
+    h, y = o.rms_norm(x, gain, EPS, r)
+    held = (h * gain if M * d_in <= 12288 else y)[:, 4]
+    assert ((held > 1.998 * 2.0 ** 127) & (held < 2.0 ** 128)).all()
+    dev = lambda a: to_dev(inputs.round_to(a, "bf16")[0])
+    with pifa.Q4Layer.from_mx(_dev(codes), _dev(scales)) as layer:
+        got = layer.norm_forward(dev(x), dev(gain[None]).reshape(-1), EPS, R=dev(r))
+    _check(got, y @ w.T, np.abs(y) @ np.abs(w).T, 2.0 ** -16 + 2.0 ** -17 + SUMS, (M, d_in))
