@@ -2343,6 +2343,7 @@ struct q4_layer {
     int device = 0;
     int64_t d_in = 0, d_out = 0;
     uint8_t* W = nullptr;  // packed (q4.hpp)
+    int top_scale = 0;     // of any group
     // Normed rows.  Graphs captured with an outgrown buffer still point to it,
     // so all are kept; each is at least twice the one before.
     static constexpr int kMaxBufs = 48;
@@ -2394,12 +2395,19 @@ pifa_status q4_create(int64_t d_in, int64_t d_out, q4_handle* out, Fill fill) {
     pifa_status s = PIFA_OK;
     if (hipGetDevice(&h->device) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
         s = PIFA_ERR_HIP;
-    } else if (hipMalloc(&h->W, (size_t)q4_packed_bytes(d_out, d_in)) != hipSuccess) {
+    } else if (const size_t bytes = (size_t)q4_packed_bytes(d_out, d_in);
+               hipMalloc(&h->W, bytes + sizeof(int)) != hipSuccess) {
         (void)hipGetLastError();
         s = PIFA_ERR_OOM;
     } else {
-        fill(h, dim3(grid_for(packed_groups(d_out) * 16 * packed_kblocks(d_in) * 4)));
-        if (hipGetLastError() != hipSuccess || hipDeviceSynchronize() != hipSuccess) s = PIFA_ERR_HIP;
+        const int64_t blocks = packed_groups(d_out) * packed_kblocks(d_in);
+        int* top = (int*)(h->W + bytes);
+        fill(h, dim3(grid_for(blocks * 64)));
+        hipLaunchKernelGGL(norm_zero, dim3(1), dim3(64), 0, 0, (float*)top, (int64_t)1);
+        hipLaunchKernelGGL(q4_top_scale, dim3(grid_for(blocks * 4)), dim3(256), 0, 0, h->W, blocks, top);
+        if (hipGetLastError() != hipSuccess || hipDeviceSynchronize() != hipSuccess ||
+            hipMemcpy(&h->top_scale, top, sizeof(int), hipMemcpyDeviceToHost) != hipSuccess)
+            s = PIFA_ERR_HIP;
     }
     if (s != PIFA_OK) {
         free_q4(h);
@@ -2427,7 +2435,10 @@ void q4_staged_launch(const Q4Args& p, hipStream_t st) {
 // 10.2; 8192 -> 4096 one row 7.2 / 9.1; 8192 -> 28672 one row 25.3 / 28.6; 2048 ->
 // 6000 four rows 6.2 / 6.6, six 7.0 / 6.8, seven 7.2 / 7.1; 1024 -> 3000 eight rows
 // 5.9 / 6.2.
-constexpr int64_t kQ4NormElems = 12288;
+bool q4_norm_in_one(const q4_layer* h, int64_t M) {
+    return M <= kQ4NormRows && M * h->d_in <= kQ4NormElems && h->top_scale <= 127 + kQ4NormTop;
+}
+
 // Rows of the workspace for up to M: at most 8 rows come with what their
 // rounding to bf16 left, which the product adds.  Without it the error against
 // 64 bits is 1.4 times that of fp32 rows, and up to 1.6 where few columns carry
@@ -2435,7 +2446,6 @@ constexpr int64_t kQ4NormElems = 12288;
 // 12288 11.5 (10.4).  More rows would need twice the products, and their rows
 // even the error out (1.4 times).
 int64_t q4_norm_rows(int64_t M) { return std::max(M, 2 * std::min<int64_t>(M, kQ4NormRows)); }
-bool q4_norm_in_one(int64_t M, int64_t K) { return M <= kQ4NormRows && M * K <= kQ4NormElems; }
 
 // Forms of a product of more than 16 rows, with the time a tile takes in us: p
 // + a K / 1000, alone on its CU (one), or two or three at a time (0: LDS leaves no
@@ -2746,7 +2756,7 @@ pifa_status q4_layer_reserve(q4_handle h, int64_t max_M) {
     if (!h || max_M < 0) return PIFA_ERR_INVALID_ARG;
     if (max_M > INT32_MAX) return PIFA_ERR_UNSUPPORTED;
     PIFA_ON_DEVICE(h->device);
-    return q4_norm_in_one(max_M, h->d_in) ? PIFA_OK : q4_ensure(h, (size_t)q4_norm_rows(max_M) * (size_t)h->d_in * 2, 0);
+    return q4_norm_in_one(h, max_M) ? PIFA_OK : q4_ensure(h, (size_t)q4_norm_rows(max_M) * (size_t)h->d_in * 2, 0);
 }
 
 pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, const void* gain, float eps, void* H,
@@ -2771,7 +2781,7 @@ pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, con
     p.M = M;
     p.N = h->d_out;
     p.K = h->d_in;
-    if (q4_norm_in_one(M, h->d_in)) {
+    if (q4_norm_in_one(h, M)) {
         p.R = (const bf16*)R;
         p.gain = (const bf16*)gain;
         p.H = (bf16*)H;

@@ -146,6 +146,22 @@ __global__ void q4_convert(uint8_t* __restrict__ codes, uint8_t* __restrict__ sc
     }
 }
 
+// The largest scale of any group, NaN aside (*top starts as 0).
+__global__ __launch_bounds__(256) void q4_top_scale(const uint8_t* __restrict__ packed, int64_t blocks, int* top) {
+    int most = 0;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < blocks * 4; i += (int64_t)gridDim.x * blockDim.x) {
+        const u32x4 s = *reinterpret_cast<const u32x4*>(packed + i / 4 * kQ4Block + 1024 + i % 4 * 16);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int v = (int)((s[e / 4] >> (8 * (e & 3))) & 255);
+            most = max(most, v == kQ4NanScale ? 0 : v);
+        }
+    }
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) most = max(most, __shfl_xor(most, s));
+    if ((threadIdx.x & (kWave - 1)) == 0) atomicMax(top, most);
+}
+
 // ------------------------------------------------------------------ products of few rows
 // acc(n, m): the weights are the first MFMA operand, so a lane holds four
 // consecutive columns n of Y of one row m (row l % 16, columns 4 (l / 16) ..).
@@ -265,6 +281,12 @@ __device__ __forceinline__ void q4_pipeline(int wave, int KB, Blk (&even)[U], Bl
 }
 
 constexpr int kQ4NormRows = 8;  // rows that come as two bf16 values each
+// The norm's form in one launch: most elements of X; values of (X + R) gain
+// beyond which a row (512 of it, for the lower bound) counts as far from 1; the
+// largest group scale of the weights, as a power of two.
+constexpr int64_t kQ4NormElems = 12288;
+constexpr float kQ4NormBig = 0x1p40f, kQ4NormSmall = 0x1p-30f;
+constexpr int kQ4NormTop = 60;
 
 // At most 16 rows.  A workgroup owns NG groups of 16 weight rows (columns of Y);
 // its waves take the 128-wide blocks of K in turn, each on registers alone, and
@@ -362,6 +384,11 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
 // take the MFMA's 16: row m is the rounded values, row 8 + m what the rounding
 // left, and their sums are added at the end.  The staged rows leave the loop
 // nothing to load but weights.
+// The sums of unscaled products could leave fp32's range where those of the
+// normed row do not, so a row with values far from 1 is staged again with rho
+// (no row of a model's; the check for it costs up to 0.2 us of 6), and
+// layers with weights past 2^kQ4NormTop take norm and product in two launches:
+// sums stay below 12288 2^40 6 2^60 < 2^117.
 //
 // LDS: for each block of K, its pieces (column chunk c, lane group q, row slot r
 // of S) at ((c * 4 + q) * S + r) * 16 bytes (S = M, the norm's form 2 M); 16 zero
@@ -417,53 +444,78 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
         // a wave takes 512 columns of a row at a time, four such units in flight
         const int segs = (K + 511) / 512, units = M * segs, full = K / 8;
         constexpr int UN = 4;
-        for (int u0 = wave; u0 < units; u0 += UN * WAVES) {
-            u32x4 x[UN], r[UN], g[UN];
+        static_assert(kQ4NormElems / 512 + kQ4NormRows <= kWave, "a bit and a lane for each unit");
+        // AGAIN: the units of `which` once more, with rho
+        auto stage = [&](auto again, uint64_t which) {
+            constexpr bool AGAIN = decltype(again)::value;
+            for (int u0 = wave; u0 < units; u0 += UN * WAVES) {
+                u32x4 x[UN], r[UN], g[UN];
 #pragma unroll
-            for (int i = 0; i < UN; ++i) {
-                const int u = u0 + i * WAVES, m = u / segs, c = (u - m * segs) * 64 + lane;
-                const int in = u < units ? full : 0;
-                x[i] = C::load((const bf16*)p.X + (int64_t)m * K, c, in);
-                r[i] = zero16();
-                g[i] = zero16();
-                if (p.R) r[i] = C::load(p.R + (int64_t)m * K, c, in);
-                if (p.gain) g[i] = C::load(p.gain, c, in);
-            }
-#pragma unroll
-            for (int i = 0; i < UN; ++i) {
-                const int u = u0 + i * WAVES, m = u / segs, c = (u - m * segs) * 64 + lane;
-                if (u >= units) break;  // uniform
-                float h[8], ss = 0.f;
-                bf16 v[8], left[8];
-                C::floats(x[i], h);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    h[e] += C::one(r[i], e);
-                    ss += h[e] * h[e];
-                    const float y = p.gain ? h[e] * C::one(g[i], e) : h[e];
-                    const NormPair pair(y);
-                    v[e] = pair.hi;
-                    left[e] = pair.lo;
-                }
-                if (p.H && blockIdx.x == 0) C::store(p.H + (int64_t)m * K, c, full, h);
-                // columns 8c .. 8c + 7: block c / 16, lane group (c / 4) % 4, piece c % 4
-                if (c < KB * 16) {
-                    char* at = xs + (((c >> 4) * 16 + (c & 3) * 4 + ((c >> 2) & 3)) * S + m) * 16;
-                    *reinterpret_cast<u32x4*>(at) = __builtin_bit_cast(u32x4, v);
-                    *reinterpret_cast<u32x4*>(at + M * 16) = __builtin_bit_cast(u32x4, left);
+                for (int i = 0; i < UN; ++i) {
+                    const int u = u0 + i * WAVES, m = u / segs, c = (u - m * segs) * 64 + lane;
+                    const int in = u < units && (!AGAIN || ((which >> u) & 1)) ? full : 0;
+                    x[i] = C::load((const bf16*)p.X + (int64_t)m * K, c, in);
+                    r[i] = zero16();
+                    g[i] = zero16();
+                    if (p.R) r[i] = C::load(p.R + (int64_t)m * K, c, in);
+                    if (p.gain) g[i] = C::load(p.gain, c, in);
                 }
 #pragma unroll
-                for (int s = 1; s < kWave; s <<= 1) ss += __shfl_xor(ss, s);
-                if (lane == 0) sums[u] = ss;
+                for (int i = 0; i < UN; ++i) {
+                    const int u = u0 + i * WAVES, m = u / segs, c = (u - m * segs) * 64 + lane;
+                    if (u >= units) break;  // uniform
+                    if (AGAIN && !((which >> u) & 1)) continue;
+                    const float f = AGAIN ? rho[m] : 1.f;
+                    float h[8], ss = 0.f, top = 0.f;
+                    bf16 v[8], left[8];
+                    C::floats(x[i], h);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        h[e] += C::one(r[i], e);
+                        ss += h[e] * h[e];
+                        const float k = AGAIN ? h[e] * f : h[e], y = p.gain ? k * C::one(g[i], e) : k;
+                        top = fmaxf(top, fabsf(y));
+                        const NormPair pair(y);
+                        v[e] = pair.hi;
+                        left[e] = pair.lo;
+                    }
+                    if (!AGAIN && p.H && blockIdx.x == 0) C::store(p.H + (int64_t)m * K, c, full, h);
+                    // columns 8c .. 8c + 7: block c / 16, lane group (c / 4) % 4, piece c % 4
+                    if (c < KB * 16) {
+                        char* at = xs + (((c >> 4) * 16 + (c & 3) * 4 + ((c >> 2) & 3)) * S + m) * 16;
+                        *reinterpret_cast<u32x4*>(at) = __builtin_bit_cast(u32x4, v);
+                        *reinterpret_cast<u32x4*>(at + M * 16) = __builtin_bit_cast(u32x4, left);
+                    }
+                    if constexpr (!AGAIN) {
+#pragma unroll
+                        for (int s = 1; s < kWave; s <<= 1) ss += __shfl_xor(ss, s);
+                        // the sign says whether the unit's values are far from 1
+                        const bool far = __any(top > kQ4NormBig) || (__any(top > 0.f) && !__any(top >= kQ4NormSmall));
+                        if (lane == 0) sums[u] = copysignf(ss, far ? -1.f : 1.f);
+                    }
+                }
             }
-        }
+        };
+        stage(std::false_type{}, 0);
         __syncthreads();
+        const uint64_t far = __ballot(lane < units && signbit(sums[lane < units ? lane : 0]));
         for (int m = wave; m < M; m += WAVES) {  // read after the barrier behind the products
             float ss = 0.f;
-            for (int s = lane; s < segs; s += kWave) ss += sums[m * segs + s];
+            for (int s = lane; s < segs; s += kWave) ss += fabsf(sums[m * segs + s]);
 #pragma unroll
             for (int s = 1; s < kWave; s <<= 1) ss += __shfl_xor(ss, s);
             if (lane == 0) rho[m] = rsqrtf(ss / (float)K + p.eps);
+        }
+        if (far) {  // the same in all waves
+            uint64_t which = 0;
+            for (int m = 0; m < M; ++m) {
+                const uint64_t row_units = ((1ull << segs) - 1) << (m * segs);
+                if (far & row_units) which |= row_units;
+            }
+            __syncthreads();
+            stage(std::true_type{}, which);
+            __syncthreads();
+            if ((int)threadIdx.x < M && ((which >> (threadIdx.x * segs)) & 1)) rho[threadIdx.x] = 1.f;
         }
     } else {
         const u32x4 xrs = raw_rsrc31(p.X, (int64_t)M * K * ES);

@@ -620,3 +620,75 @@ def test_norm_of_few_rows_next_to_the_end_of_the_range(M, d_in):
     with pifa.Q4Layer.from_mx(_dev(codes), _dev(scales)) as layer:
         got = layer.norm_forward(dev(x), dev(gain[None]).reshape(-1), EPS, R=dev(r))
     _check(got, y @ w.T, np.abs(y) @ np.abs(w).T, 2.0 ** -16 + 2.0 ** -17 + SUMS, (M, d_in))
+
+
+def _norm_want(x, r, gain, w):
+    """Y and its terms' magnitudes where rho is of fp32 sums: 0 past their range."""
+    h = x + r
+    with np.errstate(all="ignore"):
+        p = np.where((h * h).sum(1, keepdims=True) > 2.0 ** 128, 0.0, o.rho(h, EPS))
+        y = h * p * gain
+        return y @ w.T, np.abs(y) @ np.abs(w).T
+
+
+@pytest.mark.parametrize("M,d_in,d_out", [(1, 4096, 40), (7, 1728, 300), (8, 64, 17), (8, 2080, 40), (20, 512, 40)])
+def test_norm_of_rows_of_any_size(M, d_in, d_out):
+    """Rows from 2^-110 to 2^127 (past 2^64 their squares overflow, and the norm is
+    0) beside ordinary ones, which keep their values; in one launch and in two."""
+    torch = torch_mod()
+    layer, w = _layer(d_in, d_out, 91)
+    with layer:
+        st, x0 = inputs.round_to(np.random.default_rng([92, M]).uniform(0.5, 1, (M, d_in)), "bf16")
+        rst, r0 = inputs.round_to(np.random.default_rng([93, M]).uniform(-0.25, 0.25, (M, d_in)), "bf16")
+        gst, g = inputs.round_to(np.random.default_rng(94).uniform(0.5, 1.5, d_in), "bf16")
+        plain = layer.norm_forward(to_dev(st), to_dev(gst), EPS, R=to_dev(rst))
+        for k in (-110, -70, -31, -12, 30, 39, 41, 56, 70, 100, 126):
+            f = np.ones((M, 1))
+            f[M // 2] = 2.0 ** k
+            dev = lambda a: to_dev(inputs.round_to(a * f, "bf16")[0])
+            H = torch.empty(M, d_in, dtype=torch.bfloat16, device="cuda")
+            Y = layer.norm_forward(dev(x0), to_dev(gst), EPS, R=dev(r0), H=H)
+            want, mags = _norm_want(x0 * f, r0 * f, g, w)
+            two = 2.0 ** -16 if M <= 8 else 2.0 ** -8  # rows as two bf16 values, or as one
+            frac = two + 2.0 ** -17 + SUMS
+            _check(Y, want, mags + 2.0 ** -126 / frac, frac, (M, d_in, k))
+            keep = [m for m in range(M) if m != M // 2]
+            assert torch.equal(Y[keep], plain[keep]), k
+            assert (np.abs(from_dev(H) - (x0 + r0) * f) <= np.abs(x0 + r0) * f * 2.0 ** -8).all()
+
+
+@pytest.mark.parametrize("M,d_in", [(4, 512), (4, 4096), (30, 512)])
+def test_norm_and_product_agree_on_what_is_not_finite(M, d_in):
+    """An infinity or a NaN in a row makes all of it NaN, as norm and product apart do, and no other."""
+    torch, pifa = torch_mod(), _pifa()
+    layer, _ = _layer(d_in, 40, 95)
+    with layer:
+        x, _ = _x(M, d_in, 96)
+        r, _ = _x(M, d_in, 97)
+        plain = layer.norm_forward(x, None, EPS, R=r)
+        for bad in (float("inf"), float("-inf"), float("nan")):
+            for a, b in ((x.clone(), r), (x, r.clone())):
+                (a if a is not x else b)[2, d_in - 3] = bad
+                Y = layer.norm_forward(a, None, EPS, R=b)
+                apart = layer(pifa.rms_norm_forward(a, None, EPS, R=b))
+                assert torch.isnan(Y[2]).all() and torch.isnan(apart[2]).all()
+                keep = [m for m in range(M) if m != 2]
+                assert torch.equal(Y[keep], plain[keep])
+
+
+@pytest.mark.parametrize("M", [1, 3])
+@pytest.mark.parametrize("scale", [187, 188, 226])
+def test_norm_with_weights_next_to_the_end_of_the_range(M, scale):
+    """Weights of 2^60 to 2^99 by rows of 2^38: the normed rows' products are in range."""
+    pifa = _pifa()
+    d_in, d_out = 256, 24
+    rng = np.random.default_rng([98, M])
+    codes = rng.integers(0, 256, (d_out, d_in // 2), dtype=np.uint8)
+    scales = rng.integers(scale - 3, scale + 1, (d_out, d_in // 32)).astype(np.uint8)
+    scales[3, 1] = scale
+    w = o.mx_weights(codes, scales)
+    st, x = inputs.round_to(rng.standard_normal((M, d_in)) * 2.0 ** 38, "bf16")
+    with pifa.Q4Layer.from_mx(_dev(codes), _dev(scales)) as layer:
+        Y = layer.norm_forward(to_dev(st), None, EPS)
+    want, mags = _norm_want(x, np.zeros_like(x), np.ones(d_in), w)
+    _check(Y, want, mags, 2.0 ** -16 + 2.0 ** -17 + SUMS, (M, scale))
