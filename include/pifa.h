@@ -330,7 +330,8 @@ pifa_status rms_norm_forward(const void* X, const void* R, const void* gain, flo
  * (OCP e4m3, rounded to nearest even from fp32): Q stands for Q[m,k] scale[m].
  *   Q      device, M x d bytes.   scale  device, M, fp32.
  * X, R, gain, eps, H and dtype as for rms_norm_forward.  A NaN in a row, or
- * an infinity in X + R, makes the row's scale NaN.  Q and scale overlap nothing.
+ * an infinity in X + R, makes the row's scale NaN, a Y past fp32 infinite.  Q
+ * and scale overlap nothing.
  */
 pifa_status rms_norm_forward_e4m3(const void* X, const void* R, const void* gain, float eps, void* H,
                                   uint8_t* Q, float* scale, int64_t M, int64_t d, pifa_dtype dtype,

@@ -68,6 +68,19 @@ struct NormChunk {
         if (c < full) *reinterpret_cast<Bytes*>(row + c * N) = b;
     }
 };
+// Quotients by a row's scale: the product with its reciprocal, corrected by what
+// that leaves.  Before its rounding to fp32 it is within 2^-46 of the quotient, so
+// that midpoints of two e4m3 values are met as a division meets them (1999 rows
+// of 4096: divided 13.6 us, corrected 12.2, the product alone 11.8).
+struct E4m3Scale {
+    float s, inv;
+    __device__ __forceinline__ explicit E4m3Scale(float scale)
+        : s(scale <= 3.402823466e38f ? scale : 0.f), inv(1.f / scale) {}  // an infinite one: y * 0
+    __device__ __forceinline__ float operator()(float y) const {
+        const float q = y * inv;
+        return __builtin_fmaf(__builtin_fmaf(-q, s, y), inv, q);
+    }
+};
 __device__ __forceinline__ uint8_t to_e4m3(float v) {
     return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false);
 }
@@ -212,14 +225,14 @@ __global__ __launch_bounds__(TPR* ROWS) void norm_fwd(NormFwd<T> p) {
         }
     } else {
         const float s = max_or_nan(row_reduce<TPR, true>(amax, red[1]) / kE4m3Max, kE4m3Tiny);
-        const float inv = 1.f / s;
+        const E4m3Scale by(s);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) h[i][e] *= inv;
+            for (int e = 0; e < N; ++e) h[i][e] = by(h[i][e]);
             C::store_e4m3(p.Q + row, t + i * TPR, full, h[i]);
         }
-        if (tail) p.Q[row + kt] = to_e4m3(ht * inv);
+        if (tail) p.Q[row + kt] = to_e4m3(by(ht));
         if (live && t == 0) p.scale[m] = s;
     }
 }
@@ -265,7 +278,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_long(NormFwd<T> p) {
             if (p.gain) y[e] *= C::one(g, e);
         }
     };
-    float inv = 1.f;
+    E4m3Scale by(1.f);
     if constexpr (E4M3) {
         float amax = fabsf(ht);
         for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
@@ -276,9 +289,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_long(NormFwd<T> p) {
             for (int e = 0; e < N; ++e) amax = max_or_nan(fabsf(y[e]), amax);
         }
         const float s = max_or_nan(row_reduce<kNormThreads, true>(amax, red[1]) / kE4m3Max, kE4m3Tiny);
-        inv = 1.f / s;
+        by = E4m3Scale(s);
         if (threadIdx.x == 0) p.scale[blockIdx.x] = s;
-        if (tail) p.Q[row + kt] = to_e4m3(ht * inv);
+        if (tail) p.Q[row + kt] = to_e4m3(by(ht));
     } else {
         if constexpr (OUT == kNormSplit) {
             if (tail) {
@@ -297,7 +310,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_fwd_long(NormFwd<T> p) {
         if (p.H) C::store(p.H + row, c, full, h);
         if constexpr (E4M3) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) y[e] *= inv;
+            for (int e = 0; e < N; ++e) y[e] = by(y[e]);
             C::store_e4m3(p.Q + row, c, full, y);
         } else {
             if constexpr (OUT == kNormSplit) norm_store_pairs<T>(p, row, c, full, y);

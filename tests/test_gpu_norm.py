@@ -390,3 +390,46 @@ def test_backward_over_its_rows_keeps_a_bad_value_in_its_column(d, M):
         assert torch.isnan(dg[9]) and int(torch.isnan(dg).sum()) == 1
         dg[9] = ref_g[9]
         assert torch.equal(dg, ref_g)
+
+
+@pytest.mark.parametrize("d", [300, 1003, 2048, 8192, 16387, 33001])
+def test_e4m3_rounds_the_quotient(d):
+    """Q is the e4m3 value next to the fp32 quotient Y / scale, ties to even, also
+    where the quotient is a midpoint of two of them.  Rows of +-1 and eps = 3 make
+    the sums exact, so rms_norm_forward returns the very fp32 values that are
+    divided."""
+    pifa, torch = _pifa(), torch_mod()
+    rng = np.random.default_rng([60, d])
+    step = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy()
+    mid = (step[:-1] + step[1:]) / 2  # 126 midpoints
+    x = torch.from_numpy(rng.choice([-1.0, 1.0], (1, d)).astype(np.float32)).cuda()
+    ties = 0
+    for _ in range(20):
+        top = np.float32(rng.uniform(0.5, 400.0))
+        g = (mid[rng.integers(0, 126, d)].astype(np.float32) * (top / np.float32(448))).astype(np.float32)
+        g[rng.integers(0, d)] = top
+        g_dev = torch.from_numpy(g).cuda()
+        y = pifa.rms_norm_forward(x, g_dev, 3.0).cpu()
+        Q, s = pifa.rms_norm_forward_e4m3(x, g_dev, 3.0)
+        s = s.cpu()
+        assert torch.equal(s, y.abs().amax(1) / 448)
+        q = y / s[:, None]
+        ties += int(np.isin(q.abs().numpy(), mid).sum())
+        assert torch.equal(Q.view(torch.uint8).cpu(), q.to(torch.float8_e4m3fn).view(torch.uint8))
+    assert ties > 5 * d
+
+
+@pytest.mark.parametrize("d", [300, 2048, 33001])
+def test_e4m3_rows_whose_values_overflow(d):
+    """A value past fp32 makes the row's scale infinite; what is finite in it is 0, as the quotient is."""
+    pifa, torch = _pifa(), torch_mod()
+    x = torch.ones(1, d, device="cuda")
+    x[0, ::2] = 1.5
+    g = torch.ones(d, device="cuda")
+    g[2] = 3.4e38
+    g[d - 2 + d % 2 - 1] = -2.0
+    Q, s = pifa.rms_norm_forward_e4m3(x, g, EPS)
+    q = Q.float()[0]
+    assert torch.isinf(s[0]) and torch.isnan(q[2])
+    q[2] = 0
+    assert (q == 0).all()
