@@ -331,6 +331,12 @@ struct NormBwd {
     float eps;
 };
 
+// rho^2 mean(u h): rho^2 alone may leave fp32's range, and u h may where rho is 0
+// (a row whose squares overflow).
+__device__ __forceinline__ float norm_back(float rho, float uh, float d) {
+    return rho * (rho == 0.f ? 0.f : rho * (uh / d));
+}
+
 // Sums of two values over the TPR threads of each row, one barrier for both.
 template <int TPR>
 __device__ __forceinline__ float2 row_sum2(float a, float b, float2* red) {
@@ -438,7 +444,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
         const float2 sums = row_sum2<TPR>(ss, uh, red[par]);
         par ^= 1;
         const float rho = rsqrtf(sums.x / (float)p.d + p.eps);
-        const float back = rho * rho * (sums.y / (float)p.d);
+        const float back = norm_back(rho, sums.y, (float)p.d);
         const int64_t row = live ? m * p.d : 0, full = live ? nfull : 0;
         // the second reading of the row's registers converts them again: kept
         // from the first one, the fp32 values do not fit 128 registers
@@ -450,14 +456,14 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float h = C::one(cur.h[i], e), y = C::one(cur.y[i], e);
-                dg[i][e] = __builtin_fmaf(y * h, rho, dg[i][e]);
+                dg[i][e] = __builtin_fmaf(h * rho, y, dg[i][e]);
                 dx[e] = rho * (gain(i, e) * y - h * back);
                 if (add) dx[e] += C::one(cur.r[i], e);
             }
             if constexpr (EXACT && !LAST) C::store(p.dX + row, t + i * TPR, TPR * V, dx);
             else if (p.dX) C::store(p.dX + row, t + i * TPR, full, dx);
         }
-        dgt = __builtin_fmaf(cur.yt * cur.ht, rho, dgt);
+        dgt = __builtin_fmaf(cur.ht * rho, cur.yt, dgt);
         if (live && has_tail && p.dX) p.dX[row + kt] = (T)(rho * (gt * cur.yt - cur.ht * back) + cur.rt);
     };
     const int64_t first = (int64_t)blockIdx.x * ROWS;
@@ -546,7 +552,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_long(NormBwd<T> p) {
         ss = row_reduce<kNormThreads>(ss, red[par][0]);
         uh = row_reduce<kNormThreads>(uh, red[par][1]);
         const float rho = rsqrtf(ss / (float)p.d + p.eps);
-        const float back = rho * rho * (uh / (float)p.d);
+        const float back = norm_back(rho, uh, (float)p.d);
         const bool begun = m != blockIdx.x;
         for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
             float h[N], y[N], g[N], dx[N];
@@ -554,7 +560,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_long(NormBwd<T> p) {
             if (out) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const float v = y[e] * h[e] * rho;
+                    const float v = h[e] * rho * y[e];
                     out[c * N + e] = begun ? out[c * N + e] + v : v;
                 }
             }
@@ -570,7 +576,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_long(NormBwd<T> p) {
             }
         }
         if (tail) {
-            if (out) out[kt] = begun ? out[kt] + yt * ht * rho : yt * ht * rho;
+            if (out) out[kt] = begun ? out[kt] + ht * rho * yt : ht * rho * yt;
             if (p.dX) p.dX[row + kt] = (T)(rho * (gt * yt - ht * back) + (p.dR ? (float)p.dR[row + kt] : 0.f));
         }
     }

@@ -433,3 +433,29 @@ def test_e4m3_rows_whose_values_overflow(d):
     assert torch.isinf(s[0]) and torch.isnan(q[2])
     q[2] = 0
     assert (q == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [512, 1003, 33001])
+def test_backward_of_rows_of_any_size(d, dtype):
+    """Rows of zeros beside an eps whose rho^2 is past fp32, rows of 2^-60 and 2^40,
+    and rows whose squares overflow (rho is 0 for them) under a dY that u h
+    overflows with."""
+    pifa, torch = _pifa(), torch_mod()
+    M, eps = 40, 2.0 ** -130
+    rng = np.random.default_rng([70, d])
+    f = np.ones((M, 1))
+    f[5], f[6], f[7], f[8], f[9] = 0.0, 2.0 ** -60, 2.0 ** 40, 2.0 ** 80, 2.0 ** 100
+    st, h = inputs.round_to(rng.uniform(0.5, 1.0, (M, d)) * f, dtype)
+    k = np.ones((M, 1))
+    k[5], k[8], k[9] = 2.0 ** -40, 2.0 ** 50, 2.0 ** 60
+    yst, dy = inputs.round_to(rng.uniform(0.25, 0.5, (M, d)) * k, dtype)
+    gst, g = inputs.round_to(rng.uniform(0.5, 1.5, (1, d)), dtype)
+    dX, dg = pifa.rms_norm_backward(to_dev(st), to_dev(gst).reshape(-1), to_dev(yst), eps)
+    p = np.where((h * h).sum(1, keepdims=True) > 2.0 ** 128, 0.0, o.rho(h, eps))
+    u = g * dy
+    back = p * (p * (u * h).mean(1, keepdims=True))
+    want, terms = p * (u - h * back), p * (np.abs(u) + np.abs(h * back))
+    _close(from_dev(dX), want, np.abs(want) * HALF[dtype] + terms * 4 * FP + _tiny(dtype), "dX")
+    _close(from_dev(dg), (dy * h * p).sum(0), np.abs(dy * h * p).sum(0) * 3 * FP, "dgain")
+    assert (from_dev(dX)[[8, 9]] == 0).all()
