@@ -120,6 +120,8 @@ _SIGNATURES = {
 def lib():
     """Open libpifa.so (raises if it has not been built)."""
     global _lib
+    if _lib is not None:  # set once, when it is ready
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -208,8 +210,7 @@ def _remember(handle: int, **dims) -> int:
 
 
 def _recall(handle: int):
-    with _dims_lock:
-        return _dims.get(handle)
+    return _dims.get(handle)
 
 
 def _forget(handle: int) -> None:
@@ -585,8 +586,10 @@ def pifa_build_f64(W, r: int, stream=None):
 
 # Buffers of the norms and 4-bit layers: every tensor given has the element
 # type, lives on the device that is current (the kernels run there), is
-# contiguous and holds what the call reads or writes.
-def _ptr_of(t, name: str, dtype, count: int, dev: int) -> int | None:
+# contiguous and holds what the call reads or writes; an input (`whole`) nothing
+# besides, unless the caller gave the number of rows, and rows, where there is a
+# dimension for them, are d values long.  `like`: a shape that is right as it is.
+def _ptr_of(t, name: str, dtype, count: int, dev: int, whole: bool = False, d: int = 0, like=None) -> int | None:
     if t is None:
         return None
     if t.dtype != dtype:
@@ -595,8 +598,12 @@ def _ptr_of(t, name: str, dtype, count: int, dev: int) -> int | None:
         raise ValueError("%s is on %s, the call runs on cuda:%d" % (name, t.device, dev))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    if t.numel() < count:
-        raise ValueError("%s holds %d values, the call needs %d" % (name, t.numel(), count))
+    if like is None or t.shape != like:
+        have = t.numel()
+        if have != count and (whole or have < count):
+            raise ValueError("%s holds %d values, the call needs %d" % (name, have, count))
+        if d and t.dim() > 1 and t.shape[-1] != d:
+            raise ValueError("%s is %s, its rows (last dimension) should hold %d values" % (name, tuple(t.shape), d))
     return t.data_ptr()
 
 
@@ -647,26 +654,41 @@ def _rt() -> _Torch:
     return _torch
 
 
-def _rows_of(t, M, d):
-    """(M, d) of a call on the rows of t: its own, where not given."""
-    return (t.numel() // max(int(t.shape[-1]), 1) if M is None else int(M), int(t.shape[-1]) if d is None else int(d))
+def _rows_of(t, name: str, M, d):
+    """(M, d, whole, row, like) of a call on the rows of t: its own M and d, where
+    not given, and what _ptr_of is to check of the others."""
+    if M is None and d is None:
+        like = t.shape
+        if not like:
+            raise ValueError("%s has no dimension" % name)
+        d = like[-1]
+        return t.numel() // max(d, 1), d, True, d, like
+    d = t.shape[-1] if d is None else int(d)
+    if M is not None:
+        return int(M), d, False, 0, None
+    n = t.numel()
+    if d > 0 and n % d:
+        raise ValueError("%s holds %d values, no whole rows of %d" % (name, n, d))
+    return n // max(d, 1), d, True, 0, None
 
 
 def rms_norm_forward(X, gain, eps: float, R=None, H=None, Y=None, M: int | None = None, d: int | None = None,
                      stream=None):
     """The norm of the rows of X + R (R may be None), times gain (may be None).
     Returns Y (allocated when not given); H, where given, takes X + R.  The
-    rows are X's last dimension unless M and d say otherwise."""
+    rows are X's last dimension, or d values each where d is given; with M given,
+    the first M rows of buffers that may hold more."""
     rt = _rt()
-    M, d = _rows_of(X, M, d)
+    M, d, whole, row, like = _rows_of(X, "X", M, d)
     if Y is None:
         with rt.under(stream):
             Y = rt.empty_like(X)
     dt, dev, n = X.dtype, rt.device(), M * d
     code = rt.code(dt)
     _check("rms_norm_forward", lib().rms_norm_forward(
-        _ptr_of(X, "X", dt, n, dev), _ptr_of(R, "R", dt, n, dev), _ptr_of(gain, "gain", dt, d, dev), eps,
-        _ptr_of(H, "H", dt, n, dev), _ptr_of(Y, "Y", dt, n, dev), M, d, code, rt.stream(stream, dev)))
+        _ptr_of(X, "X", dt, n, dev, whole, 0, like), _ptr_of(R, "R", dt, n, dev, whole, row, like),
+        _ptr_of(gain, "gain", dt, d, dev, True), eps, _ptr_of(H, "H", dt, n, dev, False, row, like),
+        _ptr_of(Y, "Y", dt, n, dev, False, row, like), M, d, code, rt.stream(stream, dev)))
     return Y
 
 
@@ -675,7 +697,7 @@ def rms_norm_forward_e4m3(X, gain, eps: float, R=None, H=None, Q=None, scale=Non
     """The same norm in 8 bits.  Returns (Q, scale): float8_e4m3fn rows and one
     fp32 scale a row, which stand for Q * scale (allocated when not given)."""
     rt = _rt()
-    M, d = _rows_of(X, M, d)
+    M, d, whole, row, like = _rows_of(X, "X", M, d)
     with rt.under(stream):
         if Q is None:
             Q = rt.empty(X.shape, dtype=rt.e4m3, device=X.device)
@@ -684,8 +706,9 @@ def rms_norm_forward_e4m3(X, gain, eps: float, R=None, H=None, Q=None, scale=Non
     dt, dev, n = X.dtype, rt.device(), M * d
     code = rt.code(dt)
     _check("rms_norm_forward_e4m3", lib().rms_norm_forward_e4m3(
-        _ptr_of(X, "X", dt, n, dev), _ptr_of(R, "R", dt, n, dev), _ptr_of(gain, "gain", dt, d, dev), eps,
-        _ptr_of(H, "H", dt, n, dev), _ptr_of(Q, "Q", rt.e4m3, n, dev),
+        _ptr_of(X, "X", dt, n, dev, whole, 0, like), _ptr_of(R, "R", dt, n, dev, whole, row, like),
+        _ptr_of(gain, "gain", dt, d, dev, True), eps, _ptr_of(H, "H", dt, n, dev, False, row, like),
+        _ptr_of(Q, "Q", rt.e4m3, n, dev, False, row, like),
         _ptr_of(scale, "scale", rt.f32, M, dev), M, d, code, rt.stream(stream, dev)))
     return Q, scale
 
@@ -700,7 +723,7 @@ def rms_norm_backward(H, gain, dY, eps: float, dR=None, dX=None, dgain=None, wor
     Outputs and workspace are allocated when not given, under the call's stream; need_dX / need_dgain
     False skip one (None in its place)."""
     rt = _rt()
-    M, d = _rows_of(H, M, d)
+    M, d, whole, row, like = _rows_of(H, "H", M, d)
     with rt.under(stream):
         if dX is None and need_dX:
             dX = rt.empty_like(H)
@@ -712,8 +735,9 @@ def rms_norm_backward(H, gain, dY, eps: float, dR=None, dX=None, dgain=None, wor
     code = rt.code(dt)
     nwork = 0 if work is None else work.numel() * work.element_size()
     _check("rms_norm_backward", lib().rms_norm_backward(
-        _ptr_of(H, "H", dt, n, dev), _ptr_of(gain, "gain", dt, d, dev), _ptr_of(dY, "dY", dt, n, dev),
-        _ptr_of(dR, "dR", dt, n, dev), eps, _ptr_of(dX, "dX", dt, n, dev),
+        _ptr_of(H, "H", dt, n, dev, whole, 0, like), _ptr_of(gain, "gain", dt, d, dev, True),
+        _ptr_of(dY, "dY", dt, n, dev, whole, row, like), _ptr_of(dR, "dR", dt, n, dev, whole, row, like), eps,
+        _ptr_of(dX, "dX", dt, n, dev, False, row, like),
         _ptr_of(dgain, "dgain", rt.f32, d, dev), M, d, code,
         None if work is None else _ptr_of(work, "work", work.dtype, 0, dev), nwork, rt.stream(stream, dev)))
     return dX, dgain
@@ -722,13 +746,14 @@ def rms_norm_backward(H, gain, dY, eps: float, dR=None, dX=None, dgain=None, wor
 def q4_layer_create(W, d_in: int | None = None, d_out: int | None = None, dtype: int | None = None) -> int:
     """Quantizes W (d_out x d_in) to 4 bits; returns an opaque handle."""
     rt = _rt()
+    whole = d_in is None and d_out is None
     d_in = W.shape[1] if d_in is None else int(d_in)
     d_out = W.shape[0] if d_out is None else int(d_out)
     dt = _dtype_code(W) if dtype is None else int(dtype)
     dev = rt.device()
     out = _vp()
-    _check("q4_layer_create", lib().q4_layer_create(_ptr_of(W, "W", _torch_dtype(dt), d_out * d_in, dev), d_in, d_out,
-                                                    dt, ctypes.byref(out)))
+    _check("q4_layer_create", lib().q4_layer_create(_ptr_of(W, "W", _torch_dtype(dt), d_out * d_in, dev, whole), d_in,
+                                                    d_out, dt, ctypes.byref(out)))
     return _remember(out.value, d_in=d_in, d_out=d_out, dt=PIFA_BF16, dev=dev)
 
 
@@ -736,13 +761,16 @@ def q4_layer_create_mx(codes, scales, d_in: int | None = None, d_out: int | None
     """codes: uint8 d_out x d_in / 2 (the lower index in the lower half of a
     byte), scales: uint8 d_out x d_in / 32 (powers of two, biased by 127)."""
     rt = _rt()
+    whole = d_in is None and d_out is None
     d_in = 2 * codes.shape[1] if d_in is None else int(d_in)
     d_out = codes.shape[0] if d_out is None else int(d_out)
     dev = rt.device()
     out = _vp()
+    whole = whole and d_in % 32 == 0  # the library refuses others
     _check("q4_layer_create_mx", lib().q4_layer_create_mx(
-        _ptr_of(codes, "codes", rt.u8, d_out * (d_in // 2), dev),
-        _ptr_of(scales, "scales", rt.u8, d_out * (d_in // 32), dev), d_in, d_out, ctypes.byref(out)))
+        _ptr_of(codes, "codes", rt.u8, d_out * (d_in // 2), dev, whole),
+        _ptr_of(scales, "scales", rt.u8, d_out * (d_in // 32), dev, whole, d_in // 32 if whole else 0), d_in, d_out,
+        ctypes.byref(out)))
     return _remember(out.value, d_in=d_in, d_out=d_out, dt=PIFA_BF16, dev=dev)
 
 
@@ -781,32 +809,36 @@ def _q4_rows(X, name: str, d_in: int, M):
 def q4_layer_forward(handle: int, X, Y, M: int | None = None, stream=None) -> None:
     rt = _rt()
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    row = d["d_out"] if M is None else 0
     M = _q4_rows(X, "X", d["d_in"], M)
     dev = rt.device()
     _check("q4_layer_forward", lib().q4_layer_forward(
-        handle, _ptr_of(X, "X", rt.bf16, M * d["d_in"], dev), _ptr_of(Y, "Y", rt.bf16, M * d["d_out"], dev),
-        M, rt.stream(stream, dev)))
+        handle, _ptr_of(X, "X", rt.bf16, M * d["d_in"], dev),
+        _ptr_of(Y, "Y", rt.bf16, M * d["d_out"], dev, False, row), M, rt.stream(stream, dev)))
 
 
 def q4_layer_forward_e4m3(handle: int, Q, scale, Y, M: int | None = None, stream=None) -> None:
     rt = _rt()
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    row, whole = (d["d_out"], d["d_in"] > 0) if M is None else (0, False)
     M = _q4_rows(Q, "Q", d["d_in"], M)
     dev = rt.device()
     _check("q4_layer_forward_e4m3", lib().q4_layer_forward_e4m3(
-        handle, _ptr_of(Q, "Q", rt.e4m3, M * d["d_in"], dev), _ptr_of(scale, "scale", rt.f32, M, dev),
-        _ptr_of(Y, "Y", rt.bf16, M * d["d_out"], dev), M, rt.stream(stream, dev)))
+        handle, _ptr_of(Q, "Q", rt.e4m3, M * d["d_in"], dev), _ptr_of(scale, "scale", rt.f32, M, dev, whole),
+        _ptr_of(Y, "Y", rt.bf16, M * d["d_out"], dev, False, row), M, rt.stream(stream, dev)))
 
 
 def q4_layer_norm_forward(handle: int, X, gain, eps: float, R=None, H=None, Y=None, M: int | None = None,
                           stream=None) -> None:
     rt = _rt()
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
+    row_in, row_out, whole, like = (d["d_in"], d["d_out"], d["d_in"] > 0, X.shape) if M is None else (0, 0, False, None)
     M = _q4_rows(X, "X", d["d_in"], M)
     dev, bf, n = rt.device(), rt.bf16, M * d["d_in"]
     _check("q4_layer_norm_forward", lib().q4_layer_norm_forward(
-        handle, _ptr_of(X, "X", bf, n, dev), _ptr_of(R, "R", bf, n, dev), _ptr_of(gain, "gain", bf, d["d_in"], dev), eps,
-        _ptr_of(H, "H", bf, n, dev), _ptr_of(Y, "Y", bf, M * d["d_out"], dev), M, rt.stream(stream, dev)))
+        handle, _ptr_of(X, "X", bf, n, dev), _ptr_of(R, "R", bf, n, dev, whole, row_in, like),
+        _ptr_of(gain, "gain", bf, d["d_in"], dev, d["d_in"] > 0), eps, _ptr_of(H, "H", bf, n, dev, False, row_in, like),
+        _ptr_of(Y, "Y", bf, M * d["d_out"], dev, False, row_out), M, rt.stream(stream, dev)))
 
 
 def pifa_probe_mfma(iters: int = 20000, stream=None):

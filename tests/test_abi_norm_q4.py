@@ -118,3 +118,113 @@ def test_rows_of_a_4_bit_call():
     for shape in ((4, 96), (64, 4), (4, 32), ()):
         with pytest.raises(ValueError):
             rows(torch.zeros(shape), "X", 64, None)
+
+
+@pytest.fixture
+def binding(monkeypatch):
+    """The binding on CPU tensors (device -1), with a library that records the calls."""
+    torch = pytest.importorskip("torch")
+    calls = []
+
+    class Recorder:
+        def __getattr__(self, name):
+            if name == "rms_norm_backward_bytes":
+                return lambda M, d: 4 * d
+            return lambda *a: calls.append((name, a)) or pifa.PIFA_OK
+
+    rt = pifa._Torch()
+    rt.device, rt.raw_stream = (lambda: -1), (lambda dev: 0)
+    monkeypatch.setattr(pifa, "_torch", rt)
+    monkeypatch.setattr(pifa, "_lib", Recorder())
+    return torch, calls
+
+
+def _last(calls):
+    """(M, d) of the norm call made last."""
+    return calls[-1][1][6:8] if calls[-1][0] == "rms_norm_forward" else calls[-1][1][7:9]
+
+
+def test_inputs_of_another_size_are_refused(binding):
+    """A gain of other rows, or an R, dY or dR of other rows with enough values, is
+    a mistake; an output may be a larger buffer, of rows as long."""
+    torch, calls = binding
+    bf = torch.bfloat16
+    t = lambda *s: torch.zeros(*s, dtype=bf)
+    x, g = t(6, 64), t(64)
+    for kw in (dict(R=t(7, 64)), dict(R=t(12, 32)), dict(R=t(3, 128)), dict(H=t(5, 64)), dict(H=t(12, 32)),
+               dict(Y=t(3, 128)), dict(Y=t(383))):
+        with pytest.raises(ValueError):
+            pifa.rms_norm_forward(x, g, 1e-5, **kw)
+    for bad in (t(128), t(63), t(2, 64)):
+        for call in (lambda: pifa.rms_norm_forward(x, bad, 1e-5), lambda: pifa.rms_norm_forward_e4m3(x, bad, 1e-5),
+                     lambda: pifa.rms_norm_backward(x, bad, x, 1e-5), lambda: pifa.rms_norm_forward(x, bad, 1e-5, M=2)):
+            with pytest.raises(ValueError):
+                call()
+    for kw in (dict(R=t(7, 64)), dict(Q=torch.zeros(12, 32).to(torch.float8_e4m3fn)), dict(scale=torch.zeros(5))):
+        with pytest.raises(ValueError):
+            pifa.rms_norm_forward_e4m3(x, g, 1e-5, **kw)
+    for dY, kw in ((t(7, 64), {}), (t(12, 32), {}), (x, dict(dR=t(7, 64))), (x, dict(dX=t(3, 128))),
+                   (x, dict(dgain=torch.zeros(63)))):
+        with pytest.raises(ValueError):
+            pifa.rms_norm_backward(x, g, dY, 1e-5, **kw)
+    assert not calls
+    # larger outputs, other leading dimensions and flat buffers are rows as well
+    pifa.rms_norm_forward(x, g, 1e-5, R=t(2, 3, 64), H=t(9, 64), Y=t(400))
+    assert _last(calls) == (6, 64)
+    pifa.rms_norm_forward_e4m3(x, g, 1e-5, R=t(384), scale=torch.zeros(8))
+    pifa.rms_norm_backward(x, g, t(384), 1e-5, dX=t(8, 64), dgain=torch.zeros(100))
+    assert _last(calls) == (6, 64) and len(calls) == 3
+
+
+def test_rows_of_a_norm_call(binding):
+    """d given alone cuts X into rows of d, M given takes the first rows of larger buffers."""
+    torch, calls = binding
+    t = lambda *s: torch.zeros(*s, dtype=torch.float32)
+    pifa.rms_norm_forward(t(384), t(64), 1e-5, d=64)
+    assert _last(calls) == (6, 64)
+    pifa.rms_norm_forward(t(6, 64), t(32), 1e-5, R=t(384), d=32)
+    assert _last(calls) == (12, 32)
+    pifa.rms_norm_backward(t(384), None, t(6, 64), 1e-5, d=64)
+    assert _last(calls) == (6, 64)
+    pifa.rms_norm_forward(t(9, 64), t(64), 1e-5, R=t(5, 64), M=4)
+    assert _last(calls) == (4, 64)
+    pifa.rms_norm_forward(t(1000), t(64), 1e-5, M=4, d=64)
+    assert _last(calls) == (4, 64)
+    n = len(calls)
+    for X, kw in ((t(100), dict(d=64)), (t(9, 64), dict(M=10)), (t(()), {}), (t(384), dict(d=64, R=t(448)))):
+        with pytest.raises(ValueError):
+            pifa.rms_norm_forward(X, None, 1e-5, **kw)
+    assert len(calls) == n
+
+
+def test_sizes_of_a_4_bit_call(binding):
+    torch, calls = binding
+    bf, u8 = torch.bfloat16, torch.uint8
+    t = lambda *s: torch.zeros(*s, dtype=bf)
+    codes, scales = torch.zeros(24, 32, dtype=u8), torch.zeros(24, 2, dtype=u8)
+    for bad in (torch.zeros(25, 2, dtype=u8), torch.zeros(2, 24, dtype=u8), torch.zeros(24, 4, dtype=u8)):
+        with pytest.raises(ValueError):
+            pifa.q4_layer_create_mx(codes, bad)
+    with pytest.raises(ValueError):
+        pifa.q4_layer_create(t(24, 64, 2))
+    h = pifa._remember(0x5000, d_in=64, d_out=24, dt=pifa.PIFA_BF16, dev=-1)
+    try:
+        x, y, g = t(6, 64), t(6, 24), t(64)
+        q = x.to(torch.float8_e4m3fn)
+        for call in (lambda: pifa.q4_layer_forward(h, x, t(3, 48)), lambda: pifa.q4_layer_forward(h, x, t(5, 24)),
+                     lambda: pifa.q4_layer_forward_e4m3(h, q, torch.zeros(7), y),
+                     lambda: pifa.q4_layer_forward_e4m3(h, q, torch.zeros(6), t(3, 48)),
+                     lambda: pifa.q4_layer_norm_forward(h, x, t(128), 1e-5, Y=y),
+                     lambda: pifa.q4_layer_norm_forward(h, x, g, 1e-5, R=t(7, 64), Y=y),
+                     lambda: pifa.q4_layer_norm_forward(h, x, g, 1e-5, H=t(3, 128), Y=y),
+                     lambda: pifa.q4_layer_norm_forward(h, x, g, 1e-5, Y=t(12, 12))):
+            with pytest.raises(ValueError):
+                call()
+        assert not calls
+        pifa.q4_layer_forward(h, x, t(9, 24))
+        pifa.q4_layer_forward(h, t(9, 64), y, M=6)
+        pifa.q4_layer_forward_e4m3(h, q, torch.zeros(6), t(150))
+        pifa.q4_layer_norm_forward(h, x, g, 1e-5, R=t(384), H=t(7, 64), Y=y)
+        assert [c[0] for c in calls] == ["q4_layer_forward"] * 2 + ["q4_layer_forward_e4m3", "q4_layer_norm_forward"]
+    finally:
+        pifa._forget(h)
