@@ -318,7 +318,8 @@ pifa_status lowrank_layer_destroy(lowrank_handle h);
  * required.  Sums are fp32 (a row whose squares sum to
  * more than 3.4e38 has rho = 0); H and Y are each rounded once, Y from the
  * unrounded H.  H and Y may each be X or R themselves, not each other, and
- * overlap nothing otherwise.  M = 0 returns PIFA_OK without launching.
+ * overlap nothing otherwise (PIFA_ERR_INVALID_ARG).  M = 0 returns PIFA_OK
+ * without launching.
  * Asynchronous on `stream`; no workspace.
  */
 pifa_status rms_norm_forward(const void* X, const void* R, const void* gain, float eps, void* H, void* Y,
@@ -331,7 +332,7 @@ pifa_status rms_norm_forward(const void* X, const void* R, const void* gain, flo
  *   Q      device, M x d bytes.   scale  device, M, fp32.
  * X, R, gain, eps, H and dtype as for rms_norm_forward.  A NaN in a row, or
  * an infinity in X + R, makes the row's scale NaN, a Y past fp32 infinite.  Q
- * and scale overlap nothing.
+ * and scale overlap nothing (PIFA_ERR_INVALID_ARG).
  */
 pifa_status rms_norm_forward_e4m3(const void* X, const void* R, const void* gain, float eps, void* H,
                                   uint8_t* Q, float* scale, int64_t M, int64_t d, pifa_dtype dtype,
@@ -348,7 +349,8 @@ pifa_status rms_norm_forward_e4m3(const void* X, const void* R, const void* gain
  *   dR    device, M x d, dtype, or NULL: the gradient that reaches H beside
  *         the norm (through the residual stream).
  *   dX    device, M x d, dtype, or NULL to skip: the gradient of X, and of R.
- *         May be H, dY or dR itself.
+ *         May be H, dY or dR itself; outputs and workspace overlap nothing
+ *         otherwise (PIFA_ERR_INVALID_ARG).
  *   dgain device, d, fp32 (overwritten), or NULL to skip.
  *   work  device, at least rms_norm_backward_bytes(M, d) bytes, 4-byte
  *         aligned (may be NULL where that is 0 or dgain is NULL); it keeps

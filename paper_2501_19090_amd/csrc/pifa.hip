@@ -2227,6 +2227,28 @@ pifa_status pifa_build_f64(const double* W, pifa_dims dims, double* W_p, double*
 // ===================================================================== norms
 namespace {
 
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && x < y + nb && y < x + na;
+}
+
+// An output of n bytes over one of these inputs, other than in its place.
+bool overlap_part(const void* out, size_t n, std::initializer_list<const void*> in) {
+    for (const void* p : in)
+        if (out != p && overlap(out, n, p, n)) return true;
+    return false;
+}
+// An output over any of these buffers.
+struct Buffer {
+    const void* p;
+    size_t n;
+};
+bool overlap_any(const void* out, size_t n, std::initializer_list<Buffer> others) {
+    for (const Buffer& b : others)
+        if (overlap(out, n, b.p, b.n)) return true;
+    return false;
+}
+
 // A launch may not pass 2^32 threads: columns of a row in one launch (64 columns
 // of dgain take 1024 threads), rows of one launch (1024 threads at most each).
 constexpr int64_t kNormMaxD = 1ll << 27, kNormMaxRows = 1ll << 21;
@@ -2611,11 +2633,6 @@ hipError_t launch_q4(Q4Args p, hipStream_t st) {
     return hipSuccess;
 }
 
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return a && b && x < y + nb && y < x + na;
-}
-
 }  // namespace
 
 extern "C" {
@@ -2625,7 +2642,11 @@ pifa_status rms_norm_forward(const void* X, const void* R, const void* gain, flo
     const pifa_status s = check_norm(M, d, dtype, eps);
     if (s != PIFA_OK) return s;
     if (M == 0) return PIFA_OK;
-    if (!X || !Y || H == Y) return PIFA_ERR_INVALID_ARG;
+    if (!X || !Y) return PIFA_ERR_INVALID_ARG;
+    const size_t n = (size_t)M * (size_t)d * esize(dtype), row = (size_t)d * esize(dtype);
+    if (overlap_part(H, n, {X, R}) || overlap_part(Y, n, {X, R}) || overlap_any(H, n, {{gain, row}, {Y, n}}) ||
+        overlap(Y, n, gain, row))
+        return PIFA_ERR_INVALID_ARG;
     const hipStream_t st = as_stream(stream);
     const hipError_t e = dtype == PIFA_BF16 ? norm_forward_run<bf16>(X, R, gain, eps, H, Y, nullptr, nullptr, M, d, st)
                                             : norm_forward_run<float>(X, R, gain, eps, H, Y, nullptr, nullptr, M, d, st);
@@ -2638,6 +2659,11 @@ pifa_status rms_norm_forward_e4m3(const void* X, const void* R, const void* gain
     if (s != PIFA_OK) return s;
     if (M == 0) return PIFA_OK;
     if (!X || !Q || !scale) return PIFA_ERR_INVALID_ARG;
+    const size_t n = (size_t)M * (size_t)d, es = esize(dtype), row = (size_t)d * es, ns = (size_t)M * sizeof(float);
+    if (overlap_part(H, n * es, {X, R}) || overlap(H, n * es, gain, row) ||
+        overlap_any(Q, n, {{X, n * es}, {R, n * es}, {gain, row}, {H, n * es}, {scale, ns}}) ||
+        overlap_any(scale, ns, {{X, n * es}, {R, n * es}, {gain, row}, {H, n * es}}))
+        return PIFA_ERR_INVALID_ARG;
     const hipStream_t st = as_stream(stream);
     const hipError_t e = dtype == PIFA_BF16 ? norm_forward_run<bf16>(X, R, gain, eps, H, nullptr, Q, scale, M, d, st)
                                             : norm_forward_run<float>(X, R, gain, eps, H, nullptr, Q, scale, M, d, st);
@@ -2663,10 +2689,15 @@ pifa_status rms_norm_backward(const void* H, const void* gain, const void* dY, c
     }
     if (!H || !dY) return PIFA_ERR_INVALID_ARG;
     if (!dX && !dgain) return PIFA_OK;
-    if (dgain) {
-        const size_t need = rms_norm_backward_bytes(M, d);
-        if (need > 0 && (!work || work_bytes < need)) return PIFA_ERR_INVALID_ARG;
-    }
+    const size_t need = dgain ? rms_norm_backward_bytes(M, d) : 0;
+    if (need > 0 && (!work || work_bytes < need)) return PIFA_ERR_INVALID_ARG;
+    const size_t n = (size_t)M * (size_t)d * esize(dtype), row = (size_t)d * esize(dtype), ng = (size_t)d * sizeof(float);
+    const Buffer part{need > 0 ? work : nullptr, need};
+    if (overlap_part(dX, n, {H, dY, dR}) || overlap_any(dX, n, {{gain, row}, {dgain, ng}, part}) ||
+        overlap_any(dgain, ng, {{H, n}, {gain, row}, {dY, n}, {dR, n}, part}) ||
+        overlap_any(part.p, part.n, {{H, n}, {gain, row}, {dY, n}, {dR, n}}))
+        return PIFA_ERR_INVALID_ARG;
+    if (need > 0 && ((uintptr_t)work & 3) != 0) return PIFA_ERR_UNSUPPORTED;
     return dtype == PIFA_BF16 ? norm_backward_run<bf16>(H, gain, dY, dR, eps, dX, dgain, M, d, (float*)work, st)
                               : norm_backward_run<float>(H, gain, dY, dR, eps, dX, dgain, M, d, (float*)work, st);
 }

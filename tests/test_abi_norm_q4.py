@@ -228,3 +228,63 @@ def test_sizes_of_a_4_bit_call(binding):
         assert [c[0] for c in calls] == ["q4_layer_forward"] * 2 + ["q4_layer_forward_e4m3", "q4_layer_norm_forward"]
     finally:
         pifa._forget(h)
+
+
+def _at(i):
+    return ctypes.c_void_p(0x100000 + i)
+
+
+@pytest.mark.parametrize("dtype,es", [(BF16, 2), (F32, 4)])
+def test_norm_outputs_over_inputs_are_refused(dtype, es):
+    """An output may be an input, not lie over a part of it or over anything else,
+    by as little as a byte at either end."""
+    lib, M, d = pifa.lib(), 5, 24
+    n, row = M * d * es, d * es
+    far = [_at(0x10000 * (i + 1)) for i in range(8)]
+    shifts = lambda base, out, size: (_at(0x10000 * (base + 1) - out + 1), _at(0x10000 * (base + 1) + size - 1))
+
+    def forward(X=far[0], R=far[1], gain=far[2], H=far[3], Y=far[4]):
+        return lib.rms_norm_forward(X, R, gain, 1e-5, H, Y, M, d, dtype, None)
+
+    for base, size in ((0, n), (1, n), (2, row)):
+        for p in shifts(base, n, size):
+            assert forward(Y=p) == INVAL and forward(H=p) == INVAL
+    assert forward(Y=far[2]) == INVAL and forward(H=far[2]) == INVAL and forward(H=far[4]) == INVAL
+    assert forward(H=_at(0x50000 + n - 1)) == INVAL and forward(H=far[0], Y=far[0]) == INVAL
+
+    def e4m3(X=far[0], R=far[1], gain=far[2], H=far[3], Q=far[4], scale=far[5]):
+        return lib.rms_norm_forward_e4m3(X, R, gain, 1e-5, H, Q, scale, M, d, dtype, None)
+
+    for base, size in ((0, n), (1, n), (2, row)):
+        for p in shifts(base, n, size):
+            assert e4m3(H=p) == INVAL
+    for base, size in ((0, n), (1, n), (2, row), (3, n)):
+        assert e4m3(Q=far[base]) == INVAL and e4m3(scale=far[base]) == INVAL
+        for p in shifts(base, M * d, size):
+            assert e4m3(Q=p) == INVAL
+        for p in shifts(base, 4 * M, size):
+            assert e4m3(scale=p) == INVAL
+    assert e4m3(scale=_at(0x50000 + M * d - 1)) == INVAL and e4m3(Q=_at(0x60000 + 4 * M - 1)) == INVAL
+
+    M = 4 * 256  # with partial sums
+    n, need = M * d * es, pifa.rms_norm_backward_bytes(M, d)
+    assert need > 0
+
+    far = [_at(0x1000000 * (i + 1)) for i in range(8)]
+    shifts = lambda base, out, size: (_at(0x1000000 * (base + 1) - out + 1), _at(0x1000000 * (base + 1) + size - 1))
+    kw = dict(H=far[0], gain=far[1], dY=far[2], dR=far[3], dX=far[4], dgain=far[5], work=far[6])
+
+    def backward(H, gain, dY, dR, dX, dgain, work):
+        return lib.rms_norm_backward(H, gain, dY, dR, 1e-5, dX, dgain, M, d, dtype, work, need, None)
+
+    for base, size in ((0, n), (1, row), (2, n), (3, n)):
+        for p in shifts(base, n, size):
+            assert backward(**{**kw, "dX": p}) == INVAL
+        for p in shifts(base, 4 * d, size):
+            assert backward(**{**kw, "dgain": p}) == INVAL
+        for p in shifts(base, need, size):
+            assert backward(**{**kw, "work": p}) == INVAL
+    assert backward(**{**kw, "dgain": far[4]}) == INVAL and backward(**{**kw, "work": far[4]}) == INVAL
+    assert backward(**{**kw, "work": far[5]}) == INVAL and backward(**{**kw, "dX": far[1]}) == INVAL
+    for i in (1, 2, 3):  # not on 4 bytes
+        assert backward(**{**kw, "work": _at(0x7000000 + i)}) == UNSUP
