@@ -2445,10 +2445,10 @@ void q4_few_launch(const Q4Args& p, hipStream_t st) {
                        st, p);
 }
 
-template <int ACT, bool NORM, int NG, int U>
+template <bool NORM, int NG, int U>
 void q4_staged_launch(const Q4Args& p, hipStream_t st) {
-    hipLaunchKernelGGL((q4_staged<ACT, NORM, NG, 8, U>), dim3((unsigned)ceil_div(packed_groups(p.N), NG)),
-                       dim3(8 * kWave), (size_t)q4_staged_lds(p.M, p.K, ACT == kQ4Bf16 ? 2 : 1, NORM, NG * 8), st, p);
+    hipLaunchKernelGGL((q4_staged<NORM, NG, 8, U>), dim3((unsigned)ceil_div(packed_groups(p.N), NG)),
+                       dim3(8 * kWave), (size_t)q4_staged_lds(p.M, p.K, NORM, NG * 8), st, p);
 }
 
 // Whether the norm's form is one launch.  Every workgroup norms the rows again,
@@ -2586,8 +2586,8 @@ hipError_t launch_q4(Q4Args p, hipStream_t st) {
             // rows of 8192 -> 16640 19.7 / 23.8, -> 28672 28.0 / 33.0, of 4096 -> 16640
             // 12.4 / 14.3; 9 rows of 4096 -> 28672 14.3 / 12.8, 16 of 2048 -> 28672
             // 10.0 / 9.6, of 8192 -> 14336 (896 groups) 19.7 / 14.1.
-            if (ACT == kQ4Bf16 && q.M <= 2 && q4_staged_lds(q.M, q.K, 2, false, 8) <= kStreamMaxLds)
-                q4_staged_launch<ACT, false, 1, 2>(q, st);
+            if (ACT == kQ4Bf16 && q.M <= 2 && q4_staged_lds(q.M, q.K, false, 8) <= kStreamMaxLds)
+                q4_staged_launch<false, 1, 2>(q, st);
             else if (ACT == kQ4Bf16 && groups > 1024 && q.M * q.K > 49152)
                 q4_mid_launch<kQ4Bf16, 16, 128, 1, 2, 4, 4, 2>(q, st);
             else if (groups <= kCus) q4_few_launch<ACT, 1, 2>(q, st);
@@ -2820,9 +2820,9 @@ pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, con
         TimedLaunch timed(kSiteQ4Norm, st);
         // 1 / 2 / 4 groups a workgroup, one row (us): 4096^2 5.2 / 5.6 / 6.6, 4096 ->
         // 12288 10.8 / 7.8 / 8.2, 8192 -> 28672 32.8 / 27.3 / 25.4
-        if (packed_groups(p.N) <= kCus) q4_staged_launch<kQ4Bf16, true, 1, 2>(p, st);
-        else if (packed_groups(p.N) <= 1024) q4_staged_launch<kQ4Bf16, true, 2, 1>(p, st);
-        else q4_staged_launch<kQ4Bf16, true, 4, 1>(p, st);
+        if (packed_groups(p.N) <= kCus) q4_staged_launch<true, 1, 2>(p, st);
+        else if (packed_groups(p.N) <= 1024) q4_staged_launch<true, 2, 1>(p, st);
+        else q4_staged_launch<true, 4, 1>(p, st);
         return hipGetLastError() == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
     }
     s = q4_ensure(h, (size_t)q4_norm_rows(M) * (size_t)h->d_in * 2, st);

@@ -376,7 +376,7 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
 }
 
 // ------------------------------------------------------------------ few rows, staged
-// As q4_few, with the rows in LDS, which each workgroup stages while its first
+// As q4_few for bf16 rows, with them in LDS, which each workgroup stages while its first
 // weights are on their way; the norm's form norms them on the way there: the
 // product is of (X + R) gain, and rho, a factor of the row, is applied to the
 // sums.  Rounded to bf16 alone, (X + R) gain would add as much error as the
@@ -394,26 +394,25 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_few(Q4Args p) {
 // of S) at ((c * 4 + q) * S + r) * 16 bytes (S = M, the norm's form 2 M); 16 zero
 // bytes, which the lanes of rows past M read; over both, after the loop, the
 // sums of the waves.  Then rho and the partial sums of squares (512 columns each).
-__host__ __device__ inline int64_t q4_staged_rows_lds(int64_t M, int64_t K, int es, bool norm, int red_kb) {
-    const int64_t x = (norm ? 2 : 1) * M * packed_kblocks(K) * 128 * es + 16;
+__host__ __device__ inline int64_t q4_staged_rows_lds(int64_t M, int64_t K, bool norm, int red_kb) {
+    const int64_t x = (norm ? 2 : 1) * M * packed_kblocks(K) * 256 + 16;
     return x > red_kb * 1024 ? x : red_kb * 1024;
 }
-__host__ __device__ inline int64_t q4_staged_lds(int64_t M, int64_t K, int es, bool norm, int red_kb) {
-    return q4_staged_rows_lds(M, K, es, norm, red_kb) + (norm ? (M * ceil_div(K, 512) + 16) * 4 : 0);
+__host__ __device__ inline int64_t q4_staged_lds(int64_t M, int64_t K, bool norm, int red_kb) {
+    return q4_staged_rows_lds(M, K, norm, red_kb) + (norm ? (M * ceil_div(K, 512) + 16) * 4 : 0);
 }
 
-template <int ACT, bool NORM, int NG, int WAVES, int U>
+template <bool NORM, int NG, int WAVES, int U>
 __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
-    constexpr int XC = ACT == kQ4Bf16 ? 4 : 2, ES = ACT == kQ4Bf16 ? 2 : 1;
     extern __shared__ __attribute__((aligned(1024))) char dyn[];
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int row = lane & 15, q = lane >> 4;
     const int K = (int)p.K, KB = (int)packed_kblocks(p.K), M = (int)p.M;
-    const int S = NORM ? 2 * M : M, xbytes = S * KB * 128 * ES;
+    const int S = NORM ? 2 * M : M, xbytes = S * KB * 256;
     f32x4* red = reinterpret_cast<f32x4*>(dyn);  // WAVES x NG x 64, after the loop
     char* xs = dyn;
-    float* rho = reinterpret_cast<float*>(dyn + q4_staged_rows_lds(M, K, ES, NORM, WAVES * NG));
+    float* rho = reinterpret_cast<float*>(dyn + q4_staged_rows_lds(M, K, NORM, WAVES * NG));
     float* sums = rho + 16;
 
     const int64_t groups = packed_groups(p.N), g0 = (int64_t)blockIdx.x * NG;
@@ -518,13 +517,12 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
             if ((int)threadIdx.x < M && ((which >> (threadIdx.x * segs)) & 1)) rho[threadIdx.x] = 1.f;
         }
     } else {
-        const u32x4 xrs = raw_rsrc31(p.X, (int64_t)M * K * ES);
+        const u32x4 xrs = raw_rsrc31(p.X, (int64_t)M * K * 2);
         const int pieces = xbytes / 16;
         for (int i0 = wave * kWave; i0 < pieces; i0 += WAVES * kWave) {
             const int i = i0 + lane, r = i % M, at = i / M;
-            const int b = at / (4 * XC), c = (at >> 2) % XC, qq = at & 3;
-            const int k = ACT == kQ4Bf16 ? 128 * b + 32 * qq + 8 * c : 128 * b + 64 * c + 16 * qq;
-            if (i < pieces) dma16(xrs, k < K ? (uint32_t)((r * K + k) * ES) : kMaskedOffset, lds0 + i0 * 16);
+            const int b = at / 16, c = (at >> 2) & 3, qq = at & 3, k = 128 * b + 32 * qq + 8 * c;
+            if (i < pieces) dma16(xrs, k < K ? (uint32_t)((r * K + k) * 2) : kMaskedOffset, lds0 + i0 * 16);
         }
         wait_vm<0>();
         __syncthreads();
@@ -532,26 +530,22 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
     const bool live = row < M;
     const int slot = NORM && row >= kQ4NormRows ? row - kQ4NormRows + M : row;
     const bool held = NORM && row >= kQ4NormRows ? row - kQ4NormRows < M : live;
-    uint32_t xat[XC];
+    uint32_t xat[4];
 #pragma unroll
-    for (int c = 0; c < XC; ++c) xat[c] = held ? (uint32_t)(((c * 4 + q) * S + slot) * 16) : (uint32_t)xbytes;
-    const uint32_t xstep = held ? (uint32_t)(128 * ES * S) : 0u;
+    for (int c = 0; c < 4; ++c) xat[c] = held ? (uint32_t)(((c * 4 + q) * S + slot) * 16) : (uint32_t)xbytes;
+    const uint32_t xstep = held ? (uint32_t)(256 * S) : 0u;
     f32x4 acc[NG];
 #pragma unroll
     for (int j = 0; j < NG; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     auto step = [&](int b, Blk& f) {
-        u32x4 x[XC];
+        u32x4 x[4];
 #pragma unroll
-        for (int c = 0; c < XC; ++c) x[c] = *reinterpret_cast<const u32x4*>(xs + xat[c] + (uint32_t)b * xstep);
+        for (int c = 0; c < 4; ++c) x[c] = *reinterpret_cast<const u32x4*>(xs + xat[c] + (uint32_t)b * xstep);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            if constexpr (ACT == kQ4Bf16) {
-                const float s = __builtin_bit_cast(float, f.s[j] << 23);
+            const float s = __builtin_bit_cast(float, f.s[j] << 23);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) acc[j] = q4_mfma_bf16(q4_to_bf16(f.w[j][c], s), x[c], acc[j]);
-            } else {
-                acc[j] = q4_mfma_e4m3(f.w[j], f.s[j], x[0], x[1], acc[j]);
-            }
+            for (int c = 0; c < 4; ++c) acc[j] = q4_mfma_bf16(q4_to_bf16(f.w[j][c], s), x[c], acc[j]);
         }
     };
     q4_pipeline<U, WAVES>(wave, KB, even, odd, fetch_step, step);
@@ -569,7 +563,6 @@ __global__ __launch_bounds__(WAVES* kWave) void q4_staged(Q4Args p) {
             for (int i = 0; i < 4; ++i) tot[i] += __shfl(tot[i], lane ^ kQ4NormRows);
             f = live ? rho[row] : 0.f;
         }
-        if constexpr (ACT == kQ4E4m3) f = live ? p.x_scale[row] : 0.f;
         q4_store4(p, row, (g0 + wave) * 16 + 4 * q, tot, f);
     }
 }
