@@ -459,3 +459,37 @@ def test_backward_of_rows_of_any_size(d, dtype):
     _close(from_dev(dX), want, np.abs(want) * HALF[dtype] + terms * 4 * FP + _tiny(dtype), "dX")
     _close(from_dev(dg), (dy * h * p).sum(0), np.abs(dy * h * p).sum(0) * 3 * FP, "dgain")
     assert (from_dev(dX)[[8, 9]] == 0).all()
+
+
+# (type, d): whole rows of every width that has a form of its own, and ragged ones
+STEADY = [("bf16", d) for d in (512, 1024, 2048, 4096, 8192, 16384, 500, 1001, 2040, 4093, 8190, 16380)] + \
+         [("f32", d) for d in (256, 512, 1024, 2048, 4096, 8192, 255, 1023, 4095, 8191)]
+
+
+@pytest.mark.parametrize("dtype,d", STEADY)
+def test_backward_of_many_rows_a_workgroup(dtype, d):
+    """Five or more passes of every workgroup over its rows, the last group of rows
+    cut: the loop over two sets of registers, and its end.  fp64 on the GPU."""
+    pifa, torch = _pifa(), torch_mod()
+    chunks = d // (8 if dtype == "bf16" else 4)
+    at_once = 16 if chunks <= 64 else 8 if chunks <= 128 else 4 if chunks <= 256 else 2 if chunks <= 512 else 1
+    M = 5 * 256 * at_once + max(1, at_once * 37 - 1 if at_once > 1 else 131)
+    rng = torch.Generator(device="cuda").manual_seed(d)
+    tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    h, dy, dr = (torch.randn(M, d, device="cuda", generator=rng).to(tdt) for _ in range(3))
+    h[:, 3] *= 50
+    g = (1 + 0.3 * torch.randn(d, device="cuda", generator=rng)).to(tdt)
+    dX, dg = pifa.rms_norm_backward(h, g, dy, EPS, dR=dr)
+    over = h.clone()
+    dX2, dg2 = pifa.rms_norm_backward(over, g, dy, EPS, dR=dr, dX=over)
+    assert torch.equal(dX, dX2) and torch.equal(dg, dg2)
+    h, dy, dr, g = h.double(), dy.double(), dr.double(), g.double()
+    p = torch.rsqrt((h * h).mean(1, keepdim=True) + EPS)
+    u = g * dy
+    want = p * u - p ** 3 * h * (u * h).mean(1, keepdim=True) + dr
+    terms = p * u.abs() + p ** 3 * h.abs() * (u * h).abs().mean(1, keepdim=True) + dr.abs()
+    off = (dX.double() - want).abs() - want.abs() * HALF[dtype] - terms * 4 * FP
+    assert torch.isfinite(dX).all() and float(off.max()) <= 0, float(off.max())
+    # at most 7 rows and 16 slots of a workgroup, 16 partial sums of a slice and 16 slices: under 128 additions
+    off = (dg.double() - (dy * h * p).sum(0)).abs() - 3 * FP * (dy * h * p).abs().sum(0)
+    assert torch.isfinite(dg).all() and float(off.max()) <= 0, float(off.max())

@@ -8,6 +8,9 @@ of a group off at 2^-14 of the largest: 32 * 2^-14 = 2^-9 of the product of the
 group's largest value in the row and in the weights.  The norm's form rounds its rows to bf16 first: 2^-8 of every term,
 which adds up to at most 2^-8 of the sum of magnitudes.
 """
+import os
+import re
+
 import numpy as np
 import pytest
 
@@ -692,3 +695,98 @@ def test_norm_with_weights_next_to_the_end_of_the_range(M, scale):
         Y = layer.norm_forward(to_dev(st), None, EPS)
     want, mags = _norm_want(x, np.zeros_like(x), np.ones(d_in), w)
     _check(Y, want, mags, 2.0 ** -16 + 2.0 ** -17 + SUMS, (M, scale))
+
+
+def _forms():
+    """The library's table of tiles for more than 16 rows, and the one it picks, read
+    from its source: (names, [bf16, e4m3] rows of (rows, columns, then the times))."""
+    with open(os.path.join(os.path.dirname(_pifa().__file__), "csrc", "pifa.hip")) as f:
+        src = f.read()
+    names = re.findall(r"kQ4T(\w+)", src[src.index("enum Q4Forms"):src.index("kQ4FormCount")])
+    body = src[src.index("kQ4FormTable[2]"):]
+    body = body[body.index("=") + 1:body.index(";")]
+    rows = [[float(v) for v in r.split(",")] for r in re.findall(r"\{([-\d., ]+)\}", body)]
+    rows = [r + [0.0] * (8 - len(r)) for r in rows]
+    assert len(rows) == 2 * len(names)
+    return names, (rows[:len(names)], rows[len(names):])
+
+
+def _picked(act, M, N, K):
+    names, table = _forms()
+    best = None
+    for name, (bm, bn, *t) in zip(names, table[act]):
+        if t[0] == 0:
+            continue
+        tiles = -(-M // int(bm)) * -(-N // int(bn))
+        at_once = [t[0] + t[1] * K / 1000, t[2] + t[3] * K / 1000, t[4] + t[5] * K / 1000]
+        most = 3 if t[5] > 0 else 2 if t[3] > 0 else 1
+        rounds, rest = divmod(tiles, 256 * most)
+        cost = rounds * at_once[most - 1] + (at_once[(rest - 1) // 256] if rest else 0.0)
+        if best is None or cost < best[0]:
+            best = cost, name
+    return best[1]
+
+
+def _product_on_the_gpu(act, M, d_in, d_out, seed):
+    """A product of bf16 (act 0) or 8-bit rows (1) against 64 bits, weights made on the GPU."""
+    torch, pifa = torch_mod(), _pifa()
+    rng = torch.Generator(device="cuda").manual_seed(seed)
+    codes = torch.randint(0, 256, (d_out, d_in // 2), dtype=torch.uint8, device="cuda", generator=rng)
+    scales = torch.randint(118, 127, (d_out, d_in // 32), dtype=torch.uint8, device="cuda", generator=rng)
+    grid = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, -0., -.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device="cuda")
+    w = torch.stack((grid[codes.int() & 15], grid[codes.int() >> 4]), 2).view(d_out, d_in)
+    w *= torch.exp2(scales.double() - 127).repeat_interleave(32, dim=1)
+    x = torch.randn(M, d_in, device="cuda", generator=rng).bfloat16()
+    big, Y = _guarded(M, d_out)
+    with pifa.Q4Layer.from_mx(codes, scales) as layer:
+        if act == 0:
+            layer(x, Y)
+            a = x.double()
+        else:
+            q = x.float().to(torch.float8_e4m3fn)
+            f = torch.rand(M, device="cuda", generator=rng) + 0.5
+            layer.forward_e4m3(q, f, Y)
+            a = q.double() * f.double()[:, None]
+        torch.cuda.synchronize()
+    want = a @ w.t().contiguous()
+    tol = want.abs() * 2.0 ** -8 + SUMS * (a.abs() @ w.abs().t().contiguous())
+    if act == 1:
+        top = lambda v: v.abs().view(v.shape[0], -1, 32).amax(2)
+        tol += 2.0 ** -9 * (top(a) @ top(w).t().contiguous())
+    off = (Y.double() - want).abs() - tol
+    assert torch.isfinite(Y).all() and float(off.max()) <= 0, (act, M, d_in, d_out, float(off.max()))
+    assert bool((big[M * d_out:] == -17).all())
+
+
+# Every tile at sizes that pick it, where its groups of waves take many more K
+# tiles than they have stages (the larger K another parity of steps), ragged ends.
+DEEP = [(0, "16x32", 17, 100, (11072, 11296)), (0, "32x32", 1054, 100, (11488, 11808)), (0, "32x64", 2065, 102, (4288, 4384)),
+        (0, "32x128", 2050, 199, (4288, 4384)), (0, "64x64Deep", 2077, 399, (4192, 4384)), (0, "64x64", 2421, 391, (2112, 2208)),
+        (0, "64x128Deep", 65, 11277, (3104, 3232)), (0, "64x128", 2348, 858, (2080, 2144)),
+        (0, "128x128Deep", 229, 8202, (4192, 4256)), (0, "128x128Pair", 2250, 2727, (2112, 2144)),
+        (0, "128x256", 2331, 6619, (2080, 2144)), (0, "256x256", 1962, 6330, (2080, 2144)),
+        (1, "16x32", 19, 100, (11104, 11296)), (1, "32x32", 1028, 100, (11200, 11296)), (1, "32x64", 2059, 103, (6240, 6688)),
+        (1, "32x128", 1608, 583, (6176, 6688)), (1, "64x64", 2054, 196, (4192, 4384)), (1, "64x128", 2347, 406, (2080, 2208)),
+        (1, "128x128", 2562, 794, (2112, 2208)), (1, "128x128Pair", 2317, 1672, (2080, 2208)),
+        (1, "256x256", 2209, 5517, (2112, 2208))]
+
+
+def test_deep_sizes_cover_every_tile():
+    names, table = _forms()
+    assert {(a, n) for a, n, *_ in DEEP} == {(a, n) for a in (0, 1) for n, row in zip(names, table[a]) if row[2]}
+
+
+@pytest.mark.parametrize("act,tile,M,d_out,depths", DEEP)
+def test_every_tile_runs_its_ring_many_times(act, tile, M, d_out, depths):
+    for d_in in depths:
+        assert _picked(act, M, d_out, d_in) == tile
+        _product_on_the_gpu(act, M, d_in, d_out, 101)
+
+
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("d_out", [250, 5000, 8193, 11008, 16400])
+@pytest.mark.parametrize("M", [1, 2, 3, 8, 16])
+def test_few_rows_of_wide_layers(M, d_out, act):
+    """Up to 16 rows at 1, 2 and 4 groups of columns a workgroup, K of many blocks with a cut one."""
+    for d_in in (2080, 4192):
+        _product_on_the_gpu(act, M, d_in, d_out, 102)
