@@ -623,6 +623,8 @@ class _Torch:
         """The given stream, or the device's current one."""
         if stream is None and self.raw_stream is not None:
             return self.raw_stream(dev)
+        if getattr(stream, "device_index", dev) != dev:
+            raise ValueError("the stream is on cuda:%d, the call runs on cuda:%d" % (stream.device_index, dev))
         return _stream(stream)
 
     def under(self, stream):
@@ -632,8 +634,8 @@ class _Torch:
         if stream is None:
             return contextlib.nullcontext()
         import torch
+        raw = self.stream(stream, self.device())
         if not isinstance(stream, torch.cuda.Stream):
-            raw = _stream(stream)
             stream = torch.cuda.ExternalStream(raw) if raw else torch.cuda.default_stream()
         return torch.cuda.stream(stream)
 
@@ -698,11 +700,10 @@ def rms_norm_forward_e4m3(X, gain, eps: float, R=None, H=None, Q=None, scale=Non
     fp32 scale a row, which stand for Q * scale (allocated when not given)."""
     rt = _rt()
     M, d, whole, row, like = _rows_of(X, "X", M, d)
-    with rt.under(stream):
-        if Q is None:
-            Q = rt.empty(X.shape, dtype=rt.e4m3, device=X.device)
-        if scale is None:
-            scale = rt.empty(M, dtype=rt.f32, device=X.device)
+    if Q is None or scale is None:
+        with rt.under(stream):
+            Q = rt.empty(X.shape, dtype=rt.e4m3, device=X.device) if Q is None else Q
+            scale = rt.empty(M, dtype=rt.f32, device=X.device) if scale is None else scale
     dt, dev, n = X.dtype, rt.device(), M * d
     code = rt.code(dt)
     _check("rms_norm_forward_e4m3", lib().rms_norm_forward_e4m3(
@@ -724,13 +725,13 @@ def rms_norm_backward(H, gain, dY, eps: float, dR=None, dX=None, dgain=None, wor
     False skip one (None in its place)."""
     rt = _rt()
     M, d, whole, row, like = _rows_of(H, "H", M, d)
-    with rt.under(stream):
-        if dX is None and need_dX:
-            dX = rt.empty_like(H)
-        if dgain is None and need_dgain:
-            dgain = rt.empty(d, dtype=rt.f32, device=H.device)
-        if work is None and dgain is not None:
-            work = rt.empty(rms_norm_backward_bytes(M, d), dtype=rt.u8, device=H.device)
+    new_dX, new_dgain = dX is None and need_dX, dgain is None and need_dgain
+    new_work = work is None and (new_dgain or dgain is not None)
+    if new_dX or new_dgain or new_work:
+        with rt.under(stream):
+            dX = rt.empty_like(H) if new_dX else dX
+            dgain = rt.empty(d, dtype=rt.f32, device=H.device) if new_dgain else dgain
+            work = rt.empty(rms_norm_backward_bytes(M, d), dtype=rt.u8, device=H.device) if new_work else work
     dt, dev, n = H.dtype, rt.device(), M * d
     code = rt.code(dt)
     nwork = 0 if work is None else work.numel() * work.element_size()

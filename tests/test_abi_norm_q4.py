@@ -288,3 +288,28 @@ def test_norm_outputs_over_inputs_are_refused(dtype, es):
     assert backward(**{**kw, "work": far[5]}) == INVAL and backward(**{**kw, "dX": far[1]}) == INVAL
     for i in (1, 2, 3):  # not on 4 bytes
         assert backward(**{**kw, "work": _at(0x7000000 + i)}) == UNSUP
+
+
+def test_streams_of_another_device_are_refused(binding):
+    torch, calls = binding
+
+    class Stream:
+        cuda_stream = 0x40
+
+        def __init__(self, device_index):
+            self.device_index = device_index
+
+    x, y = torch.zeros(2, 64), torch.zeros(2, 64)
+    pifa.rms_norm_forward(x, None, 1e-5, Y=y, stream=Stream(-1))  # the binding's device here
+    pifa.rms_norm_forward(x, None, 1e-5, Y=y, stream=0x40)
+    assert [c[1][-1] for c in calls] == [0x40, 0x40]
+    h = pifa._remember(0x5000, d_in=64, d_out=64, dt=pifa.PIFA_BF16, dev=-1)
+    try:
+        for call in (lambda st: pifa.rms_norm_forward(x, None, 1e-5, Y=y, stream=st),
+                     lambda st: pifa.rms_norm_backward(x, None, x, 1e-5, dX=y, need_dgain=False, stream=st),
+                     lambda st: pifa.q4_layer_forward(h, x.bfloat16(), y.bfloat16(), stream=st)):
+            with pytest.raises(ValueError):
+                call(Stream(1))
+    finally:
+        pifa._forget(h)
+    assert len(calls) == 2
