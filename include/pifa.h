@@ -443,7 +443,8 @@ pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* sc
 pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, const void* gain, float eps,
                                   void* H, void* Y, int64_t M, void* stream);
 
-/* Pre-size the workspace for q4_layer_norm_forward of up to max_M rows. */
+/* Pre-size the workspace for q4_layer_norm_forward of up to max_M rows (also
+ * while a stream is being captured). */
 pifa_status q4_layer_reserve(q4_handle h, int64_t max_M);
 
 /*

@@ -2394,7 +2394,13 @@ pifa_status q4_ensure(q4_layer* h, size_t need, hipStream_t st) {
     if (h->n_ws == q4_layer::kMaxBufs) return PIFA_ERR_OOM;
     need = std::max(need, 2 * h->ws_bytes);
     void* p = nullptr;
-    if (hipMalloc(&p, need) != hipSuccess) {
+    // an allocation is no part of a graph: one that another stream is capturing
+    // meanwhile stays valid in the relaxed mode only
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    PIFA_HIP(hipThreadExchangeStreamCaptureMode(&mode));
+    const hipError_t e = hipMalloc(&p, need);
+    PIFA_HIP(hipThreadExchangeStreamCaptureMode(&mode));
+    if (e != hipSuccess) {
         (void)hipGetLastError();
         return PIFA_ERR_OOM;
     }

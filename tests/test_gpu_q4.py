@@ -790,3 +790,29 @@ def test_few_rows_of_wide_layers(M, d_out, act):
     """Up to 16 rows at 1, 2 and 4 groups of columns a workgroup, K of many blocks with a cut one."""
     for d_in in (2080, 4192):
         _product_on_the_gpu(act, M, d_in, d_out, 102)
+
+
+def test_workspace_is_reserved_during_a_capture():
+    """Reserving during a capture leaves it valid, and the captured call takes what was reserved."""
+    torch, pifa = torch_mod(), _pifa()
+    layer, _ = _layer(64, 24, 111)
+    with layer:
+        x, _ = _x(40, 64, 112)
+        want = layer.norm_forward(x, None, EPS)
+        fresh, _ = _layer(64, 24, 111)
+        torch.cuda.synchronize()
+        y, eager = torch.zeros_like(want), torch.zeros_like(want)
+        side, other = torch.cuda.Stream(), torch.cuda.Stream()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graph, stream=side):
+                fresh.reserve(40)
+                fresh.norm_forward(x, None, EPS, Y=y)
+                layer.reserve(800)
+        for _ in range(3):
+            y.zero_()
+            graph.replay()
+            layer.norm_forward(x, None, EPS, Y=eager, stream=other)
+            torch.cuda.synchronize()
+            assert torch.equal(y, want) and torch.equal(eager, want)
+        fresh.close()
