@@ -816,3 +816,17 @@ def test_workspace_is_reserved_during_a_capture():
             torch.cuda.synchronize()
             assert torch.equal(y, want) and torch.equal(eager, want)
         fresh.close()
+
+
+@pytest.mark.parametrize("M", [9, 12, 16, 17, 33, 130])
+@pytest.mark.parametrize("d_in,d_out", [(512, 200), (4096, 16400)])
+def test_norm_of_more_rows_is_norm_and_product(M, d_in, d_out):
+    """From 9 rows on the rows are rounded to bf16 as separate calls round them, and nothing else is."""
+    torch, pifa = torch_mod(), _pifa()
+    layer, _ = _layer(d_in, d_out, 121)
+    with layer:
+        (x, _), (r, _) = _x(M, d_in, 122), _x(M, d_in, 123)
+        g = (1 + 0.2 * torch.randn(d_in, device="cuda")).to(torch.bfloat16)
+        H, H2 = torch.empty_like(x), torch.empty_like(x)
+        apart = layer(pifa.rms_norm_forward(x, g, EPS, R=r, H=H))
+        assert torch.equal(layer.norm_forward(x, g, EPS, R=r, H=H2), apart) and torch.equal(H, H2)
