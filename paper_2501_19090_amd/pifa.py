@@ -821,11 +821,11 @@ def q4_layer_forward(handle: int, X, Y, M: int | None = None, stream=None) -> No
 def q4_layer_forward_e4m3(handle: int, Q, scale, Y, M: int | None = None, stream=None) -> None:
     rt = _rt()
     d = _recall(handle) or {"d_in": 0, "d_out": 0}
-    row, whole = (d["d_out"], d["d_in"] > 0) if M is None else (0, False)
+    row = d["d_out"] if M is None else 0
     M = _q4_rows(Q, "Q", d["d_in"], M)
     dev = rt.device()
     _check("q4_layer_forward_e4m3", lib().q4_layer_forward_e4m3(
-        handle, _ptr_of(Q, "Q", rt.e4m3, M * d["d_in"], dev), _ptr_of(scale, "scale", rt.f32, M, dev, whole),
+        handle, _ptr_of(Q, "Q", rt.e4m3, M * d["d_in"], dev), _ptr_of(scale, "scale", rt.f32, M, dev),
         _ptr_of(Y, "Y", rt.bf16, M * d["d_out"], dev, False, row), M, rt.stream(stream, dev)))
 
 

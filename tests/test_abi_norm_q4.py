@@ -212,7 +212,7 @@ def test_sizes_of_a_4_bit_call(binding):
         x, y, g = t(6, 64), t(6, 24), t(64)
         q = x.to(torch.float8_e4m3fn)
         for call in (lambda: pifa.q4_layer_forward(h, x, t(3, 48)), lambda: pifa.q4_layer_forward(h, x, t(5, 24)),
-                     lambda: pifa.q4_layer_forward_e4m3(h, q, torch.zeros(7), y),
+                     lambda: pifa.q4_layer_forward_e4m3(h, q, torch.zeros(5), y),
                      lambda: pifa.q4_layer_forward_e4m3(h, q, torch.zeros(6), t(3, 48)),
                      lambda: pifa.q4_layer_norm_forward(h, x, t(128), 1e-5, Y=y),
                      lambda: pifa.q4_layer_norm_forward(h, x, g, 1e-5, R=t(7, 64), Y=y),
@@ -223,7 +223,7 @@ def test_sizes_of_a_4_bit_call(binding):
         assert not calls
         pifa.q4_layer_forward(h, x, t(9, 24))
         pifa.q4_layer_forward(h, t(9, 64), y, M=6)
-        pifa.q4_layer_forward_e4m3(h, q, torch.zeros(6), t(150))
+        pifa.q4_layer_forward_e4m3(h, q, torch.zeros(9), t(150))  # scales of a larger batch's buffer
         pifa.q4_layer_norm_forward(h, x, g, 1e-5, R=t(384), H=t(7, 64), Y=y)
         assert [c[0] for c in calls] == ["q4_layer_forward"] * 2 + ["q4_layer_forward_e4m3", "q4_layer_norm_forward"]
     finally:
