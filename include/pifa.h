@@ -375,6 +375,9 @@ size_t rms_norm_backward_bytes(int64_t M, int64_t d);
  * d_in must be a multiple of 32 and at most 2^21, d_out at most 2^27
  * (PIFA_ERR_UNSUPPORTED).
  *
+ * These layers go forward only: a weight in 4 bits takes no gradient, and none
+ * of X is offered.
+ *
  * (A low-rank pair U V^T keeps its accuracy in this format as two such layers
  * in a row.  PIFA's W_p and C do not: C rebuilds the non-pivot outputs with
  * cancellation, which multiplies the weights' rounding.)
@@ -430,15 +433,21 @@ pifa_status q4_layer_forward_e4m3(q4_handle h, const uint8_t* Q, const float* sc
  *   H = X + R,   Y = (H rho gain) W^T.
  * X, R, gain, eps and H as for rms_norm_forward with d = d_in and bf16, but X,
  * R and gain 16-byte aligned, and H and Y overlapping neither each other nor X,
- * R and gain (PIFA_ERR_INVALID_ARG): workgroups that still read them follow
- * those that write.  For M <= 8 with M d_in <= 12288 it is one launch:
- * rho scales whole rows of the product, so it is applied to the sums.  More are
- * normed into the layer's workspace first (M x d_in bf16; up to 8 rows twice
- * that, with what the rounding left, so that only more rows are rounded
- * between norm and product), and such calls on one handle must not overlap.  The workspace grows on demand; memory it outgrows is kept until
- * the layer is destroyed, so graphs captured with it stay valid.  A call
- * whose stream is being captured does not grow it (PIFA_ERR_TOO_LARGE):
- * reserve first.
+ * R and gain (PIFA_ERR_INVALID_ARG), H not X or R themselves either: in one
+ * launch, workgroups that still read them follow those that write, and whether
+ * a call is one launch is not for its caller to know.
+ * For M <= 8 with M d_in <= 12288 (and group scales up to 2^60) it is one launch:
+ * rho scales whole rows of the product, so it is applied to the sums.  Other
+ * calls norm the rows into the layer's workspace first, and such calls on one
+ * handle must not overlap.
+ * Up to 8 rows are held as two bf16 values each, which loses nothing against
+ * fp32 rows.  From 9 rows on the normed rows are rounded to bf16 between norm
+ * and product, with the bits that rms_norm_forward and q4_layer_forward give:
+ * about 1.4 times the error, against 64 bits, of a chain that rounds Y alone.
+ * The workspace (M x d_in bf16, twice that for up to 8 rows) grows on demand;
+ * memory it outgrows is kept until the layer is destroyed, so graphs captured
+ * with it stay valid.  A call whose stream is being captured does not grow it
+ * (PIFA_ERR_TOO_LARGE): reserve first.
  */
 pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, const void* gain, float eps,
                                   void* H, void* Y, int64_t M, void* stream);

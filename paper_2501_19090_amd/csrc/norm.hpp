@@ -11,9 +11,11 @@
 // neighbouring threads hold neighbouring chunks.  Sums, rho and the quotient
 // are fp32; each result is rounded once, from the unrounded h.
 //
-// Measured (bf16, X, R, H and Y of 4096 rows of 8192): 47 us, 5.7 TB/s (a copy of
-// 1 GiB: 5.2).  The gradients of 4096 x 4096 31 us (4.3 TB/s), of 8192 x 8192 104
-// us (5.2 TB/s).  One row of 4096 takes 2.6 us, one of 64 2.2: a launch.
+// Measured, calls in a row, both launches of the gradients: X, R, H and Y of 4096
+// rows of 8192 in bf16 47 to 48 us, 5.6 TB/s (a copy of 1 GiB: 5.2), in fp32 97
+// us, 5.5 TB/s.  The gradients of 4096 x 4096 31 us (4.3 TB/s), of 8192 x 8192
+// 103 us (5.2 TB/s).  One row of 4096 takes 2.7 us, one of 64 2.3: a launch (in a
+// trace the kernel of the former is 2.2).
 #pragma once
 
 #include <type_traits>
@@ -27,7 +29,7 @@ constexpr float kE4m3Max = 448.f;      // largest e4m3 value
 constexpr float kE4m3Tiny = 0x1p-126f; // smallest row scale: its inverse is finite
 
 // The full chunks of a row; the d % N elements behind them are handled one
-// per thread (norm_tail), which costs rows of whole chunks a uniform branch.
+// per thread, which costs rows of whole chunks a uniform branch.
 template <typename T>
 struct NormChunk {
     static constexpr int N = 16 / (int)sizeof(T);
@@ -449,7 +451,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd(NormBwd<T> p) {
         const float back = norm_back(rho, sums.y, (float)p.d);
         const int64_t row = live ? m * p.d : 0, full = live ? nfull : 0;
         // the second reading of the row's registers converts them again: kept
-        // from the first one, the fp32 values do not fit 128 registers
+        // from the first one, the fp32 values do not fit 128 registers (of bf16
+        // rows of two chunks a thread 8 to 14 are spilled all the same)
 #pragma unroll
         for (int i = 0; i < V; ++i) asm volatile("" : "+v"(cur.h[i]), "+v"(cur.y[i]), "+v"(g[i]));
 #pragma unroll

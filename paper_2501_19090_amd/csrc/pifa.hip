@@ -2314,7 +2314,7 @@ hipError_t norm_forward_run(const void* X, const void* R, const void* gain, floa
 // partial sums of dgain.  More threads a row than chunks, or two chunks each
 // where one fits, lose (4096 rows, us): 512: 64 threads 8.7, 128 10.6; 2048: 256
 // 17.6, 512 22.0; 4096: 512 31.0, 1024 39.8, 256 x 2 40.4; 8192: 1024 55.6, 512 x
-// 2 66.7; 16384: 1024 x 2 122.7, read twice 343.
+// 2 66.7; 16384: 1024 x 2 126, read twice 343.
 int64_t norm_bwd_rows(int64_t d, int64_t n) {
     const int64_t chunks = d / n;
     return chunks <= 64 ? 16 : chunks <= 128 ? 8 : chunks <= 256 ? 4 : chunks <= 512 ? 2 : 1;
@@ -2480,7 +2480,8 @@ int64_t q4_norm_rows(int64_t M) { return std::max(M, 2 * std::min<int64_t>(M, kQ
 // room).  A form whose p is 0 is not there: another is faster everywhere.
 // Measured at K = 4096 and 11008 over 17 to 4096 rows with hot weights.  bf16,
 // 118 drawn sizes (K 288 to 12736, N 270 to 22327, M 20 to 3859): the form picked
-// is the measured best or within 8% of it at 112, and within 32% at all.
+// is the measured best or within 8% of it at 112, and within 32% at all; e4m3, 100
+// sizes drawn alike: at 86, and within 16% at all.
 // The codes of bf16 products are converted once for every wave along the rows:
 // tiles of 64 x 128 and 128 x 128 with one (us, against the best of the others):
 // 64 rows of 8192 -> 28672 43 / 54, 128 rows 65 / 79; 203 rows of 4096 -> 22016
@@ -2587,7 +2588,10 @@ hipError_t launch_q4(Q4Args p, hipStream_t st) {
             // 8192 -> 28672 23.0 / 24.9; three rows of 4096^2 4.0 / 4.3, of 2048 ->
             // 6000 3.9 / 3.6, of 8192 -> 28672 28.0 / 25.1.
             // 1 / 2 / 4 groups a workgroup, eight bf16 rows: 4096^2 5.0 / 5.4 / 6.5,
-            // 2048 -> 6000 5.1 / 3.9 / 4.4, 4096 -> 11008 10.2 / 9.0 / 7.4.
+            // 2048 -> 6000 5.1 / 3.9 / 4.4, 4096 -> 11008 10.2 / 9.0 / 7.4.  Eight
+            // e4m3 rows: 3.8 / 4.1 / 4.7, 3.7 / 3.3 / 3.7, 7.2 / 7.3 / 6.4 (one: 3.2 /
+            // 3.5 / 4.2, 3.1 / 3.0 / 3.5, 5.9 / 6.3 / 6.2); the rule loses most next
+            // to its border, 8192 -> 9600 (600 groups) 11.5 / 11.2 / 8.9.
             // Tiles, which read the rows once for 128 columns, against 4 groups: 16
             // rows of 8192 -> 16640 19.7 / 23.8, -> 28672 28.0 / 33.0, of 4096 -> 16640
             // 12.4 / 14.3; 9 rows of 4096 -> 28672 14.3 / 12.8, 16 of 2048 -> 28672

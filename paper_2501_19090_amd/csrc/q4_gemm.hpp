@@ -25,9 +25,11 @@
 // fragments so that a lane's accumulators are 4 TN consecutive columns of a
 // row of Y: row i of fragment j is column (i / 4) * 4 TN + 4 j + i % 4.
 //
-// Measured: 4096 rows of 4096 -> 11008 in bf16 279 us, 1.32 PFLOP/s (a library
-// product of 8192^3: 1.40), matrix cores busy in 65% of the cycles CUs work; 1999
-// rows of 11008 -> 4096 in e4m3 79 us, 2.29 PFLOP/s (library: 2.64), 56%.
+// Measured on several boards, calls in a row: 4096 rows of 4096 -> 11008 in bf16
+// 279 to 292 us, 1.32 to 1.26 PFLOP/s (a library product of 8192^3: 1.40); 1999
+// rows of 11008 -> 4096 in e4m3 79 to 83 us, 2.29 to 2.17 PFLOP/s (library: 2.64).
+// Under the profiler the kernels take 296 to 326 and 81 to 84 us, with the matrix
+// cores busy in 65% and 56% of the cycles CUs work.
 #pragma once
 
 #include "common.hpp"

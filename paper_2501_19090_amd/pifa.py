@@ -955,7 +955,9 @@ class Q4Layer:
         return Y
 
     def norm_forward(self, X, gain, eps: float, R=None, H=None, Y=None, stream=None):
-        """The product of the norm of X + R; H, where given, takes X + R."""
+        """The product of the norm of X + R; H, where given, takes X + R.  Normed
+        rows are rounded to bf16 from 9 of them on.  Calls that use the layer's
+        workspace (see q4_layer_norm_forward in include/pifa.h) must not overlap."""
         Y = self._out(Y, X, stream)
         q4_layer_norm_forward(self.handle, X, gain, eps, R, H, Y, None, stream)
         return Y
