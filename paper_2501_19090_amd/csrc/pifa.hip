@@ -2399,7 +2399,7 @@ pifa_status q4_ensure(q4_layer* h, size_t need, hipStream_t st) {
     hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
     PIFA_HIP(hipThreadExchangeStreamCaptureMode(&mode));
     const hipError_t e = hipMalloc(&p, need);
-    PIFA_HIP(hipThreadExchangeStreamCaptureMode(&mode));
+    (void)hipThreadExchangeStreamCaptureMode(&mode);
     if (e != hipSuccess) {
         (void)hipGetLastError();
         return PIFA_ERR_OOM;
