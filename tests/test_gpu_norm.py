@@ -493,3 +493,33 @@ def test_backward_of_many_rows_a_workgroup(dtype, d):
     # at most 7 rows and 16 slots of a workgroup, 16 partial sums of a slice and 16 slices: under 128 additions
     off = (dg.double() - (dy * h * p).sum(0)).abs() - 3 * FP * (dy * h * p).abs().sum(0)
     assert torch.isfinite(dg).all() and float(off.max()) <= 0, float(off.max())
+
+
+def test_rows_past_2_31_elements():
+    """Offsets of the last rows pass 31 bits: the values of a call of their own."""
+    pifa, torch = _pifa(), torch_mod()
+    M, d = (1 << 21) + 3, 1032
+    rng = torch.Generator(device="cuda").manual_seed(80)
+    x = torch.empty(M, d, dtype=torch.bfloat16, device="cuda")
+    x.normal_(generator=rng)
+    g, _ = _gain(d, "bf16", 81)
+    last = slice(M - 40, M)
+    H = torch.empty_like(x)
+    Y = pifa.rms_norm_forward(x, g, EPS, R=x, H=H)
+    h2, rows = torch.empty(40, d, dtype=torch.bfloat16, device="cuda"), x[last].clone()
+    assert torch.equal(Y[last], pifa.rms_norm_forward(rows, g, EPS, R=rows, H=h2)) and torch.equal(H[last], h2)
+    Q, s = pifa.rms_norm_forward_e4m3(x, g, EPS)
+    q2, s2 = pifa.rms_norm_forward_e4m3(rows, g, EPS)
+    assert torch.equal(Q[last].view(torch.uint8), q2.view(torch.uint8)) and torch.equal(s[last], s2)
+    del Q, H
+    dX, dg = pifa.rms_norm_backward(x, g, Y, EPS, dR=x)
+    dX2, _ = pifa.rms_norm_backward(rows, g, Y[last].clone(), EPS, dR=rows)
+    assert torch.equal(dX[last], dX2)
+    want, mags = torch.zeros(d, dtype=torch.float64, device="cuda"), torch.zeros(d, dtype=torch.float64, device="cuda")
+    for m in range(0, M, 1 << 17):
+        h, y = x[m:m + (1 << 17)].double(), Y[m:m + (1 << 17)].double()
+        t = y * h * torch.rsqrt((h * h).mean(1, keepdim=True) + EPS)
+        want += t.sum(0)
+        mags += t.abs().sum(0)
+    # a thread adds 2^21 / 256 / 4 rows one by one: 2^11 roundings of 2^-24 of the sum so far, and those of the terms
+    assert bool(((dg.double() - want).abs() <= (2.0 ** -13 + 3 * FP) * mags).all())

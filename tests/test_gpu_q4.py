@@ -727,7 +727,7 @@ def _picked(act, M, N, K):
     return best[1]
 
 
-def _product_on_the_gpu(act, M, d_in, d_out, seed):
+def _product_on_the_gpu(act, M, d_in, d_out, seed, sums=SUMS):
     """A product of bf16 (act 0) or 8-bit rows (1) against 64 bits, weights made on the GPU."""
     torch, pifa = torch_mod(), _pifa()
     rng = torch.Generator(device="cuda").manual_seed(seed)
@@ -749,7 +749,7 @@ def _product_on_the_gpu(act, M, d_in, d_out, seed):
             a = q.double() * f.double()[:, None]
         torch.cuda.synchronize()
     want = a @ w.t().contiguous()
-    tol = want.abs() * 2.0 ** -8 + SUMS * (a.abs() @ w.abs().t().contiguous())
+    tol = want.abs() * 2.0 ** -8 + sums * (a.abs() @ w.abs().t().contiguous())
     if act == 1:
         top = lambda v: v.abs().view(v.shape[0], -1, 32).amax(2)
         tol += 2.0 ** -9 * (top(a) @ top(w).t().contiguous())
@@ -830,3 +830,13 @@ def test_norm_of_more_rows_is_norm_and_product(M, d_in, d_out):
         H, H2 = torch.empty_like(x), torch.empty_like(x)
         apart = layer(pifa.rms_norm_forward(x, g, EPS, R=r, H=H))
         assert torch.equal(layer.norm_forward(x, g, EPS, R=r, H=H2), apart) and torch.equal(H, H2)
+
+
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("d_in,rows", [(32640, (1, 2, 3)), (32768, (1, 2)), (65536, (1, 2, 16, 40)), (1 << 21, (1, 2, 16, 20, 70, 257))])
+def test_deep_layers(d_in, rows, act):
+    """Up to the largest d_in: rows at the end of what LDS holds, and offsets of 256
+    rows below 2^31.  One lane's chain of sums is at most d_in / 32 additions of
+    2^-23 of the terms."""
+    for M in rows:
+        _product_on_the_gpu(act, M, d_in, 40, 103, max(SUMS, d_in / 32 * 2.0 ** -23))
