@@ -457,6 +457,186 @@ pifa_status q4_layer_norm_forward(q4_handle h, const void* X, const void* R, con
 pifa_status q4_layer_reserve(q4_handle h, int64_t max_M);
 
 /*
+ * Layer norm of the rows a layer reads, with the residual's addition:
+ *   H = X + R,   c = H - mean_k H[m,k],   rho_m = (mean_k c[m,k]^2 + eps)^-1/2,
+ *   Y[m,k] = c[m,k] rho_m gain[k] + bias[k]
+ *   X     device, M x d, dtype.
+ *   R     device, M x d, dtype, or NULL (H = X).
+ *   gain  device, d, dtype, or NULL (ones).   bias  device, d, dtype, or NULL (zeros).
+ *   eps   positive and finite.
+ *   H     device, M x d, dtype, or NULL (not stored).
+ *   Y     device, M x d, dtype.
+ * Limits, alignment, stream and M = 0 as for rms_norm_forward.  Sums are fp32, that of the
+ * squares taken after the mean is off (a row whose squares of c sum to more than
+ * 3.4e38 has rho = 0); H and Y are each rounded once, Y from the unrounded H.
+ * H and Y may each be X or R themselves, not each other, and overlap nothing
+ * otherwise (PIFA_ERR_INVALID_ARG).
+ */
+pifa_status layer_norm_forward(const void* X, const void* R, const void* gain, const void* bias, float eps,
+                               void* H, void* Y, int64_t M, int64_t d, pifa_dtype dtype, void* stream);
+
+/*
+ * Gradients of layer_norm_forward.  With u = gain dY, hat = c rho, of the stored H:
+ *   dX[m,k] = rho (u[m,k] - mean_j u[m,j] - hat[m,k] mean_j(u[m,j] hat[m,j])) + dR[m,k],
+ *   dgain[k] = sum_m dY[m,k] hat[m,k],   dbias[k] = sum_m dY[m,k].
+ *   H     device, M x d, dtype: the forward's H (its X if it had no R).
+ *   gain  device, d, dtype, or NULL (ones).
+ *   dY    device, M x d, dtype.
+ *   dR    device, M x d, dtype, or NULL: the gradient that reaches H beside
+ *         the norm (through the residual stream).
+ *   dX    device, M x d, dtype, or NULL to skip: the gradient of X, and of R.
+ *         May be H, dY or dR itself; outputs and workspace overlap nothing
+ *         otherwise (PIFA_ERR_INVALID_ARG).
+ *   dgain, dbias  device, d, fp32 (overwritten), or NULL to skip.
+ *   work  device, at least layer_norm_backward_bytes(M, d) bytes, 4-byte
+ *         aligned (may be NULL where that is 0 or both dgain and dbias are
+ *         NULL); it keeps nothing between calls, and calls that may overlap
+ *         need one each.
+ * The sums over the rows are fp32 in a fixed order (two calls give the same
+ * bits).  M = 0 zeroes dgain and dbias.  Asynchronous on `stream`.
+ */
+pifa_status layer_norm_backward(const void* H, const void* gain, const void* dY, const void* dR, float eps,
+                                void* dX, float* dgain, float* dbias, int64_t M, int64_t d, pifa_dtype dtype,
+                                void* work, size_t work_bytes, void* stream);
+
+/* Workspace of layer_norm_backward for M rows of d (partial sums); 0 for sizes
+ * it does not take. */
+size_t layer_norm_backward_bytes(int64_t M, int64_t d);
+
+/*
+ * Low-rank adapters of many requests beside one shared projection (any layer of
+ * this library).  n adapters of rank r lie in slots: A (device, n x r x d_in,
+ * bf16) and B (device, n x d_out x r, bf16); one of a smaller rank is filled up
+ * with zeros.  Row m of a batch has adapter ids[m], or none where ids[m] is not
+ * in [0, n).
+ *
+ * adapter_plan sorts a batch's rows by adapter; each adapter_forward and
+ * adapter_backward over rows with these ids goes by the plan.
+ *   ids   device, M, int32.
+ *   plan  device, at least adapter_plan_bytes(M, n) bytes, 16-byte aligned.
+ * Every call that a plan is given to has to have its M and n (a call on the
+ * device finds others, and writes nothing).  M up to 2^20, n up to 4096, r up to
+ * 1024, d_in and d_out up to 2^19 (PIFA_ERR_UNSUPPORTED).  Asynchronous on
+ * `stream`; it allocates nothing and may be captured, ids then being those at
+ * each replay.
+ */
+pifa_status adapter_plan(const int32_t* ids, int64_t M, int64_t n, void* plan, size_t plan_bytes, void* stream);
+
+/* Bytes of a plan; 0 for sizes it does not take. */
+size_t adapter_plan_bytes(int64_t M, int64_t n);
+
+/*
+ * Y[m,:] = Y0[m,:] + scale[a] (X[m,:] A_a^T) B_a^T,  a = ids[m];  Y[m,:] = Y0[m,:] for rows without.
+ *   X      device, M x d_in, bf16.
+ *   scale  device, n, fp32, or NULL (ones).
+ *   plan   as adapter_plan wrote it, on this stream or one waited for.
+ *   Y0     device, M x d_out, bf16: the projection's output, or NULL (zeros).
+ *   Y      device, M x d_out, bf16; every element is written.  May be Y0 itself
+ *          and overlaps nothing otherwise (PIFA_ERR_INVALID_ARG).
+ *   work   device, at least adapter_forward_bytes(...) bytes, 16-byte aligned; it
+ *          keeps nothing between calls, and calls that may overlap need one each.
+ * No alignment is required of the others.  X A^T is held in fp32 and multiplied
+ * as two bf16 values; Y is rounded once.  A row's sums depend on how many rows
+ * the batch has of each adapter (K is cut by their tiles), and are the same in
+ * each call on the same batch.  M = 0 returns PIFA_OK without launching.
+ * Asynchronous on `stream`.
+ */
+pifa_status adapter_forward(const void* X, const void* A, const void* B, const float* scale, const void* plan,
+                            const void* Y0, void* Y, int64_t M, int64_t d_in, int64_t d_out, int64_t r, int64_t n,
+                            void* work, size_t work_bytes, void* stream);
+size_t adapter_forward_bytes(int64_t M, int64_t d_in, int64_t d_out, int64_t r, int64_t n);
+
+/*
+ * Gradients of adapter_forward.  With U[m,:] = scale[a] dY[m,:] B_a and T[m,:] = scale[a] X[m,:] A_a^T:
+ *   dX[m,:] = dX0[m,:] + U[m,:] A_a,   dA_a = sum_m U[m,:]^T X[m,:],   dB_a = sum_m dY[m,:]^T T[m,:]
+ * over the rows m of adapter a; dX[m,:] = dX0[m,:] for rows without.
+ *   dY   device, M x d_out, bf16.
+ *   dX0  device, M x d_in, bf16: the gradient through the projection itself, or
+ *        NULL (zeros).
+ *   dX   device, M x d_in, bf16, or NULL to skip.  May be dX0 itself.
+ *   dA   device, n x r x d_in, fp32 (overwritten; zeros for adapters without
+ *        rows), or NULL to skip.
+ *   dB   device, n x d_out x r, fp32, likewise.
+ *   work device, at least adapter_backward_bytes(...) bytes, 16-byte aligned, as
+ *        for adapter_forward.
+ * X, A, B, scale, plan and limits as there.  Outputs and workspace overlap
+ * nothing (PIFA_ERR_INVALID_ARG).  U and T are fp32 in dA and dB, two bf16 values
+ * in dX.  Sums are fp32 in a fixed order.  M = 0 zeroes dA and dB.  The scale
+ * takes no gradient.  Asynchronous on `stream`.
+ */
+pifa_status adapter_backward(const void* X, const void* A, const void* B, const float* scale, const void* plan,
+                             const void* dY, const void* dX0, void* dX, float* dA, float* dB, int64_t M,
+                             int64_t d_in, int64_t d_out, int64_t r, int64_t n, void* work, size_t work_bytes,
+                             void* stream);
+size_t adapter_backward_bytes(int64_t M, int64_t d_in, int64_t d_out, int64_t r, int64_t n);
+
+/*
+ * AdamW over many tensors in one launch.  Step t, for every value:
+ *   g' = g grad_scale,   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2,
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ */
+typedef struct {
+    float* p;             /* device, n, fp32: read and written                    */
+    const void* g;        /* device, n, of the handle's gradient type             */
+    void* m;              /* device, n: fp32, or e4m3 codes (state_bits 8)        */
+    void* v;              /* likewise                                             */
+    uint8_t* m_scale;     /* state_bits 8: device, one for each 32 values of m    */
+    uint8_t* v_scale;     /* likewise                                             */
+    void* p_bf16;         /* device, n, bf16: takes p rounded, or NULL            */
+    int64_t n;            /* values, 0 or more                                    */
+    double weight_decay;  /* 0 or more                                            */
+} adamw_tensor;
+typedef struct adamw_state* adamw_handle;
+
+/*
+ * A handle for the tensors (a host array, copied; the memory that its entries
+ * point to stays the caller's, and stays where it is as long as the handle is used).
+ *   state_bits  32: m and v are fp32.  8: OCP e4m3 codes, groups of 32
+ *               consecutive values of a tensor (the last may be shorter) sharing
+ *               the power of two scale - 127; a group's scale is the smallest at
+ *               which its largest magnitude is at most 448 units, and 255 makes the
+ *               group NaN (one with an infinity or a NaN gets it).  All zeros is the
+ *               state before the first step.
+ *   g_dtype     of every gradient.
+ *   seed        of the random bits below (state_bits 8).
+ * No output (p, m, v, scales, p_bf16) may overlap another or a gradient
+ * (PIFA_ERR_INVALID_ARG): a tensor named twice is refused.  Pointers need their
+ * element's alignment (PIFA_ERR_UNSUPPORTED).  At most 2^23 chunks of 4096
+ * values, cut tensor by tensor.  Synchronises the device.
+ *
+ * Moments in 8 bits are rounded to one of their two neighbours (q steps and a rest
+ * f of a step, 0 <= f < 1: up where 65536 f + b >= 65535.5), with b 16 bits of
+ *   mix(mix(mix(mix(mix(seed) + t) + tensor) + i / 4096) + i % 4096),
+ *   mix(x): x = (x ^ x >> 16) 0x6A09E667, x = (x ^ x >> 15) 0xBB67AE85, x ^ x >> 16   (32 bits),
+ * the upper 16 for m, the lower for v, i a value's index in its tensor; to the
+ * nearest they would not move at all where a step changes them by less than half a
+ * unit.  A v above zero becomes the smallest value at least.  The update takes m
+ * and v before they are rounded.
+ */
+pifa_status adamw_create(const adamw_tensor* tensors, int64_t count, int state_bits, pifa_dtype g_dtype,
+                         uint32_t seed, adamw_handle* out);
+pifa_status adamw_destroy(adamw_handle h);
+
+/*
+ * One step.
+ *   lr >= 0, 0 <= beta1, beta2 < 1, eps > 0, all finite.
+ *   step        the number t >= 1 of this step, or 0: one more than that of the
+ *               handle's last step in stream order, counted on the device (one
+ *               more launch, of one thread).  A captured call with 0 counts on at
+ *               each replay; one with a number replays that number, and its
+ *               random bits.
+ *   grad_scale  device, one fp32 value that multiplies every gradient (that of a
+ *               clipped norm), or NULL (1).
+ * Calls on one handle must not overlap.  Asynchronous on `stream`; it allocates
+ * nothing.
+ */
+pifa_status adamw_step(adamw_handle h, double lr, double beta1, double beta2, double eps, int64_t step,
+                       const float* grad_scale, void* stream);
+
+/* Number of the handle's last step, 0 before the first (synchronises the device). */
+pifa_status adamw_count(adamw_handle h, int64_t* steps);
+
+/*
  * Online Error-Accumulation-Minimization reconstruction (Sec. 4; Part 1 of
  * Algorithm "MPIFA" in the appendix "Experiment Details").  A calibration
  * handle keeps the running sums of one layer with input width d_in = n:

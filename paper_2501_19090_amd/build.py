@@ -16,14 +16,14 @@ ARCH = "gfx950"
 
 # Packed fp32 instructions stay off: only scalar / plain vector fp32 code.
 HIPCC_FLAGS = [
-    "--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-result",
 ]
 
 
 def sources():
-    return [os.path.join(CSRC, "pifa.hip")]
+    return [os.path.join(CSRC, f) for f in ("pifa.hip", "tune.hip")]
 
 
 def source_digest() -> str:
@@ -56,22 +56,37 @@ def forward_kernel_digest() -> str:
     return h.hexdigest()[:16]
 
 
+def _report(out: str) -> str:
+    return "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
+
+
 def build(verbose: bool = False) -> str:
-    """Always recompile (this is the build check); returns the library path."""
+    """Always recompile (this is the build check), the sources side by side;
+    returns the library path."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [hipcc] + HIPCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-o", tmp] + sources()
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        if os.path.exists(tmp):
-            os.remove(tmp)
-        raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out)
-    os.replace(tmp, LIB)
+    tag = ".tmp%d" % os.getpid()
+    objects = [os.path.splitext(src)[0] + tag + ".o" for src in sources()]
+    try:
+        runs = []
+        for src, obj in zip(sources(), objects):
+            cmd = [hipcc] + HIPCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-c", "-o", obj, src]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            runs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+        for run, out in [(run, _report(run.communicate()[0])) for run in runs]:
+            if run.returncode != 0:
+                raise RuntimeError("hipcc failed:\n" + out)
+            if verbose and out.strip():
+                print(out)
+        link = subprocess.run([hipcc, "--offload-arch=" + ARCH, "-fPIC", "-shared", "-o", LIB + tag] + objects,
+                              stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if link.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + _report(link.stdout))
+        os.replace(LIB + tag, LIB)
+    finally:
+        for f in objects + [LIB + tag]:
+            if os.path.exists(f):
+                os.remove(f)
     return LIB
 
 

@@ -590,7 +590,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_long(NormBwd<T> p) {
 // dgain = the sum of P <= 256 partial rows of d, in a fixed order: a workgroup
 // of 16 x 64 threads takes 64 columns; a thread's loads are all in flight.
 constexpr int kNormMaxGroups = 256;
-__global__ __launch_bounds__(kNormThreads) void norm_dgain(const float* __restrict__ part, int P, int64_t d,
+[[maybe_unused]] static __global__ __launch_bounds__(kNormThreads) void norm_dgain(const float* __restrict__ part, int P, int64_t d,
                                                           float* __restrict__ dgain) {
     constexpr int SLICES = kNormThreads / kWave, EACH = kNormMaxGroups / SLICES;
     __shared__ float red[kNormThreads];
@@ -614,7 +614,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_dgain(const float* __restri
 }
 
 // dgain of no rows (a fill kernel: a captured graph may hold it)
-__global__ void norm_zero(float* p, int64_t n) {
+static __global__ void norm_zero(float* p, int64_t n) {
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) p[i] = 0.f;
 }
 

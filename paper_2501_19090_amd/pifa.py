@@ -38,6 +38,12 @@ class pifa_dims(ctypes.Structure):
     _fields_ = [("d_in", ctypes.c_int64), ("d_out", ctypes.c_int64), ("r", ctypes.c_int64)]
 
 
+class adamw_tensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("p_bf16", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("weight_decay", ctypes.c_double)]
+
+
 class PifaError(RuntimeError):
     def __init__(self, fn: str, status: int):
         self.status = status
@@ -51,6 +57,7 @@ _vp = ctypes.c_void_p
 _i64 = ctypes.c_int64
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _f32 = ctypes.c_float
+_f64 = ctypes.c_double
 _st = ctypes.c_int
 
 _SIGNATURES = {
@@ -107,6 +114,21 @@ _SIGNATURES = {
     "q4_layer_forward_e4m3": (_st, [_vp, _vp, _vp, _vp, _i64, _vp]),
     "q4_layer_norm_forward": (_st, [_vp, _vp, _vp, _vp, _f32, _vp, _vp, _i64, _vp]),
     "q4_layer_reserve": (_st, [_vp, _i64]),
+    "layer_norm_forward": (_st, [_vp, _vp, _vp, _vp, _f32, _vp, _vp, _i64, _i64, ctypes.c_int, _vp]),
+    "layer_norm_backward": (_st, [_vp, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _i64, _i64, ctypes.c_int, _vp,
+                                  ctypes.c_size_t, _vp]),
+    "layer_norm_backward_bytes": (ctypes.c_size_t, [_i64, _i64]),
+    "adapter_plan": (_st, [_vp, _i64, _i64, _vp, ctypes.c_size_t, _vp]),
+    "adapter_plan_bytes": (ctypes.c_size_t, [_i64, _i64]),
+    "adapter_forward": (_st, [_vp] * 7 + [_i64] * 5 + [_vp, ctypes.c_size_t, _vp]),
+    "adapter_forward_bytes": (ctypes.c_size_t, [_i64] * 5),
+    "adapter_backward": (_st, [_vp] * 10 + [_i64] * 5 + [_vp, ctypes.c_size_t, _vp]),
+    "adapter_backward_bytes": (ctypes.c_size_t, [_i64] * 5),
+    "adamw_create": (_st, [ctypes.POINTER(adamw_tensor), _i64, ctypes.c_int, ctypes.c_int, ctypes.c_uint32,
+                           ctypes.POINTER(_vp)]),
+    "adamw_destroy": (_st, [_vp]),
+    "adamw_step": (_st, [_vp, _f64, _f64, _f64, _f64, _i64, _vp, _vp]),
+    "adamw_count": (_st, [_vp, ctypes.POINTER(_i64)]),
     "pifa_probe_mfma": (_st, [_i64, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
     "pifa_probe_mfma_random": (_st, [_i64, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double), _vp]),
     "pifa_probe_hbm_read": (_st, [_vp, _i64, ctypes.c_int, ctypes.POINTER(ctypes.c_double), _vp]),
@@ -613,8 +635,9 @@ class _Torch:
 
     def __init__(self):
         import torch
-        self.empty, self.empty_like = torch.empty, torch.empty_like
+        self.empty, self.empty_like, self.zeros = torch.empty, torch.empty_like, torch.zeros
         self.bf16, self.f32, self.u8, self.e4m3 = torch.bfloat16, torch.float32, torch.uint8, torch.float8_e4m3fn
+        self.i32 = torch.int32
         self.codes = {torch.bfloat16: PIFA_BF16, torch.float32: PIFA_F32}
         self.device = torch.cuda.current_device
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -842,6 +865,190 @@ def q4_layer_norm_forward(handle: int, X, gain, eps: float, R=None, H=None, Y=No
         _ptr_of(Y, "Y", bf, M * d["d_out"], dev, False, row_out), M, rt.stream(stream, dev)))
 
 
+def layer_norm_forward(X, gain, bias, eps: float, R=None, H=None, Y=None, M: int | None = None, d: int | None = None,
+                       stream=None):
+    """The layer norm of the rows of X + R (R may be None), times gain plus bias
+    (either may be None).  Returns Y (allocated when not given); H, where given,
+    takes X + R.  Rows, M and d as for rms_norm_forward."""
+    rt = _rt()
+    M, d, whole, row, like = _rows_of(X, "X", M, d)
+    if Y is None:
+        with rt.under(stream):
+            Y = rt.empty_like(X)
+    dt, dev, n = X.dtype, rt.device(), M * d
+    code = rt.code(dt)
+    _check("layer_norm_forward", lib().layer_norm_forward(
+        _ptr_of(X, "X", dt, n, dev, whole, 0, like), _ptr_of(R, "R", dt, n, dev, whole, row, like),
+        _ptr_of(gain, "gain", dt, d, dev, True), _ptr_of(bias, "bias", dt, d, dev, True), eps,
+        _ptr_of(H, "H", dt, n, dev, False, row, like), _ptr_of(Y, "Y", dt, n, dev, False, row, like), M, d, code,
+        rt.stream(stream, dev)))
+    return Y
+
+
+def layer_norm_backward_bytes(M: int, d: int) -> int:
+    return int(lib().layer_norm_backward_bytes(int(M), int(d)))
+
+
+def layer_norm_backward(H, gain, dY, eps: float, dR=None, dX=None, dgain=None, dbias=None, work=None,
+                        M: int | None = None, d: int | None = None, stream=None, need_dX: bool = True,
+                        need_dgain: bool = True, need_dbias: bool = True):
+    """Gradients of layer_norm_forward: (dX, dgain, dbias), dX plus dR where given.
+    Outputs and workspace are allocated when not given, under the call's stream;
+    need_dX / need_dgain / need_dbias False skip one (None in its place)."""
+    rt = _rt()
+    M, d, whole, row, like = _rows_of(H, "H", M, d)
+    new_dX, new_dgain, new_dbias = dX is None and need_dX, dgain is None and need_dgain, dbias is None and need_dbias
+    new_work = work is None and (new_dgain or new_dbias or dgain is not None or dbias is not None)
+    if new_dX or new_dgain or new_dbias or new_work:
+        with rt.under(stream):
+            dX = rt.empty_like(H) if new_dX else dX
+            dgain = rt.empty(d, dtype=rt.f32, device=H.device) if new_dgain else dgain
+            dbias = rt.empty(d, dtype=rt.f32, device=H.device) if new_dbias else dbias
+            work = rt.empty(layer_norm_backward_bytes(M, d), dtype=rt.u8, device=H.device) if new_work else work
+    dt, dev, n = H.dtype, rt.device(), M * d
+    code = rt.code(dt)
+    nwork = 0 if work is None else work.numel() * work.element_size()
+    _check("layer_norm_backward", lib().layer_norm_backward(
+        _ptr_of(H, "H", dt, n, dev, whole, 0, like), _ptr_of(gain, "gain", dt, d, dev, True),
+        _ptr_of(dY, "dY", dt, n, dev, whole, row, like), _ptr_of(dR, "dR", dt, n, dev, whole, row, like), eps,
+        _ptr_of(dX, "dX", dt, n, dev, False, row, like), _ptr_of(dgain, "dgain", rt.f32, d, dev),
+        _ptr_of(dbias, "dbias", rt.f32, d, dev), M, d, code,
+        None if work is None else _ptr_of(work, "work", work.dtype, 0, dev), nwork, rt.stream(stream, dev)))
+    return dX, dgain, dbias
+
+
+def adapter_plan_bytes(M: int, n: int) -> int:
+    return int(lib().adapter_plan_bytes(int(M), int(n)))
+
+
+def adapter_plan(ids, n: int, plan, stream=None) -> None:
+    """Sorts the rows of a batch by their adapters, ids (int32, one a row; outside
+    [0, n): none), into plan (uint8, adapter_plan_bytes(M, n)).  See AdapterPlan."""
+    rt = _rt()
+    dev, M, n = rt.device(), ids.numel(), int(n)
+    _check("adapter_plan", lib().adapter_plan(_ptr_of(ids, "ids", rt.i32, M, dev, True), M, n,
+                                              _ptr_of(plan, "plan", rt.u8, 0, dev), plan.numel(),
+                                              rt.stream(stream, dev)))
+
+
+def adapter_forward_bytes(M: int, d_in: int, d_out: int, r: int, n: int) -> int:
+    return int(lib().adapter_forward_bytes(int(M), int(d_in), int(d_out), int(r), int(n)))
+
+
+def adapter_backward_bytes(M: int, d_in: int, d_out: int, r: int, n: int) -> int:
+    return int(lib().adapter_backward_bytes(int(M), int(d_in), int(d_out), int(r), int(n)))
+
+
+def _adapter_dims(A, B, plan):
+    """(M, d_in, d_out, r, n) of a call with these weights and this plan."""
+    if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+        raise ValueError("A is %s, B %s: n x r x d_in and n x d_out x r are expected" % (tuple(A.shape), tuple(B.shape)))
+    if plan.n != A.shape[0]:
+        raise ValueError("the plan is for %d adapters, A holds %d" % (plan.n, A.shape[0]))
+    return plan.M, A.shape[2], B.shape[1], A.shape[1], plan.n
+
+
+def adapter_forward(X, A, B, plan, scale=None, Y0=None, Y=None, work=None, stream=None):
+    """Y0 (may be None: zeros) plus each row's adapter: scale (X A^T) B^T.  A is n x r
+    x d_in, B n x d_out x r, plan an AdapterPlan of the rows' ids.  Returns Y
+    (allocated when not given; may be Y0).  Rows are the last dimension."""
+    rt = _rt()
+    M, d_in, d_out, r, n = _adapter_dims(A, B, plan)
+    dev, bf = rt.device(), rt.bf16
+    if Y is None or work is None:
+        with rt.under(stream):
+            Y = rt.empty((*X.shape[:-1], d_out), dtype=bf, device=X.device) if Y is None else Y
+            work = rt.empty(adapter_forward_bytes(M, d_in, d_out, r, n), dtype=rt.u8, device=X.device) if work is None else work
+    _check("adapter_forward", lib().adapter_forward(
+        _ptr_of(X, "X", bf, M * d_in, dev, True, d_in), _ptr_of(A, "A", bf, n * r * d_in, dev, True),
+        _ptr_of(B, "B", bf, n * r * d_out, dev, True), _ptr_of(scale, "scale", rt.f32, n, dev, True), plan.pointer(dev),
+        _ptr_of(Y0, "Y0", bf, M * d_out, dev, True, d_out), _ptr_of(Y, "Y", bf, M * d_out, dev, False, d_out), M, d_in,
+        d_out, r, n, _ptr_of(work, "work", rt.u8, 0, dev), work.numel(), rt.stream(stream, dev)))
+    return Y
+
+
+def adapter_backward(X, A, B, plan, dY, scale=None, dX0=None, dX=None, dA=None, dB=None, work=None, stream=None,
+                     need_dX: bool = True, need_dA: bool = True, need_dB: bool = True):
+    """Gradients of adapter_forward: (dX, dA, dB), dX plus dX0 where given (dX may be
+    dX0), dA and dB in fp32.  Outputs and workspace are allocated when not given,
+    under the call's stream; need_dX / need_dA / need_dB False skip one (None in
+    its place)."""
+    rt = _rt()
+    M, d_in, d_out, r, n = _adapter_dims(A, B, plan)
+    dev, bf, f32 = rt.device(), rt.bf16, rt.f32
+    new_dX, new_dA, new_dB = dX is None and need_dX, dA is None and need_dA, dB is None and need_dB
+    if new_dX or new_dA or new_dB or work is None:
+        with rt.under(stream):
+            dX = rt.empty_like(X) if new_dX else dX
+            dA = rt.empty(A.shape, dtype=f32, device=A.device) if new_dA else dA
+            dB = rt.empty(B.shape, dtype=f32, device=B.device) if new_dB else dB
+            work = rt.empty(adapter_backward_bytes(M, d_in, d_out, r, n), dtype=rt.u8, device=X.device) if work is None else work
+    _check("adapter_backward", lib().adapter_backward(
+        _ptr_of(X, "X", bf, M * d_in, dev, True, d_in), _ptr_of(A, "A", bf, n * r * d_in, dev, True),
+        _ptr_of(B, "B", bf, n * r * d_out, dev, True), _ptr_of(scale, "scale", f32, n, dev, True), plan.pointer(dev),
+        _ptr_of(dY, "dY", bf, M * d_out, dev, True, d_out), _ptr_of(dX0, "dX0", bf, M * d_in, dev, True, d_in),
+        _ptr_of(dX, "dX", bf, M * d_in, dev, False, d_in), _ptr_of(dA, "dA", f32, n * r * d_in, dev, True),
+        _ptr_of(dB, "dB", f32, n * r * d_out, dev, True), M, d_in, d_out, r, n, _ptr_of(work, "work", rt.u8, 0, dev),
+        work.numel(), rt.stream(stream, dev)))
+    return dX, dA, dB
+
+
+def adamw_create(params, grads, states, weight_decay=0.0, copies=None, seed: int = 0) -> int:
+    """A handle for one step of many tensors: params (fp32), grads (all fp32 or all
+    bf16), states (m, v) in fp32 or (m, v, m_scale, v_scale) in 8 bits
+    (float8_e4m3fn codes, uint8 scales, one for each 32 values), copies: bf16
+    tensors (or None each) that take the parameters.  weight_decay: one for all
+    or one each.  The tensors have to live as long as the handle (see AdamW)."""
+    rt = _rt()
+    params, grads, states = list(params), list(grads), [tuple(s) for s in states]
+    count = len(params)
+    copies = [None] * count if copies is None else list(copies)
+    decay = [float(w) for w in weight_decay] if hasattr(weight_decay, "__len__") else [float(weight_decay)] * count
+    if not count == len(grads) == len(states) == len(copies) == len(decay):
+        raise ValueError("%d params, %d grads, %d states, %d copies, %d decays" % (count, len(grads), len(states),
+                                                                                   len(copies), len(decay)))
+    bits = 8 if states and len(states[0]) == 4 else 32
+    g_type = grads[0].dtype if grads else rt.f32
+    code, dev = rt.code(g_type), rt.device()
+    table = (adamw_tensor * max(count, 1))()
+    for t, p, g, s, c, w in zip(table, params, grads, states, copies, decay):
+        if len(s) != (4 if bits == 8 else 2):
+            raise ValueError("states are (m, v) of every tensor, or (m, v, m_scale, v_scale)")
+        n, groups = p.numel(), -(-p.numel() // 32)
+        kind = rt.e4m3 if bits == 8 else rt.f32
+        t.p, t.g = _ptr_of(p, "params", rt.f32, n, dev, True), _ptr_of(g, "grads", g_type, n, dev, True)
+        t.m, t.v = _ptr_of(s[0], "m", kind, n, dev, True), _ptr_of(s[1], "v", kind, n, dev, True)
+        if bits == 8:
+            t.m_scale = _ptr_of(s[2], "m_scale", rt.u8, groups, dev, True)
+            t.v_scale = _ptr_of(s[3], "v_scale", rt.u8, groups, dev, True)
+        t.p_bf16, t.n, t.weight_decay = _ptr_of(c, "copies", rt.bf16, n, dev, True), n, w
+    out = _vp()
+    _check("adamw_create", lib().adamw_create(table, count, bits, code, int(seed) & 0xFFFFFFFF, ctypes.byref(out)))
+    return out.value
+
+
+def adamw_destroy(handle: int) -> None:
+    _check("adamw_destroy", lib().adamw_destroy(handle))
+
+
+def adamw_step(handle: int, lr: float, beta1: float, beta2: float, eps: float, step: int = 0, grad_scale=None,
+               stream=None) -> None:
+    """One step.  step: its number, from 1 on; 0: the handle counts on the device.
+    grad_scale: a device fp32 value that multiplies the gradients."""
+    rt = _rt()
+    dev = rt.device()
+    _check("adamw_step", lib().adamw_step(handle, lr, beta1, beta2, eps, int(step),
+                                          _ptr_of(grad_scale, "grad_scale", rt.f32, 1, dev, True),
+                                          rt.stream(stream, dev)))
+
+
+def adamw_count(handle: int) -> int:
+    """Number of the handle's last step."""
+    out = _i64()
+    _check("adamw_count", lib().adamw_count(handle, ctypes.byref(out)))
+    return int(out.value)
+
+
 def pifa_probe_mfma(iters: int = 20000, stream=None):
     """(dense bf16 MFMA TFLOP/s, shader clock in MHz) of an MFMA-only kernel."""
     tf, mhz = ctypes.c_double(), ctypes.c_double()
@@ -876,7 +1083,7 @@ def pifa_profile_reset() -> None:
     _check("pifa_profile_reset", lib().pifa_profile_reset())
 
 
-def pifa_profile_read(max_sites: int = 32) -> dict:
+def pifa_profile_read(max_sites: int = 64) -> dict:
     """{site name: (launches, total milliseconds)} since the last reset."""
     names = (ctypes.c_char_p * max_sites)()
     launches = (_i64 * max_sites)()
@@ -977,6 +1184,75 @@ class Q4Layer:
     def close(self):
         if self.handle:
             q4_layer_destroy(self.handle)
+            self.handle = 0
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AdapterPlan:
+    """The rows of a batch, sorted by adapter: ``AdapterPlan(ids, n)`` for the layers of
+    one batch, ``update(ids)`` for the next one of as many rows (in the same
+    memory, so that a captured graph may hold it)."""
+
+    def __init__(self, ids, n: int, stream=None):
+        rt = _rt()
+        self.M, self.n = ids.numel(), int(n)
+        with rt.under(stream):
+            self.buffer = rt.empty(adapter_plan_bytes(self.M, self.n), dtype=rt.u8, device=ids.device)
+        self.update(ids, stream)
+
+    def update(self, ids, stream=None):
+        if ids.numel() != self.M:
+            raise ValueError("the plan is for %d rows, ids holds %d" % (self.M, ids.numel()))
+        adapter_plan(ids, self.n, self.buffer, stream)
+
+    def pointer(self, dev: int) -> int:
+        return _ptr_of(self.buffer, "plan", self.buffer.dtype, 0, dev)
+
+
+class AdamW:
+    """Owns an AdamW handle and the tensors it points to.  Without states they are
+    zeros, in 8 bits with bits=8; ``states`` holds them, (m, v) or (m, v, m_scale,
+    v_scale) a tensor."""
+
+    def __init__(self, params, grads, weight_decay=0.0, bits: int = 32, copies=None, states=None, seed: int = 0):
+        rt = _rt()
+        self.handle = 0
+        self.params, self.grads = list(params), list(grads)
+        self.copies = None if copies is None else list(copies)
+        if states is None:
+            if bits not in (8, 32):
+                raise ValueError("bits is %r: 8 or 32" % (bits,))
+            zeros = lambda p, dtype, n: rt.zeros(n, dtype=dtype, device=p.device)
+            if bits == 32:
+                states = [(rt.zeros(p.shape, dtype=rt.f32, device=p.device), rt.zeros(p.shape, dtype=rt.f32, device=p.device))
+                          for p in self.params]
+            else:
+                states = [tuple(rt.zeros(p.shape, dtype=rt.u8, device=p.device).view(rt.e4m3) for _ in range(2)) +
+                          tuple(zeros(p, rt.u8, -(-p.numel() // 32)) for _ in range(2)) for p in self.params]
+        self.states = [tuple(s) for s in states]
+        self.handle = adamw_create(self.params, self.grads, self.states, weight_decay, self.copies, seed)
+
+    def step(self, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 0,
+             grad_scale=None, stream=None):
+        adamw_step(self.handle, lr, beta1, beta2, eps, step, grad_scale, stream)
+
+    def count(self) -> int:
+        return adamw_count(self.handle)
+
+    def close(self):
+        if self.handle:
+            adamw_destroy(self.handle)
             self.handle = 0
 
     def __enter__(self):

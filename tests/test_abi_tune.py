@@ -1,0 +1,326 @@
+"""Argument errors of the layer norms, adapters and AdamW steps, found before any
+device work."""
+import ctypes
+
+import pytest
+
+from paper_2501_19090_amd import pifa
+
+INVAL, UNSUP, OK = pifa.PIFA_ERR_INVALID_ARG, pifa.PIFA_ERR_UNSUPPORTED, pifa.PIFA_OK
+BF16, F32 = pifa.PIFA_BF16, pifa.PIFA_F32
+FAR = 1 << 32  # between buffers that share nothing
+
+
+def _at(i, off=0):
+    return ctypes.c_void_p(FAR * (i + 1) + off)
+
+
+def _caller(name, ok):
+    f = getattr(pifa.lib(), name)
+    return lambda **kw: f(*{**ok, **kw}.values())
+
+
+# ------------------------------------------------------------------ layer norm
+NORM = dict(X=_at(0), R=None, gain=None, bias=None, eps=1e-5, H=None, Y=_at(1), M=4, d=8, dtype=BF16, stream=None)
+NORM_BACK = dict(H=_at(0), gain=None, dY=_at(1), dR=None, eps=1e-5, dX=_at(2), dgain=_at(3), dbias=_at(4), M=4, d=8,
+                 dtype=BF16, work=None, work_bytes=0, stream=None)
+
+
+def test_layer_norm_rejects_bad_args():
+    call = _caller("layer_norm_forward", NORM)
+    for kw in (dict(X=None), dict(Y=None), dict(M=-1), dict(d=0), dict(dtype=5), dict(H=_at(1)), dict(eps=0.0),
+               dict(eps=-1e-5), dict(eps=float("inf")), dict(eps=float("nan"))):
+        assert call(**kw) == INVAL, kw
+    assert call(d=(1 << 27) + 1) == UNSUP and call(M=1 << 31) == UNSUP
+    assert call(M=0, X=None, Y=None) == OK
+    back = _caller("layer_norm_backward", NORM_BACK)
+    for kw in (dict(H=None), dict(dY=None), dict(M=-1), dict(d=0), dict(eps=0.0), dict(dtype=-1)):
+        assert back(**kw) == INVAL, kw
+    assert back(d=(1 << 27) + 1) == UNSUP and back(dX=None, dgain=None, dbias=None) == OK  # nothing asked
+    need = pifa.layer_norm_backward_bytes(4096, 4096)
+    big = dict(M=4096, d=4096)
+    assert need > 0 and back(**big, work=None, work_bytes=need) == INVAL
+    assert back(**big, work=_at(5), work_bytes=need - 1) == INVAL
+    assert back(**big, dgain=None, work=_at(5), work_bytes=need - 1) == INVAL  # dbias alone needs it too
+    assert back(**big, work=_at(5, 2), work_bytes=need) == UNSUP
+
+
+def test_layer_norm_workspace_holds_partial_sums():
+    size = pifa.layer_norm_backward_bytes
+    assert size(0, 8) == 0 and size(4, 0) == 0 and size(-1, 8) == 0 and size(1 << 31, 8) == 0
+    assert size(1, 4096) == 0  # one row: no partial sums
+    assert size(2, (1 << 27) + 1) == 0
+    for d in (1, 100, 4096, 8192, 40000):
+        last = 0
+        for M in (1, 2, 16, 17, 300, 4096, 1 << 20):
+            n = size(M, d)
+            assert n % (8 * d) == 0 and n <= 256 * 8 * d and n >= last
+            last = n
+
+
+@pytest.mark.parametrize("dtype,es", [(BF16, 2), (F32, 4)])
+def test_layer_norm_outputs_over_inputs_are_refused(dtype, es):
+    """An output may be an input, not lie over a part of it or over anything else,
+    by as little as a byte at either end."""
+    M, d = 5, 24
+    n, row = M * d * es, d * es
+    ok = dict(X=_at(0), R=_at(1), gain=_at(2), bias=_at(3), eps=1e-5, H=_at(4), Y=_at(5), M=M, d=d, dtype=dtype, stream=None)
+    call = _caller("layer_norm_forward", ok)
+    ends = lambda i, out, size: (_at(i, 1 - out), _at(i, size - 1))
+    for i, size in ((0, n), (1, n), (2, row), (3, row)):
+        for p in ends(i, n, size):
+            assert call(H=p) == INVAL and call(Y=p) == INVAL
+    for i in (2, 3):
+        assert call(H=_at(i)) == INVAL and call(Y=_at(i)) == INVAL
+    assert call(H=_at(5)) == INVAL and call(H=_at(0), Y=_at(0)) == INVAL and call(H=_at(5, n - 1)) == INVAL
+
+    M = 1024  # with partial sums
+    n, need = M * d * es, pifa.layer_norm_backward_bytes(M, d)
+    ok = dict(H=_at(0), gain=_at(1), dY=_at(2), dR=_at(3), eps=1e-5, dX=_at(4), dgain=_at(5), dbias=_at(6), M=M, d=d,
+              dtype=dtype, work=_at(7), work_bytes=need, stream=None)
+    back = _caller("layer_norm_backward", ok)
+    assert need > 0
+    sizes = dict(dX=n, dgain=4 * d, dbias=4 * d, work=need)
+    for i, size in ((0, n), (1, row), (2, n), (3, n)):
+        for name, out in sizes.items():
+            for p in ends(i, out, size):
+                assert back(**{name: p}) == INVAL, (name, i)
+    for a, b in (("dX", 5), ("dX", 6), ("dX", 7), ("dgain", 6), ("dgain", 7), ("dbias", 7), ("dX", 1), ("dgain", 2)):
+        assert back(**{a: _at(b)}) == INVAL, (a, b)
+
+
+# ------------------------------------------------------------------ adapters
+DIMS = dict(M=70, d_in=48, d_out=40, r=6, n=3)
+SIZE = dict(X=2 * 70 * 48, A=2 * 3 * 6 * 48, B=2 * 3 * 40 * 6, scale=12, Y0=2 * 70 * 40, Y=2 * 70 * 40, dY=2 * 70 * 40,
+            dX0=2 * 70 * 48, dX=2 * 70 * 48, dA=4 * 3 * 6 * 48, dB=4 * 3 * 40 * 6)
+
+
+def _adapter(kind):
+    names = ["X", "A", "B", "scale", "plan"] + (["Y0", "Y"] if kind == "forward" else ["dY", "dX0", "dX", "dA", "dB"])
+    need = getattr(pifa, "adapter_%s_bytes" % kind)(*DIMS.values())
+    assert need > 0
+    ok = {k: _at(i) for i, k in enumerate(names)}
+    ok.update(DIMS, work=_at(20), work_bytes=need, stream=None)
+    sizes = {**{k: SIZE.get(k) for k in names}, "plan": pifa.adapter_plan_bytes(70, 3), "work": need}
+    return ok, sizes, _caller("adapter_" + kind, ok)
+
+
+def test_adapter_plan_rejects_bad_args():
+    need = pifa.adapter_plan_bytes(70, 3)
+    assert need > 4 * 70 and pifa.adapter_plan_bytes(0, 3) > 0
+    for M, n in ((-1, 3), (70, 0), ((1 << 20) + 1, 3), (70, 4097)):
+        assert pifa.adapter_plan_bytes(M, n) == 0
+    call = _caller("adapter_plan", dict(ids=_at(0), M=70, n=3, plan=_at(1), plan_bytes=need, stream=None))
+    for kw in (dict(ids=None), dict(plan=None), dict(M=-1), dict(n=0), dict(plan_bytes=need - 1), dict(plan=_at(0)),
+               dict(plan=_at(0, 279)), dict(ids=_at(1, need - 1))):
+        assert call(**kw) == INVAL, kw
+    for kw in (dict(M=(1 << 20) + 1), dict(n=4097), dict(plan=_at(1, 8)), dict(ids=_at(0, 2))):
+        assert call(**{**kw, "plan_bytes": 1 << 40}) == UNSUP, kw
+
+
+@pytest.mark.parametrize("kind", ["forward", "backward"])
+def test_adapters_reject_bad_args(kind):
+    ok, sizes, call = _adapter(kind)
+    for kw in (dict(X=None), dict(A=None), dict(B=None), dict(plan=None), dict(work=None), dict(M=-1), dict(d_in=0),
+               dict(d_out=0), dict(r=0), dict(n=0), dict(work_bytes=ok["work_bytes"] - 1),
+               dict(Y=None) if kind == "forward" else dict(dY=None)):
+        assert call(**kw) == INVAL, kw
+    for kw in (dict(M=(1 << 20) + 1), dict(n=4097), dict(r=1025), dict(d_in=(1 << 19) + 1), dict(d_out=(1 << 19) + 1)):
+        assert call(**kw) == UNSUP, kw
+        assert getattr(pifa, "adapter_%s_bytes" % kind)(*{**DIMS, **kw}.values()) == 0
+    assert call(X=_at(0, 1)) == UNSUP and call(scale=_at(3, 2)) == UNSUP and call(work=_at(20, 8)) == UNSUP
+    if kind == "forward":
+        assert call(M=0, X=None, Y=None, work=None) == OK
+    else:
+        assert call(dX=None, dA=None, dB=None) == OK and call(M=0, dA=None, dB=None, X=None) == OK
+
+
+@pytest.mark.parametrize("kind", ["forward", "backward"])
+def test_adapter_outputs_over_anything_are_refused(kind):
+    ok, sizes, call = _adapter(kind)
+    outs = ["Y", "work"] if kind == "forward" else ["dX", "dA", "dB", "work"]
+    place = lambda name: ok[name].value // FAR - 1
+    inplace = {("Y", "Y0"), ("dX", "dX0")}
+    for out in outs:
+        for other in sizes:
+            if other == out:
+                continue
+            for p in (_at(place(other), 2 - sizes[out]), _at(place(other), sizes[other] - 2)):
+                assert call(**{out: p}) == INVAL, (out, other)
+            if (out, other) not in inplace:
+                assert call(**{out: ok[other]}) == INVAL, (out, other)
+
+
+# ------------------------------------------------------------------ AdamW
+def _tensor(i, n=100, **kw):
+    t = dict(p=_at(10 * i), g=_at(10 * i + 1), m=_at(10 * i + 2), v=_at(10 * i + 3), m_scale=_at(10 * i + 4),
+             v_scale=_at(10 * i + 5), p_bf16=_at(10 * i + 6), n=n, weight_decay=0.1)
+    t.update(kw)
+    s = pifa.adamw_tensor()
+    for k, v in t.items():
+        setattr(s, k, v.value if isinstance(v, ctypes.c_void_p) else v)
+    return s
+
+
+def _create(*tensors, bits=8, dtype=F32, out=True):
+    h = ctypes.c_void_p()
+    table = (pifa.adamw_tensor * max(1, len(tensors)))(*tensors)
+    s = pifa.lib().adamw_create(table, len(tensors), bits, dtype, 1, ctypes.byref(h) if out else None)
+    assert h.value is None
+    return s
+
+
+def test_adamw_rejects_bad_args():
+    assert _create() == INVAL and _create(_tensor(0), bits=16) == INVAL and _create(_tensor(0), dtype=3) == INVAL
+    assert _create(_tensor(0), out=False) == INVAL
+    assert pifa.lib().adamw_create(None, 1, 8, F32, 1, ctypes.byref(ctypes.c_void_p())) == INVAL
+    for kw in (dict(p=None), dict(g=None), dict(m=None), dict(v=None), dict(m_scale=None), dict(v_scale=None), dict(n=-1),
+               dict(weight_decay=-0.1), dict(weight_decay=float("nan")), dict(weight_decay=float("inf"))):
+        assert _create(_tensor(0), _tensor(1, **kw)) == INVAL, kw
+    assert _create(_tensor(0, n=1 << 36)) == UNSUP  # more chunks than a launch
+    for kw in (dict(p=_at(0, 2)), dict(g=_at(1, 2)), dict(p_bf16=_at(6, 1))):
+        assert _create(_tensor(0, **kw)) == UNSUP, kw
+    assert _create(_tensor(0, m=_at(2, 2)), bits=32) == UNSUP
+    lib, count = pifa.lib(), ctypes.c_int64()
+    assert lib.adamw_step(None, 1e-3, 0.9, 0.999, 1e-8, 1, None, None) == INVAL
+    assert lib.adamw_count(None, ctypes.byref(count)) == INVAL and lib.adamw_destroy(None) == OK
+
+
+def test_adamw_outputs_over_anything_are_refused():
+    """Two outputs, or an output and a gradient, share not a byte; a tensor named twice shares all."""
+    assert _create(_tensor(0), _tensor(0)) == INVAL
+    sizes = dict(p=400, m=100, v=100, m_scale=4, v_scale=4, p_bf16=200, g=400)
+    place = {k: 10 + i for i, k in enumerate(("p", "g", "m", "v", "m_scale", "v_scale", "p_bf16"))}
+    for a in sizes:
+        if a == "g":
+            continue
+        for b in sizes:
+            # of another tensor, by the last and the first bytes; and of the same one
+            for p in (_at(place[b], 4 - sizes[a]), _at(place[b], sizes[b] - 4), _at(place[b])):
+                assert _create(_tensor(0, **{a: p}), _tensor(1)) == INVAL, (a, b)
+                assert _create(_tensor(1), _tensor(0, **{a: p})) == INVAL, (a, b)
+            if a != b:
+                assert _create(_tensor(1, **{a: _at(place[b])})) == INVAL, (a, b)
+
+
+# ------------------------------------------------------------------ binding
+@pytest.fixture
+def binding(monkeypatch):
+    """The binding on CPU tensors (device -1), with a library that records the calls."""
+    torch = pytest.importorskip("torch")
+    calls = []
+
+    class Recorder:
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return lambda *a: 64
+            return lambda *a: calls.append((name, a)) or pifa.PIFA_OK
+
+    rt = pifa._Torch()
+    rt.device, rt.raw_stream = (lambda: -1), (lambda dev: 0)
+    monkeypatch.setattr(pifa, "_torch", rt)
+    monkeypatch.setattr(pifa, "_lib", Recorder())
+    return torch, calls
+
+
+def test_layer_norm_inputs_of_another_size_are_refused(binding):
+    torch, calls = binding
+    t = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)
+    x, g = t(6, 64), t(64)
+    for kw in (dict(R=t(7, 64)), dict(R=t(12, 32)), dict(H=t(5, 64)), dict(Y=t(3, 128)), dict(R=x.float())):
+        with pytest.raises((ValueError, TypeError)):
+            pifa.layer_norm_forward(x, g, g, 1e-5, **kw)
+    for bad in (t(128), t(63), t(2, 64)):
+        for args in ((bad, g), (g, bad), (None, bad)):
+            with pytest.raises(ValueError):
+                pifa.layer_norm_forward(x, *args, 1e-5)
+    for kw in (dict(dR=t(7, 64)), dict(dX=t(3, 128)), dict(dgain=torch.zeros(63)), dict(dbias=torch.zeros(63)),
+               dict(dbias=t(64))):
+        with pytest.raises((ValueError, TypeError)):
+            pifa.layer_norm_backward(x, g, x, 1e-5, **kw)
+    assert not calls
+    pifa.layer_norm_forward(x, g, None, 1e-5, R=t(2, 3, 64), H=t(9, 64), Y=t(400))
+    pifa.layer_norm_backward(x, None, t(384), 1e-5, dX=t(8, 64), dbias=torch.zeros(100))
+    assert [c[1][7:9] if "forward" in c[0] else c[1][8:10] for c in calls] == [(6, 64), (6, 64)]
+
+
+def test_adapter_sizes(binding):
+    torch, calls = binding
+    bf = torch.bfloat16
+    t = lambda *s: torch.zeros(*s, dtype=bf)
+    plan = pifa.AdapterPlan(torch.zeros(10, dtype=torch.int32), 3)
+    x, a, b, y = t(10, 16), t(3, 4, 16), t(3, 8, 4), t(10, 8)
+    with pytest.raises(ValueError):
+        plan.update(torch.zeros(9, dtype=torch.int32))
+    with pytest.raises(TypeError):
+        pifa.AdapterPlan(torch.zeros(10, dtype=torch.int64), 3)
+    n = len(calls)
+    for args, kw in (((t(9, 16), a, b), {}), ((t(16, 10), a, b), {}), ((x, t(4, 4, 16), b), {}), ((x, a, t(3, 4, 8)), {}),
+                     ((x, t(2, 4, 16), t(2, 8, 4)), {}), ((x, a[0], b), {}), ((x, a, b), dict(Y0=t(9, 8))),
+                     ((x, a, b), dict(Y=t(8, 10))), ((x, a, b), dict(scale=torch.zeros(2))), ((x, a, b), dict(scale=t(3))),
+                     ((x.float(), a, b), {}), ((x, a.float(), b), {}), ((x, a, b), dict(work=torch.zeros(64)))):
+        with pytest.raises((ValueError, TypeError)):
+            pifa.adapter_forward(*args, plan, **kw)
+        if "Y0" not in kw and "Y" not in kw:
+            with pytest.raises((ValueError, TypeError)):
+                pifa.adapter_backward(*args, plan, y, **kw)
+    for kw in (dict(dX0=t(9, 16)), dict(dX=t(16, 10)), dict(dA=torch.zeros(3, 4, 15)), dict(dB=t(3, 8, 4))):
+        with pytest.raises((ValueError, TypeError)):
+            pifa.adapter_backward(x, a, b, plan, y, **kw)
+    assert len(calls) == n
+    pifa.adapter_forward(t(2, 5, 16), a, b, plan, Y0=y, Y=t(12, 8))
+    dX, dA, dB = pifa.adapter_backward(x, a, b, plan, y, need_dX=False)
+    assert dX is None and dA.shape == a.shape and dB.shape == b.shape and dA.dtype == torch.float32
+    assert calls[-2][1][7:12] == (10, 16, 8, 4, 3) and calls[-1][1][10:15] == (10, 16, 8, 4, 3)
+
+
+def test_adamw_tensors(binding):
+    torch, calls = binding
+    f = lambda n: torch.zeros(n)
+    ok = dict(params=[f(40), f(7)], grads=[f(40), f(7)], states=[(f(40), f(40)), (f(7), f(7))])
+    e = lambda n: torch.zeros(n, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    u = lambda n: torch.zeros(n, dtype=torch.uint8)
+    eight = [(e(40), e(40), u(2), u(2)), (e(7), e(7), u(1), u(1))]
+    for kw in (dict(grads=[f(40)]), dict(grads=[f(40), f(8)]), dict(grads=[f(40), f(7).bfloat16()]), dict(params=[f(40), f(7).half()]),
+               dict(states=[(f(40), f(40)), eight[1]]), dict(states=[eight[0], (f(7), f(7))]),
+               dict(states=[eight[0], (e(7), e(7), u(2), u(1))]), dict(weight_decay=[0.1]), dict(copies=[None]),
+               dict(copies=[None, f(7)]), dict(copies=[f(40).bfloat16(), f(9).bfloat16()])):
+        with pytest.raises((ValueError, TypeError)):
+            pifa.adamw_create(**{**ok, **kw})
+    with pytest.raises(ValueError):
+        pifa.AdamW(ok["params"], ok["grads"], bits=16)
+    assert not calls
+    pifa.adamw_create(**ok)
+    pifa.adamw_create(**{**ok, "states": eight, "copies": [f(40).bfloat16(), None]}, weight_decay=[0.1, 0.0], seed=-1)
+    table, count, bits, dtype, seed, _ = calls[-1][1]
+    assert (count, bits, dtype, seed) == (2, 8, F32, 0xFFFFFFFF) and table[0].weight_decay == 0.1 and table[1].n == 7
+    with pytest.raises(TypeError):
+        pifa.adamw_step(0x40, 1e-3, 0.9, 0.99, 1e-8, 1, grad_scale=torch.zeros(1, dtype=torch.float64))
+    with pytest.raises(ValueError):
+        pifa.adamw_step(0x40, 1e-3, 0.9, 0.99, 1e-8, 1, grad_scale=torch.zeros(2))
+    opt = pifa.AdamW(ok["params"], ok["grads"], bits=8)
+    assert [tuple(x.dtype for x in s) for s in opt.states] == [(torch.float8_e4m3fn,) * 2 + (torch.uint8,) * 2] * 2
+    opt.step(1e-3, step=4)
+    assert calls[-1][0] == "adamw_step" and calls[-1][1][5] == 4
+    opt.handle = 0
+
+
+def test_streams_of_another_device_are_refused(binding):
+    torch, calls = binding
+
+    class Stream:
+        cuda_stream, device_index = 0x40, 1
+
+    x = torch.zeros(4, 16, dtype=torch.bfloat16)
+    plan = pifa.AdapterPlan(torch.zeros(4, dtype=torch.int32), 1)
+    n = len(calls)
+    a, b, w = torch.zeros(1, 2, 16, dtype=torch.bfloat16), torch.zeros(1, 16, 2, dtype=torch.bfloat16), torch.zeros(64, dtype=torch.uint8)
+    for call in (lambda st: pifa.layer_norm_forward(x, None, None, 1e-5, Y=x, stream=st),
+                 lambda st: pifa.layer_norm_backward(x, None, x, 1e-5, dX=x, need_dgain=False, need_dbias=False, stream=st),
+                 lambda st: plan.update(torch.zeros(4, dtype=torch.int32), st),
+                 lambda st: pifa.adapter_forward(x, a, b, plan, Y=x, work=w, stream=st),
+                 lambda st: pifa.adapter_backward(x, a, b, plan, x, dX=x, need_dA=False, need_dB=False, work=w, stream=st),
+                 lambda st: pifa.adamw_step(0x40, 1e-3, 0.9, 0.99, 1e-8, 1, stream=st)):
+        with pytest.raises(ValueError):
+            call(Stream())
+    assert len(calls) == n
