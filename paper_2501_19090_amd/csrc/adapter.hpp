@@ -4,60 +4,64 @@
 //   t = s_a (X A_a^T)      Y  = Y0 + t B_a^T
 //   u = s_a (dY B_a)       dX = dX0 + u A_a,   dA_a = sum over its rows of u^T X,   dB_a = sum of dY^T t
 //
-// A plan sorts the rows by adapter, once a batch; every layer's call goes by it.
-// Each product then runs over tiles of up to 64 rows of one adapter, wherever
-// they stand in X and Y, on matrix instructions of 16 x 16 x 32 bf16 values; the
-// ranks are small, so all of them are bound by the rows that they stream.
-//   shrink: rows times A^T (or B), over K, in waves that take 32 columns in turn;
-//           with few tiles K is cut over workgroups too.  t and u stay fp32.
+// A plan deals the rows to tiles of up to 64 rows of one adapter, once a batch;
+// every layer's call goes by it.  The products run on matrix instructions of 16 x
+// 16 x 32 bf16 values; the ranks are small, so that all of them are bound by the
+// rows that they stream, wherever these stand in X and Y.
+//   shrink: rows times A^T (or B), in waves that take 32 columns in turn; K is cut
+//           over workgroups too, as far as the chip is not full of tiles.
+//   finish: the parts' sums, rounded as the next products read them.
 //   expand: t times B^T (or u times A) onto the rows of Y0.
 //   grads:  sums over rows; a lane holds 8 rows of 8 columns and turns them round
 //           in its registers, so that the rows become the instruction's K.
-// t and u reach the matrix cores as two bf16 values each (16 bits) where the
-// result is bf16, as three (24 bits) where it is fp32.  All sums are fp32 and in a
-// fixed order.
+// t and u are fp32 sums; they reach the matrix cores as two bf16 values each (16
+// bits) where the result is bf16, as three (24 bits) where it is fp32.  All sums
+// are fp32 and in a fixed order.
 #pragma once
 
 #include "common.hpp"
 
 namespace pifa {
 
-constexpr int kAdTile = 64;      // rows of a tile
-constexpr int kAdPiece = 512;    // rows of an adapter that one workgroup of grads sums over
+constexpr int kAdTile = 64;        // rows of a tile
+constexpr int kAdPieceTiles = 8;   // tiles of an adapter that one workgroup of grads sums over
+constexpr int kAdPiece = kAdTile * kAdPieceTiles;
 constexpr int kAdMaxSlots = 4096;
 constexpr int64_t kAdMaxRows = 1 << 20;
-constexpr int kAdMaxSplit = 8;   // of K
+constexpr int kAdMaxSplit = 8;     // of K
 constexpr int kAdThreads = 512;
 constexpr int kAdWaves = kAdThreads / kWave;
 
 // ------------------------------------------------------------------ plan
-// A plan in memory: a header, then arrays of int32.  Tiles and pieces are found
-// by a binary search in their prefix sums; rows without an adapter are bucket n.
+// A plan in memory: a header, then arrays of int32.  Rows without an adapter are
+// bucket n, whose tiles come last.
 struct AdapterHeader {
-    int32_t M, n;      // of the call that wrote it
-    int32_t tiles;     // of rows with an adapter
-    int32_t tiles_all; // with those of rows without
-    int32_t active;    // rows with an adapter
-    int32_t pieces;    // of all adapters; one without rows has an empty one
-    int32_t multi;     // adapters of more than one piece
-    int32_t pad[9];
+    int32_t M, n;       // of the call that wrote it
+    int32_t tiles;      // of rows with an adapter
+    int32_t tiles_all;  // with those of rows without
+    int32_t pieces;     // of all adapters; one without rows has one of no tiles
+    int32_t multi;      // adapters of more than one piece
+    int32_t pad[10];
 };
 struct AdapterTile {
-    int32_t adapter, first;  // n: none
+    int32_t adapter, count;  // of its 64 rows, those that are there
+};
+struct AdapterPiece {
+    int32_t adapter, first, tiles;
+    int32_t slot;  // its partial sums, or -1 where it is its adapter's only one
 };
 struct AdapterMulti {
-    int32_t adapter, slot, pieces;  // its partial sums
+    int32_t adapter, slot, pieces;
 };
 
 struct AdapterPlan {
     AdapterHeader* head;
-    int32_t* seg;         // n + 2: first sorted row of each adapter, of the rows without, M
-    int32_t* perm;        // M: rows in the order of their adapters
-    AdapterTile* tiles;   // M / 64 + min(n, M) + 1
-    AdapterTile* pieces;  // M / 512 + n
-    int32_t* slots;       // for each piece: its partial sums, or -1 where it is its adapter's only one
-    AdapterMulti* multi;  // M / 512
-    int32_t* hist;        // for each block of 1024 rows: its rows of each bucket (n + 1)
+    AdapterTile* tiles;    // M / 64 + min(n, M) + 1
+    int32_t* rows;         // 64 of each tile, -1 behind the last one
+    int32_t* count;        // n + 1: rows of each bucket
+    AdapterPiece* pieces;  // M / 512 + n
+    AdapterMulti* multi;   // M / 512
+    int32_t* hist;         // for each block of 1024 rows: its rows of each bucket (n + 1)
 };
 
 __host__ __device__ inline int64_t adapter_max_tiles(int64_t M, int64_t n) { return M / kAdTile + (n < M ? n : M) + 1; }
@@ -73,11 +77,10 @@ __host__ __device__ inline size_t adapter_layout(void* base, int64_t M, int64_t 
         return (int32_t*)r;
     };
     p->head = (AdapterHeader*)take(16);
-    p->seg = take(n + 2);
-    p->perm = take(M);
     p->tiles = (AdapterTile*)take(2 * adapter_max_tiles(M, n));
-    p->pieces = (AdapterTile*)take(2 * adapter_max_pieces(M, n));
-    p->slots = take(adapter_max_pieces(M, n));
+    p->rows = take(kAdTile * adapter_max_tiles(M, n));
+    p->count = take(n + 1);
+    p->pieces = (AdapterPiece*)take(4 * adapter_max_pieces(M, n));
     p->multi = (AdapterMulti*)take(3 * (M / kAdPiece + 1));
     p->hist = take(adapter_blocks(M) > 1 ? adapter_blocks(M) * (n + 1) : 0);
     return (size_t)(at - (uint8_t*)base);
@@ -98,7 +101,7 @@ static __global__ __launch_bounds__(1024) void adapter_hist(const int32_t* ids, 
     for (int a = threadIdx.x; a <= n; a += 1024) p.hist[(int64_t)blockIdx.x * (n + 1) + a] = count[a];
 }
 
-// v[i] becomes the sum of those before it, v[len] the sum of all (len + 1 <= 4 * 1024 + 2 words).
+// v[i] becomes the sum of those before it, v[len] the sum of all (len <= kAdMaxSlots + 1).
 __device__ __forceinline__ void adapter_scan(int* v, int len, int* red) {
     constexpr int EACH = (kAdMaxSlots + 2 + 1023) / 1024;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -144,7 +147,7 @@ __device__ __forceinline__ int adapter_find(const int* v, int len, int x) {
 // before it, then those in the waves before, then in the lanes before.  Block 0
 // also writes the header and the lists.
 static __global__ __launch_bounds__(1024) void adapter_place(const int32_t* ids, int64_t M, int n, AdapterPlan p) {
-    __shared__ int at[kAdMaxSlots + 2], total[kAdMaxSlots + 2], list[kAdMaxSlots + 2];
+    __shared__ int at[kAdMaxSlots + 2], total[kAdMaxSlots + 2], tile0[kAdMaxSlots + 2];
     __shared__ int red[16];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, nb = gridDim.x;
     const int64_t m = (int64_t)blockIdx.x * 1024 + t;
@@ -166,13 +169,9 @@ static __global__ __launch_bounds__(1024) void adapter_place(const int32_t* ids,
         }
     }
     __syncthreads();
-    for (int a = t; a <= n; a += 1024) list[a] = total[a];
+    for (int a = t; a <= n; a += 1024) tile0[a] = (total[a] + kAdTile - 1) / kAdTile;
     __syncthreads();
-    adapter_scan(list, n + 1, red);  // first sorted row of each bucket
-    for (int a = t; a <= n; a += 1024) at[a] += list[a];
-    if (blockIdx.x == 0)
-        for (int a = t; a <= n + 1; a += 1024) p.seg[a] = list[a];
-    __syncthreads();
+    adapter_scan(tile0, n + 1, red);  // first tile of each bucket
     for (int w = 0; w < 16 && (int64_t)blockIdx.x * 1024 + 64 * w < M; ++w) {
         if (wave == w) {
             const bool live = m < M;
@@ -182,67 +181,59 @@ static __global__ __launch_bounds__(1024) void adapter_place(const int32_t* ids,
                 same &= (mine >> b) & 1 ? set : ~set;
             }
             const int rank = __popcll(same & ((1ull << lane) - 1));
-            if (live) p.perm[at[mine] + rank] = (int32_t)m;
+            if (live) p.rows[(int64_t)tile0[mine] * kAdTile + at[mine] + rank] = (int32_t)m;
             __builtin_amdgcn_wave_barrier();
             if (live && rank == 0) at[mine] += __popcll(same);
         }
         __syncthreads();
     }
     if (blockIdx.x != 0) return;
-    const int active = list[n];
-    // tiles: at[] is free now
-    for (int a = t; a <= n; a += 1024) at[a] = (total[a] + kAdTile - 1) / kAdTile;
-    __syncthreads();
-    adapter_scan(at, n + 1, red);
-    const int tiles = at[n], tiles_all = at[n + 1];
+    const int tiles = tile0[n], tiles_all = tile0[n + 1];
     for (int i = t; i < tiles_all; i += 1024) {
-        const int a = adapter_find(at, n + 1, i);
-        p.tiles[i] = AdapterTile{a, list[a] + (i - at[a]) * kAdTile};
+        const int a = adapter_find(tile0, n + 1, i);
+        p.tiles[i] = AdapterTile{a, min(kAdTile, total[a] - (i - tile0[a]) * kAdTile)};
+    }
+    for (int a = wave; a <= n; a += 16) {  // a wave each: the last tile's rows that are not there
+        const int64_t last = (int64_t)tile0[a + 1] * kAdTile, end = (int64_t)tile0[a] * kAdTile + total[a];
+        if (end + lane < last) p.rows[end + lane] = -1;
+    }
+    for (int a = t; a <= n; a += 1024) p.count[a] = total[a];
+    __syncthreads();
+    auto piece_count = [&](int a) { return max(1, (total[a] + kAdPiece - 1) / kAdPiece); };
+    for (int a = t; a < n; a += 1024) at[a] = piece_count(a);
+    __syncthreads();
+    adapter_scan(at, n, red);  // first piece of each adapter
+    // places for the partial sums of adapters of more than one piece, behind the first pieces' LDS
+    __shared__ int slot0[kAdMaxSlots + 2], multi0[kAdMaxSlots + 2];
+    for (int a = t; a < n; a += 1024) {
+        const int k = piece_count(a);
+        slot0[a] = k > 1 ? k : 0;
+        multi0[a] = k > 1 ? 1 : 0;
     }
     __syncthreads();
-    for (int a = t; a < n; a += 1024) at[a] = max(1, (total[a] + kAdPiece - 1) / kAdPiece);
-    __syncthreads();
-    adapter_scan(at, n, red);
+    adapter_scan(slot0, n, red);
+    adapter_scan(multi0, n, red);
     const int pieces = at[n];
     for (int i = t; i < pieces; i += 1024) {
-        const int a = adapter_find(at, n, i);
-        p.pieces[i] = AdapterTile{a, list[a] + (i - at[a]) * kAdPiece};
+        const int a = adapter_find(at, n, i), first = tile0[a] + (i - at[a]) * kAdPieceTiles;
+        p.pieces[i] = AdapterPiece{a, first, min(kAdPieceTiles, tile0[a + 1] - first),
+                                   at[a + 1] - at[a] > 1 ? slot0[a] + i - at[a] : -1};
     }
-    __syncthreads();
-    // adapters of more than one piece, and places for their partial sums
-    __shared__ int nmulti;
-    int* where = list;  // free now
-    for (int a = t; a < n; a += 1024) where[a] = at[a + 1] - at[a] > 1 ? at[a + 1] - at[a] : 0;
-    __syncthreads();
-    adapter_scan(where, n, red);
-    for (int i = t; i < pieces; i += 1024) {
-        const int a = adapter_find(at, n, i);
-        p.slots[i] = at[a + 1] - at[a] > 1 ? where[a] + i - at[a] : -1;
-    }
-    for (int a = t; a < n; a += 1024) total[a] = at[a + 1] - at[a] > 1 ? 1 : 0;
-    __syncthreads();
-    adapter_scan(total, n, red);
     for (int a = t; a < n; a += 1024)
-        if (total[a + 1] != total[a]) p.multi[total[a]] = AdapterMulti{a, where[a], at[a + 1] - at[a]};
-    if (t == 0) {
-        nmulti = total[n];
-        *p.head = AdapterHeader{(int32_t)M, n, tiles, tiles_all, active, pieces, nmulti, {}};
-    }
+        if (multi0[a + 1] != multi0[a]) p.multi[multi0[a]] = AdapterMulti{a, slot0[a], at[a + 1] - at[a]};
+    if (t == 0) *p.head = AdapterHeader{(int32_t)M, n, tiles, tiles_all, pieces, multi0[n], {}};
 }
 
 // ------------------------------------------------------------------ shared pieces
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-
 struct __attribute__((packed, aligned(2))) AdapterAny16 {
     u32x4 v;
 };
-struct __attribute__((packed, aligned(4))) AdapterAnyF4 {
-    f32x4 v;
-};
+
+__device__ __forceinline__ u32x4 adapter_load(const bf16* p) { return reinterpret_cast<const AdapterAny16*>(p)->v; }
 
 // Eight values from k on of a row of K, zeros behind its end.
 __device__ __forceinline__ u32x4 adapter_load8(const bf16* row, int64_t k, int64_t K) {
-    if (k + 8 <= K) return reinterpret_cast<const AdapterAny16*>(row + k)->v;
+    if (k + 8 <= K) return adapter_load(row + k);
     u32x4 v = zero16();
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -273,19 +264,22 @@ struct AdapterShrink {
     const bf16* P;       // rows (M x K)
     const bf16* W;       // n x r x K
     const float* scale;  // or null: ones
-    float* T;            // splits x active x rp
+    float* T;            // splits x 64 tiles x rp
     int64_t K;
 };
 
+// A tile's rows times 16 JB of an adapter's; slices s0 to s1 of 32 columns, a wave
+// taking every eighth.  The next slice's operands are loaded before this one's
+// are multiplied.
 template <int JB, int RG>
-__device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, const AdapterPlan& p, const AdapterTile tile,
-                                                    int rows, int64_t r, int j0, int64_t s0, int64_t s1, int64_t rp,
-                                                    float* out, float* lds) {
+__device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, const int32_t* rows, const AdapterTile tile,
+                                                    int64_t r, int j0, int64_t s0, int64_t s1, int64_t rp, float* out,
+                                                    float* lds) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const bf16* x[RG];
     const bf16* w[JB];
 #pragma unroll
-    for (int g = 0; g < RG; ++g) x[g] = j.P + (int64_t)p.perm[tile.first + min(16 * g + i, rows - 1)] * j.K;
+    for (int g = 0; g < RG; ++g) x[g] = j.P + (int64_t)rows[min(16 * g + i, tile.count - 1)] * j.K;
 #pragma unroll
     for (int b = 0; b < JB; ++b)
         w[b] = j.W + ((int64_t)tile.adapter * r + min((int64_t)(j0 + 16 * b + i), r - 1)) * j.K;
@@ -294,31 +288,45 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
     for (int g = 0; g < RG; ++g)
 #pragma unroll
         for (int b = 0; b < JB; ++b) acc[g][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int64_t whole = j.K / 32;  // slices of 32 full columns
-    int64_t s = s0 + wave;
-    for (; s < min(s1, whole); s += kAdWaves) {
+    struct Stage {
+        u32x4 x[RG], w[JB];
+    };
+    auto load = [&](int64_t s, Stage& f) {
         const int64_t k = 32 * s + 8 * q;
-        u32x4 xv[RG], wv[JB];
 #pragma unroll
-        for (int g = 0; g < RG; ++g) xv[g] = reinterpret_cast<const AdapterAny16*>(x[g] + k)->v;
+        for (int g = 0; g < RG; ++g) f.x[g] = adapter_load(x[g] + k);
 #pragma unroll
-        for (int b = 0; b < JB; ++b) wv[b] = reinterpret_cast<const AdapterAny16*>(w[b] + k)->v;
+        for (int b = 0; b < JB; ++b) f.w[b] = adapter_load(w[b] + k);
+    };
+    auto multiply = [&](const Stage& f) {
 #pragma unroll
         for (int g = 0; g < RG; ++g)
 #pragma unroll
-            for (int b = 0; b < JB; ++b) acc[g][b] = adapter_mfma(xv[g], wv[b], acc[g][b]);
+            for (int b = 0; b < JB; ++b) acc[g][b] = adapter_mfma(f.x[g], f.w[b], acc[g][b]);
+    };
+    const int64_t whole = min(s1, j.K / 32);  // slices of 32 full columns
+    const int64_t first = s0 + wave, count = first < whole ? (whole - first + kAdWaves - 1) / kAdWaves : 0;
+    if (count > 0) {
+        const int64_t last = first + (count - 1) * kAdWaves;
+        Stage even, odd;
+        load(first, even);
+        for (int64_t c = 0; c < count; c += 2) {
+            load(min(first + (c + 1) * kAdWaves, last), odd);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(even);
+            load(min(first + (c + 2) * kAdWaves, last), even);
+            __builtin_amdgcn_sched_barrier(0);
+            if (c + 1 < count) multiply(odd);
+        }
     }
-    if (s < s1) {  // the row's last columns
-        const int64_t k = 32 * s + 8 * q;
-        u32x4 xv[RG], wv[JB];
+    if (first + count * kAdWaves < s1) {  // the row's last columns
+        const int64_t k = 32 * (first + count * kAdWaves) + 8 * q;
+        Stage f;
 #pragma unroll
-        for (int g = 0; g < RG; ++g) xv[g] = adapter_load8(x[g], k, j.K);
+        for (int g = 0; g < RG; ++g) f.x[g] = adapter_load8(x[g], k, j.K);
 #pragma unroll
-        for (int b = 0; b < JB; ++b) wv[b] = adapter_load8(w[b], k, j.K);
-#pragma unroll
-        for (int g = 0; g < RG; ++g)
-#pragma unroll
-            for (int b = 0; b < JB; ++b) acc[g][b] = adapter_mfma(xv[g], wv[b], acc[g][b]);
+        for (int b = 0; b < JB; ++b) f.w[b] = adapter_load8(w[b], k, j.K);
+        multiply(f);
     }
     // the waves' sums, 16 rows at a time, in two halves of LDS in turn
     constexpr int COLS = 16 * JB;
@@ -336,17 +344,18 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
             float v = 0.f;
 #pragma unroll
             for (int u = 0; u < kAdWaves; ++u) v += part[u * 16 * COLS + at];
-            if (row < rows) out[(int64_t)(tile.first + row) * rp + col] = col < r ? v * scale : 0.f;
+            if (row < tile.count) out[(int64_t)row * rp + col] = col < r ? v * scale : 0.f;
         }
     }
 }
 
-// Workgroups: x: tiles, y: splits of K, z: blocks of 16 JB columns of t, jobs outermost.
+// Workgroups: x: tiles, y: parts of K, z: blocks of 16 JB columns of t, jobs outermost.
 template <int JB>
 __global__ __launch_bounds__(kAdThreads) void adapter_shrink(AdapterShrink j0, AdapterShrink j1, AdapterPlan p, int64_t M,
                                                              int n, int64_t r, int target) {
     __shared__ float lds[2 * kAdWaves * 16 * 16 * JB];
-    const AdapterHeader& h = *p.head;
+    const AdapterHeader h = *p.head;
+    const AdapterTile tile = p.tiles[blockIdx.x];
     if (h.M != M || h.n != n || (int)blockIdx.x >= h.tiles) return;
     const int64_t rp = adapter_rp(r);
     const int cols = (int)ceil_div(rp, 16 * JB), job = blockIdx.z / cols, c0 = (blockIdx.z % cols) * 16 * JB;
@@ -355,291 +364,410 @@ __global__ __launch_bounds__(kAdThreads) void adapter_shrink(AdapterShrink j0, A
     const int splits = adapter_splits(h.tiles, slices, target);
     if ((int)blockIdx.y >= splits) return;
     const int64_t each = ceil_div(slices, splits), s0 = each * blockIdx.y, s1 = min(s0 + each, slices);
+    const int32_t* rows = p.rows + (int64_t)blockIdx.x * kAdTile;
+    float* out = j.T + ((int64_t)blockIdx.y * h.tiles + blockIdx.x) * kAdTile * rp;
+    if (tile.count <= 16) adapter_shrink_tile<JB, 1>(j, rows, tile, r, c0, s0, s1, rp, out, lds);
+    else adapter_shrink_tile<JB, 4>(j, rows, tile, r, c0, s0, s1, rp, out, lds);
+}
+
+// ------------------------------------------------------------------ finish
+// The nearest bf16 value, and that nearest to what it leaves.
+__device__ __forceinline__ void adapter_split2(float v, bf16& hi, bf16& lo) {
+    hi = (bf16)v;
+    lo = (bf16)(v - (float)hi);
+}
+// v as three bf16 values that add up to all its bits.
+__device__ __forceinline__ void adapter_split3(float v, bf16 (&s)[3]) {
+    adapter_split2(v, s[0], s[1]);
+    s[2] = (bf16)((v - (float)s[0]) - (float)s[1]);
+}
+
+struct AdapterFinish {
+    const float* T;   // splits x 64 tiles x rp
+    bf16* halves;     // or null: 64 tiles x 2 x rp, the values and what they leave
+    uint16_t* turned; // or null: 3 x rp x 64 tiles
+    int64_t K;        // that t was summed over
+};
+
+// Four columns of a row of t, the parts' sums added, all parts' loads in flight.
+__device__ __forceinline__ f32x4 adapter_t4(const float* t, int splits, int64_t stride) {
+    f32x4 part[kAdMaxSplit], v;
+#pragma unroll
+    for (int s = 0; s < kAdMaxSplit; ++s) part[s] = *reinterpret_cast<const f32x4*>(t + (s < splits ? s : 0) * stride);
+    v = part[0];
+#pragma unroll
+    for (int s = 1; s < kAdMaxSplit; ++s)
+        if (s < splits) v += part[s];
+    return v;
+}
+
+// Workgroups: x: tiles, y: blocks of 16 columns, z: jobs.
+static __global__ __launch_bounds__(256) void adapter_finish(AdapterFinish j0, AdapterFinish j1, AdapterPlan p, int64_t M,
+                                                            int n, int64_t r, int64_t width, int target) {
+    __shared__ float lds[16][kAdTile + 4];
+    const AdapterHeader h = *p.head;
     const AdapterTile tile = p.tiles[blockIdx.x];
-    const int rows = min(kAdTile, p.seg[tile.adapter + 1] - tile.first);
-    float* out = j.T + (int64_t)blockIdx.y * h.active * rp;
-    if (rows <= 16) adapter_shrink_tile<JB, 1>(j, p, tile, rows, r, c0, s0, s1, rp, out, lds);
-    else adapter_shrink_tile<JB, 4>(j, p, tile, rows, r, c0, s0, s1, rp, out, lds);
+    if (h.M != M || h.n != n || (int)blockIdx.x >= h.tiles) return;
+    const AdapterFinish j = blockIdx.z ? j1 : j0;
+    const int64_t rp = adapter_rp(r);
+    const int row = threadIdx.x >> 2, c = (threadIdx.x & 3) * 4, c0 = blockIdx.y * 16 + c;
+    const int64_t at = (int64_t)blockIdx.x * kAdTile + row;
+    f32x4 v = adapter_t4(j.T + at * rp + c0, adapter_splits(h.tiles, ceil_div(j.K, 32), target), (int64_t)h.tiles * kAdTile * rp);
+    if (row >= tile.count) v = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (j.halves) {
+        bf16 hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) adapter_split2(v[e], hi[e], lo[e]);
+        bf16* to = j.halves + at * 2 * rp + c0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            to[e] = hi[e];
+            to[rp + e] = lo[e];
+        }
+    }
+    if (!j.turned) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lds[c + e][row] = v[e];
+    __syncthreads();
+    const int col = threadIdx.x >> 4, r0 = (threadIdx.x & 15) * 4;
+    bf16 s[4][3];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) adapter_split3(lds[col][r0 + e], s[e]);
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+        bf16* to = (bf16*)j.turned + ((int64_t)u * rp + blockIdx.y * 16 + col) * width + (int64_t)blockIdx.x * kAdTile + r0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[e] = s[e][u];
+    }
 }
 
 // ------------------------------------------------------------------ expand
 struct AdapterExpand {
-    const float* T;    // splits x active x rp
-    const bf16* W;     // n x d x r
-    const bf16* base;  // or null: zeros
-    bf16* out;         // M x d; may be base
+    const float* T;      // splits x 64 tiles x rp, or
+    const bf16* halves;  // as finish leaves them
+    const bf16* W;       // n x d x r
+    const bf16* base;    // or null: zeros
+    bf16* out;           // M x d; may be base
     int64_t d;
-    int64_t K;         // that t was summed over
+    int64_t K;           // that t was summed over
 };
-
-// Eight columns from k on of a row of t, the splits' sums added.
-__device__ __forceinline__ void adapter_t8(const float* t, int splits, int64_t stride, float (&v)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    for (int s = 0; s < splits; ++s) {
-        const f32x4 a = reinterpret_cast<const AdapterAnyF4*>(t + s * stride)->v;
-        const f32x4 b = reinterpret_cast<const AdapterAnyF4*>(t + s * stride + 4)->v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] += a[e];
-            v[4 + e] += b[e];
-        }
-    }
-}
-// The nearest bf16 values, and those nearest to what they leave.
-__device__ __forceinline__ void adapter_split8(const float (&v)[8], u32x4& hi, u32x4& lo) {
-    bf16x8 h, l;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        h[e] = (bf16)v[e];
-        l[e] = (bf16)(v[e] - (float)h[e]);
-    }
-    hi = __builtin_bit_cast(u32x4, h);
-    lo = __builtin_bit_cast(u32x4, l);
-}
 
 // The 64 columns of W that a wave takes as operands: instruction u's row i is column
 // c0 + 32 (u / 2) + 8 (i / 4) + 4 (u % 2) + i % 4, so that two instructions leave
 // a lane with 8 columns in a row.
-__device__ __forceinline__ u32x4 adapter_w8(const bf16* W, int64_t c0, int u, int i, int64_t d, int64_t k, int64_t r) {
-    return adapter_load8(W + min(c0 + 32 * (u / 2) + 8 * (i / 4) + 4 * (u % 2) + i % 4, d - 1) * r, k, r);
+__device__ __forceinline__ const bf16* adapter_w_row(const bf16* W, int64_t c0, int u, int i, int64_t d, int64_t r) {
+    return W + min(c0 + 32 * (u / 2) + 8 * (i / 4) + 4 * (u % 2) + i % 4, d - 1) * r;
+}
+__device__ __forceinline__ u32x4 adapter_w8(const bf16* row, int64_t k, int64_t r) {
+    if (r % 8 != 0) return adapter_load8(row, k, r);
+    const u32x4 v = adapter_load(row + (k < r ? k : 0));
+    return k < r ? v : zero16();
+}
+
+// The rows of G groups of 16 from g0 on.  SUM: t is still in parts (few rows).
+// FULL: all 64 columns are there.
+template <int KB, bool SUM, bool FULL, int G>
+__device__ __forceinline__ void adapter_expand_rows(const AdapterExpand& j, const int32_t* rows, int count, int g0,
+                                                    int64_t tile, int64_t c0, const bf16* W,
+                                                    const u32x4 (&w)[KB > 0 ? KB : 1][4], int64_t r, int64_t rp, int splits,
+                                                    int64_t stride) {
+    const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+    constexpr int NB = KB > 0 ? KB : 1;
+    int64_t at[G];
+    u32x4 base[G][2];
+#pragma unroll
+    for (int g = 0; g < G; ++g) at[g] = (int64_t)rows[min(16 * (g0 + g) + i, count - 1)] * j.d;
+    if (j.base) {
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int64_t c = c0 + 32 * u + 8 * q;
+                if constexpr (FULL) base[g][u] = adapter_load(j.base + at[g] + c);
+                else base[g][u] = adapter_load8(j.base + at[g], min(c, j.d), j.d);
+            }
+    } else {
+#pragma unroll
+        for (int g = 0; g < G; ++g) base[g][0] = base[g][1] = zero16();
+    }
+    // t's operands of a group and a block of 32 columns (KB = 0: of 16, both halves in one)
+    auto halves = [&](int g, int64_t k, u32x4& hi, u32x4& lo) {
+        const int64_t row = tile * kAdTile + min(16 * (g0 + g) + i, count - 1);
+        if constexpr (SUM) {
+            const f32x4 a = adapter_t4(j.T + row * rp + k, splits, stride), b = adapter_t4(j.T + row * rp + k + 4, splits, stride);
+            bf16x8 h, l;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                bf16 x, y;
+                adapter_split2(e < 4 ? a[e % 4] : b[e % 4], x, y);
+                h[e] = x;
+                l[e] = y;
+            }
+            hi = __builtin_bit_cast(u32x4, h);
+            lo = __builtin_bit_cast(u32x4, l);
+        } else {
+            hi = *reinterpret_cast<const u32x4*>(j.halves + row * 2 * rp + k);
+            lo = *reinterpret_cast<const u32x4*>(j.halves + row * 2 * rp + rp + k);
+        }
+    };
+    auto finish = [&](int g, const f32x4(&acc)[4]) {
+        if (16 * (g0 + g) + i >= count) return;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int64_t c = c0 + 32 * u + 8 * q;
+            const bf16x8 b = __builtin_bit_cast(bf16x8, base[g][u]);
+            bf16x8 y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = (bf16)((float)b[e] + acc[2 * u + e / 4][e % 4]);
+            bf16* to = j.out + at[g] + c;
+            if (FULL || c + 8 <= j.d) {
+                reinterpret_cast<AdapterAny16*>(to)->v = __builtin_bit_cast(u32x4, y);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < j.d) to[e] = y[e];
+            }
+        }
+    };
+    if constexpr (KB >= 0) {
+        u32x4 hi[2][NB], lo[2][NB];  // the next group's are loaded before this one's rows are stored
+        auto fetch = [&](int g) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) halves(g, KB == 0 ? 8 * (q & 1) : 32 * b + 8 * q, hi[g & 1][b], lo[g & 1][b]);
+        };
+        fetch(0);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            if (g + 1 < G) fetch(g + 1);
+            f32x4 acc[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if constexpr (KB == 0) {
+                    acc[u] = adapter_mfma(w[0][u], q < 2 ? hi[g & 1][0] : lo[g & 1][0], acc[u]);
+                } else {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        acc[u] = adapter_mfma(w[b][u], hi[g & 1][b], acc[u]);
+                        acc[u] = adapter_mfma(w[b][u], lo[g & 1][b], acc[u]);
+                    }
+                }
+            }
+            finish(g, acc);
+        }
+    } else {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            f32x4 acc[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int64_t k = 8 * q; k < rp; k += 32) {
+                u32x4 hi, lo;
+                halves(g, k, hi, lo);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const u32x4 wk = adapter_w8(adapter_w_row(W, c0, u, i, j.d, r), k, r);
+                    acc[u] = adapter_mfma(wk, hi, acc[u]);
+                    acc[u] = adapter_mfma(wk, lo, acc[u]);
+                }
+            }
+            finish(g, acc);
+        }
+    }
+}
+
+// A wave's 64 columns of a tile.
+template <int KB, bool SUM, bool FULL>
+__device__ __forceinline__ void adapter_expand_tile(const AdapterExpand& j, const AdapterPlan& p, const AdapterHeader& h,
+                                                    const AdapterTile tile, int64_t c0, int64_t r, int target) {
+    const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+    const int64_t rp = adapter_rp(r);
+    const int32_t* rows = p.rows + (int64_t)blockIdx.y * kAdTile;
+    const bf16* W = j.W + (int64_t)tile.adapter * j.d * r;
+    constexpr int NB = KB > 0 ? KB : 1;
+    u32x4 w[NB][4];
+    if constexpr (KB >= 0) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                w[b][u] = adapter_w8(adapter_w_row(W, c0, u, i, j.d, r), KB == 0 ? 8 * (q & 1) : 32 * b + 8 * q, r);
+    }
+    const int splits = SUM ? adapter_splits(h.tiles, ceil_div(j.K, 32), target) : 1;
+    const int64_t stride = (int64_t)h.tiles * kAdTile * rp;
+    const int groups = (tile.count + 15) / 16;
+    if constexpr (!SUM) {
+        if (groups == 4) {
+            adapter_expand_rows<KB, SUM, FULL, 4>(j, rows, tile.count, 0, blockIdx.y, c0, W, w, r, rp, splits, stride);
+            return;
+        }
+    }
+    for (int g = 0; g < groups; ++g)
+        adapter_expand_rows<KB, SUM, FULL, 1>(j, rows, tile.count, g, blockIdx.y, c0, W, w, r, rp, splits, stride);
 }
 
 // Workgroups: x: 64 columns a wave, y: tiles (those of rows without an adapter
 // last, which are copied).  KB: blocks of 32 columns of t, whose operands of W
 // stay in registers over the tile's rows; 0: up to 16 columns, both halves of t
 // in one instruction; -1: any number, read again for every 16 rows.
-template <int KB>
+template <int KB, bool SUM>
 __global__ __launch_bounds__(256) void adapter_expand(AdapterExpand j, AdapterPlan p, int64_t M, int n, int64_t r,
                                                       int target) {
-    const AdapterHeader& h = *p.head;
-    if (h.M != M || h.n != n || (int)blockIdx.y >= h.tiles_all) return;
+    const AdapterHeader h = *p.head;
     const AdapterTile tile = p.tiles[blockIdx.y];
-    const bool none = tile.adapter >= n;
-    if (none && j.out == j.base) return;
-    const int rows = min(kAdTile, p.seg[tile.adapter + 1] - tile.first);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
-    const int64_t c0 = ((int64_t)blockIdx.x * 4 + wave) * 64;
+    if (h.M != M || h.n != n || (int)blockIdx.y >= h.tiles_all) return;
+    const int64_t c0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64;
     if (c0 >= j.d) return;
-    const int groups = (rows + 15) / 16;
-    const int64_t rp = adapter_rp(r), stride = (int64_t)h.active * rp;
-    const int splits = none ? 0 : adapter_splits(h.tiles, ceil_div(j.K, 32), target);
-    const bf16* W = j.W + (int64_t)(none ? 0 : tile.adapter) * j.d * r;
-    constexpr int KW = KB > 0 ? KB : 1;
-    u32x4 w[KW][4];
-    if (KB >= 0 && !none) {
-#pragma unroll
-        for (int b = 0; b < KW; ++b)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) w[b][u] = adapter_w8(W, c0, u, i, j.d, KB == 0 ? 8 * (q & 1) : 32 * b + 8 * q, r);
+    if (tile.adapter >= n) {
+        if (j.out == j.base) return;
+        const int64_t c = c0 + (threadIdx.x & 63);
+        if (c >= j.d) return;
+        for (int m = 0; m < tile.count; ++m) {
+            const int64_t at = (int64_t)p.rows[(int64_t)blockIdx.y * kAdTile + m] * j.d + c;
+            ((uint16_t*)j.out)[at] = j.base ? ((const uint16_t*)j.base)[at] : (uint16_t)0;
+        }
+        return;
     }
-    for (int g = 0; g < groups; ++g) {
-        const int pos = tile.first + min(16 * g + i, rows - 1);
-        const int64_t row = (int64_t)p.perm[pos] * j.d;
-        u32x4 base[2] = {zero16(), zero16()};
-        if (j.base) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) base[u] = adapter_load8(j.base + row, min(c0 + 32 * u + 8 * q, j.d), j.d);
-        }
-        f32x4 acc[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (!none) {
-            const float* t = j.T + (int64_t)pos * rp;
-            float v[8];
-            u32x4 hi, lo;
-            if constexpr (KB == 0) {
-                adapter_t8(t + 8 * (q & 1), splits, stride, v);
-                adapter_split8(v, hi, lo);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) acc[u] = adapter_mfma(w[0][u], q < 2 ? hi : lo, acc[u]);
-            } else {
-                auto block = [&](int64_t k, const u32x4(&wk)[4]) {
-                    adapter_t8(t + k, splits, stride, v);
-                    adapter_split8(v, hi, lo);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        acc[u] = adapter_mfma(wk[u], hi, acc[u]);
-                        acc[u] = adapter_mfma(wk[u], lo, acc[u]);
-                    }
-                };
-                if constexpr (KB > 0) {
-#pragma unroll
-                    for (int b = 0; b < KB; ++b) block(32 * b + 8 * q, w[b]);
-                } else {
-                    for (int64_t k = 8 * q; k < rp; k += 32) {
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) w[0][u] = adapter_w8(W, c0, u, i, j.d, k, r);
-                        block(k, w[0]);
-                    }
-                }
-            }
-        }
-        if (16 * g + i < rows) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int64_t c = c0 + 32 * u + 8 * q;
-                bf16x8 y, b = __builtin_bit_cast(bf16x8, base[u]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = none ? b[e] : (bf16)((float)b[e] + acc[2 * u + e / 4][e % 4]);
-                if (c + 8 <= j.d) {
-                    reinterpret_cast<AdapterAny16*>(j.out + row + c)->v = __builtin_bit_cast(u32x4, y);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (c + e < j.d) j.out[row + c + e] = y[e];
-                }
-            }
-        }
-    }
+    if (c0 + 64 <= j.d) adapter_expand_tile<KB, SUM, true>(j, p, h, tile, c0, r, target);
+    else adapter_expand_tile<KB, SUM, false>(j, p, h, tile, c0, r, target);
 }
 
 // ------------------------------------------------------------------ backward
-// W (n x rows x cols) to its transpose (n x cols x rows), of adapters that have rows.
+// Two rows' values in a register each: the lower or the upper ones of both.
+__device__ __forceinline__ uint32_t adapter_pair(uint32_t even, uint32_t odd, int half) {
+    return __builtin_amdgcn_perm(odd, even, half ? 0x07060302u : 0x05040100u);
+}
+
+// W (n x rows x cols) to its transpose (n x cols x rows), of adapters that have
+// rows: a thread takes 8 x 8 values.
 static __global__ __launch_bounds__(256) void adapter_transpose(const bf16* A, bf16* At, int64_t ar, int64_t ac,
                                                                const bf16* B, bf16* Bt, int64_t br, int64_t bc,
                                                                AdapterPlan p, int64_t M, int n) {
-    __shared__ uint16_t tile[64][66];
-    if (p.head->M != M || p.head->n != n) return;
+    const AdapterHeader h = *p.head;
     const int a = blockIdx.y;
-    if (p.seg[a] == p.seg[a + 1]) return;
-    const int64_t ta = ceil_div(ar, 64) * ceil_div(ac, 64);
-    const bool second = (int64_t)blockIdx.x >= ta;
-    const int64_t t = second ? blockIdx.x - ta : blockIdx.x, rows = second ? br : ar, cols = second ? bc : ac;
-    const uint16_t* from = (const uint16_t*)(second ? B : A) + a * rows * cols;
-    uint16_t* to = (uint16_t*)(second ? Bt : At) + a * rows * cols;
-    const int64_t r0 = t / ceil_div(cols, 64) * 64, c0 = t % ceil_div(cols, 64) * 64;
-    for (int k = threadIdx.x; k < 64 * 64; k += 256) {
-        const int64_t row = r0 + k / 64, col = c0 + k % 64;
-        if (row < rows && col < cols) tile[k / 64][k % 64] = from[row * cols + col];
-    }
-    __syncthreads();
-    for (int k = threadIdx.x; k < 64 * 64; k += 256) {
-        const int64_t col = c0 + k / 64, row = r0 + k % 64;
-        if (row < rows && col < cols) to[col * rows + row] = tile[k % 64][k / 64];
+    if (h.M != M || h.n != n || p.count[a] == 0) return;
+    const int64_t ta = ceil_div(ar, 8) * ceil_div(ac, 8), tb = Bt ? ceil_div(br, 8) * ceil_div(bc, 8) : 0;
+    int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool second = t >= ta;
+    if (second) t -= ta;
+    if (second && t >= tb) return;
+    const int64_t rows = second ? br : ar, cols = second ? bc : ac;
+    const bf16* from = (second ? B : A) + a * rows * cols;
+    bf16* to = (second ? Bt : At) + a * rows * cols;
+    // neighbouring threads read neighbouring columns where rows are long, rows where they are short
+    const int64_t cw = ceil_div(cols, 8), r0 = t / cw * 8, c0 = t % cw * 8;
+    if (r0 + 8 <= rows && c0 + 8 <= cols) {
+        u32x4 x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = adapter_load(from + (r0 + e) * cols + c0);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            u32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = adapter_pair(x[2 * e][c / 2], x[2 * e + 1][c / 2], c & 1);
+            reinterpret_cast<AdapterAny16*>(to + (c0 + c) * rows + r0)->v = y;
+        }
+    } else {
+        for (int64_t c = c0; c < min(c0 + 8, cols); ++c)
+            for (int64_t k = r0; k < min(r0 + 8, rows); ++k) to[c * rows + k] = from[k * cols + c];
     }
 }
 
 struct AdapterGrads {
-    const bf16* P;    // rows (M x d)
-    const float* T;   // splits x active x rp
-    float* out;       // n x r x d (by_column: n x d x r)
-    float* part;      // the same of one adapter for each slot
+    const bf16* P;           // rows (M x d)
+    const uint16_t* turned;  // 3 x rp x 64 tiles
+    float* out;              // n x r x d (by_column: n x d x r)
+    float* part;             // the same of one adapter for each slot
     int64_t d;
-    int64_t K;        // that t was summed over
     bool by_column;
 };
-
-// v as three bf16 values that add up to all its bits.
-__device__ __forceinline__ void adapter_split3(float v, bf16 (&s)[3]) {
-    s[0] = (bf16)v;
-    v -= (float)s[0];
-    s[1] = (bf16)v;
-    s[2] = (bf16)(v - (float)s[1]);
-}
 
 constexpr int kAdCols = 128;  // columns of P that a workgroup of grads takes
 
 // Workgroups: x: columns of both jobs, y: pieces, z: blocks of 16 JB columns of t.
-// Each wave takes 32 rows at a time: 8 loads of 8 columns a lane, 8 rows apart
-// from lane group to lane group, turned round to 8 operands of 8 rows each.
+// Each wave takes 32 rows at a time, every eighth such step: 8 loads of 8 columns
+// a lane, 8 rows apart from lane group to lane group, turned round to 8 operands
+// of 8 rows each.
 template <int JB>
 __global__ __launch_bounds__(kAdThreads) void adapter_grads(AdapterGrads j0, AdapterGrads j1, int blocks0, AdapterPlan p,
-                                                            int64_t M, int n, int64_t r, int target) {
+                                                            int64_t M, int n, int64_t r, int64_t width) {
     constexpr int COLS = 16 * JB;
-    constexpr int kPitch = 32 + 8;  // rows of a column of t in LDS, padded
-    union alignas(16) Shared {
-        uint16_t t[kAdWaves][3][COLS][kPitch];
-        struct {
-            float part[2][kAdWaves][16 * COLS];
-            float out[COLS][kAdCols + 1];
-        } sum;
-    };
-    __shared__ Shared lds;
-    const AdapterHeader& h = *p.head;
+    __shared__ float part[2][kAdWaves][16 * COLS];
+    __shared__ float sums[COLS][kAdCols + 1];
+    const AdapterHeader h = *p.head;
+    const AdapterPiece piece = p.pieces[blockIdx.y];
     if (h.M != M || h.n != n || (int)blockIdx.y >= h.pieces) return;
     const bool second = (int)blockIdx.x >= blocks0;
     const AdapterGrads j = second ? j1 : j0;
     const int64_t c0 = (int64_t)(second ? blockIdx.x - blocks0 : blockIdx.x) * kAdCols;
     const int b0 = blockIdx.z * COLS;
-    const AdapterTile piece = p.pieces[blockIdx.y];
-    const int slot = p.slots[blockIdx.y];
-    const int rows = min(kAdPiece, p.seg[piece.adapter + 1] - piece.first);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
-    const int64_t rp = adapter_rp(r), stride = (int64_t)h.active * rp;
-    const int splits = adapter_splits(h.tiles, ceil_div(j.K, 32), target);
+    const int64_t rp = adapter_rp(r), c = c0 + 8 * i;
+    const bool full = c0 + kAdCols <= j.d;
 
     f32x4 acc[8][JB];
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
+    for (int u = 0; u < 8; ++u)
 #pragma unroll
-        for (int b = 0; b < JB; ++b) acc[c][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int m0 = 32 * wave; m0 < rows; m0 += 32 * kAdWaves) {
-        u32x4 x[8];
+        for (int b = 0; b < JB; ++b) acc[u][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int64_t first = (int64_t)piece.first * kAdTile;
+    for (int s = wave; s < 2 * piece.tiles; s += kAdWaves) {
+        const int64_t at = first + 32 * s + 8 * q;
+        int32_t row[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int m = m0 + 8 * q + e;
-            x[e] = zero16();
-            if (m < rows) x[e] = adapter_load8(j.P + (int64_t)p.perm[piece.first + m] * j.d, min(c0 + 8 * i, j.d), j.d);
-        }
-        // t of these rows, as three bf16 values, with the rows of a column in a row
-        for (int k = lane; k < 32 * COLS / 4; k += kWave) {
-            const int m = k / (COLS / 4), col = k % (COLS / 4) * 4;
-            f32x4 v = {0.f, 0.f, 0.f, 0.f};
-            if (m0 + m < rows) {
-                const float* from = j.T + (int64_t)(piece.first + m0 + m) * rp + b0 + col;
-                for (int s = 0; s < splits; ++s) v += reinterpret_cast<const AdapterAnyF4*>(from + s * stride)->v;
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                bf16 s[3];
-                adapter_split3(v[e], s);
-#pragma unroll
-                for (int u = 0; u < 3; ++u) lds.t[wave][u][col + e][m] = __builtin_bit_cast(uint16_t, s[u]);
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        u32x4 turned[8];
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)  // rows 2e, 2e + 1 of column 8 i + c
-                turned[c][e] = __builtin_amdgcn_perm(x[2 * e + 1][c / 2], x[2 * e][c / 2], c & 1 ? 0x07060302u : 0x05040100u);
+        for (int e = 0; e < 8; ++e) row[e] = p.rows[at + e];
+        u32x4 t[3][JB];
 #pragma unroll
         for (int u = 0; u < 3; ++u)
 #pragma unroll
-            for (int b = 0; b < JB; ++b) {
-                const u32x4 tv = *reinterpret_cast<const u32x4*>(&lds.t[wave][u][16 * b + i][8 * q]);
+            for (int b = 0; b < JB; ++b)
+                t[u][b] = *reinterpret_cast<const u32x4*>(j.turned + ((int64_t)u * rp + b0 + 16 * b + i) * width + at);
+        u32x4 x[8];
+        if (full) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) acc[c][b] = adapter_mfma(turned[c], tv, acc[c][b]);
+            for (int e = 0; e < 8; ++e) x[e] = adapter_load(j.P + (int64_t)max(row[e], 0) * j.d + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = row[e] >= 0 ? x[e] : zero16();
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = zero16();
+                if (row[e] >= 0) x[e] = adapter_load8(j.P + (int64_t)row[e] * j.d, min(c, j.d), j.d);
             }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
-    __syncthreads();
-    // the waves' sums: acc[c][b], row 4 q + e is column 8 (4 q + e) + c of P, column i is column 16 b + i of t
+        }
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
+        for (int k = 0; k < 8; ++k) {
+            u32x4 turned;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) turned[e] = adapter_pair(x[2 * e][k / 2], x[2 * e + 1][k / 2], k & 1);
+#pragma unroll
+            for (int u = 0; u < 3; ++u)
+#pragma unroll
+                for (int b = 0; b < JB; ++b) acc[k][b] = adapter_mfma(turned, t[u][b], acc[k][b]);
+        }
+    }
+    // the waves' sums: acc[k][b], row 4 q + e is column 8 (4 q + e) + k of P, column i is column 16 b + i of t
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
 #pragma unroll
         for (int b = 0; b < JB; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) lds.sum.part[c & 1][wave][(4 * q + e) * COLS + 16 * b + i] = acc[c][b][e];
+            for (int e = 0; e < 4; ++e) part[k & 1][wave][(4 * q + e) * COLS + 16 * b + i] = acc[k][b][e];
         __syncthreads();
         for (int at = threadIdx.x; at < 16 * COLS; at += kAdThreads) {
             float v = 0.f;
 #pragma unroll
-            for (int u = 0; u < kAdWaves; ++u) v += lds.sum.part[c & 1][u][at];
-            lds.sum.out[at % COLS][8 * (at / COLS) + c] = v;
+            for (int u = 0; u < kAdWaves; ++u) v += part[k & 1][u][at];
+            sums[at % COLS][8 * (at / COLS) + k] = v;
         }
     }
     __syncthreads();
-    float* out = slot < 0 ? j.out + piece.adapter * r * j.d : j.part + slot * r * j.d;
+    float* out = piece.slot < 0 ? j.out + piece.adapter * r * j.d : j.part + piece.slot * r * j.d;
     const int cols = (int)min((int64_t)kAdCols, j.d - c0), js = (int)min((int64_t)COLS, r - b0);
     for (int at = threadIdx.x; at < COLS * kAdCols; at += kAdThreads) {
-        const int a = j.by_column ? at % COLS : at / kAdCols, c = j.by_column ? at / COLS : at % kAdCols;
-        if (a >= js || c >= cols) continue;
-        out[j.by_column ? (c0 + c) * r + b0 + a : (b0 + a) * j.d + c0 + c] = lds.sum.out[a][c];
+        const int a = j.by_column ? at % COLS : at / kAdCols, k = j.by_column ? at / COLS : at % kAdCols;
+        if (a >= js || k >= cols) continue;
+        out[j.by_column ? (c0 + k) * r + b0 + a : (b0 + a) * j.d + c0 + k] = sums[a][k];
     }
 }
 
@@ -648,21 +776,32 @@ __global__ __launch_bounds__(kAdThreads) void adapter_grads(AdapterGrads j0, Ada
 static __global__ __launch_bounds__(256) void adapter_sum(const float* part0, float* out0, int64_t n0, int blocks0,
                                                          const float* part1, float* out1, int64_t n1, AdapterPlan p,
                                                          int64_t M, int n) {
-    if (p.head->M != M || p.head->n != n || (int)blockIdx.y >= p.head->multi) return;
+    const AdapterHeader h = *p.head;
     const AdapterMulti a = p.multi[blockIdx.y];
+    if (h.M != M || h.n != n || (int)blockIdx.y >= h.multi) return;
     const bool second = (int)blockIdx.x >= blocks0;
     const int64_t count = second ? n1 : n0;
     const float* from = (second ? part1 : part0) + a.slot * count;
     float* to = (second ? out1 : out0) + a.adapter * count;
-    const int64_t first = (int64_t)(second ? blockIdx.x - blocks0 : blockIdx.x) * 1024;
+    const int64_t first = (int64_t)(second ? blockIdx.x - blocks0 : blockIdx.x) * 1024 + threadIdx.x;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.pieces; s += 4) {
+        float x[4][4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int64_t k = first + e * 256 + threadIdx.x;
-        if (k >= count) continue;
-        float v = from[k];
-        for (int s = 1; s < a.pieces; ++s) v += from[s * count + k];
-        to[k] = v;
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t k = first + 256 * e;
+                x[u][e] = from[min(s + u, a.pieces - 1) * count + (k < count ? k : 0)];
+            }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += s + u < a.pieces ? x[u][e] : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (first + 256 * e < count) to[first + 256 * e] = v[e];
 }
 
 }  // namespace pifa

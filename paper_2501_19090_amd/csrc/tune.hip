@@ -130,11 +130,21 @@ bool aligned(std::initializer_list<const void*> p, uintptr_t to) {
     return true;
 }
 
-// Bytes of t (or u): at most 8 parts of K of M rows, and where K is cut at all,
-// fewer than 2 kAdTarget tiles' parts.
-size_t adapter_t_bytes(int64_t M, int64_t r) {
-    const int64_t rows = std::min<int64_t>(kAdMaxSplit * M, std::max<int64_t>(M, 2 * kAdTarget * kAdTile));
-    return (size_t)round_up(rows * adapter_rp(r) * 4, 256);
+// Up to as many rows t stays in parts, which expand adds up itself.
+constexpr int64_t kAdFewRows = 256;
+
+// Bytes of t (or u): at most 8 parts of K of every tile, and where K is cut at all,
+// fewer than 2 kAdTarget tiles' parts; of its forms for expand and for grads.
+size_t adapter_t_bytes(int64_t M, int64_t r, int64_t n) {
+    const int64_t tiles = adapter_max_tiles(M, n);
+    const int64_t parts = std::min<int64_t>(kAdMaxSplit * tiles, std::max<int64_t>(tiles, 2 * kAdTarget));
+    return (size_t)(parts * kAdTile * adapter_rp(r) * 4);
+}
+size_t adapter_halves_bytes(int64_t M, int64_t r, int64_t n) {
+    return (size_t)(adapter_max_tiles(M, n) * kAdTile * 2 * adapter_rp(r) * 2);
+}
+size_t adapter_turned_bytes(int64_t M, int64_t r, int64_t n) {
+    return (size_t)(adapter_max_tiles(M, n) * kAdTile * 3 * adapter_rp(r) * 2);
 }
 size_t adapter_partial_bytes(int64_t M, int64_t r, int64_t d) {
     return (size_t)round_up(2 * (M / kAdPiece) * r * d * 4, 256);
@@ -160,12 +170,23 @@ hipError_t launch_shrink(const AdapterShrink& a, const AdapterShrink* b, const A
     return hipGetLastError();
 }
 
+hipError_t launch_finish(const AdapterFinish& a, const AdapterFinish* b, const AdapterPlan& p, int64_t M, int64_t n,
+                         int64_t r, hipStream_t st) {
+    TimedLaunch timed(kSiteAdapterShrink, st);
+    const int64_t tiles = adapter_max_tiles(M, n);
+    hipLaunchKernelGGL(adapter_finish, dim3((unsigned)tiles, (unsigned)(adapter_rp(r) / 16), b ? 2 : 1), dim3(256), 0, st, a,
+                       b ? *b : a, p, M, (int)n, r, tiles * kAdTile, kAdTarget);
+    return hipGetLastError();
+}
+
+template <bool SUM>
 hipError_t launch_expand(const AdapterExpand& a, const AdapterPlan& p, int64_t M, int64_t n, int64_t r, hipStream_t st) {
     TimedLaunch timed(kSiteAdapterExpand, st);
-    const dim3 grid((unsigned)ceil_div(a.d, 256), (unsigned)adapter_max_tiles(M, n));
-    const int64_t rp = adapter_rp(r);
+    // columns keep to their XCD over the tiles, so that it reads only its part of W
+    const int64_t blocks = ceil_div(a.d, 256), rp = adapter_rp(r);
+    const dim3 grid((unsigned)(blocks > 8 ? round_up(blocks, 8) : blocks), (unsigned)adapter_max_tiles(M, n));
     auto launch = [&](auto kb) {
-        hipLaunchKernelGGL((adapter_expand<decltype(kb)::value>), grid, dim3(256), 0, st, a, p, M, (int)n, r, kAdTarget);
+        hipLaunchKernelGGL((adapter_expand<decltype(kb)::value, SUM>), grid, dim3(256), 0, st, a, p, M, (int)n, r, kAdTarget);
     };
     using std::integral_constant;
     if (rp == 16) launch(integral_constant<int, 0>{});
@@ -333,7 +354,8 @@ pifa_status adapter_plan(const int32_t* ids, int64_t M, int64_t n, void* plan, s
 }
 
 size_t adapter_forward_bytes(int64_t M, int64_t d_in, int64_t d_out, int64_t r, int64_t n) {
-    return check_adapter(M, d_in, d_out, r, n) == PIFA_OK ? adapter_t_bytes(M, r) : 0;
+    if (check_adapter(M, d_in, d_out, r, n) != PIFA_OK) return 0;
+    return adapter_t_bytes(M, r, n) + (M > kAdFewRows ? adapter_halves_bytes(M, r, n) : 0);
 }
 
 pifa_status adapter_forward(const void* X, const void* A, const void* B, const float* scale, const void* plan,
@@ -355,15 +377,21 @@ pifa_status adapter_forward(const void* X, const void* A, const void* B, const f
     const hipStream_t st = as_stream(stream);
     const AdapterPlan p = adapter_read_plan(plan, M, n);
     float* T = (float*)work;
-    if (launch_shrink({(const bf16*)X, (const bf16*)A, scale, T, d_in}, nullptr, p, M, n, r, st) != hipSuccess ||
-        launch_expand({T, (const bf16*)B, (const bf16*)Y0, (bf16*)Y, d_out, d_in}, p, M, n, r, st) != hipSuccess)
+    bf16* halves = (bf16*)((uint8_t*)work + adapter_t_bytes(M, r, n));
+    if (launch_shrink({(const bf16*)X, (const bf16*)A, scale, T, d_in}, nullptr, p, M, n, r, st) != hipSuccess)
+        return PIFA_ERR_HIP;
+    const AdapterExpand expand{T, halves, (const bf16*)B, (const bf16*)Y0, (bf16*)Y, d_out, d_in};
+    if (M <= kAdFewRows) return launch_expand<true>(expand, p, M, n, r, st) == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+    if (launch_finish({T, halves, nullptr, d_in}, nullptr, p, M, n, r, st) != hipSuccess ||
+        launch_expand<false>(expand, p, M, n, r, st) != hipSuccess)
         return PIFA_ERR_HIP;
     return PIFA_OK;
 }
 
 size_t adapter_backward_bytes(int64_t M, int64_t d_in, int64_t d_out, int64_t r, int64_t n) {
     if (check_adapter(M, d_in, d_out, r, n) != PIFA_OK) return 0;
-    return 2 * adapter_t_bytes(M, r) + (size_t)round_up(2 * n * r * d_in, 256) + (size_t)round_up(2 * n * r * d_out, 256) +
+    return 2 * adapter_t_bytes(M, r, n) + adapter_halves_bytes(M, r, n) + 2 * adapter_turned_bytes(M, r, n) +
+           (size_t)round_up(2 * n * r * d_in, 256) + (size_t)round_up(2 * n * r * d_out, 256) +
            adapter_partial_bytes(M, r, d_in) + adapter_partial_bytes(M, r, d_out);
 }
 
@@ -402,34 +430,41 @@ pifa_status adapter_backward(const void* X, const void* A, const void* B, const 
         at += bytes;
         return r;
     };
-    float* T = (float*)take(adapter_t_bytes(M, r));
-    float* U = (float*)take(adapter_t_bytes(M, r));
+    float* T = (float*)take(adapter_t_bytes(M, r, n));
+    float* U = (float*)take(adapter_t_bytes(M, r, n));
+    bf16* halves = (bf16*)take(adapter_halves_bytes(M, r, n));
+    uint16_t* turned_u = (uint16_t*)take(adapter_turned_bytes(M, r, n));
+    uint16_t* turned_t = (uint16_t*)take(adapter_turned_bytes(M, r, n));
     bf16* At = (bf16*)take((size_t)round_up(2 * n * r * d_in, 256));
     bf16* Bt = (bf16*)take((size_t)round_up(2 * n * r * d_out, 256));
     float* part_a = (float*)take(adapter_partial_bytes(M, r, d_in));
     float* part_b = (float*)take(adapter_partial_bytes(M, r, d_out));
+    const int64_t blocks_r = ceil_div(r, 8);
     {
         TimedLaunch timed(kSiteAdapterGrads, st);
-        const int64_t ta = ceil_div(r, 64) * ceil_div(d_in, 64), tb = ceil_div(r, 64) * ceil_div(d_out, 64);
-        hipLaunchKernelGGL(adapter_transpose, dim3((unsigned)(ta + tb), (unsigned)n), dim3(256), 0, st, (const bf16*)A, At,
-                           r, d_in, (const bf16*)B, Bt, d_out, r, p, M, (int)n);
+        const int64_t work_items = blocks_r * (ceil_div(d_out, 8) + (dX ? ceil_div(d_in, 8) : 0));
+        hipLaunchKernelGGL(adapter_transpose, dim3((unsigned)ceil_div(work_items, 256), (unsigned)n), dim3(256), 0, st,
+                           (const bf16*)B, Bt, d_out, r, (const bf16*)A, dX ? At : nullptr, r, d_in, p, M, (int)n);
         if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
     }
     const AdapterShrink t{(const bf16*)X, (const bf16*)A, scale, T, d_in}, u{(const bf16*)dY, Bt, scale, U, d_out};
-    if (launch_shrink(u, dB ? &t : nullptr, p, M, n, r, st) != hipSuccess) return PIFA_ERR_HIP;
-    if (dX && launch_expand({U, At, (const bf16*)dX0, (bf16*)dX, d_in, d_out}, p, M, n, r, st) != hipSuccess)
+    const AdapterFinish done_u{U, dX ? halves : nullptr, dA ? turned_u : nullptr, d_out}, done_t{T, nullptr, turned_t, d_in};
+    if (launch_shrink(u, dB ? &t : nullptr, p, M, n, r, st) != hipSuccess ||
+        launch_finish(done_u, dB ? &done_t : nullptr, p, M, n, r, st) != hipSuccess)
+        return PIFA_ERR_HIP;
+    if (dX && launch_expand<false>({U, halves, At, (const bf16*)dX0, (bf16*)dX, d_in, d_out}, p, M, n, r, st) != hipSuccess)
         return PIFA_ERR_HIP;
     if (!dA && !dB) return PIFA_OK;
-    const AdapterGrads ga{(const bf16*)X, U, dA, part_a, d_in, d_out, false};
-    const AdapterGrads gb{(const bf16*)dY, T, dB, part_b, d_out, d_in, true};
+    const AdapterGrads ga{(const bf16*)X, turned_u, dA, part_a, d_in, false};
+    const AdapterGrads gb{(const bf16*)dY, turned_t, dB, part_b, d_out, true};
     {
         TimedLaunch timed(kSiteAdapterGrads, st);
-        const int64_t rp = adapter_rp(r), jb = std::min<int64_t>(4, rp / 16);
+        const int64_t rp = adapter_rp(r), jb = std::min<int64_t>(4, rp / 16), width = adapter_max_tiles(M, n) * kAdTile;
         const int64_t b0 = dA ? ceil_div(d_in, kAdCols) : 0, b1 = dB ? ceil_div(d_out, kAdCols) : 0;
         const dim3 grid((unsigned)(b0 + b1), (unsigned)adapter_max_pieces(M, n), (unsigned)ceil_div(rp, 16 * jb));
-        if (jb == 1) hipLaunchKernelGGL((adapter_grads<1>), grid, dim3(kAdThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r, kAdTarget);
-        else if (jb == 2) hipLaunchKernelGGL((adapter_grads<2>), grid, dim3(kAdThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r, kAdTarget);
-        else hipLaunchKernelGGL((adapter_grads<4>), grid, dim3(kAdThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r, kAdTarget);
+        if (jb == 1) hipLaunchKernelGGL((adapter_grads<1>), grid, dim3(kAdThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r, width);
+        else if (jb == 2) hipLaunchKernelGGL((adapter_grads<2>), grid, dim3(kAdThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r, width);
+        else hipLaunchKernelGGL((adapter_grads<4>), grid, dim3(kAdThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r, width);
         if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
     }
     if (M > kAdPiece) {

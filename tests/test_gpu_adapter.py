@@ -178,8 +178,8 @@ def test_gradients_against_differences():
                                  (1 << 20, 5)])
 @pytest.mark.parametrize("kind", ["mixed", "runs", "one", "none"])
 def test_plan(M, n, kind):
-    """The plan's rows are a stable sort by adapter, those without at the end; its
-    tiles and pieces cover each adapter's rows in order."""
+    """The plan's tiles hold the rows in a stable order by adapter, those without at
+    the end; its pieces cover each adapter's tiles in order."""
     pifa, torch = _pifa(), torch_mod()
     rng = np.random.default_rng([M, n])
     ids = _ids(kind, M, n, rng) if M else np.zeros(0, np.int32)
@@ -189,34 +189,41 @@ def test_plan(M, n, kind):
     torch.cuda.synchronize()
     assert (big[size:] == 123).all()
     words = big[:size].cpu().numpy().view(np.int32)
-    pad = lambda k: -(-k // 16) * 16
-    head, at = words[:16], 16
-    seg, at = words[at:at + n + 2], at + pad(n + 2)
-    perm, at = words[at:at + M], at + pad(M)
-    tiles, at = words[at:], at + pad(2 * (M // 64 + min(n, M) + 1))
-    pieces, at = words[at:], at + pad(2 * (M // 512 + n))
-    slots, at = words[at:], at + pad(M // 512 + n)
-    multi = words[at:]
+    tmax, at = M // 64 + min(n, M) + 1, 16
+    head = words[:16]
+
+    def take(k):
+        nonlocal at
+        at += -(-k // 16) * 16
+        return words[at - -(-k // 16) * 16:at]
+
+    tiles, rows = take(2 * tmax), take(64 * tmax)
+    counts, pieces, multi = take(n + 1)[:n + 1], take(4 * (M // 512 + n)), take(3 * (M // 512 + 1))
     bucket = np.where((ids >= 0) & (ids < n), ids, n)
-    assert np.array_equal(perm, np.argsort(bucket, kind="stable"))
+    order = np.argsort(bucket, kind="stable")
     count = np.bincount(bucket, minlength=n + 1)
-    assert np.array_equal(seg, np.concatenate([[0], np.cumsum(count)]))
-    cut = lambda rows, least, of: [(a, seg[a] + rows * i) for a in range(of) for i in range(max(least, -(-count[a] // rows)))]
-    want = cut(64, 0, n + 1)
-    assert head[0] == M and head[1] == n and head[4] == M - count[n]
-    assert head[3] == len(want) and head[2] == sum(a < n for a, _ in want)
-    assert np.array_equal(tiles[:2 * len(want)].reshape(-1, 2), np.array(want, np.int32).reshape(-1, 2))
-    want = cut(512, 1, n)
-    assert head[5] == len(want) and np.array_equal(pieces[:2 * len(want)].reshape(-1, 2), np.array(want, np.int32))
-    slot, where = 0, []
-    for a in range(n):
-        k = max(1, -(-count[a] // 512))
-        where += [slot + i if k > 1 else -1 for i in range(k)]
-        if k > 1:
-            assert np.array_equal(multi[:3], [a, slot, k])
-            multi, slot = multi[3:], slot + k
-    assert np.array_equal(slots[:len(where)], where) and slot <= 2 * (M // 512)
-    assert head[6] == sum(-(-count[a] // 512) > 1 for a in range(n))
+    start = np.concatenate([[0], np.cumsum(count)])
+    assert np.array_equal(counts, count)
+    first, want_tiles, want_rows, want_pieces, want_multi, slot = [], [], [], [], [], 0
+    for a in range(n + 1):
+        first.append(len(want_tiles))
+        for k in range(0, count[a], 64):
+            c = min(64, count[a] - k)
+            want_tiles.append((a, c))
+            want_rows.append(np.concatenate([order[start[a] + k:start[a] + k + c], np.full(64 - c, -1)]))
+        if a < n:
+            of = -(-count[a] // 64)
+            k = max(1, -(-count[a] // 512))
+            want_pieces += [(a, first[a] + 8 * i, min(8, of - 8 * i), slot + i if k > 1 else -1) for i in range(k)]
+            if k > 1:
+                want_multi.append((a, slot, k))
+                slot += k
+    assert list(head[:6]) == [M, n, first[n], len(want_tiles), len(want_pieces), len(want_multi)]
+    flat = lambda v: np.array(v, np.int32).ravel()
+    assert np.array_equal(tiles[:2 * len(want_tiles)], flat(want_tiles))
+    assert np.array_equal(rows[:64 * len(want_tiles)], flat(want_rows))
+    assert np.array_equal(pieces[:4 * len(want_pieces)], flat(want_pieces))
+    assert np.array_equal(multi[:3 * len(want_multi)], flat(want_multi)) and slot <= 2 * (M // 512)
 
 
 def test_special_values_stay_in_their_rows():
