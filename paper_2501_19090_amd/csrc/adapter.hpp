@@ -29,8 +29,9 @@ constexpr int kAdPiece = kAdTile * kAdPieceTiles;
 constexpr int kAdMaxSlots = 4096;
 constexpr int64_t kAdMaxRows = 1 << 20;
 constexpr int kAdMaxSplit = 8;     // of K
-constexpr int kAdThreads = 512;
+constexpr int kAdThreads = 256;    // of shrink and expand
 constexpr int kAdWaves = kAdThreads / kWave;
+constexpr int kAdSlice = 64;       // columns that a wave of shrink takes at a time
 
 // ------------------------------------------------------------------ plan
 // A plan in memory: a header, then arrays of int32.  Rows without an adapter are
@@ -247,11 +248,12 @@ __device__ __forceinline__ f32x4 adapter_mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// How many workgroups share a tile's K: as many as bring `tiles` to `target`.
-__host__ __device__ inline int adapter_splits(int tiles, int64_t slices, int target) {
-    int s = tiles > 0 ? (target + tiles - 1) / tiles : 1;
+// How many workgroups share a tile's K: as many as leave all of them, `target` at
+// most, on the chip at once.
+__host__ __device__ inline int adapter_splits(int tiles, int64_t K, int target) {
+    int s = tiles > 0 ? target / tiles : 1;
     if (s > kAdMaxSplit) s = kAdMaxSplit;
-    const int64_t most = slices / kAdWaves;  // a slice for every wave
+    const int64_t most = ceil_div(K, kAdSlice) / kAdWaves;  // a slice for every wave
     if (s > most) s = (int)most;
     return s < 1 ? 1 : s;
 }
@@ -268,101 +270,115 @@ struct AdapterShrink {
     int64_t K;
 };
 
-// A tile's rows times 16 JB of an adapter's; slices s0 to s1 of 32 columns, a wave
-// taking every eighth.  The next slice's operands are loaded before this one's
-// are multiplied.
+// A tile's rows (RG groups of 16) times 16 JB of an adapter's; slices s0 to s1 of
+// 64 columns, a wave taking every fourth.  The matrix instruction's operands have a
+// row in each of 16 neighbouring lanes, which the caches would serve one by one; so
+// a wave loads lines of 128 bytes, eight neighbouring lanes each, and turns them in
+// LDS of its own (16-byte places of a row exchanged by its number, so that
+// neighbouring rows' are in other banks).  The next slice is on its way meanwhile.
 template <int JB, int RG>
 __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, const int32_t* rows, const AdapterTile tile,
                                                     int64_t r, int j0, int64_t s0, int64_t s1, int64_t rp, float* out,
-                                                    float* lds) {
+                                                    u32x4* lds) {
+    constexpr int NX = 2 * RG, NW = 2 * JB;  // loads of a slice: 8 rows each
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
-    const bf16* x[RG];
-    const bf16* w[JB];
+    const int row8 = lane >> 3, c8 = lane & 7;
+    const bf16* x[NX];
+    const bf16* w[NW];
 #pragma unroll
-    for (int g = 0; g < RG; ++g) x[g] = j.P + (int64_t)rows[min(16 * g + i, tile.count - 1)] * j.K;
+    for (int k = 0; k < NX; ++k) x[k] = j.P + (int64_t)rows[min(8 * k + row8, tile.count - 1)] * j.K + 8 * c8;
 #pragma unroll
-    for (int b = 0; b < JB; ++b)
-        w[b] = j.W + ((int64_t)tile.adapter * r + min((int64_t)(j0 + 16 * b + i), r - 1)) * j.K;
+    for (int k = 0; k < NW; ++k)
+        w[k] = j.W + ((int64_t)tile.adapter * r + min((int64_t)(j0 + 8 * k + row8), r - 1)) * j.K + 8 * c8;
     f32x4 acc[RG][JB];
 #pragma unroll
     for (int g = 0; g < RG; ++g)
 #pragma unroll
         for (int b = 0; b < JB; ++b) acc[g][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    struct Stage {
-        u32x4 x[RG], w[JB];
+    u32x4* mine = lds + wave * (NX + NW) * kWave;
+    u32x4 f[NX + NW];
+    auto load = [&](int64_t s) {
+#pragma unroll
+        for (int k = 0; k < NX; ++k) f[k] = adapter_load(x[k] + kAdSlice * s);
+#pragma unroll
+        for (int k = 0; k < NW; ++k) f[NX + k] = adapter_load(w[k] + kAdSlice * s);
     };
-    auto load = [&](int64_t s, Stage& f) {
-        const int64_t k = 32 * s + 8 * q;
+    auto turn = [&] {
 #pragma unroll
-        for (int g = 0; g < RG; ++g) f.x[g] = adapter_load(x[g] + k);
-#pragma unroll
-        for (int b = 0; b < JB; ++b) f.w[b] = adapter_load(w[b] + k);
+        for (int k = 0; k < NX + NW; ++k) {
+            const int row = 8 * k + row8;
+            mine[row * 8 + (c8 ^ (row >> 1 & 7))] = f[k];
+        }
     };
-    auto multiply = [&](const Stage& f) {
+    auto multiply = [&] {
 #pragma unroll
-        for (int g = 0; g < RG; ++g)
+        for (int h = 0; h < 2; ++h) {  // 32 columns each
+            u32x4 a[RG], b[JB];
 #pragma unroll
-            for (int b = 0; b < JB; ++b) acc[g][b] = adapter_mfma(f.x[g], f.w[b], acc[g][b]);
+            for (int g = 0; g < RG; ++g) a[g] = mine[(16 * g + i) * 8 + ((4 * h + q) ^ (i >> 1 & 7))];
+#pragma unroll
+            for (int k = 0; k < JB; ++k) b[k] = mine[(8 * NX + 16 * k + i) * 8 + ((4 * h + q) ^ (i >> 1 & 7))];
+#pragma unroll
+            for (int g = 0; g < RG; ++g)
+#pragma unroll
+                for (int k = 0; k < JB; ++k) acc[g][k] = adapter_mfma(a[g], b[k], acc[g][k]);
+        }
     };
-    const int64_t whole = min(s1, j.K / 32);  // slices of 32 full columns
+    const int64_t whole = min(s1, j.K / kAdSlice);  // slices of 64 full columns
     const int64_t first = s0 + wave, count = first < whole ? (whole - first + kAdWaves - 1) / kAdWaves : 0;
     if (count > 0) {
         const int64_t last = first + (count - 1) * kAdWaves;
-        Stage even, odd;
-        load(first, even);
-        for (int64_t c = 0; c < count; c += 2) {
-            load(min(first + (c + 1) * kAdWaves, last), odd);
+        load(first);
+        for (int64_t c = 0; c < count; ++c) {
+            turn();
+            load(min(first + (c + 1) * kAdWaves, last));
             __builtin_amdgcn_sched_barrier(0);
-            multiply(even);
-            load(min(first + (c + 2) * kAdWaves, last), even);
-            __builtin_amdgcn_sched_barrier(0);
-            if (c + 1 < count) multiply(odd);
+            multiply();
         }
     }
-    if (first + count * kAdWaves < s1) {  // the row's last columns
-        const int64_t k = 32 * (first + count * kAdWaves) + 8 * q;
-        Stage f;
+    if (const int64_t s = first + count * kAdWaves; s < s1) {  // the row's last columns
 #pragma unroll
-        for (int g = 0; g < RG; ++g) f.x[g] = adapter_load8(x[g], k, j.K);
+        for (int k = 0; k < NX; ++k) f[k] = adapter_load8(x[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
 #pragma unroll
-        for (int b = 0; b < JB; ++b) f.w[b] = adapter_load8(w[b], k, j.K);
-        multiply(f);
+        for (int k = 0; k < NW; ++k) f[NX + k] = adapter_load8(w[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
+        turn();
+        multiply();
     }
-    // the waves' sums, 16 rows at a time, in two halves of LDS in turn
+    // the waves' sums
     constexpr int COLS = 16 * JB;
     const float scale = j.scale ? j.scale[tile.adapter] : 1.f;
+    float* part = (float*)lds;  // waves x 16 RG x COLS: no more than the slices took
+    __syncthreads();
 #pragma unroll
-    for (int g = 0; g < RG; ++g) {
-        float* part = lds + (g & 1) * kAdWaves * 16 * COLS;
+    for (int g = 0; g < RG; ++g)
 #pragma unroll
         for (int b = 0; b < JB; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[(wave * 16 + 4 * q + e) * COLS + 16 * b + i] = acc[g][b][e];
-        __syncthreads();
-        for (int at = threadIdx.x; at < 16 * COLS; at += kAdThreads) {
-            const int row = 16 * g + at / COLS, col = j0 + at % COLS;
-            float v = 0.f;
+            for (int e = 0; e < 4; ++e) part[((wave * RG + g) * 16 + 4 * q + e) * COLS + 16 * b + i] = acc[g][b][e];
+    __syncthreads();
+    for (int at = threadIdx.x; at < 16 * RG * COLS; at += kAdThreads) {
+        const int row = at / COLS, col = j0 + at % COLS;
+        float v = 0.f;
 #pragma unroll
-            for (int u = 0; u < kAdWaves; ++u) v += part[u * 16 * COLS + at];
-            if (row < tile.count) out[(int64_t)row * rp + col] = col < r ? v * scale : 0.f;
-        }
+        for (int u = 0; u < kAdWaves; ++u) v += part[u * 16 * RG * COLS + at];
+        if (row < tile.count) out[(int64_t)row * rp + col] = col < r ? v * scale : 0.f;
     }
 }
 
 // Workgroups: x: tiles, y: parts of K, z: blocks of 16 JB columns of t, jobs outermost.
 template <int JB>
-__global__ __launch_bounds__(kAdThreads) void adapter_shrink(AdapterShrink j0, AdapterShrink j1, AdapterPlan p, int64_t M,
+__global__ __launch_bounds__(kAdThreads, 2) void adapter_shrink(AdapterShrink j0, AdapterShrink j1, AdapterPlan p, int64_t M,
                                                              int n, int64_t r, int target) {
-    __shared__ float lds[2 * kAdWaves * 16 * 16 * JB];
+    __shared__ u32x4 lds[kAdWaves * (8 + 2 * JB) * kWave];
     const AdapterHeader h = *p.head;
     const AdapterTile tile = p.tiles[blockIdx.x];
     if (h.M != M || h.n != n || (int)blockIdx.x >= h.tiles) return;
     const int64_t rp = adapter_rp(r);
     const int cols = (int)ceil_div(rp, 16 * JB), job = blockIdx.z / cols, c0 = (blockIdx.z % cols) * 16 * JB;
     const AdapterShrink j = job ? j1 : j0;
-    const int64_t slices = ceil_div(j.K, 32);
-    const int splits = adapter_splits(h.tiles, slices, target);
+    const int splits = adapter_splits(h.tiles, j.K, target);
     if ((int)blockIdx.y >= splits) return;
+    const int64_t slices = ceil_div(j.K, kAdSlice);
     const int64_t each = ceil_div(slices, splits), s0 = each * blockIdx.y, s1 = min(s0 + each, slices);
     const int32_t* rows = p.rows + (int64_t)blockIdx.x * kAdTile;
     float* out = j.T + ((int64_t)blockIdx.y * h.tiles + blockIdx.x) * kAdTile * rp;
@@ -382,12 +398,22 @@ __device__ __forceinline__ void adapter_split3(float v, bf16 (&s)[3]) {
     s[2] = (bf16)((v - (float)s[0]) - (float)s[1]);
 }
 
+// t as operands in the order of a wave's lanes, 16 bytes each:
+//   halves: for each group of 16 rows and 32 columns, the values' and what they
+//           leave (up to 16 columns: both in one, in its two halves of K);
+//   turned: for 32 rows and 16 columns, three parts, K along the rows.
 struct AdapterFinish {
-    const float* T;   // splits x 64 tiles x rp
-    bf16* halves;     // or null: 64 tiles x 2 x rp, the values and what they leave
-    uint16_t* turned; // or null: 3 x rp x 64 tiles
-    int64_t K;        // that t was summed over
+    const float* T;  // splits x 64 tiles x rp
+    u32x4* halves;   // or null
+    u32x4* turned;   // or null
+    int64_t K;       // that t was summed over
 };
+__device__ __forceinline__ int64_t adapter_half_at(int64_t group, int64_t rp, int64_t k32, int lo) {
+    return (rp == 16 ? group : (group * (rp / 32) + k32) * 2 + lo) * kWave;
+}
+__device__ __forceinline__ int64_t adapter_turned_at(int64_t step, int64_t rp, int part, int64_t c16) {
+    return ((step * 3 + part) * (rp / 16) + c16) * kWave;
+}
 
 // Four columns of a row of t, the parts' sums added, all parts' loads in flight.
 __device__ __forceinline__ f32x4 adapter_t4(const float* t, int splits, int64_t stride) {
@@ -403,233 +429,217 @@ __device__ __forceinline__ f32x4 adapter_t4(const float* t, int splits, int64_t 
 
 // Workgroups: x: tiles, y: blocks of 16 columns, z: jobs.
 static __global__ __launch_bounds__(256) void adapter_finish(AdapterFinish j0, AdapterFinish j1, AdapterPlan p, int64_t M,
-                                                            int n, int64_t r, int64_t width, int target) {
-    __shared__ float lds[16][kAdTile + 4];
+                                                            int n, int64_t r, int target) {
+    __shared__ float lds[kAdTile][17];
     const AdapterHeader h = *p.head;
     const AdapterTile tile = p.tiles[blockIdx.x];
     if (h.M != M || h.n != n || (int)blockIdx.x >= h.tiles) return;
     const AdapterFinish j = blockIdx.z ? j1 : j0;
-    const int64_t rp = adapter_rp(r);
-    const int row = threadIdx.x >> 2, c = (threadIdx.x & 3) * 4, c0 = blockIdx.y * 16 + c;
-    const int64_t at = (int64_t)blockIdx.x * kAdTile + row;
-    f32x4 v = adapter_t4(j.T + at * rp + c0, adapter_splits(h.tiles, ceil_div(j.K, 32), target), (int64_t)h.tiles * kAdTile * rp);
-    if (row >= tile.count) v = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (j.halves) {
-        bf16 hi[4], lo[4];
+    const int64_t rp = adapter_rp(r), x = blockIdx.x;
+    const int t = threadIdx.x, y = blockIdx.y;
+    {
+        const int row = t >> 2, c = (t & 3) * 4;
+        f32x4 v = adapter_t4(j.T + (x * kAdTile + row) * rp + 16 * y + c, adapter_splits(h.tiles, j.K, target),
+                             (int64_t)h.tiles * kAdTile * rp);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) adapter_split2(v[e], hi[e], lo[e]);
-        bf16* to = j.halves + at * 2 * rp + c0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            to[e] = hi[e];
-            to[rp + e] = lo[e];
-        }
+        for (int e = 0; e < 4; ++e) lds[row][c + e] = row < tile.count ? v[e] : 0.f;
     }
-    if (!j.turned) return;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) lds[c + e][row] = v[e];
     __syncthreads();
-    const int col = threadIdx.x >> 4, r0 = (threadIdx.x & 15) * 4;
-    bf16 s[4][3];
+    if (j.halves && t < 128) {  // 64 rows x 2 of 8 columns
+        const int row = t & 63, c = t >> 6, lane = row & 15;
+        bf16x8 hi, lo;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) adapter_split3(lds[col][r0 + e], s[e]);
+        for (int e = 0; e < 8; ++e) {
+            bf16 a, b;
+            adapter_split2(lds[row][8 * c + e], a, b);
+            hi[e] = a;
+            lo[e] = b;
+        }
+        const int64_t group = x * 4 + row / 16;
+        const int q = rp == 16 ? c : 2 * (y & 1) + c;
+        j.halves[adapter_half_at(group, rp, y / 2, 0) + 16 * q + lane] = __builtin_bit_cast(u32x4, hi);
+        j.halves[adapter_half_at(group, rp, y / 2, 1) + 16 * (rp == 16 ? q + 2 : q) + lane] = __builtin_bit_cast(u32x4, lo);
+    }
+    if (j.turned && t >= 128) {  // 16 columns x 8 of 8 rows
+        const int col = t & 15, r8 = (t >> 4) & 7;
+        bf16x8 s[3];
 #pragma unroll
-    for (int u = 0; u < 3; ++u) {
-        bf16* to = (bf16*)j.turned + ((int64_t)u * rp + blockIdx.y * 16 + col) * width + (int64_t)blockIdx.x * kAdTile + r0;
+        for (int e = 0; e < 8; ++e) {
+            bf16 v[3];
+            adapter_split3(lds[8 * r8 + e][col], v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) to[e] = s[e][u];
+            for (int u = 0; u < 3; ++u) s[u][e] = v[u];
+        }
+#pragma unroll
+        for (int u = 0; u < 3; ++u)
+            j.turned[adapter_turned_at(2 * x + r8 / 4, rp, u, y) + 16 * (r8 & 3) + col] = __builtin_bit_cast(u32x4, s[u]);
     }
 }
 
 // ------------------------------------------------------------------ expand
 struct AdapterExpand {
-    const float* T;      // splits x 64 tiles x rp, or
-    const bf16* halves;  // as finish leaves them
-    const bf16* W;       // n x d x r
-    const bf16* base;    // or null: zeros
-    bf16* out;           // M x d; may be base
+    const float* T;       // splits x 64 tiles x rp, or
+    const u32x4* halves;  // as finish leaves them
+    const bf16* W;        // n x d x r
+    const bf16* base;     // or null: zeros
+    bf16* out;            // M x d; may be base
     int64_t d;
-    int64_t K;           // that t was summed over
+    int64_t K;            // that t was summed over
 };
 
-// The 64 columns of W that a wave takes as operands: instruction u's row i is column
-// c0 + 32 (u / 2) + 8 (i / 4) + 4 (u % 2) + i % 4, so that two instructions leave
-// a lane with 8 columns in a row.
-__device__ __forceinline__ const bf16* adapter_w_row(const bf16* W, int64_t c0, int u, int i, int64_t d, int64_t r) {
-    return W + min(c0 + 32 * (u / 2) + 8 * (i / 4) + 4 * (u % 2) + i % 4, d - 1) * r;
-}
-__device__ __forceinline__ u32x4 adapter_w8(const bf16* row, int64_t k, int64_t r) {
-    if (r % 8 != 0) return adapter_load8(row, k, r);
-    const u32x4 v = adapter_load(row + (k < r ? k : 0));
-    return k < r ? v : zero16();
-}
+constexpr int kAdWide = 128;  // columns that a wave of expand takes
 
-// The rows of G groups of 16 from g0 on.  SUM: t is still in parts (few rows).
-// FULL: all 64 columns are there.
+// A wave's columns c0 to c0 + 127 of the rows of G groups of 16 from g0 on.
+// Instruction u's column i is c0 + 8 i + u, so that a lane ends up with 8 columns in
+// a row and 16 neighbouring lanes with 256 bytes of each row of Y.  W's rows of
+// these columns are turned in LDS like the rows of shrink, KB blocks of 32 (KB = 0:
+// 16) columns of t at a time.  SUM: t is still in parts.  FULL: all columns are there.
 template <int KB, bool SUM, bool FULL, int G>
 __device__ __forceinline__ void adapter_expand_rows(const AdapterExpand& j, const int32_t* rows, int count, int g0,
-                                                    int64_t tile, int64_t c0, const bf16* W,
-                                                    const u32x4 (&w)[KB > 0 ? KB : 1][4], int64_t r, int64_t rp, int splits,
-                                                    int64_t stride) {
+                                                    int64_t tile, int64_t c0, const bf16* W, u32x4* lds, int64_t r,
+                                                    int splits, int64_t stride) {
     const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
-    constexpr int NB = KB > 0 ? KB : 1;
-    int64_t at[G];
-    u32x4 base[G][2];
+    constexpr int NB = KB > 0 ? KB : 1, CH = KB > 0 ? 4 * KB : 2;  // pieces of 8 columns of t in a row
+    constexpr int PITCH = CH + 1;
+    const int64_t rp = adapter_rp(r);
+    int64_t at[G][4];
+    u32x4 base[G][4];
 #pragma unroll
-    for (int g = 0; g < G; ++g) at[g] = (int64_t)rows[min(16 * (g0 + g) + i, count - 1)] * j.d;
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) at[g][e] = (int64_t)max(rows[16 * (g0 + g) + 4 * q + e], 0) * j.d;
     if (j.base) {
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int64_t c = c0 + 32 * u + 8 * q;
-                if constexpr (FULL) base[g][u] = adapter_load(j.base + at[g] + c);
-                else base[g][u] = adapter_load8(j.base + at[g], min(c, j.d), j.d);
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (FULL) base[g][e] = adapter_load(j.base + at[g][e] + c0 + 8 * i);
+                else base[g][e] = adapter_load8(j.base + at[g][e], min(c0 + 8 * i, j.d), j.d);
             }
     } else {
 #pragma unroll
-        for (int g = 0; g < G; ++g) base[g][0] = base[g][1] = zero16();
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) base[g][e] = zero16();
     }
-    // t's operands of a group and a block of 32 columns (KB = 0: of 16, both halves in one)
-    auto halves = [&](int g, int64_t k, u32x4& hi, u32x4& lo) {
-        const int64_t row = tile * kAdTile + min(16 * (g0 + g) + i, count - 1);
-        if constexpr (SUM) {
-            const f32x4 a = adapter_t4(j.T + row * rp + k, splits, stride), b = adapter_t4(j.T + row * rp + k + 4, splits, stride);
-            bf16x8 h, l;
+    f32x4 acc[G][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                bf16 x, y;
-                adapter_split2(e < 4 ? a[e % 4] : b[e % 4], x, y);
-                h[e] = x;
-                l[e] = y;
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) acc[g][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int64_t k0 = 0; k0 < rp; k0 += 8 * CH) {
+        u32x4 wv[2 * CH];
+#pragma unroll
+        for (int k = 0; k < 2 * CH; ++k) {
+            const int col = (kWave * k + lane) / CH, c = (kWave * k + lane) % CH;
+            const bf16* row = W + min(c0 + col, j.d - 1) * r;
+            const int64_t from = k0 + 8 * c;
+            if (r % 8 != 0) {
+                wv[k] = adapter_load8(row, from, r);
+            } else {
+                wv[k] = adapter_load(row + (from < r ? from : 0));
+                if (from >= r) wv[k] = zero16();
             }
-            hi = __builtin_bit_cast(u32x4, h);
-            lo = __builtin_bit_cast(u32x4, l);
-        } else {
-            hi = *reinterpret_cast<const u32x4*>(j.halves + row * 2 * rp + k);
-            lo = *reinterpret_cast<const u32x4*>(j.halves + row * 2 * rp + rp + k);
         }
-    };
-    auto finish = [&](int g, const f32x4(&acc)[4]) {
-        if (16 * (g0 + g) + i >= count) return;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int64_t c = c0 + 32 * u + 8 * q;
-            const bf16x8 b = __builtin_bit_cast(bf16x8, base[g][u]);
+        for (int k = 0; k < 2 * CH; ++k) {
+            const int col = (kWave * k + lane) / CH, c = (kWave * k + lane) % CH;
+            lds[(col % 8 * 16 + col / 8) * PITCH + c] = wv[k];
+        }
+        u32x4 w[NB][8];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) w[b][u] = lds[(u * 16 + i) * PITCH + (KB == 0 ? q & 1 : 4 * b + q)];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int64_t group = 4 * tile + g0 + g;
+            u32x4 hi[NB], lo[NB];
+            if constexpr (SUM) {
+                const float* t = j.T + (16 * group + min(i, count - 1 - 16 * (g0 + g))) * rp + k0;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const int64_t k = KB == 0 ? 8 * (q & 1) : 32 * b + 8 * q;
+                    const f32x4 x = adapter_t4(t + k, splits, stride), y = adapter_t4(t + k + 4, splits, stride);
+                    bf16x8 h, l;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        bf16 s[2];
+                        adapter_split2(e < 4 ? x[e % 4] : y[e % 4], s[0], s[1]);
+                        h[e] = s[0];
+                        l[e] = s[1];
+                    }
+                    hi[b] = __builtin_bit_cast(u32x4, h);
+                    lo[b] = __builtin_bit_cast(u32x4, l);
+                }
+                if constexpr (KB == 0) hi[0] = q < 2 ? hi[0] : lo[0];
+            } else {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    hi[b] = j.halves[adapter_half_at(group, rp, k0 / 32 + b, 0) + lane];
+                    if constexpr (KB != 0) lo[b] = j.halves[adapter_half_at(group, rp, k0 / 32 + b, 1) + lane];
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    acc[g][u] = adapter_mfma(hi[b], w[b][u], acc[g][u]);
+                    if constexpr (KB != 0) acc[g][u] = adapter_mfma(lo[b], w[b][u], acc[g][u]);
+                }
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (16 * (g0 + g) + 4 * q + e >= count) continue;
+            const bf16x8 b = __builtin_bit_cast(bf16x8, base[g][e]);
             bf16x8 y;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = (bf16)((float)b[e] + acc[2 * u + e / 4][e % 4]);
-            bf16* to = j.out + at[g] + c;
+            for (int u = 0; u < 8; ++u) y[u] = (bf16)((float)b[u] + acc[g][u][e]);
+            const int64_t c = c0 + 8 * i;
+            bf16* to = j.out + at[g][e] + c;
             if (FULL || c + 8 <= j.d) {
                 reinterpret_cast<AdapterAny16*>(to)->v = __builtin_bit_cast(u32x4, y);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (c + e < j.d) to[e] = y[e];
+                for (int u = 0; u < 8; ++u)
+                    if (c + u < j.d) to[u] = y[u];
             }
         }
-    };
-    if constexpr (KB >= 0) {
-        u32x4 hi[2][NB], lo[2][NB];  // the next group's are loaded before this one's rows are stored
-        auto fetch = [&](int g) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) halves(g, KB == 0 ? 8 * (q & 1) : 32 * b + 8 * q, hi[g & 1][b], lo[g & 1][b]);
-        };
-        fetch(0);
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            if (g + 1 < G) fetch(g + 1);
-            f32x4 acc[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if constexpr (KB == 0) {
-                    acc[u] = adapter_mfma(w[0][u], q < 2 ? hi[g & 1][0] : lo[g & 1][0], acc[u]);
-                } else {
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        acc[u] = adapter_mfma(w[b][u], hi[g & 1][b], acc[u]);
-                        acc[u] = adapter_mfma(w[b][u], lo[g & 1][b], acc[u]);
-                    }
-                }
-            }
-            finish(g, acc);
-        }
-    } else {
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            f32x4 acc[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int64_t k = 8 * q; k < rp; k += 32) {
-                u32x4 hi, lo;
-                halves(g, k, hi, lo);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const u32x4 wk = adapter_w8(adapter_w_row(W, c0, u, i, j.d, r), k, r);
-                    acc[u] = adapter_mfma(wk, hi, acc[u]);
-                    acc[u] = adapter_mfma(wk, lo, acc[u]);
-                }
-            }
-            finish(g, acc);
-        }
-    }
 }
 
-// A wave's 64 columns of a tile.
-template <int KB, bool SUM, bool FULL>
-__device__ __forceinline__ void adapter_expand_tile(const AdapterExpand& j, const AdapterPlan& p, const AdapterHeader& h,
-                                                    const AdapterTile tile, int64_t c0, int64_t r, int target) {
-    const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
-    const int64_t rp = adapter_rp(r);
-    const int32_t* rows = p.rows + (int64_t)blockIdx.y * kAdTile;
-    const bf16* W = j.W + (int64_t)tile.adapter * j.d * r;
-    constexpr int NB = KB > 0 ? KB : 1;
-    u32x4 w[NB][4];
-    if constexpr (KB >= 0) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-                w[b][u] = adapter_w8(adapter_w_row(W, c0, u, i, j.d, r), KB == 0 ? 8 * (q & 1) : 32 * b + 8 * q, r);
-    }
-    const int splits = SUM ? adapter_splits(h.tiles, ceil_div(j.K, 32), target) : 1;
-    const int64_t stride = (int64_t)h.tiles * kAdTile * rp;
-    const int groups = (tile.count + 15) / 16;
-    if constexpr (!SUM) {
-        if (groups == 4) {
-            adapter_expand_rows<KB, SUM, FULL, 4>(j, rows, tile.count, 0, blockIdx.y, c0, W, w, r, rp, splits, stride);
-            return;
-        }
-    }
-    for (int g = 0; g < groups; ++g)
-        adapter_expand_rows<KB, SUM, FULL, 1>(j, rows, tile.count, g, blockIdx.y, c0, W, w, r, rp, splits, stride);
-}
-
-// Workgroups: x: 64 columns a wave, y: tiles (those of rows without an adapter
-// last, which are copied).  KB: blocks of 32 columns of t, whose operands of W
-// stay in registers over the tile's rows; 0: up to 16 columns, both halves of t
-// in one instruction; -1: any number, read again for every 16 rows.
-template <int KB, bool SUM>
-__global__ __launch_bounds__(256) void adapter_expand(AdapterExpand j, AdapterPlan p, int64_t M, int n, int64_t r,
-                                                      int target) {
+// Workgroups: x: 128 columns a wave, y: tiles (those of rows without an adapter
+// last, which are copied), z: the tile's groups of 16 rows, G each.  KB: as above, for
+// ranks of up to 16 (0), 32 (1) and 64 at a time (2).
+template <int KB, bool SUM, int G>
+__global__ __launch_bounds__(kAdThreads, SUM ? 1 : 2) void adapter_expand(AdapterExpand j, AdapterPlan p, int64_t M, int n, int64_t r,
+                                                             int target) {
+    __shared__ u32x4 lds[kAdWaves][kAdWide * (KB > 0 ? 4 * KB + 1 : 3)];
     const AdapterHeader h = *p.head;
     const AdapterTile tile = p.tiles[blockIdx.y];
-    if (h.M != M || h.n != n || (int)blockIdx.y >= h.tiles_all) return;
-    const int64_t c0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64;
+    const int g0 = blockIdx.z * G, wave = threadIdx.x >> 6;
+    if (h.M != M || h.n != n || (int)blockIdx.y >= h.tiles_all || 16 * g0 >= tile.count) return;
+    const int64_t c0 = ((int64_t)blockIdx.x * kAdWaves + wave) * kAdWide;
     if (c0 >= j.d) return;
+    const int32_t* rows = p.rows + (int64_t)blockIdx.y * kAdTile;
     if (tile.adapter >= n) {
         if (j.out == j.base) return;
-        const int64_t c = c0 + (threadIdx.x & 63);
-        if (c >= j.d) return;
-        for (int m = 0; m < tile.count; ++m) {
-            const int64_t at = (int64_t)p.rows[(int64_t)blockIdx.y * kAdTile + m] * j.d + c;
-            ((uint16_t*)j.out)[at] = j.base ? ((const uint16_t*)j.base)[at] : (uint16_t)0;
-        }
+        for (int m = 16 * g0; m < min(tile.count, 16 * (g0 + G)); ++m)
+            for (int64_t c = c0 + (threadIdx.x & 63); c < min(c0 + kAdWide, j.d); c += kWave) {
+                const int64_t at = (int64_t)rows[m] * j.d + c;
+                ((uint16_t*)j.out)[at] = j.base ? ((const uint16_t*)j.base)[at] : (uint16_t)0;
+            }
         return;
     }
-    if (c0 + 64 <= j.d) adapter_expand_tile<KB, SUM, true>(j, p, h, tile, c0, r, target);
-    else adapter_expand_tile<KB, SUM, false>(j, p, h, tile, c0, r, target);
+    const bf16* W = j.W + (int64_t)tile.adapter * j.d * r;
+    const int splits = SUM ? adapter_splits(h.tiles, j.K, target) : 1;
+    const int64_t stride = (int64_t)h.tiles * kAdTile * adapter_rp(r);
+    if (c0 + kAdWide <= j.d)
+        adapter_expand_rows<KB, SUM, true, G>(j, rows, tile.count, g0, blockIdx.y, c0, W, lds[wave], r, splits, stride);
+    else
+        adapter_expand_rows<KB, SUM, false, G>(j, rows, tile.count, g0, blockIdx.y, c0, W, lds[wave], r, splits, stride);
 }
 
 // ------------------------------------------------------------------ backward
@@ -674,25 +684,26 @@ static __global__ __launch_bounds__(256) void adapter_transpose(const bf16* A, b
 }
 
 struct AdapterGrads {
-    const bf16* P;           // rows (M x d)
-    const uint16_t* turned;  // 3 x rp x 64 tiles
-    float* out;              // n x r x d (by_column: n x d x r)
-    float* part;             // the same of one adapter for each slot
+    const bf16* P;        // rows (M x d)
+    const u32x4* turned;  // as finish leaves it
+    float* out;           // n x r x d (by_column: n x d x r)
+    float* part;          // the same of one adapter for each slot
     int64_t d;
     bool by_column;
 };
 
 constexpr int kAdCols = 128;  // columns of P that a workgroup of grads takes
+constexpr int kAdGradThreads = 512, kAdGradWaves = kAdGradThreads / kWave;
 
 // Workgroups: x: columns of both jobs, y: pieces, z: blocks of 16 JB columns of t.
 // Each wave takes 32 rows at a time, every eighth such step: 8 loads of 8 columns
 // a lane, 8 rows apart from lane group to lane group, turned round to 8 operands
 // of 8 rows each.
 template <int JB>
-__global__ __launch_bounds__(kAdThreads) void adapter_grads(AdapterGrads j0, AdapterGrads j1, int blocks0, AdapterPlan p,
-                                                            int64_t M, int n, int64_t r, int64_t width) {
+__global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0, AdapterGrads j1, int blocks0, AdapterPlan p,
+                                                            int64_t M, int n, int64_t r) {
     constexpr int COLS = 16 * JB;
-    __shared__ float part[2][kAdWaves][16 * COLS];
+    __shared__ float part[2][kAdGradWaves][16 * COLS];
     __shared__ float sums[COLS][kAdCols + 1];
     const AdapterHeader h = *p.head;
     const AdapterPiece piece = p.pieces[blockIdx.y];
@@ -711,7 +722,7 @@ __global__ __launch_bounds__(kAdThreads) void adapter_grads(AdapterGrads j0, Ada
 #pragma unroll
         for (int b = 0; b < JB; ++b) acc[u][b] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int64_t first = (int64_t)piece.first * kAdTile;
-    for (int s = wave; s < 2 * piece.tiles; s += kAdWaves) {
+    for (int s = wave; s < 2 * piece.tiles; s += kAdGradWaves) {
         const int64_t at = first + 32 * s + 8 * q;
         int32_t row[8];
 #pragma unroll
@@ -721,7 +732,7 @@ __global__ __launch_bounds__(kAdThreads) void adapter_grads(AdapterGrads j0, Ada
         for (int u = 0; u < 3; ++u)
 #pragma unroll
             for (int b = 0; b < JB; ++b)
-                t[u][b] = *reinterpret_cast<const u32x4*>(j.turned + ((int64_t)u * rp + b0 + 16 * b + i) * width + at);
+                t[u][b] = j.turned[adapter_turned_at(2 * piece.first + s, rp, u, b0 / 16 + b) + lane];
         u32x4 x[8];
         if (full) {
 #pragma unroll
@@ -754,17 +765,17 @@ __global__ __launch_bounds__(kAdThreads) void adapter_grads(AdapterGrads j0, Ada
 #pragma unroll
             for (int e = 0; e < 4; ++e) part[k & 1][wave][(4 * q + e) * COLS + 16 * b + i] = acc[k][b][e];
         __syncthreads();
-        for (int at = threadIdx.x; at < 16 * COLS; at += kAdThreads) {
+        for (int at = threadIdx.x; at < 16 * COLS; at += kAdGradThreads) {
             float v = 0.f;
 #pragma unroll
-            for (int u = 0; u < kAdWaves; ++u) v += part[k & 1][u][at];
+            for (int u = 0; u < kAdGradWaves; ++u) v += part[k & 1][u][at];
             sums[at % COLS][8 * (at / COLS) + k] = v;
         }
     }
     __syncthreads();
     float* out = piece.slot < 0 ? j.out + piece.adapter * r * j.d : j.part + piece.slot * r * j.d;
     const int cols = (int)min((int64_t)kAdCols, j.d - c0), js = (int)min((int64_t)COLS, r - b0);
-    for (int at = threadIdx.x; at < COLS * kAdCols; at += kAdThreads) {
+    for (int at = threadIdx.x; at < COLS * kAdCols; at += kAdGradThreads) {
         const int a = j.by_column ? at % COLS : at / kAdCols, k = j.by_column ? at / COLS : at % kAdCols;
         if (a >= js || k >= cols) continue;
         out[j.by_column ? (c0 + k) * r + b0 + a : (b0 + a) * j.d + c0 + k] = sums[a][k];

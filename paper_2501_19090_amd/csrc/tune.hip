@@ -112,8 +112,8 @@ pifa_status layer_norm_backward_run(const void* H, const void* gain, const void*
 namespace {
 
 constexpr int64_t kAdMaxD = 1 << 19, kAdMaxRank = 1024;
-// Workgroups that a shrink of few tiles is cut into.
-constexpr int kAdTarget = 256;
+// Workgroups of a shrink that the chip holds at once, for one or two jobs.
+int adapter_target(int64_t r, int jobs) { return (int)((r <= 16 ? 4 : r <= 32 ? 3 : 2) * kCus / jobs); }
 
 pifa_status check_plan(int64_t M, int64_t n) {
     if (M < 0 || n < 1) return PIFA_ERR_INVALID_ARG;
@@ -134,10 +134,10 @@ bool aligned(std::initializer_list<const void*> p, uintptr_t to) {
 constexpr int64_t kAdFewRows = 256;
 
 // Bytes of t (or u): at most 8 parts of K of every tile, and where K is cut at all,
-// fewer than 2 kAdTarget tiles' parts; of its forms for expand and for grads.
+// no more parts than its target; of its forms for expand and for grads.
 size_t adapter_t_bytes(int64_t M, int64_t r, int64_t n) {
     const int64_t tiles = adapter_max_tiles(M, n);
-    const int64_t parts = std::min<int64_t>(kAdMaxSplit * tiles, std::max<int64_t>(tiles, 2 * kAdTarget));
+    const int64_t parts = std::min<int64_t>(kAdMaxSplit * tiles, std::max<int64_t>(tiles, adapter_target(r, 1)));
     return (size_t)(parts * kAdTile * adapter_rp(r) * 4);
 }
 size_t adapter_halves_bytes(int64_t M, int64_t r, int64_t n) {
@@ -158,42 +158,43 @@ AdapterPlan adapter_read_plan(const void* plan, int64_t M, int64_t n) {
 
 // One or two shrinks in a launch.
 hipError_t launch_shrink(const AdapterShrink& a, const AdapterShrink* b, const AdapterPlan& p, int64_t M, int64_t n,
-                         int64_t r, hipStream_t st) {
+                         int64_t r, int target, hipStream_t st) {
     TimedLaunch timed(kSiteAdapterShrink, st);
     const int64_t rp = adapter_rp(r), jb = std::min<int64_t>(4, rp / 16), most = std::max(a.K, b ? b->K : 0);
-    const dim3 grid((unsigned)adapter_max_tiles(M, n), (unsigned)adapter_splits(1, ceil_div(most, 32), kAdTarget),
+    const dim3 grid((unsigned)adapter_max_tiles(M, n), (unsigned)adapter_splits(1, most, target),
                     (unsigned)(ceil_div(rp, 16 * jb) * (b ? 2 : 1)));
     const AdapterShrink& second = b ? *b : a;
-    if (jb == 1) hipLaunchKernelGGL((adapter_shrink<1>), grid, dim3(kAdThreads), 0, st, a, second, p, M, (int)n, r, kAdTarget);
-    else if (jb == 2) hipLaunchKernelGGL((adapter_shrink<2>), grid, dim3(kAdThreads), 0, st, a, second, p, M, (int)n, r, kAdTarget);
-    else hipLaunchKernelGGL((adapter_shrink<4>), grid, dim3(kAdThreads), 0, st, a, second, p, M, (int)n, r, kAdTarget);
+    if (jb == 1) hipLaunchKernelGGL((adapter_shrink<1>), grid, dim3(kAdThreads), 0, st, a, second, p, M, (int)n, r, target);
+    else if (jb == 2) hipLaunchKernelGGL((adapter_shrink<2>), grid, dim3(kAdThreads), 0, st, a, second, p, M, (int)n, r, target);
+    else hipLaunchKernelGGL((adapter_shrink<4>), grid, dim3(kAdThreads), 0, st, a, second, p, M, (int)n, r, target);
     return hipGetLastError();
 }
 
 hipError_t launch_finish(const AdapterFinish& a, const AdapterFinish* b, const AdapterPlan& p, int64_t M, int64_t n,
-                         int64_t r, hipStream_t st) {
+                         int64_t r, int target, hipStream_t st) {
     TimedLaunch timed(kSiteAdapterShrink, st);
     const int64_t tiles = adapter_max_tiles(M, n);
     hipLaunchKernelGGL(adapter_finish, dim3((unsigned)tiles, (unsigned)(adapter_rp(r) / 16), b ? 2 : 1), dim3(256), 0, st, a,
-                       b ? *b : a, p, M, (int)n, r, tiles * kAdTile, kAdTarget);
+                       b ? *b : a, p, M, (int)n, r, target);
     return hipGetLastError();
 }
 
 template <bool SUM>
-hipError_t launch_expand(const AdapterExpand& a, const AdapterPlan& p, int64_t M, int64_t n, int64_t r, hipStream_t st) {
+hipError_t launch_expand(const AdapterExpand& a, const AdapterPlan& p, int64_t M, int64_t n, int64_t r, int target,
+                         hipStream_t st) {
     TimedLaunch timed(kSiteAdapterExpand, st);
     // columns keep to their XCD over the tiles, so that it reads only its part of W
-    const int64_t blocks = ceil_div(a.d, 256), rp = adapter_rp(r);
-    const dim3 grid((unsigned)(blocks > 8 ? round_up(blocks, 8) : blocks), (unsigned)adapter_max_tiles(M, n));
+    const int64_t blocks = ceil_div(a.d, kAdWaves * kAdWide);
+    const unsigned x = (unsigned)(blocks > 8 ? round_up(blocks, 8) : blocks), y = (unsigned)adapter_max_tiles(M, n);
     auto launch = [&](auto kb) {
-        hipLaunchKernelGGL((adapter_expand<decltype(kb)::value, SUM>), grid, dim3(256), 0, st, a, p, M, (int)n, r, kAdTarget);
+        constexpr int KB = decltype(kb)::value;
+        if constexpr (SUM) hipLaunchKernelGGL((adapter_expand<KB, SUM, 1>), dim3(x, y, 4), dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
+        else hipLaunchKernelGGL((adapter_expand<KB, SUM, 2>), dim3(x, y, 2), dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
     };
     using std::integral_constant;
-    if (rp == 16) launch(integral_constant<int, 0>{});
-    else if (rp == 32) launch(integral_constant<int, 1>{});
-    else if (rp == 64) launch(integral_constant<int, 2>{});
-    else if (rp == 128) launch(integral_constant<int, 4>{});
-    else launch(integral_constant<int, -1>{});
+    if (r <= 16) launch(integral_constant<int, 0>{});
+    else if (r <= 32) launch(integral_constant<int, 1>{});
+    else launch(integral_constant<int, 2>{});
     return hipGetLastError();
 }
 
@@ -376,14 +377,15 @@ pifa_status adapter_forward(const void* X, const void* A, const void* B, const f
     if (!aligned({X, A, B, Y0, Y}, 2) || !aligned({scale}, 4) || !aligned({plan, work}, 16)) return PIFA_ERR_UNSUPPORTED;
     const hipStream_t st = as_stream(stream);
     const AdapterPlan p = adapter_read_plan(plan, M, n);
+    const int target = adapter_target(r, 1);
     float* T = (float*)work;
-    bf16* halves = (bf16*)((uint8_t*)work + adapter_t_bytes(M, r, n));
-    if (launch_shrink({(const bf16*)X, (const bf16*)A, scale, T, d_in}, nullptr, p, M, n, r, st) != hipSuccess)
+    u32x4* halves = (u32x4*)((uint8_t*)work + adapter_t_bytes(M, r, n));
+    if (launch_shrink({(const bf16*)X, (const bf16*)A, scale, T, d_in}, nullptr, p, M, n, r, target, st) != hipSuccess)
         return PIFA_ERR_HIP;
     const AdapterExpand expand{T, halves, (const bf16*)B, (const bf16*)Y0, (bf16*)Y, d_out, d_in};
-    if (M <= kAdFewRows) return launch_expand<true>(expand, p, M, n, r, st) == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
-    if (launch_finish({T, halves, nullptr, d_in}, nullptr, p, M, n, r, st) != hipSuccess ||
-        launch_expand<false>(expand, p, M, n, r, st) != hipSuccess)
+    if (M <= kAdFewRows) return launch_expand<true>(expand, p, M, n, r, target, st) == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+    if (launch_finish({T, halves, nullptr, d_in}, nullptr, p, M, n, r, target, st) != hipSuccess ||
+        launch_expand<false>(expand, p, M, n, r, target, st) != hipSuccess)
         return PIFA_ERR_HIP;
     return PIFA_OK;
 }
@@ -432,13 +434,14 @@ pifa_status adapter_backward(const void* X, const void* A, const void* B, const 
     };
     float* T = (float*)take(adapter_t_bytes(M, r, n));
     float* U = (float*)take(adapter_t_bytes(M, r, n));
-    bf16* halves = (bf16*)take(adapter_halves_bytes(M, r, n));
-    uint16_t* turned_u = (uint16_t*)take(adapter_turned_bytes(M, r, n));
-    uint16_t* turned_t = (uint16_t*)take(adapter_turned_bytes(M, r, n));
+    u32x4* halves = (u32x4*)take(adapter_halves_bytes(M, r, n));
+    u32x4* turned_u = (u32x4*)take(adapter_turned_bytes(M, r, n));
+    u32x4* turned_t = (u32x4*)take(adapter_turned_bytes(M, r, n));
     bf16* At = (bf16*)take((size_t)round_up(2 * n * r * d_in, 256));
     bf16* Bt = (bf16*)take((size_t)round_up(2 * n * r * d_out, 256));
     float* part_a = (float*)take(adapter_partial_bytes(M, r, d_in));
     float* part_b = (float*)take(adapter_partial_bytes(M, r, d_out));
+    const int target = adapter_target(r, dB ? 2 : 1);
     const int64_t blocks_r = ceil_div(r, 8);
     {
         TimedLaunch timed(kSiteAdapterGrads, st);
@@ -449,22 +452,22 @@ pifa_status adapter_backward(const void* X, const void* A, const void* B, const 
     }
     const AdapterShrink t{(const bf16*)X, (const bf16*)A, scale, T, d_in}, u{(const bf16*)dY, Bt, scale, U, d_out};
     const AdapterFinish done_u{U, dX ? halves : nullptr, dA ? turned_u : nullptr, d_out}, done_t{T, nullptr, turned_t, d_in};
-    if (launch_shrink(u, dB ? &t : nullptr, p, M, n, r, st) != hipSuccess ||
-        launch_finish(done_u, dB ? &done_t : nullptr, p, M, n, r, st) != hipSuccess)
+    if (launch_shrink(u, dB ? &t : nullptr, p, M, n, r, target, st) != hipSuccess ||
+        launch_finish(done_u, dB ? &done_t : nullptr, p, M, n, r, target, st) != hipSuccess)
         return PIFA_ERR_HIP;
-    if (dX && launch_expand<false>({U, halves, At, (const bf16*)dX0, (bf16*)dX, d_in, d_out}, p, M, n, r, st) != hipSuccess)
+    if (dX && launch_expand<false>({U, halves, At, (const bf16*)dX0, (bf16*)dX, d_in, d_out}, p, M, n, r, target, st) != hipSuccess)
         return PIFA_ERR_HIP;
     if (!dA && !dB) return PIFA_OK;
     const AdapterGrads ga{(const bf16*)X, turned_u, dA, part_a, d_in, false};
     const AdapterGrads gb{(const bf16*)dY, turned_t, dB, part_b, d_out, true};
     {
         TimedLaunch timed(kSiteAdapterGrads, st);
-        const int64_t rp = adapter_rp(r), jb = std::min<int64_t>(4, rp / 16), width = adapter_max_tiles(M, n) * kAdTile;
+        const int64_t rp = adapter_rp(r), jb = std::min<int64_t>(4, rp / 16);
         const int64_t b0 = dA ? ceil_div(d_in, kAdCols) : 0, b1 = dB ? ceil_div(d_out, kAdCols) : 0;
         const dim3 grid((unsigned)(b0 + b1), (unsigned)adapter_max_pieces(M, n), (unsigned)ceil_div(rp, 16 * jb));
-        if (jb == 1) hipLaunchKernelGGL((adapter_grads<1>), grid, dim3(kAdThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r, width);
-        else if (jb == 2) hipLaunchKernelGGL((adapter_grads<2>), grid, dim3(kAdThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r, width);
-        else hipLaunchKernelGGL((adapter_grads<4>), grid, dim3(kAdThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r, width);
+        if (jb == 1) hipLaunchKernelGGL((adapter_grads<1>), grid, dim3(kAdGradThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r);
+        else if (jb == 2) hipLaunchKernelGGL((adapter_grads<2>), grid, dim3(kAdGradThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r);
+        else hipLaunchKernelGGL((adapter_grads<4>), grid, dim3(kAdGradThreads), 0, st, ga, gb, (int)b0, p, M, (int)n, r);
         if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
     }
     if (M > kAdPiece) {
