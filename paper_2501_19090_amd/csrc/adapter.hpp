@@ -487,159 +487,144 @@ struct AdapterExpand {
     int64_t K;            // that t was summed over
 };
 
-constexpr int kAdWide = 128;  // columns that a wave of expand takes
+constexpr int kAdWide = 128;  // columns that a workgroup of expand takes
 
-// A wave's columns c0 to c0 + 127 of the rows of G groups of 16 from g0 on.
-// Instruction u's column i is c0 + 8 i + u, so that a lane ends up with 8 columns in
-// a row and 16 neighbouring lanes with 256 bytes of each row of Y.  W's rows of
-// these columns are turned in LDS like the rows of shrink, KB blocks of 32 (KB = 0:
-// 16) columns of t at a time.  SUM: t is still in parts.  FULL: all columns are there.
-template <int KB, bool SUM, bool FULL, int G>
-__device__ __forceinline__ void adapter_expand_rows(const AdapterExpand& j, const int32_t* rows, int count, int g0,
-                                                    int64_t tile, int64_t c0, const bf16* W, u32x4* lds, int64_t r,
-                                                    int splits, int64_t stride) {
-    const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
-    constexpr int NB = KB > 0 ? KB : 1, CH = KB > 0 ? 4 * KB : 2;  // pieces of 8 columns of t in a row
-    constexpr int PITCH = CH + 1;
-    const int64_t rp = adapter_rp(r);
-    int64_t at[G][4];
-    u32x4 base[G][4];
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) at[g][e] = (int64_t)max(rows[16 * (g0 + g) + 4 * q + e], 0) * j.d;
-    if (j.base) {
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (FULL) base[g][e] = adapter_load(j.base + at[g][e] + c0 + 8 * i);
-                else base[g][e] = adapter_load8(j.base + at[g][e], min(c0 + 8 * i, j.d), j.d);
-            }
-    } else {
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) base[g][e] = zero16();
-    }
-    f32x4 acc[G][8];
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int u = 0; u < 8; ++u) acc[g][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int64_t k0 = 0; k0 < rp; k0 += 8 * CH) {
-        u32x4 wv[2 * CH];
-#pragma unroll
-        for (int k = 0; k < 2 * CH; ++k) {
-            const int col = (kWave * k + lane) / CH, c = (kWave * k + lane) % CH;
-            const bf16* row = W + min(c0 + col, j.d - 1) * r;
-            const int64_t from = k0 + 8 * c;
-            if (r % 8 != 0) {
-                wv[k] = adapter_load8(row, from, r);
-            } else {
-                wv[k] = adapter_load(row + (from < r ? from : 0));
-                if (from >= r) wv[k] = zero16();
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < 2 * CH; ++k) {
-            const int col = (kWave * k + lane) / CH, c = (kWave * k + lane) % CH;
-            lds[(col % 8 * 16 + col / 8) * PITCH + c] = wv[k];
-        }
-        u32x4 w[NB][8];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int u = 0; u < 8; ++u) w[b][u] = lds[(u * 16 + i) * PITCH + (KB == 0 ? q & 1 : 4 * b + q)];
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const int64_t group = 4 * tile + g0 + g;
-            u32x4 hi[NB], lo[NB];
-            if constexpr (SUM) {
-                const float* t = j.T + (16 * group + min(i, count - 1 - 16 * (g0 + g))) * rp + k0;
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const int64_t k = KB == 0 ? 8 * (q & 1) : 32 * b + 8 * q;
-                    const f32x4 x = adapter_t4(t + k, splits, stride), y = adapter_t4(t + k + 4, splits, stride);
-                    bf16x8 h, l;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        bf16 s[2];
-                        adapter_split2(e < 4 ? x[e % 4] : y[e % 4], s[0], s[1]);
-                        h[e] = s[0];
-                        l[e] = s[1];
-                    }
-                    hi[b] = __builtin_bit_cast(u32x4, h);
-                    lo[b] = __builtin_bit_cast(u32x4, l);
-                }
-                if constexpr (KB == 0) hi[0] = q < 2 ? hi[0] : lo[0];
-            } else {
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    hi[b] = j.halves[adapter_half_at(group, rp, k0 / 32 + b, 0) + lane];
-                    if constexpr (KB != 0) lo[b] = j.halves[adapter_half_at(group, rp, k0 / 32 + b, 1) + lane];
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    acc[g][u] = adapter_mfma(hi[b], w[b][u], acc[g][u]);
-                    if constexpr (KB != 0) acc[g][u] = adapter_mfma(lo[b], w[b][u], acc[g][u]);
-                }
-        }
-    }
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (16 * (g0 + g) + 4 * q + e >= count) continue;
-            const bf16x8 b = __builtin_bit_cast(bf16x8, base[g][e]);
-            bf16x8 y;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) y[u] = (bf16)((float)b[u] + acc[g][u][e]);
-            const int64_t c = c0 + 8 * i;
-            bf16* to = j.out + at[g][e] + c;
-            if (FULL || c + 8 <= j.d) {
-                reinterpret_cast<AdapterAny16*>(to)->v = __builtin_bit_cast(u32x4, y);
-            } else {
-#pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    if (c + u < j.d) to[u] = y[u];
-            }
-        }
-}
-
-// Workgroups: x: 128 columns a wave, y: tiles (those of rows without an adapter
-// last, which are copied), z: the tile's groups of 16 rows, G each.  KB: as above, for
-// ranks of up to 16 (0), 32 (1) and 64 at a time (2).
-template <int KB, bool SUM, int G>
-__global__ __launch_bounds__(kAdThreads, SUM ? 1 : 2) void adapter_expand(AdapterExpand j, AdapterPlan p, int64_t M, int n, int64_t r,
-                                                             int target) {
-    __shared__ u32x4 lds[kAdWaves][kAdWide * (KB > 0 ? 4 * KB + 1 : 3)];
+// Workgroups: x: 128 columns, y: tiles (those of rows without an adapter last, which
+// are copied); a wave for each of the tile's groups of 16 rows.  Instruction u's
+// column i is c0 + 8 i + u, so that a lane ends up with 8 columns in a row and 16
+// neighbouring lanes with 256 bytes of each row of Y.  The waves share W's rows of
+// these columns, which go through LDS in the order of the operands, KB blocks of 32
+// columns of t at a time; 0: up to 16 columns, both halves of t in one instruction.
+// (W in registers, 64 rows a wave: eight waves a CU instead of twenty, and 1999 rows
+// of 11008 with rank 64 take 30 us.)  SUM: t is still in parts.  FULL: all
+// columns of every workgroup are there.
+template <int KB, bool SUM, bool FULL>
+__global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(AdapterExpand j, AdapterPlan p, int64_t M, int n,
+                                                                          int64_t r, int target) {
+    constexpr int NB = KB > 0 ? KB : 1, CH = KB > 0 ? 4 * KB : 2;  // pieces of 8 columns of t in a row of LDS
+    constexpr int PITCH = CH + 1, PIECES = kAdWide * CH / kAdThreads;
+    __shared__ u32x4 lds[kAdWide * PITCH];
     const AdapterHeader h = *p.head;
     const AdapterTile tile = p.tiles[blockIdx.y];
-    const int g0 = blockIdx.z * G, wave = threadIdx.x >> 6;
-    if (h.M != M || h.n != n || (int)blockIdx.y >= h.tiles_all || 16 * g0 >= tile.count) return;
-    const int64_t c0 = ((int64_t)blockIdx.x * kAdWaves + wave) * kAdWide;
+    if (h.M != M || h.n != n || (int)blockIdx.y >= h.tiles_all) return;
+    const int64_t c0 = (int64_t)blockIdx.x * kAdWide;
     if (c0 >= j.d) return;
     const int32_t* rows = p.rows + (int64_t)blockIdx.y * kAdTile;
     if (tile.adapter >= n) {
         if (j.out == j.base) return;
-        for (int m = 16 * g0; m < min(tile.count, 16 * (g0 + G)); ++m)
-            for (int64_t c = c0 + (threadIdx.x & 63); c < min(c0 + kAdWide, j.d); c += kWave) {
-                const int64_t at = (int64_t)rows[m] * j.d + c;
-                ((uint16_t*)j.out)[at] = j.base ? ((const uint16_t*)j.base)[at] : (uint16_t)0;
-            }
+        const int64_t c = c0 + threadIdx.x % kAdWide;
+        if (c >= j.d) return;
+        for (int m = threadIdx.x / kAdWide; m < tile.count; m += kAdThreads / kAdWide) {
+            const int64_t at = (int64_t)rows[m] * j.d + c;
+            ((uint16_t*)j.out)[at] = j.base ? ((const uint16_t*)j.base)[at] : (uint16_t)0;
+        }
         return;
     }
-    const bf16* W = j.W + (int64_t)tile.adapter * j.d * r;
+    const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    const int64_t rp = adapter_rp(r), c = c0 + 8 * i;
+    const bool live = 16 * g < tile.count;  // of the wave
+    const bool add = j.base != nullptr;
+    const bf16* from = add ? j.base : j.out;
+    int row[4];
+    {
+        const int4 four = *reinterpret_cast<const int4*>(rows + 16 * g + 4 * q);
+        row[0] = four.x, row[1] = four.y, row[2] = four.z, row[3] = four.w;
+    }
+    // t's operands
     const int splits = SUM ? adapter_splits(h.tiles, j.K, target) : 1;
-    const int64_t stride = (int64_t)h.tiles * kAdTile * adapter_rp(r);
-    if (c0 + kAdWide <= j.d)
-        adapter_expand_rows<KB, SUM, true, G>(j, rows, tile.count, g0, blockIdx.y, c0, W, lds[wave], r, splits, stride);
-    else
-        adapter_expand_rows<KB, SUM, false, G>(j, rows, tile.count, g0, blockIdx.y, c0, W, lds[wave], r, splits, stride);
+    const int64_t group = 4 * (int64_t)blockIdx.y + g;
+    u32x4 hi[NB], lo[NB];
+    auto operands = [&](int64_t k0) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            if constexpr (SUM) {
+                const float* t = j.T + (16 * group + min(i, max(0, tile.count - 1 - 16 * g))) * rp + k0 +
+                                 (KB == 0 ? 8 * (q & 1) : 32 * b + 8 * q);
+                const int64_t stride = (int64_t)h.tiles * kAdTile * rp;
+                const f32x4 x = adapter_t4(t, splits, stride), y = adapter_t4(t + 4, splits, stride);
+                bf16x8 v[2];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    bf16 s[2];
+                    adapter_split2(e < 4 ? x[e % 4] : y[e % 4], s[0], s[1]);
+                    v[0][e] = s[0];
+                    v[1][e] = s[1];
+                }
+                hi[b] = __builtin_bit_cast(u32x4, v[0]);
+                lo[b] = __builtin_bit_cast(u32x4, v[1]);
+                if constexpr (KB == 0) hi[0] = q < 2 ? hi[0] : lo[0];
+            } else {
+                hi[b] = j.halves[adapter_half_at(group, rp, k0 / 32 + b, 0) + lane];
+                if constexpr (KB != 0) lo[b] = j.halves[adapter_half_at(group, rp, k0 / 32 + b, 1) + lane];
+            }
+        }
+    };
+    // W's rows of the workgroup's columns: thread's piece k is 8 columns of t of one of them
+    const bf16* W = j.W + (int64_t)tile.adapter * j.d * r;
+    u32x4 piece[PIECES];
+    auto column = [&](int k) { return (k * kAdThreads + (int)threadIdx.x) / CH; };
+    auto pieces = [&](int64_t k0) {
+        const int64_t at = k0 + 8 * (threadIdx.x % CH);
+        if (r % 8 == 0) {
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) piece[k] = adapter_load(W + min(c0 + column(k), j.d - 1) * r + (at < r ? at : 0));
+        } else {
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) piece[k] = adapter_load8(W + min(c0 + column(k), j.d - 1) * r, at, r);
+        }
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) piece[k] = at < r ? piece[k] : zero16();
+    };
+    operands(0);
+    pieces(0);
+    u32x4 base[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const bf16* at = from + (int64_t)max(row[e], 0) * j.d;
+        if constexpr (FULL) base[e] = adapter_load(at + c);
+        else base[e] = adapter_load8(at, min(c, j.d), j.d);
+    }
+    f32x4 acc[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int64_t k0 = 0;;) {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+            lds[(column(k) % 8 * 16 + column(k) / 8) * PITCH + threadIdx.x % CH] = piece[k];
+        __syncthreads();
+        if (live) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const u32x4 w = lds[(u * 16 + i) * PITCH + (KB == 0 ? q & 1 : 4 * b + q)];
+                    acc[u] = adapter_mfma(hi[b], w, acc[u]);
+                    if constexpr (KB != 0) acc[u] = adapter_mfma(lo[b], w, acc[u]);
+                }
+        }
+        k0 += 8 * CH;
+        if (k0 >= rp) break;
+        operands(k0);
+        pieces(k0);
+        __syncthreads();
+    }
+    if (!live) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const bf16x8 b = __builtin_bit_cast(bf16x8, base[e]);
+        bf16x8 y;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) y[u] = (bf16)((add ? (float)b[u] : 0.f) + acc[u][e]);
+        if (row[e] < 0) continue;
+        bf16* to = j.out + (int64_t)row[e] * j.d + c;
+        if (FULL || c + 8 <= j.d) {
+            reinterpret_cast<AdapterAny16*>(to)->v = __builtin_bit_cast(u32x4, y);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (c + u < j.d) to[u] = y[u];
+        }
+    }
 }
 
 // ------------------------------------------------------------------ backward

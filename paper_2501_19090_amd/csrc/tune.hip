@@ -184,12 +184,12 @@ hipError_t launch_expand(const AdapterExpand& a, const AdapterPlan& p, int64_t M
                          hipStream_t st) {
     TimedLaunch timed(kSiteAdapterExpand, st);
     // columns keep to their XCD over the tiles, so that it reads only its part of W
-    const int64_t blocks = ceil_div(a.d, kAdWaves * kAdWide);
-    const unsigned x = (unsigned)(blocks > 8 ? round_up(blocks, 8) : blocks), y = (unsigned)adapter_max_tiles(M, n);
+    const int64_t blocks = ceil_div(a.d, kAdWide);
+    const dim3 grid((unsigned)(blocks > 8 ? round_up(blocks, 8) : blocks), (unsigned)adapter_max_tiles(M, n));
     auto launch = [&](auto kb) {
         constexpr int KB = decltype(kb)::value;
-        if constexpr (SUM) hipLaunchKernelGGL((adapter_expand<KB, SUM, 1>), dim3(x, y, 4), dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
-        else hipLaunchKernelGGL((adapter_expand<KB, SUM, 2>), dim3(x, y, 2), dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
+        if (a.d % kAdWide == 0) hipLaunchKernelGGL((adapter_expand<KB, SUM, true>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
+        else hipLaunchKernelGGL((adapter_expand<KB, SUM, false>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
     };
     using std::integral_constant;
     if (r <= 16) launch(integral_constant<int, 0>{});
