@@ -29,8 +29,10 @@ constexpr int kAdPiece = kAdTile * kAdPieceTiles;
 constexpr int kAdMaxSlots = 4096;
 constexpr int64_t kAdMaxRows = 1 << 20;
 constexpr int kAdMaxSplit = 8;     // of K
-constexpr int kAdThreads = 256;    // of shrink and expand
-constexpr int kAdWaves = kAdThreads / kWave;
+constexpr int kAdThreads = 256;    // of expand
+// Waves of shrink: as many as have room in a CU's LDS twice (ranks of up to 16:
+// 18.7 us with eight, 20.1 with four, 4096 rows of 4096; of 64: 15.8 and 13.2, 1999).
+__host__ __device__ constexpr int adapter_waves(int64_t r) { return r <= 32 ? 8 : 4; }
 constexpr int kAdSlice = 64;       // columns that a wave of shrink takes at a time
 
 // ------------------------------------------------------------------ plan
@@ -250,10 +252,10 @@ __device__ __forceinline__ f32x4 adapter_mfma(u32x4 a, u32x4 b, f32x4 c) {
 
 // How many workgroups share a tile's K: as many as leave all of them, `target` at
 // most, on the chip at once.
-__host__ __device__ inline int adapter_splits(int tiles, int64_t K, int target) {
+__host__ __device__ inline int adapter_splits(int tiles, int64_t K, int64_t r, int target) {
     int s = tiles > 0 ? target / tiles : 1;
     if (s > kAdMaxSplit) s = kAdMaxSplit;
-    const int64_t most = ceil_div(K, kAdSlice) / kAdWaves;  // a slice for every wave
+    const int64_t most = ceil_div(K, kAdSlice) / adapter_waves(r);  // a slice for every wave
     if (s > most) s = (int)most;
     return s < 1 ? 1 : s;
 }
@@ -271,7 +273,7 @@ struct AdapterShrink {
 };
 
 // A tile's rows (RG groups of 16) times 16 JB of an adapter's; slices s0 to s1 of
-// 64 columns, a wave taking every fourth.  The matrix instruction's operands have a
+// 64 columns, the waves taking them in turn.  The matrix instruction's operands have a
 // row in each of 16 neighbouring lanes, which the caches would serve one by one; so
 // a wave loads lines of 128 bytes, eight neighbouring lanes each, and turns them in
 // LDS of its own (16-byte places of a row exchanged by its number, so that
@@ -281,6 +283,7 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
                                                     int64_t r, int j0, int64_t s0, int64_t s1, int64_t rp, float* out,
                                                     u32x4* lds) {
     constexpr int NX = 2 * RG, NW = 2 * JB;  // loads of a slice: 8 rows each
+    constexpr int WAVES = adapter_waves(16 * JB);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int row8 = lane >> 3, c8 = lane & 7;
     const bf16* x[NX];
@@ -325,18 +328,18 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
         }
     };
     const int64_t whole = min(s1, j.K / kAdSlice);  // slices of 64 full columns
-    const int64_t first = s0 + wave, count = first < whole ? (whole - first + kAdWaves - 1) / kAdWaves : 0;
+    const int64_t first = s0 + wave, count = first < whole ? (whole - first + WAVES - 1) / WAVES : 0;
     if (count > 0) {
-        const int64_t last = first + (count - 1) * kAdWaves;
+        const int64_t last = first + (count - 1) * WAVES;
         load(first);
         for (int64_t c = 0; c < count; ++c) {
             turn();
-            load(min(first + (c + 1) * kAdWaves, last));
+            load(min(first + (c + 1) * WAVES, last));
             __builtin_amdgcn_sched_barrier(0);
             multiply();
         }
     }
-    if (const int64_t s = first + count * kAdWaves; s < s1) {  // the row's last columns
+    if (const int64_t s = first + count * WAVES; s < s1) {  // the row's last columns
 #pragma unroll
         for (int k = 0; k < NX; ++k) f[k] = adapter_load8(x[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
 #pragma unroll
@@ -356,27 +359,27 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
 #pragma unroll
             for (int e = 0; e < 4; ++e) part[((wave * RG + g) * 16 + 4 * q + e) * COLS + 16 * b + i] = acc[g][b][e];
     __syncthreads();
-    for (int at = threadIdx.x; at < 16 * RG * COLS; at += kAdThreads) {
+    for (int at = threadIdx.x; at < 16 * RG * COLS; at += WAVES * kWave) {
         const int row = at / COLS, col = j0 + at % COLS;
         float v = 0.f;
 #pragma unroll
-        for (int u = 0; u < kAdWaves; ++u) v += part[u * 16 * RG * COLS + at];
+        for (int u = 0; u < WAVES; ++u) v += part[u * 16 * RG * COLS + at];
         if (row < tile.count) out[(int64_t)row * rp + col] = col < r ? v * scale : 0.f;
     }
 }
 
 // Workgroups: x: tiles, y: parts of K, z: blocks of 16 JB columns of t, jobs outermost.
 template <int JB>
-__global__ __launch_bounds__(kAdThreads, 2) void adapter_shrink(AdapterShrink j0, AdapterShrink j1, AdapterPlan p, int64_t M,
+__global__ __launch_bounds__(adapter_waves(16 * JB) * kWave, JB == 4 ? 2 : 1) void adapter_shrink(AdapterShrink j0, AdapterShrink j1, AdapterPlan p, int64_t M,
                                                              int n, int64_t r, int target) {
-    __shared__ u32x4 lds[kAdWaves * (8 + 2 * JB) * kWave];
+    __shared__ u32x4 lds[adapter_waves(16 * JB) * (8 + 2 * JB) * kWave];
     const AdapterHeader h = *p.head;
     const AdapterTile tile = p.tiles[blockIdx.x];
     if (h.M != M || h.n != n || (int)blockIdx.x >= h.tiles) return;
     const int64_t rp = adapter_rp(r);
     const int cols = (int)ceil_div(rp, 16 * JB), job = blockIdx.z / cols, c0 = (blockIdx.z % cols) * 16 * JB;
     const AdapterShrink j = job ? j1 : j0;
-    const int splits = adapter_splits(h.tiles, j.K, target);
+    const int splits = adapter_splits(h.tiles, j.K, r, target);
     if ((int)blockIdx.y >= splits) return;
     const int64_t slices = ceil_div(j.K, kAdSlice);
     const int64_t each = ceil_div(slices, splits), s0 = each * blockIdx.y, s1 = min(s0 + each, slices);
@@ -439,7 +442,7 @@ static __global__ __launch_bounds__(256) void adapter_finish(AdapterFinish j0, A
     const int t = threadIdx.x, y = blockIdx.y;
     {
         const int row = t >> 2, c = (t & 3) * 4;
-        f32x4 v = adapter_t4(j.T + (x * kAdTile + row) * rp + 16 * y + c, adapter_splits(h.tiles, j.K, target),
+        f32x4 v = adapter_t4(j.T + (x * kAdTile + row) * rp + 16 * y + c, adapter_splits(h.tiles, j.K, r, target),
                              (int64_t)h.tiles * kAdTile * rp);
 #pragma unroll
         for (int e = 0; e < 4; ++e) lds[row][c + e] = row < tile.count ? v[e] : 0.f;
@@ -531,7 +534,7 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
         row[0] = four.x, row[1] = four.y, row[2] = four.z, row[3] = four.w;
     }
     // t's operands
-    const int splits = SUM ? adapter_splits(h.tiles, j.K, target) : 1;
+    const int splits = SUM ? adapter_splits(h.tiles, j.K, r, target) : 1;
     const int64_t group = 4 * (int64_t)blockIdx.y + g;
     u32x4 hi[NB], lo[NB];
     auto operands = [&](int64_t k0) {

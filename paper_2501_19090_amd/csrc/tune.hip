@@ -113,7 +113,7 @@ namespace {
 
 constexpr int64_t kAdMaxD = 1 << 19, kAdMaxRank = 1024;
 // Workgroups of a shrink that the chip holds at once, for one or two jobs.
-int adapter_target(int64_t r, int jobs) { return (int)((r <= 16 ? 4 : r <= 32 ? 3 : 2) * kCus / jobs); }
+int adapter_target(int64_t r, int jobs) { return (int)((r > 16 && r <= 32 ? 1 : 2) * kCus / jobs); }
 
 pifa_status check_plan(int64_t M, int64_t n) {
     if (M < 0 || n < 1) return PIFA_ERR_INVALID_ARG;
@@ -161,12 +161,13 @@ hipError_t launch_shrink(const AdapterShrink& a, const AdapterShrink* b, const A
                          int64_t r, int target, hipStream_t st) {
     TimedLaunch timed(kSiteAdapterShrink, st);
     const int64_t rp = adapter_rp(r), jb = std::min<int64_t>(4, rp / 16), most = std::max(a.K, b ? b->K : 0);
-    const dim3 grid((unsigned)adapter_max_tiles(M, n), (unsigned)adapter_splits(1, most, target),
+    const dim3 grid((unsigned)adapter_max_tiles(M, n), (unsigned)adapter_splits(1, most, r, target),
                     (unsigned)(ceil_div(rp, 16 * jb) * (b ? 2 : 1)));
+    const dim3 block((unsigned)adapter_waves(r) * kWave);
     const AdapterShrink& second = b ? *b : a;
-    if (jb == 1) hipLaunchKernelGGL((adapter_shrink<1>), grid, dim3(kAdThreads), 0, st, a, second, p, M, (int)n, r, target);
-    else if (jb == 2) hipLaunchKernelGGL((adapter_shrink<2>), grid, dim3(kAdThreads), 0, st, a, second, p, M, (int)n, r, target);
-    else hipLaunchKernelGGL((adapter_shrink<4>), grid, dim3(kAdThreads), 0, st, a, second, p, M, (int)n, r, target);
+    if (jb == 1) hipLaunchKernelGGL((adapter_shrink<1>), grid, block, 0, st, a, second, p, M, (int)n, r, target);
+    else if (jb == 2) hipLaunchKernelGGL((adapter_shrink<2>), grid, block, 0, st, a, second, p, M, (int)n, r, target);
+    else hipLaunchKernelGGL((adapter_shrink<4>), grid, block, 0, st, a, second, p, M, (int)n, r, target);
     return hipGetLastError();
 }
 
