@@ -499,9 +499,9 @@ constexpr int kAdWide = 128;  // columns that a workgroup of expand takes
 // these columns, which go through LDS in the order of the operands, KB blocks of 32
 // columns of t at a time; 0: up to 16 columns, both halves of t in one instruction.
 // (W in registers, 64 rows a wave: eight waves a CU instead of twenty, and 1999 rows
-// of 11008 with rank 64 take 30 us.)  SUM: t is still in parts.  FULL: all
-// columns of every workgroup are there.
-template <int KB, bool SUM, bool FULL>
+// of 11008 with rank 64 take 30 us.)  ONE: those blocks are all.  SUM: t is still in
+// parts.  FULL: all columns of every workgroup are there.
+template <int KB, bool ONE, bool SUM, bool FULL>
 __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(AdapterExpand j, AdapterPlan p, int64_t M, int n,
                                                                           int64_t r, int target) {
     constexpr int NB = KB > 0 ? KB : 1, CH = KB > 0 ? 4 * KB : 2;  // pieces of 8 columns of t in a row of LDS
@@ -579,7 +579,6 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
         for (int k = 0; k < PIECES; ++k) piece[k] = at < r ? piece[k] : zero16();
     };
     operands(0);
-    pieces(0);
     u32x4 base[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -587,6 +586,7 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
         if constexpr (FULL) base[e] = adapter_load(at + c);
         else base[e] = adapter_load8(at, min(c, j.d), j.d);
     }
+    pieces(0);
     f32x4 acc[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -605,6 +605,7 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
                     if constexpr (KB != 0) acc[u] = adapter_mfma(lo[b], w, acc[u]);
                 }
         }
+        if constexpr (ONE) break;
         k0 += 8 * CH;
         if (k0 >= rp) break;
         operands(k0);
@@ -690,8 +691,8 @@ constexpr int kAdGradThreads = 512, kAdGradWaves = kAdGradThreads / kWave;
 template <int JB>
 __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0, AdapterGrads j1, int blocks0, AdapterPlan p,
                                                             int64_t M, int n, int64_t r) {
-    constexpr int COLS = 16 * JB;
-    __shared__ float part[2][kAdGradWaves][16 * COLS];
+    constexpr int COLS = 16 * JB, ROUND = 8 / JB;  // operands whose sums LDS holds at once
+    __shared__ float part[ROUND][kAdGradWaves][16 * COLS];
     __shared__ float sums[COLS][kAdCols + 1];
     const AdapterHeader h = *p.head;
     const AdapterPiece piece = p.pieces[blockIdx.y];
@@ -747,17 +748,21 @@ __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0,
     }
     // the waves' sums: acc[k][b], row 4 q + e is column 8 (4 q + e) + k of P, column i is column 16 b + i of t
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k0 = 0; k0 < 8; k0 += ROUND) {
+        if (k0 > 0) __syncthreads();
 #pragma unroll
-        for (int b = 0; b < JB; ++b)
+        for (int k = 0; k < ROUND; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[k & 1][wave][(4 * q + e) * COLS + 16 * b + i] = acc[k][b][e];
+            for (int b = 0; b < JB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[k][wave][(4 * q + e) * COLS + 16 * b + i] = acc[k0 + k][b][e];
         __syncthreads();
-        for (int at = threadIdx.x; at < 16 * COLS; at += kAdGradThreads) {
+        for (int at = threadIdx.x; at < ROUND * 16 * COLS; at += kAdGradThreads) {
+            const int k = at / (16 * COLS), cell = at % (16 * COLS);
             float v = 0.f;
 #pragma unroll
-            for (int u = 0; u < kAdGradWaves; ++u) v += part[k & 1][u][at];
-            sums[at % COLS][8 * (at / COLS) + k] = v;
+            for (int u = 0; u < kAdGradWaves; ++u) v += part[k][u][cell];
+            sums[cell % COLS][8 * (cell / COLS) + k0 + k] = v;
         }
     }
     __syncthreads();

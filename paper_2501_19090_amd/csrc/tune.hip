@@ -187,15 +187,19 @@ hipError_t launch_expand(const AdapterExpand& a, const AdapterPlan& p, int64_t M
     // columns keep to their XCD over the tiles, so that it reads only its part of W
     const int64_t blocks = ceil_div(a.d, kAdWide);
     const dim3 grid((unsigned)(blocks > 8 ? round_up(blocks, 8) : blocks), (unsigned)adapter_max_tiles(M, n));
-    auto launch = [&](auto kb) {
+    auto launch = [&](auto kb, auto one) {
         constexpr int KB = decltype(kb)::value;
-        if (a.d % kAdWide == 0) hipLaunchKernelGGL((adapter_expand<KB, SUM, true>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
-        else hipLaunchKernelGGL((adapter_expand<KB, SUM, false>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
+        constexpr bool ONE = decltype(one)::value;
+        if (a.d % kAdWide == 0)
+            hipLaunchKernelGGL((adapter_expand<KB, ONE, SUM, true>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
+        else
+            hipLaunchKernelGGL((adapter_expand<KB, ONE, SUM, false>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
     };
     using std::integral_constant;
-    if (r <= 16) launch(integral_constant<int, 0>{});
-    else if (r <= 32) launch(integral_constant<int, 1>{});
-    else launch(integral_constant<int, 2>{});
+    if (r <= 16) launch(integral_constant<int, 0>{}, std::true_type{});
+    else if (r <= 32) launch(integral_constant<int, 1>{}, std::true_type{});
+    else if (r <= 64) launch(integral_constant<int, 2>{}, std::true_type{});
+    else launch(integral_constant<int, 2>{}, std::false_type{});
     return hipGetLastError();
 }
 
