@@ -8,7 +8,7 @@
 // every layer's call goes by it.  The products run on matrix instructions of 16 x
 // 16 x 32 bf16 values; the ranks are small, so that all of them are bound by the
 // rows that they stream, wherever these stand in X and Y.
-//   shrink: rows times A^T (or B), in waves that take 32 columns in turn; K is cut
+//   shrink: rows times A^T (or B), in waves that take 64 columns in turn; K is cut
 //           over workgroups too, as far as the chip is not full of tiles.
 //   finish: the parts' sums, rounded as the next products read them.
 //   expand: t times B^T (or u times A) onto the rows of Y0.
@@ -250,6 +250,11 @@ __device__ __forceinline__ f32x4 adapter_mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Two rows' values in a register each: the lower or the upper ones of both.
+__device__ __forceinline__ uint32_t adapter_pair(uint32_t even, uint32_t odd, int half) {
+    return __builtin_amdgcn_perm(odd, even, half ? 0x07060302u : 0x05040100u);
+}
+
 // How many workgroups share a tile's K: as many as leave all of them, `target` at
 // most, on the chip at once.
 __host__ __device__ inline int adapter_splits(int tiles, int64_t K, int64_t r, int target) {
@@ -266,7 +271,8 @@ __host__ __device__ inline int64_t adapter_rp(int64_t r) { return r <= 16 ? 16 :
 // ------------------------------------------------------------------ shrink
 struct AdapterShrink {
     const bf16* P;       // rows (M x K)
-    const bf16* W;       // n x r x K
+    const bf16* W;       // n x r x K, or
+    bool by_column;      // n x K x r
     const float* scale;  // or null: ones
     float* T;            // splits x 64 tiles x rp
     int64_t K;
@@ -278,7 +284,11 @@ struct AdapterShrink {
 // a wave loads lines of 128 bytes, eight neighbouring lanes each, and turns them in
 // LDS of its own (16-byte places of a row exchanged by its number, so that
 // neighbouring rows' are in other banks).  The next slice is on its way meanwhile.
-template <int JB, int RG>
+// COL: the adapter's columns lie in the rows of W; a lane takes eight of them from
+// 2 JB neighbouring rows and turns these round first.  Columns past the rank come
+// from the rows behind and are left out of t; slices whose rows have not enough
+// rows behind them are loaded value by value.
+template <int JB, int RG, bool COL>
 __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, const int32_t* rows, const AdapterTile tile,
                                                     int64_t r, int j0, int64_t s0, int64_t s1, int64_t rp, float* out,
                                                     u32x4* lds) {
@@ -290,9 +300,11 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
     const bf16* w[NW];
 #pragma unroll
     for (int k = 0; k < NX; ++k) x[k] = j.P + (int64_t)rows[min(8 * k + row8, tile.count - 1)] * j.K + 8 * c8;
+    const int piece = lane % NW, group = lane / NW;  // COL: columns 8 piece on, of rows NW group on
 #pragma unroll
     for (int k = 0; k < NW; ++k)
-        w[k] = j.W + ((int64_t)tile.adapter * r + min((int64_t)(j0 + 8 * k + row8), r - 1)) * j.K + 8 * c8;
+        w[k] = j.W + (COL ? ((int64_t)tile.adapter * j.K + NW * group + k) * r + j0 + 8 * piece
+                          : ((int64_t)tile.adapter * r + min((int64_t)(j0 + 8 * k + row8), r - 1)) * j.K + 8 * c8);
     f32x4 acc[RG][JB];
 #pragma unroll
     for (int g = 0; g < RG; ++g)
@@ -304,13 +316,26 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
 #pragma unroll
         for (int k = 0; k < NX; ++k) f[k] = adapter_load(x[k] + kAdSlice * s);
 #pragma unroll
-        for (int k = 0; k < NW; ++k) f[NX + k] = adapter_load(w[k] + kAdSlice * s);
+        for (int k = 0; k < NW; ++k) f[NX + k] = adapter_load(w[k] + kAdSlice * s * (COL ? r : 1));
     };
     auto turn = [&] {
 #pragma unroll
-        for (int k = 0; k < NX + NW; ++k) {
+        for (int k = 0; k < (COL ? NX : NX + NW); ++k) {
             const int row = 8 * k + row8;
             mine[row * 8 + (c8 ^ (row >> 1 & 7))] = f[k];
+        }
+        if constexpr (COL) {
+            struct alignas(2 * NW) Run {  // of a column, NW rows
+                uint32_t v[NW / 2];
+            };
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                Run v;
+#pragma unroll
+                for (int k = 0; k < NW / 2; ++k) v.v[k] = adapter_pair(f[NX + 2 * k][e / 2], f[NX + 2 * k + 1][e / 2], e & 1);
+                const int row = 8 * piece + e, at = NW * group;
+                *((Run*)(mine + (8 * NX + row) * 8 + ((at / 8) ^ (row >> 1 & 7))) + at % 8 / NW) = v;
+            }
         }
     };
     auto multiply = [&] {
@@ -327,7 +352,9 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
                 for (int k = 0; k < JB; ++k) acc[g][k] = adapter_mfma(a[g], b[k], acc[g][k]);
         }
     };
-    const int64_t whole = min(s1, j.K / kAdSlice);  // slices of 64 full columns
+    // slices of 64 full columns; behind, one or two for different waves
+    const int64_t behind = COL ? max((int64_t)0, ceil_div(j0 + 16 * JB, r) - 1) : 0;
+    const int64_t whole = min(s1, max((int64_t)0, j.K - behind) / kAdSlice);
     const int64_t first = s0 + wave, count = first < whole ? (whole - first + WAVES - 1) / WAVES : 0;
     if (count > 0) {
         const int64_t last = first + (count - 1) * WAVES;
@@ -343,7 +370,14 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
 #pragma unroll
         for (int k = 0; k < NX; ++k) f[k] = adapter_load8(x[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
 #pragma unroll
-        for (int k = 0; k < NW; ++k) f[NX + k] = adapter_load8(w[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
+        for (int k = 0; k < NW; ++k) {
+            if constexpr (COL) {
+                const bool there = kAdSlice * s + NW * group + k < j.K;
+                f[NX + k] = adapter_load8(w[k] - j0 - 8 * piece + (there ? kAdSlice * s * r : 0), there ? j0 + 8 * piece : r, r);
+            } else {
+                f[NX + k] = adapter_load8(w[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
+            }
+        }
         turn();
         multiply();
     }
@@ -385,8 +419,13 @@ __global__ __launch_bounds__(adapter_waves(16 * JB) * kWave, JB == 4 ? 2 : 1) vo
     const int64_t each = ceil_div(slices, splits), s0 = each * blockIdx.y, s1 = min(s0 + each, slices);
     const int32_t* rows = p.rows + (int64_t)blockIdx.x * kAdTile;
     float* out = j.T + ((int64_t)blockIdx.y * h.tiles + blockIdx.x) * kAdTile * rp;
-    if (tile.count <= 16) adapter_shrink_tile<JB, 1>(j, rows, tile, r, c0, s0, s1, rp, out, lds);
-    else adapter_shrink_tile<JB, 4>(j, rows, tile, r, c0, s0, s1, rp, out, lds);
+    if (j.by_column) {
+        if (tile.count <= 16) adapter_shrink_tile<JB, 1, true>(j, rows, tile, r, c0, s0, s1, rp, out, lds);
+        else adapter_shrink_tile<JB, 4, true>(j, rows, tile, r, c0, s0, s1, rp, out, lds);
+    } else {
+        if (tile.count <= 16) adapter_shrink_tile<JB, 1, false>(j, rows, tile, r, c0, s0, s1, rp, out, lds);
+        else adapter_shrink_tile<JB, 4, false>(j, rows, tile, r, c0, s0, s1, rp, out, lds);
+    }
 }
 
 // ------------------------------------------------------------------ finish
@@ -483,7 +522,7 @@ static __global__ __launch_bounds__(256) void adapter_finish(AdapterFinish j0, A
 struct AdapterExpand {
     const float* T;       // splits x 64 tiles x rp, or
     const u32x4* halves;  // as finish leaves them
-    const bf16* W;        // n x d x r
+    const bf16* W;        // n x d x r (COL: n x r x d)
     const bf16* base;     // or null: zeros
     bf16* out;            // M x d; may be base
     int64_t d;
@@ -500,12 +539,13 @@ constexpr int kAdWide = 128;  // columns that a workgroup of expand takes
 // columns of t at a time; 0: up to 16 columns, both halves of t in one instruction.
 // (W in registers, 64 rows a wave: eight waves a CU instead of twenty, and 1999 rows
 // of 11008 with rank 64 take 30 us.)  ONE: those blocks are all.  SUM: t is still in
-// parts.  FULL: all columns of every workgroup are there.
-template <int KB, bool ONE, bool SUM, bool FULL>
+// parts.  COL: W's rows are the columns of t; a thread takes 8 columns of 8 of them
+// and turns them round.  FULL: all columns of every workgroup are there.
+template <int KB, bool ONE, bool SUM, bool COL, bool FULL>
 __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(AdapterExpand j, AdapterPlan p, int64_t M, int n,
                                                                           int64_t r, int target) {
     constexpr int NB = KB > 0 ? KB : 1, CH = KB > 0 ? 4 * KB : 2;  // pieces of 8 columns of t in a row of LDS
-    constexpr int PITCH = CH + 1, PIECES = kAdWide * CH / kAdThreads;
+    constexpr int PITCH = CH + 1, PIECES = COL ? 8 : kAdWide * CH / kAdThreads;
     __shared__ u32x4 lds[kAdWide * PITCH];
     const AdapterHeader h = *p.head;
     const AdapterTile tile = p.tiles[blockIdx.y];
@@ -562,21 +602,55 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
             }
         }
     };
-    // W's rows of the workgroup's columns: thread's piece k is 8 columns of t of one of them
+    // W's values for the workgroup's columns: thread's piece k is 8 columns of t of one
+    // of them (COL: 8 of them, of one column of t)
     const bf16* W = j.W + (int64_t)tile.adapter * j.d * r;
     u32x4 piece[PIECES];
-    auto column = [&](int k) { return (k * kAdThreads + (int)threadIdx.x) / CH; };
+    const int tc = threadIdx.x / CH, th = threadIdx.x % CH;
     auto pieces = [&](int64_t k0) {
-        const int64_t at = k0 + 8 * (threadIdx.x % CH);
-        if (r % 8 == 0) {
+        const int64_t at = k0 + 8 * th;
+        if constexpr (COL) {
+            if (tc >= 16) return;
 #pragma unroll
-            for (int k = 0; k < PIECES; ++k) piece[k] = adapter_load(W + min(c0 + column(k), j.d - 1) * r + (at < r ? at : 0));
+            for (int k = 0; k < 8; ++k) {
+                const bf16* row = W + min(at + k, r - 1) * j.d;
+                if constexpr (FULL) piece[k] = adapter_load(row + c0 + 8 * tc);
+                else piece[k] = adapter_load8(row, min(c0 + 8 * tc, j.d), j.d);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) piece[k] = at + k < r ? piece[k] : zero16();
+        } else {
+            const bf16* row[PIECES];
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) row[k] = W + min(c0 + k * (kAdThreads / CH) + tc, j.d - 1) * r;
+            if (r % 8 == 0) {
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k) piece[k] = adapter_load(row[k] + (at < r ? at : 0));
+            } else {
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k) piece[k] = adapter_load8(row[k], at, r);
+            }
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) piece[k] = at < r ? piece[k] : zero16();
+        }
+    };
+    auto place = [&] {
+        if constexpr (COL) {
+            if (tc >= 16) return;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                u32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = adapter_pair(piece[2 * e][u / 2], piece[2 * e + 1][u / 2], u & 1);
+                lds[(u * 16 + tc) * PITCH + th] = v;
+            }
         } else {
 #pragma unroll
-            for (int k = 0; k < PIECES; ++k) piece[k] = adapter_load8(W + min(c0 + column(k), j.d - 1) * r, at, r);
+            for (int k = 0; k < PIECES; ++k) {
+                const int col = k * (kAdThreads / CH) + tc;
+                lds[(col % 8 * 16 + col / 8) * PITCH + th] = piece[k];
+            }
         }
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) piece[k] = at < r ? piece[k] : zero16();
     };
     operands(0);
     u32x4 base[4];
@@ -591,9 +665,7 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
 #pragma unroll
     for (int u = 0; u < 8; ++u) acc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int64_t k0 = 0;;) {
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k)
-            lds[(column(k) % 8 * 16 + column(k) / 8) * PITCH + threadIdx.x % CH] = piece[k];
+        place();
         __syncthreads();
         if (live) {
 #pragma unroll
@@ -632,46 +704,6 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
 }
 
 // ------------------------------------------------------------------ backward
-// Two rows' values in a register each: the lower or the upper ones of both.
-__device__ __forceinline__ uint32_t adapter_pair(uint32_t even, uint32_t odd, int half) {
-    return __builtin_amdgcn_perm(odd, even, half ? 0x07060302u : 0x05040100u);
-}
-
-// W (n x rows x cols) to its transpose (n x cols x rows), of adapters that have
-// rows: a thread takes 8 x 8 values.
-static __global__ __launch_bounds__(256) void adapter_transpose(const bf16* A, bf16* At, int64_t ar, int64_t ac,
-                                                               const bf16* B, bf16* Bt, int64_t br, int64_t bc,
-                                                               AdapterPlan p, int64_t M, int n) {
-    const AdapterHeader h = *p.head;
-    const int a = blockIdx.y;
-    if (h.M != M || h.n != n || p.count[a] == 0) return;
-    const int64_t ta = ceil_div(ar, 8) * ceil_div(ac, 8), tb = Bt ? ceil_div(br, 8) * ceil_div(bc, 8) : 0;
-    int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const bool second = t >= ta;
-    if (second) t -= ta;
-    if (second && t >= tb) return;
-    const int64_t rows = second ? br : ar, cols = second ? bc : ac;
-    const bf16* from = (second ? B : A) + a * rows * cols;
-    bf16* to = (second ? Bt : At) + a * rows * cols;
-    // neighbouring threads read neighbouring columns where rows are long, rows where they are short
-    const int64_t cw = ceil_div(cols, 8), r0 = t / cw * 8, c0 = t % cw * 8;
-    if (r0 + 8 <= rows && c0 + 8 <= cols) {
-        u32x4 x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = adapter_load(from + (r0 + e) * cols + c0);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            u32x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = adapter_pair(x[2 * e][c / 2], x[2 * e + 1][c / 2], c & 1);
-            reinterpret_cast<AdapterAny16*>(to + (c0 + c) * rows + r0)->v = y;
-        }
-    } else {
-        for (int64_t c = c0; c < min(c0 + 8, cols); ++c)
-            for (int64_t k = r0; k < min(r0 + 8, rows); ++k) to[c * rows + k] = from[k * cols + c];
-    }
-}
-
 struct AdapterGrads {
     const bf16* P;        // rows (M x d)
     const u32x4* turned;  // as finish leaves it

@@ -180,7 +180,7 @@ hipError_t launch_finish(const AdapterFinish& a, const AdapterFinish* b, const A
     return hipGetLastError();
 }
 
-template <bool SUM>
+template <bool SUM, bool COL>
 hipError_t launch_expand(const AdapterExpand& a, const AdapterPlan& p, int64_t M, int64_t n, int64_t r, int target,
                          hipStream_t st) {
     TimedLaunch timed(kSiteAdapterExpand, st);
@@ -191,9 +191,9 @@ hipError_t launch_expand(const AdapterExpand& a, const AdapterPlan& p, int64_t M
         constexpr int KB = decltype(kb)::value;
         constexpr bool ONE = decltype(one)::value;
         if (a.d % kAdWide == 0)
-            hipLaunchKernelGGL((adapter_expand<KB, ONE, SUM, true>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
+            hipLaunchKernelGGL((adapter_expand<KB, ONE, SUM, COL, true>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
         else
-            hipLaunchKernelGGL((adapter_expand<KB, ONE, SUM, false>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
+            hipLaunchKernelGGL((adapter_expand<KB, ONE, SUM, COL, false>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
     };
     using std::integral_constant;
     if (r <= 16) launch(integral_constant<int, 0>{}, std::true_type{});
@@ -385,12 +385,12 @@ pifa_status adapter_forward(const void* X, const void* A, const void* B, const f
     const int target = adapter_target(r, 1);
     float* T = (float*)work;
     u32x4* halves = (u32x4*)((uint8_t*)work + adapter_t_bytes(M, r, n));
-    if (launch_shrink({(const bf16*)X, (const bf16*)A, scale, T, d_in}, nullptr, p, M, n, r, target, st) != hipSuccess)
+    if (launch_shrink({(const bf16*)X, (const bf16*)A, false, scale, T, d_in}, nullptr, p, M, n, r, target, st) != hipSuccess)
         return PIFA_ERR_HIP;
     const AdapterExpand expand{T, halves, (const bf16*)B, (const bf16*)Y0, (bf16*)Y, d_out, d_in};
-    if (M <= kAdFewRows) return launch_expand<true>(expand, p, M, n, r, target, st) == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
+    if (M <= kAdFewRows) return launch_expand<true, false>(expand, p, M, n, r, target, st) == hipSuccess ? PIFA_OK : PIFA_ERR_HIP;
     if (launch_finish({T, halves, nullptr, d_in}, nullptr, p, M, n, r, target, st) != hipSuccess ||
-        launch_expand<false>(expand, p, M, n, r, target, st) != hipSuccess)
+        launch_expand<false, false>(expand, p, M, n, r, target, st) != hipSuccess)
         return PIFA_ERR_HIP;
     return PIFA_OK;
 }
@@ -398,7 +398,6 @@ pifa_status adapter_forward(const void* X, const void* A, const void* B, const f
 size_t adapter_backward_bytes(int64_t M, int64_t d_in, int64_t d_out, int64_t r, int64_t n) {
     if (check_adapter(M, d_in, d_out, r, n) != PIFA_OK) return 0;
     return 2 * adapter_t_bytes(M, r, n) + adapter_halves_bytes(M, r, n) + 2 * adapter_turned_bytes(M, r, n) +
-           (size_t)round_up(2 * n * r * d_in, 256) + (size_t)round_up(2 * n * r * d_out, 256) +
            adapter_partial_bytes(M, r, d_in) + adapter_partial_bytes(M, r, d_out);
 }
 
@@ -442,25 +441,16 @@ pifa_status adapter_backward(const void* X, const void* A, const void* B, const 
     u32x4* halves = (u32x4*)take(adapter_halves_bytes(M, r, n));
     u32x4* turned_u = (u32x4*)take(adapter_turned_bytes(M, r, n));
     u32x4* turned_t = (u32x4*)take(adapter_turned_bytes(M, r, n));
-    bf16* At = (bf16*)take((size_t)round_up(2 * n * r * d_in, 256));
-    bf16* Bt = (bf16*)take((size_t)round_up(2 * n * r * d_out, 256));
     float* part_a = (float*)take(adapter_partial_bytes(M, r, d_in));
     float* part_b = (float*)take(adapter_partial_bytes(M, r, d_out));
     const int target = adapter_target(r, dB ? 2 : 1);
-    const int64_t blocks_r = ceil_div(r, 8);
-    {
-        TimedLaunch timed(kSiteAdapterGrads, st);
-        const int64_t work_items = blocks_r * (ceil_div(d_out, 8) + (dX ? ceil_div(d_in, 8) : 0));
-        hipLaunchKernelGGL(adapter_transpose, dim3((unsigned)ceil_div(work_items, 256), (unsigned)n), dim3(256), 0, st,
-                           (const bf16*)B, Bt, d_out, r, (const bf16*)A, dX ? At : nullptr, r, d_in, p, M, (int)n);
-        if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
-    }
-    const AdapterShrink t{(const bf16*)X, (const bf16*)A, scale, T, d_in}, u{(const bf16*)dY, Bt, scale, U, d_out};
+    const AdapterShrink t{(const bf16*)X, (const bf16*)A, false, scale, T, d_in};
+    const AdapterShrink u{(const bf16*)dY, (const bf16*)B, true, scale, U, d_out};
     const AdapterFinish done_u{U, dX ? halves : nullptr, dA ? turned_u : nullptr, d_out}, done_t{T, nullptr, turned_t, d_in};
     if (launch_shrink(u, dB ? &t : nullptr, p, M, n, r, target, st) != hipSuccess ||
         launch_finish(done_u, dB ? &done_t : nullptr, p, M, n, r, target, st) != hipSuccess)
         return PIFA_ERR_HIP;
-    if (dX && launch_expand<false>({U, halves, At, (const bf16*)dX0, (bf16*)dX, d_in, d_out}, p, M, n, r, target, st) != hipSuccess)
+    if (dX && launch_expand<false, true>({U, halves, (const bf16*)A, (const bf16*)dX0, (bf16*)dX, d_in, d_out}, p, M, n, r, target, st) != hipSuccess)
         return PIFA_ERR_HIP;
     if (!dA && !dB) return PIFA_OK;
     const AdapterGrads ga{(const bf16*)X, turned_u, dA, part_a, d_in, false};
