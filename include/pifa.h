@@ -619,7 +619,8 @@ pifa_status adamw_destroy(adamw_handle h);
 
 /*
  * One step.
- *   lr >= 0, 0 <= beta1, beta2 < 1, eps > 0, all finite.
+ *   lr >= 0, 0 <= beta1, beta2 < 1, eps >= 2^-126, all finite (a v below 2^-126
+ *               counts as zero beside eps).
  *   step        the number t >= 1 of this step, or 0: one more than that of the
  *               handle's last step in stream order, counted on the device (one
  *               more launch, of one thread).  A captured call with 0 counts on at

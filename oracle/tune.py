@@ -116,8 +116,7 @@ def e4m3_round(x, bits, smallest):
     low = E4M3_UNITS[code]
     step = np.where(code < 126, E4M3_UNITS[np.minimum(code + 1, 126)] - low, 32.0 * 512)
     rest = (a - low) / step
-    # the sum is an fp32 one; only fractions below 2^-8 of the last bit of `bits` are lost in it
-    code = code + (np.float32(rest * 65536) + bits.astype(np.float32) >= np.float32(65535.5))
+    code = code + (rest * 65536 + bits >= 65535.5)  # exact: 24 bits of rest, 16 of bits
     code = np.where(a > 0, np.maximum(code, smallest), code)
     code = code | np.where(x < 0, 128, 0)
     code = np.where(np.repeat(bad, 32), 127, code)

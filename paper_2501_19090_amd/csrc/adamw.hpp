@@ -16,7 +16,7 @@
 // neighbour, which keeps the moment right on average: a step spreads v by about
 // (0.09 (1 - b2))^1/2 of it, and over its memory of 1 / (1 - b2) steps that comes to
 // a deviation of 0.2 v, 0.1 of its root.  The update takes m and v before they
-// are rounded.
+// are rounded; a v below fp32's normal range counts as zero in it.
 #pragma once
 
 #include "common.hpp"
@@ -72,15 +72,13 @@ __device__ __forceinline__ float adamw_scale(uint32_t byte) {
     return __builtin_bit_cast(float, bits);
 }
 
-// Code of x, given in steps of the smallest e4m3 value (2^-9) and at most 448 * 512:
-// from 8 steps on a code is the value's exponent and its upper 3 bits, below it
-// is the number of steps.  rnd: 16 random bits, a half more than which stands
-// against what is left, in 1 / 65536 of a step.
+// Code of x >= 0, given in steps of the smallest e4m3 value (2^-9) and at most 448 *
+// 512.  From 8 steps on a code is the value's exponent and its upper 3 bits, below it
+// is the number of steps; both with 20 more bits behind them, to which the random
+// ones and half of their last are added.  rnd: 16 bits, times 16, and 8.
 __device__ __forceinline__ uint32_t adamw_e4m3(float x, uint32_t rnd) {
-    const uint32_t large = (__builtin_bit_cast(uint32_t, x) + (rnd << 4 | 8)) >> 20;
-    const float whole = floorf(x);
-    const uint32_t small = (uint32_t)whole + ((x - whole) * 65536.f + (float)rnd >= 65535.5f ? 1u : 0u);
-    return x >= 8.f ? large - 1032u : small;
+    const uint32_t large = __builtin_bit_cast(uint32_t, x) - (1032u << 20), small = (uint32_t)(x * 0x1p20f);
+    return ((x >= 8.f ? large : small) + rnd) >> 20;
 }
 
 // The number of a step that the handle counts itself.
@@ -123,29 +121,33 @@ __device__ __forceinline__ float adamw_top(float v) {
     return v;
 }
 
-// Four codes of a group whose largest magnitude is `top`, and the scale's byte;
-// LEAST: the code that a value above zero has at least.
-template <uint32_t LEAST>
+// Four codes of a group whose largest magnitude is `top`, and the scale's byte.
+// LEAST: no value is below zero, and one above it has the smallest code at least.
+template <bool LEAST>
 __device__ __forceinline__ uint32_t adamw_pack(const float (&x)[4], float top, const uint32_t (&rnd)[4], uint32_t* byte) {
     const uint32_t t = __builtin_bit_cast(uint32_t, top) & 0x7FFFFFFFu;
-    if (t >= 0x7F800000u) {
-        *byte = 255;
-        return 0x7F7F7F7Fu;
-    }
+    const bool bad = t >= 0x7F800000u;
     // the smallest k with top <= 448 2^k; 448 is 1.75 * 2^8
     const int k = max(-126, (int)(t >> 23) - 127 - 8 + ((t & 0x7FFFFFu) > 0x600000u ? 1 : 0));
-    *byte = (uint32_t)(k + 127);
-    const float inv = __builtin_bit_cast(float, (uint32_t)(127 - k) << 23);
+    *byte = bad ? 255u : (uint32_t)(k + 127);
     uint32_t out = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const float a = fabsf(x[e]) * inv * 512.f;
+        const float a = __builtin_amdgcn_ldexpf(fabsf(x[e]), 9 - k);
         uint32_t c = adamw_e4m3(a, rnd[e]);
-        if (LEAST && a > 0.f) c = max(c, LEAST);
-        if (x[e] < 0.f) c |= 0x80u;
+        if constexpr (LEAST) c = max(c, min(__builtin_bit_cast(uint32_t, a), 1u));
+        else c |= __builtin_bit_cast(uint32_t, x[e]) >> 24 & 0x80u;
         out |= c << (8 * e);
     }
-    return out;
+    return bad ? 0x7F7F7F7Fu : out;
+}
+
+// m / d, rounded as a division rounds it but for one in some thousands: the product
+// with the reciprocal, corrected by what that leaves (of an infinite d: nothing).
+__device__ __forceinline__ float adamw_quotient(float m, float d) {
+    const float y = __builtin_amdgcn_rcpf(d), q = m * y;
+    const float c = __builtin_fmaf(__builtin_fmaf(-q, d, m), y, q);
+    return d <= 3.402823466e38f ? c : q;
 }
 
 template <bool EIGHT, typename G>
@@ -225,15 +227,15 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_update(AdamwArgs h) {
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            p[i][e] = p[i][e] * keep - step.rate * m[i][e] / (__builtin_sqrtf(v[i][e]) * step.root + h.eps);
+            p[i][e] = p[i][e] * keep - adamw_quotient(step.rate * m[i][e], __builtin_amdgcn_sqrtf(v[i][e]) * step.root + h.eps);
         uint32_t mb = 0, vb = 0;
         if constexpr (EIGHT) {
             uint32_t rm[4], rv[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t rnd = adamw_mix(key + (uint32_t)(at + e));
-                rm[e] = rnd >> 16;
-                rv[e] = rnd & 0xFFFFu;
+                rm[e] = (rnd >> 12 & 0xFFFF0u) | 8u;
+                rv[e] = (rnd << 4 & 0xFFFF0u) | 8u;
                 if (at + e >= left) m[i][e] = v[i][e] = 0.f;
             }
             auto top = [](const float(&x)[4]) {
@@ -242,8 +244,8 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_update(AdamwArgs h) {
                 for (int e = 1; e < 4; ++e) t = (t > fabsf(x[e]) || t != t) ? t : fabsf(x[e]);
                 return adamw_top(t);
             };
-            mc[i] = adamw_pack<0>(m[i], top(m[i]), rm, &mb);
-            vc[i] = adamw_pack<1>(v[i], top(v[i]), rv, &vb);
+            mc[i] = adamw_pack<false>(m[i], top(m[i]), rm, &mb);
+            vc[i] = adamw_pack<true>(v[i], top(v[i]), rv, &vb);
             if (at < left && at % kAdamwGroup == 0) {
                 T.m_scale[e0 / kAdamwGroup] = (uint8_t)mb;
                 T.v_scale[e0 / kAdamwGroup] = (uint8_t)vb;

@@ -179,6 +179,28 @@ struct LayerNormBwd {
     float eps;
 };
 
+// Adds a chunk's h to sh and its u = g y to su; of bf16 values two at a time, their
+// products exact.
+template <typename T>
+__device__ __forceinline__ void layer_norm_sums_of(u32x4 h, u32x4 y, u32x4 g, bool gain, float& sh, float& su) {
+    if constexpr (sizeof(T) == 2) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        const auto pair = [](uint32_t w) { return __builtin_bit_cast(bf16x2, w); };
+        constexpr uint32_t ones = 0x3F803F80u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sh = __builtin_amdgcn_fdot2_f32_bf16(pair(h[k]), pair(ones), sh, false);
+            su = __builtin_amdgcn_fdot2_f32_bf16(pair(y[k]), pair(gain ? g[k] : ones), su, false);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            sh += NormChunk<T>::one(h, k);
+            su = __builtin_fmaf(gain ? NormChunk<T>::one(g, k) : 1.f, NormChunk<T>::one(y, k), su);
+        }
+    }
+}
+
 // mean(u hat), where rho is 0 (a row whose squares sum past fp32) and the sum of
 // u c may be infinite: 0.
 __device__ __forceinline__ float layer_norm_back(float rho, float uc, float d) {
@@ -253,47 +275,49 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p
         const bool live = !LAST || m < p.M;
         float sh = cur.ht, su = gt * cur.yt;
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                // written-out fused steps: every form of this kernel gives the same bits
-                sh += C::one(cur.h[i], e);
-                su = __builtin_fmaf(gain(i, e), C::one(cur.y[i], e), su);
-            }
+        for (int i = 0; i < V; ++i) layer_norm_sums_of<T>(cur.h[i], cur.y[i], g[i], p.gain != nullptr, sh, su);
         const float2 sums = row_sum2<TPR>(sh, su, red[0]);
         const float mean = sums.x / (float)p.d, ubar = sums.y / (float)p.d;
         const float ct = has_tail ? cur.ht - mean : 0.f;
         float ss = ct * ct, uc = (gt * cur.yt - ubar) * ct;
-        // each reading of the row's registers converts them again: kept as fp32
-        // the values do not fit 128 registers
+        // h and u less their means, kept for the results where the registers hold them;
+        // written-out fused steps: every form of this kernel gives the same bits
+        float c[V == 1 ? N : 1], v[V == 1 ? N : 1];
+        auto centre = [&](int i, int e, float& ce, float& ve) {
+            ce = EXACT || t + i * TPR < nfull ? C::one(cur.h[i], e) - mean : 0.f;
+            ve = __builtin_fmaf(gain(i, e), C::one(cur.y[i], e), -ubar);
+        };
 #pragma unroll
-        for (int i = 0; i < V; ++i) asm volatile("" : "+v"(cur.h[i]), "+v"(cur.y[i]), "+v"(g[i]));
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const bool in = EXACT || t + i * TPR < nfull;
+        for (int i = 0; i < V; ++i)
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const float c = in ? C::one(cur.h[i], e) - mean : 0.f;
-                ss = __builtin_fmaf(c, c, ss);
-                uc = __builtin_fmaf(__builtin_fmaf(gain(i, e), C::one(cur.y[i], e), -ubar), c, uc);
+                float ce, ve;
+                centre(i, e, ce, ve);
+                ss = __builtin_fmaf(ce, ce, ss);
+                uc = __builtin_fmaf(ve, ce, uc);
+                if constexpr (V == 1) c[e] = ce, v[e] = ve;
             }
-        }
         const float2 again = row_sum2<TPR>(ss, uc, red[1]);
         const float rho = rsqrtf(again.x / (float)p.d + p.eps);
         const float back = layer_norm_back(rho, again.y, (float)p.d);
         const int64_t row = live ? m * p.d : 0, full = live ? nfull : 0;
+        if constexpr (V > 1) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) asm volatile("" : "+v"(cur.h[i]), "+v"(cur.y[i]), "+v"(g[i]));
+            for (int i = 0; i < V; ++i) asm volatile("" : "+v"(cur.h[i]), "+v"(cur.y[i]), "+v"(g[i]));
+        }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             float dx[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const float hat = (C::one(cur.h[i], e) - mean) * rho, y = C::one(cur.y[i], e);
+                float ce, ve;
+                if constexpr (V == 1) ce = c[e], ve = v[e];
+                else centre(i, e, ce, ve);
+                const float hat = ce * rho, y = C::one(cur.y[i], e);
                 dg[i][e] = __builtin_fmaf(hat, y, dg[i][e]);
                 db[i][e] += y;
-                dx[e] = rho * (__builtin_fmaf(gain(i, e), y, -ubar) - hat * back);
-                if (add) dx[e] += C::one(cur.r[i], e);
+                dx[e] = __builtin_fmaf(-hat, back, ve);
+                dx[e] = add ? __builtin_fmaf(rho, dx[e], C::one(cur.r[i], e)) : rho * dx[e];
             }
             if constexpr (EXACT && !LAST) C::store(p.dX + row, t + i * TPR, TPR * V, dx);
             else if (p.dX) C::store(p.dX + row, t + i * TPR, full, dx);

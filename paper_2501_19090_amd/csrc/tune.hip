@@ -539,7 +539,7 @@ pifa_status adamw_count(adamw_handle h, int64_t* steps) {
 pifa_status adamw_step(adamw_handle h, double lr, double beta1, double beta2, double eps, int64_t step,
                        const float* grad_scale, void* stream) {
     if (!h || !(lr >= 0.0) || std::isinf(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
-        !((float)eps > 0.f) || std::isinf((float)eps) || step < 0)
+        !((float)eps >= 0x1p-126f) || std::isinf((float)eps) || step < 0)
         return PIFA_ERR_INVALID_ARG;
     if ((uintptr_t)grad_scale % 4 != 0) return PIFA_ERR_UNSUPPORTED;
     PIFA_ON_DEVICE(h->device);
