@@ -89,26 +89,28 @@ static __global__ void adamw_tick(AdamwStep* count, int64_t t, double lr, double
     count->root = (float)(1.0 / sqrt(1.0 - pow(b2, (double)t)));
 }
 
-// Groups of four values; EIGHT: eight neighbouring lanes hold a group of 32.
+// Groups of four values; EIGHT: eight neighbouring lanes hold a group of 32.  All
+// but the bf16 copy, which the next forward reads, is streamed: 50.3 M values in
+// fp32 take 253 us instead of 279.
 template <typename T>
 struct AdamwQuad {
-    struct __attribute__((packed, aligned(sizeof(T)))) Any {
+    struct Four {
         T v[4];
     };
     __device__ __forceinline__ static void load(const void* base, int64_t at, float (&v)[4]) {
-        const Any a = *reinterpret_cast<const Any*>((const T*)base + at);
+        const Four a = load_streamed<Four>((const T*)base + at);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = (float)a.v[e];
     }
-    __device__ __forceinline__ static void store(void* base, int64_t at, const float (&v)[4]) {
-        Any a;
+    __device__ __forceinline__ static void store(void* base, int64_t at, const float (&v)[4], bool streamed = true) {
+        struct __attribute__((packed, aligned(sizeof(T)))) Any {
+            Four f;
+        } a;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) a.v[e] = (T)v[e];
-        *reinterpret_cast<Any*>((T*)base + at) = a;
+        for (int e = 0; e < 4; ++e) a.f.v[e] = (T)v[e];
+        if (streamed) store_streamed((T*)base + at, a.f);
+        else *reinterpret_cast<Any*>((T*)base + at) = a;
     }
-};
-struct __attribute__((packed, aligned(1))) AdamwCodes {
-    uint32_t w;
 };
 
 // Largest magnitude over the eight lanes of a group; a NaN survives.
@@ -178,8 +180,8 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_update(AdamwArgs h) {
             AdamwQuad<float>::load(T.p, e0, p[i]);
             AdamwQuad<G>::load(T.g, e0, g[i]);
             if constexpr (EIGHT) {
-                mc[i] = reinterpret_cast<const AdamwCodes*>((const uint8_t*)T.m + e0)->w;
-                vc[i] = reinterpret_cast<const AdamwCodes*>((const uint8_t*)T.v + e0)->w;
+                mc[i] = load_streamed<uint32_t>((const uint8_t*)T.m + e0);
+                vc[i] = load_streamed<uint32_t>((const uint8_t*)T.v + e0);
             } else {
                 AdamwQuad<float>::load(T.m, e0, m[i]);
                 AdamwQuad<float>::load(T.v, e0, v[i]);
@@ -254,13 +256,13 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_update(AdamwArgs h) {
         if (at + 4 <= left) {
             AdamwQuad<float>::store(T.p, e0, p[i]);
             if constexpr (EIGHT) {
-                reinterpret_cast<AdamwCodes*>((uint8_t*)T.m + e0)->w = mc[i];
-                reinterpret_cast<AdamwCodes*>((uint8_t*)T.v + e0)->w = vc[i];
+                store_streamed((uint8_t*)T.m + e0, mc[i]);
+                store_streamed((uint8_t*)T.v + e0, vc[i]);
             } else {
                 AdamwQuad<float>::store(T.m, e0, m[i]);
                 AdamwQuad<float>::store(T.v, e0, v[i]);
             }
-            if (T.copy) AdamwQuad<bf16>::store(T.copy, e0, p[i]);
+            if (T.copy) AdamwQuad<bf16>::store(T.copy, e0, p[i], false);
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {

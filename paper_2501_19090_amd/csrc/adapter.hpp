@@ -657,7 +657,8 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const bf16* at = from + (int64_t)max(row[e], 0) * j.d;
-        if constexpr (FULL) base[e] = adapter_load(at + c);
+        // its last reader (1999 rows of 11008: 38.2 us a call, 40.8 through the caches)
+        if constexpr (FULL) base[e] = load_streamed<u32x4>(at + c);
         else base[e] = adapter_load8(at, min(c, j.d), j.d);
     }
     pieces(0);
@@ -757,7 +758,7 @@ __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0,
         u32x4 x[8];
         if (full) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = adapter_load(j.P + (int64_t)max(row[e], 0) * j.d + c);
+            for (int e = 0; e < 8; ++e) x[e] = load_streamed<u32x4>(j.P + (int64_t)max(row[e], 0) * j.d + c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = row[e] >= 0 ? x[e] : zero16();
         } else {
