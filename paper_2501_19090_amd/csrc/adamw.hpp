@@ -20,6 +20,7 @@
 #pragma once
 
 #include "common.hpp"
+#include "streamed.hpp"
 
 namespace pifa {
 

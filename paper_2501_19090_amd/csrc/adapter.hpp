@@ -20,6 +20,7 @@
 #pragma once
 
 #include "common.hpp"
+#include "streamed.hpp"
 
 namespace pifa {
 
@@ -246,6 +247,21 @@ __device__ __forceinline__ u32x4 adapter_load8(const bf16* row, int64_t k, int64
     return v;
 }
 
+// The same of rows of at least 8 values, without a branch (whose end would wait for
+// all loads): the row's last eight, moved down.
+__device__ __forceinline__ u32x4 adapter_edge8(const bf16* row, int64_t k, int64_t K) {
+    const int64_t at = min(k, K - 8);
+    u32x4 v = adapter_load(row + at);
+    const int s = (int)min(k - at, (int64_t)8);  // values to move
+    const u32x4 z = zero16();
+    if (s & 4) v = u32x4{v[2], v[3], 0u, 0u};
+    if (s & 2) v = u32x4{v[1], v[2], v[3], 0u};
+    const uint32_t odd = (s & 1) ? 16 : 0;
+    v = u32x4{__builtin_amdgcn_alignbit(v[1], v[0], odd), __builtin_amdgcn_alignbit(v[2], v[1], odd),
+              __builtin_amdgcn_alignbit(v[3], v[2], odd), v[3] >> odd};
+    return s == 8 ? z : v;
+}
+
 __device__ __forceinline__ f32x4 adapter_mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
@@ -285,9 +301,10 @@ struct AdapterShrink {
 // LDS of its own (16-byte places of a row exchanged by its number, so that
 // neighbouring rows' are in other banks).  The next slice is on its way meanwhile.
 // COL: the adapter's columns lie in the rows of W; a lane takes eight of them from
-// 2 JB neighbouring rows and turns these round first.  Columns past the rank come
-// from the rows behind and are left out of t; slices whose rows have not enough
-// rows behind them are loaded value by value.
+// 2 JB neighbouring rows and turns these round first.  Columns past the rank are left
+// out of t; where the rank is no multiple of 8 they come from the rows behind, and
+// slices whose rows have not enough rows behind them end the loop like those of the
+// last columns.
 template <int JB, int RG, bool COL>
 __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, const int32_t* rows, const AdapterTile tile,
                                                     int64_t r, int j0, int64_t s0, int64_t s1, int64_t rp, float* out,
@@ -301,9 +318,10 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
 #pragma unroll
     for (int k = 0; k < NX; ++k) x[k] = j.P + (int64_t)rows[min(8 * k + row8, tile.count - 1)] * j.K + 8 * c8;
     const int piece = lane % NW, group = lane / NW;  // COL: columns 8 piece on, of rows NW group on
+    const int col = j0 + 8 * piece;
 #pragma unroll
     for (int k = 0; k < NW; ++k)
-        w[k] = j.W + (COL ? ((int64_t)tile.adapter * j.K + NW * group + k) * r + j0 + 8 * piece
+        w[k] = j.W + (COL ? ((int64_t)tile.adapter * j.K + NW * group + k) * r + (r % 8 != 0 || col < r ? col : 0)
                           : ((int64_t)tile.adapter * r + min((int64_t)(j0 + 8 * k + row8), r - 1)) * j.K + 8 * c8);
     f32x4 acc[RG][JB];
 #pragma unroll
@@ -352,8 +370,8 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
                 for (int k = 0; k < JB; ++k) acc[g][k] = adapter_mfma(a[g], b[k], acc[g][k]);
         }
     };
-    // slices of 64 full columns; behind, one or two for different waves
-    const int64_t behind = COL ? max((int64_t)0, ceil_div(j0 + 16 * JB, r) - 1) : 0;
+    // slices of 64 full columns; behind them one or two, for different waves
+    const int64_t behind = COL && r % 8 != 0 ? max((int64_t)0, ceil_div(j0 + 16 * JB, r) - 1) : 0;
     const int64_t whole = min(s1, max((int64_t)0, j.K - behind) / kAdSlice);
     const int64_t first = s0 + wave, count = first < whole ? (whole - first + WAVES - 1) / WAVES : 0;
     if (count > 0) {
@@ -366,39 +384,44 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
             multiply();
         }
     }
-    if (const int64_t s = first + count * WAVES; s < s1) {  // the row's last columns
+    if (const int64_t s = first + count * WAVES; s < s1) {
+        auto rest = [&](auto load8) {
 #pragma unroll
-        for (int k = 0; k < NX; ++k) f[k] = adapter_load8(x[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
+            for (int k = 0; k < NX; ++k) f[k] = load8(x[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
 #pragma unroll
-        for (int k = 0; k < NW; ++k) {
-            if constexpr (COL) {
-                const bool there = kAdSlice * s + NW * group + k < j.K;
-                f[NX + k] = adapter_load8(w[k] - j0 - 8 * piece + (there ? kAdSlice * s * r : 0), there ? j0 + 8 * piece : r, r);
-            } else {
-                f[NX + k] = adapter_load8(w[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
+            for (int k = 0; k < NW; ++k) {
+                if constexpr (COL) {
+                    const int64_t at = kAdSlice * s + NW * group + k;  // row of W
+                    f[NX + k] = load8(j.W + ((int64_t)tile.adapter * j.K + min(at, j.K - 1)) * r, (int64_t)col, r);
+                    f[NX + k] = at < j.K ? f[NX + k] : zero16();
+                } else {
+                    f[NX + k] = load8(w[k] - 8 * c8, kAdSlice * s + 8 * c8, j.K);
+                }
             }
-        }
+        };
+        if (j.K >= 8 && r >= 8) rest([](const bf16* row, int64_t k, int64_t K) { return adapter_edge8(row, k, K); });
+        else rest([](const bf16* row, int64_t k, int64_t K) { return adapter_load8(row, k, K); });
         turn();
         multiply();
     }
     // the waves' sums
-    constexpr int COLS = 16 * JB;
+    constexpr int COLS = 16 * JB, PITCH = COLS + 4;  // the lanes of an instruction's four rows in other banks
     const float scale = j.scale ? j.scale[tile.adapter] : 1.f;
-    float* part = (float*)lds;  // waves x 16 RG x COLS: no more than the slices took
+    float* part = (float*)lds;
     __syncthreads();
 #pragma unroll
     for (int g = 0; g < RG; ++g)
 #pragma unroll
         for (int b = 0; b < JB; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) part[((wave * RG + g) * 16 + 4 * q + e) * COLS + 16 * b + i] = acc[g][b][e];
+            for (int e = 0; e < 4; ++e) part[((wave * RG + g) * 16 + 4 * q + e) * PITCH + 16 * b + i] = acc[g][b][e];
     __syncthreads();
     for (int at = threadIdx.x; at < 16 * RG * COLS; at += WAVES * kWave) {
-        const int row = at / COLS, col = j0 + at % COLS;
+        const int row = at / COLS, c = at % COLS;
         float v = 0.f;
 #pragma unroll
-        for (int u = 0; u < WAVES; ++u) v += part[u * 16 * RG * COLS + at];
-        if (row < tile.count) out[(int64_t)row * rp + col] = col < r ? v * scale : 0.f;
+        for (int u = 0; u < WAVES; ++u) v += part[(u * 16 * RG + row) * PITCH + c];
+        if (row < tile.count) out[(int64_t)row * rp + j0 + c] = j0 + c < r ? v * scale : 0.f;
     }
 }
 
@@ -406,7 +429,9 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
 template <int JB>
 __global__ __launch_bounds__(adapter_waves(16 * JB) * kWave, JB == 4 ? 2 : 1) void adapter_shrink(AdapterShrink j0, AdapterShrink j1, AdapterPlan p, int64_t M,
                                                              int n, int64_t r, int target) {
-    __shared__ u32x4 lds[adapter_waves(16 * JB) * (8 + 2 * JB) * kWave];
+    constexpr int WAVES = adapter_waves(16 * JB), SLICES = WAVES * (8 + 2 * JB) * kWave,
+                  SUMS = WAVES * kAdTile * (16 * JB + 4) / 4;  // of 16 bytes
+    __shared__ u32x4 lds[SLICES > SUMS ? SLICES : SUMS];
     const AdapterHeader h = *p.head;
     const AdapterTile tile = p.tiles[blockIdx.x];
     if (h.M != M || h.n != n || (int)blockIdx.x >= h.tiles) return;
@@ -540,29 +565,12 @@ constexpr int kAdWide = 128;  // columns that a workgroup of expand takes
 // (W in registers, 64 rows a wave: eight waves a CU instead of twenty, and 1999 rows
 // of 11008 with rank 64 take 30 us.)  ONE: those blocks are all.  SUM: t is still in
 // parts.  COL: W's rows are the columns of t; a thread takes 8 columns of 8 of them
-// and turns them round.  FULL: all columns of every workgroup are there.
+// and turns them round.  FULL: all columns of the workgroup are there.
 template <int KB, bool ONE, bool SUM, bool COL, bool FULL>
-__global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(AdapterExpand j, AdapterPlan p, int64_t M, int n,
-                                                                          int64_t r, int target) {
+__device__ __forceinline__ void adapter_expand_tile(const AdapterExpand& j, const AdapterHeader& h, const AdapterTile tile,
+                                                    const int32_t* rows, int64_t c0, int64_t r, int target, u32x4* lds) {
     constexpr int NB = KB > 0 ? KB : 1, CH = KB > 0 ? 4 * KB : 2;  // pieces of 8 columns of t in a row of LDS
     constexpr int PITCH = CH + 1, PIECES = COL ? 8 : kAdWide * CH / kAdThreads;
-    __shared__ u32x4 lds[kAdWide * PITCH];
-    const AdapterHeader h = *p.head;
-    const AdapterTile tile = p.tiles[blockIdx.y];
-    if (h.M != M || h.n != n || (int)blockIdx.y >= h.tiles_all) return;
-    const int64_t c0 = (int64_t)blockIdx.x * kAdWide;
-    if (c0 >= j.d) return;
-    const int32_t* rows = p.rows + (int64_t)blockIdx.y * kAdTile;
-    if (tile.adapter >= n) {
-        if (j.out == j.base) return;
-        const int64_t c = c0 + threadIdx.x % kAdWide;
-        if (c >= j.d) return;
-        for (int m = threadIdx.x / kAdWide; m < tile.count; m += kAdThreads / kAdWide) {
-            const int64_t at = (int64_t)rows[m] * j.d + c;
-            ((uint16_t*)j.out)[at] = j.base ? ((const uint16_t*)j.base)[at] : (uint16_t)0;
-        }
-        return;
-    }
     const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int64_t rp = adapter_rp(r), c = c0 + 8 * i;
     const bool live = 16 * g < tile.count;  // of the wave
@@ -615,6 +623,7 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
             for (int k = 0; k < 8; ++k) {
                 const bf16* row = W + min(at + k, r - 1) * j.d;
                 if constexpr (FULL) piece[k] = adapter_load(row + c0 + 8 * tc);
+                else if (j.d >= 8) piece[k] = adapter_edge8(row, c0 + 8 * tc, j.d);
                 else piece[k] = adapter_load8(row, min(c0 + 8 * tc, j.d), j.d);
             }
 #pragma unroll
@@ -626,6 +635,9 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
             if (r % 8 == 0) {
 #pragma unroll
                 for (int k = 0; k < PIECES; ++k) piece[k] = adapter_load(row[k] + (at < r ? at : 0));
+            } else if (r >= 8) {
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k) piece[k] = adapter_edge8(row[k], at, r);
             } else {
 #pragma unroll
                 for (int k = 0; k < PIECES; ++k) piece[k] = adapter_load8(row[k], at, r);
@@ -659,6 +671,7 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
         const bf16* at = from + (int64_t)max(row[e], 0) * j.d;
         // its last reader (1999 rows of 11008: 38.2 us a call, 40.8 through the caches)
         if constexpr (FULL) base[e] = load_streamed<u32x4>(at + c);
+        else if (j.d >= 8) base[e] = adapter_edge8(at, c, j.d);
         else base[e] = adapter_load8(at, min(c, j.d), j.d);
     }
     pieces(0);
@@ -704,6 +717,30 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : 4) void adapter_expand(Adapte
     }
 }
 
+template <int KB, bool ONE, bool SUM, bool COL>
+__global__ __launch_bounds__(kAdThreads, SUM ? 2 : ONE ? 4 : 3) void adapter_expand(AdapterExpand j, AdapterPlan p, int64_t M, int n,
+                                                                          int64_t r, int target) {
+    __shared__ u32x4 lds[kAdWide * (KB > 0 ? 4 * KB + 1 : 3)];
+    const AdapterHeader h = *p.head;
+    const AdapterTile tile = p.tiles[blockIdx.y];
+    if (h.M != M || h.n != n || (int)blockIdx.y >= h.tiles_all) return;
+    const int64_t c0 = (int64_t)blockIdx.x * kAdWide;
+    if (c0 >= j.d) return;
+    const int32_t* rows = p.rows + (int64_t)blockIdx.y * kAdTile;
+    if (tile.adapter >= n) {
+        if (j.out == j.base) return;
+        const int64_t c = c0 + threadIdx.x % kAdWide;
+        if (c >= j.d) return;
+        for (int m = threadIdx.x / kAdWide; m < tile.count; m += kAdThreads / kAdWide) {
+            const int64_t at = (int64_t)rows[m] * j.d + c;
+            ((uint16_t*)j.out)[at] = j.base ? ((const uint16_t*)j.base)[at] : (uint16_t)0;
+        }
+        return;
+    }
+    if (c0 + kAdWide <= j.d) adapter_expand_tile<KB, ONE, SUM, COL, true>(j, h, tile, rows, c0, r, target, lds);
+    else adapter_expand_tile<KB, ONE, SUM, COL, false>(j, h, tile, rows, c0, r, target, lds);
+}
+
 // ------------------------------------------------------------------ backward
 struct AdapterGrads {
     const bf16* P;        // rows (M x d)
@@ -725,7 +762,8 @@ template <int JB>
 __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0, AdapterGrads j1, int blocks0, AdapterPlan p,
                                                             int64_t M, int n, int64_t r) {
     constexpr int COLS = 16 * JB, ROUND = 8 / JB;  // operands whose sums LDS holds at once
-    __shared__ float part[ROUND][kAdGradWaves][16 * COLS];
+    constexpr int PITCH = COLS + 4;                // the lanes of an instruction's four rows in other banks
+    __shared__ float part[ROUND][kAdGradWaves][16 * PITCH];
     __shared__ float sums[COLS][kAdCols + 1];
     const AdapterHeader h = *p.head;
     const AdapterPiece piece = p.pieces[blockIdx.y];
@@ -761,6 +799,11 @@ __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0,
             for (int e = 0; e < 8; ++e) x[e] = load_streamed<u32x4>(j.P + (int64_t)max(row[e], 0) * j.d + c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = row[e] >= 0 ? x[e] : zero16();
+        } else if (j.d >= 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = adapter_edge8(j.P + (int64_t)max(row[e], 0) * j.d, c, j.d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = row[e] >= 0 ? x[e] : zero16();
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -788,14 +831,14 @@ __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0,
 #pragma unroll
             for (int b = 0; b < JB; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) part[k][wave][(4 * q + e) * COLS + 16 * b + i] = acc[k0 + k][b][e];
+                for (int e = 0; e < 4; ++e) part[k][wave][(4 * q + e) * PITCH + 16 * b + i] = acc[k0 + k][b][e];
         __syncthreads();
         for (int at = threadIdx.x; at < ROUND * 16 * COLS; at += kAdGradThreads) {
-            const int k = at / (16 * COLS), cell = at % (16 * COLS);
+            const int k = at / (16 * COLS), row = at / COLS % 16, a = at % COLS;
             float v = 0.f;
 #pragma unroll
-            for (int u = 0; u < kAdGradWaves; ++u) v += part[k][u][cell];
-            sums[cell % COLS][8 * (cell / COLS) + k0 + k] = v;
+            for (int u = 0; u < kAdGradWaves; ++u) v += part[k][u][row * PITCH + a];
+            sums[a][8 * row + k0 + k] = v;
         }
     }
     __syncthreads();

@@ -14,6 +14,7 @@
 #pragma once
 
 #include "norm.hpp"
+#include "streamed.hpp"
 
 namespace pifa {
 

@@ -190,10 +190,7 @@ hipError_t launch_expand(const AdapterExpand& a, const AdapterPlan& p, int64_t M
     auto launch = [&](auto kb, auto one) {
         constexpr int KB = decltype(kb)::value;
         constexpr bool ONE = decltype(one)::value;
-        if (a.d % kAdWide == 0)
-            hipLaunchKernelGGL((adapter_expand<KB, ONE, SUM, COL, true>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
-        else
-            hipLaunchKernelGGL((adapter_expand<KB, ONE, SUM, COL, false>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
+        hipLaunchKernelGGL((adapter_expand<KB, ONE, SUM, COL>), grid, dim3(kAdThreads), 0, st, a, p, M, (int)n, r, target);
     };
     using std::integral_constant;
     if (r <= 16) launch(integral_constant<int, 0>{}, std::true_type{});
