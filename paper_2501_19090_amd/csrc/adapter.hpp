@@ -762,8 +762,7 @@ template <int JB>
 __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0, AdapterGrads j1, int blocks0, AdapterPlan p,
                                                             int64_t M, int n, int64_t r) {
     constexpr int COLS = 16 * JB, ROUND = 8 / JB;  // operands whose sums LDS holds at once
-    constexpr int PITCH = COLS + 4;                // the lanes of an instruction's four rows in other banks
-    __shared__ float part[ROUND][kAdGradWaves][16 * PITCH];
+    __shared__ float part[ROUND][kAdGradWaves][16 * COLS];
     __shared__ float sums[COLS][kAdCols + 1];
     const AdapterHeader h = *p.head;
     const AdapterPiece piece = p.pieces[blockIdx.y];
@@ -822,7 +821,9 @@ __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0,
                 for (int b = 0; b < JB; ++b) acc[k][b] = adapter_mfma(turned, t[u][b], acc[k][b]);
         }
     }
-    // the waves' sums: acc[k][b], row 4 q + e is column 8 (4 q + e) + k of P, column i is column 16 b + i of t
+    // the waves' sums: acc[k][b], row 4 q + e is column 8 (4 q + e) + k of P, column i is
+    // column 16 b + i of t.  In LDS the rows lie as 4 e + q and their columns are moved on, so
+    // that the lanes of a store are in different banks.
 #pragma unroll
     for (int k0 = 0; k0 < 8; k0 += ROUND) {
         if (k0 > 0) __syncthreads();
@@ -831,14 +832,15 @@ __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0,
 #pragma unroll
             for (int b = 0; b < JB; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) part[k][wave][(4 * q + e) * PITCH + 16 * b + i] = acc[k0 + k][b][e];
+                for (int e = 0; e < 4; ++e)
+                    part[k][wave][(4 * e + q) * COLS + (16 * (b + q * JB / 4) + i) % COLS] = acc[k0 + k][b][e];
         __syncthreads();
         for (int at = threadIdx.x; at < ROUND * 16 * COLS; at += kAdGradThreads) {
-            const int k = at / (16 * COLS), row = at / COLS % 16, a = at % COLS;
+            const int k = at / (16 * COLS), cell = at % (16 * COLS), e = cell / (4 * COLS), u4 = cell / COLS % 4;
             float v = 0.f;
 #pragma unroll
-            for (int u = 0; u < kAdGradWaves; ++u) v += part[k][u][row * PITCH + a];
-            sums[a][8 * row + k0 + k] = v;
+            for (int u = 0; u < kAdGradWaves; ++u) v += part[k][u][cell];
+            sums[(cell + COLS - 16 * (u4 * JB / 4)) % COLS][8 * (4 * u4 + e) + k0 + k] = v;
         }
     }
     __syncthreads();
