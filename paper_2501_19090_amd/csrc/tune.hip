@@ -113,7 +113,9 @@ namespace {
 
 constexpr int64_t kAdMaxD = 1 << 19, kAdMaxRank = 1024;
 // Workgroups of a shrink that the chip holds at once, for one or two jobs.
-int adapter_target(int64_t r, int jobs) { return (int)((r > 16 && r <= 32 ? 1 : 2) * kCus / jobs); }
+int adapter_target(int64_t r, int jobs) {
+    return (int)((r > 16 && r <= 32 ? 1 : 2) * kCus / (jobs * ceil_div(adapter_rp(r), 64)));
+}
 
 pifa_status check_plan(int64_t M, int64_t n) {
     if (M < 0 || n < 1) return PIFA_ERR_INVALID_ARG;
