@@ -728,12 +728,24 @@ __global__ __launch_bounds__(kAdThreads, SUM ? 2 : ONE ? 4 : 3) void adapter_exp
     if (c0 >= j.d) return;
     const int32_t* rows = p.rows + (int64_t)blockIdx.y * kAdTile;
     if (tile.adapter >= n) {
+        // rows without an adapter, 8 columns a lane
         if (j.out == j.base) return;
-        const int64_t c = c0 + threadIdx.x % kAdWide;
-        if (c >= j.d) return;
-        for (int m = threadIdx.x / kAdWide; m < tile.count; m += kAdThreads / kAdWide) {
-            const int64_t at = (int64_t)rows[m] * j.d + c;
-            ((uint16_t*)j.out)[at] = j.base ? ((const uint16_t*)j.base)[at] : (uint16_t)0;
+        const int64_t c = c0 + 8 * (threadIdx.x & 15);
+        const bool inside = c + 8 <= j.d;
+        int row[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) row[e] = rows[16 * e + (threadIdx.x >> 4)];
+        u32x4 v[4] = {zero16(), zero16(), zero16(), zero16()};
+        if (j.base && inside) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = load_streamed<u32x4>(j.base + max(row[e], 0) * j.d + c);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (row[e] < 0) continue;
+            if (inside) store_streamed(j.out + row[e] * j.d + c, v[e]);
+            else for (int64_t at = row[e] * j.d + c; at < (row[e] + 1) * j.d; ++at)
+                ((uint16_t*)j.out)[at] = j.base ? ((const uint16_t*)j.base)[at] : (uint16_t)0;
         }
         return;
     }
