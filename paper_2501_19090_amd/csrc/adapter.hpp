@@ -833,35 +833,49 @@ __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0,
                 for (int b = 0; b < JB; ++b) acc[k][b] = adapter_mfma(turned, t[u][b], acc[k][b]);
         }
     }
-    // the waves' sums: acc[k][b], row 4 q + e is column 8 (4 q + e) + k of P, column i is
-    // column 16 b + i of t.  In LDS the rows lie as 4 e + q and their columns are moved on, so
-    // that the lanes of a store are in different banks.
+    if (piece.tiles > 0) {  // the same for all
+        // the waves' sums: acc[k][b], row 4 q + e is column 8 (4 q + e) + k of P, column i is
+        // column 16 b + i of t.  In LDS the rows lie as 4 e + q and their columns are moved on, so
+        // that the lanes of a store are in different banks.
 #pragma unroll
-    for (int k0 = 0; k0 < 8; k0 += ROUND) {
-        if (k0 > 0) __syncthreads();
+        for (int k0 = 0; k0 < 8; k0 += ROUND) {
+            if (k0 > 0) __syncthreads();
 #pragma unroll
-        for (int k = 0; k < ROUND; ++k)
+            for (int k = 0; k < ROUND; ++k)
 #pragma unroll
-            for (int b = 0; b < JB; ++b)
+                for (int b = 0; b < JB; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    part[k][wave][(4 * e + q) * COLS + (16 * (b + q * JB / 4) + i) % COLS] = acc[k0 + k][b][e];
-        __syncthreads();
-        for (int at = threadIdx.x; at < ROUND * 16 * COLS; at += kAdGradThreads) {
-            const int k = at / (16 * COLS), cell = at % (16 * COLS), e = cell / (4 * COLS), u4 = cell / COLS % 4;
-            float v = 0.f;
+                    for (int e = 0; e < 4; ++e)
+                        part[k][wave][(4 * e + q) * COLS + (16 * (b + q * JB / 4) + i) % COLS] = acc[k0 + k][b][e];
+            __syncthreads();
+            for (int at = threadIdx.x; at < ROUND * 16 * COLS; at += kAdGradThreads) {
+                const int k = at / (16 * COLS), cell = at % (16 * COLS), e = cell / (4 * COLS), u4 = cell / COLS % 4;
+                float v = 0.f;
 #pragma unroll
-            for (int u = 0; u < kAdGradWaves; ++u) v += part[k][u][cell];
-            sums[(cell + COLS - 16 * (u4 * JB / 4)) % COLS][8 * (4 * u4 + e) + k0 + k] = v;
+                for (int u = 0; u < kAdGradWaves; ++u) v += part[k][u][cell];
+                sums[(cell + COLS - 16 * (u4 * JB / 4)) % COLS][8 * (4 * u4 + e) + k0 + k] = v;
+            }
         }
+        __syncthreads();
     }
-    __syncthreads();
+    // 4 neighbouring values a lane
     float* out = piece.slot < 0 ? j.out + piece.adapter * r * j.d : j.part + piece.slot * r * j.d;
     const int cols = (int)min((int64_t)kAdCols, j.d - c0), js = (int)min((int64_t)COLS, r - b0);
-    for (int at = threadIdx.x; at < COLS * kAdCols; at += kAdGradThreads) {
-        const int a = j.by_column ? at % COLS : at / kAdCols, k = j.by_column ? at / COLS : at % kAdCols;
-        if (a >= js || k >= cols) continue;
-        out[j.by_column ? (c0 + k) * r + b0 + a : (b0 + a) * j.d + c0 + k] = sums[a][k];
+#pragma unroll
+    for (int u = 0; u < COLS * kAdCols / 4 / kAdGradThreads; ++u) {
+        const int at = u * kAdGradThreads + threadIdx.x;
+        const int a = j.by_column ? 4 * (at % (COLS / 4)) : at / (kAdCols / 4);
+        const int k = j.by_column ? at / (COLS / 4) : 4 * (at % (kAdCols / 4));
+        const int left = j.by_column ? (k < cols ? js - a : 0) : a < js ? cols - k : 0;
+        if (left <= 0) continue;
+        float* to = out + (j.by_column ? (c0 + k) * r + b0 + a : (b0 + a) * j.d + c0 + k);
+        f32x4 v{0.f, 0.f, 0.f, 0.f};
+        if (piece.tiles > 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = j.by_column ? sums[a + e][k] : sums[a][k + e];
+        }
+        if (left >= 4) store_streamed(to, v);
+        else for (int e = 0; e < left; ++e) to[e] = v[e];
     }
 }
 
