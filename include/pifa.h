@@ -514,11 +514,11 @@ size_t layer_norm_backward_bytes(int64_t M, int64_t d);
  * adapter_backward over rows with these ids goes by the plan.
  *   ids   device, M, int32.
  *   plan  device, at least adapter_plan_bytes(M, n) bytes, 16-byte aligned.
- * Every call that a plan is given to has to have its M and n (a call on the
- * device finds others, and writes nothing).  M up to 2^20, n up to 4096, r up to
- * 1024, d_in and d_out up to 2^19 (PIFA_ERR_UNSUPPORTED).  Asynchronous on
- * `stream`; it allocates nothing and may be captured, ids then being those at
- * each replay.
+ * Every call that a plan is given to has to have its M and n: the kernels write
+ * nothing by a plan that holds others, if its buffer has the bytes of the call's M
+ * and n.  M up to 2^20, n up to 4096, r up to 1024, d_in and d_out up to 2^19
+ * (PIFA_ERR_UNSUPPORTED).  Asynchronous on `stream`; it allocates nothing and may
+ * be captured, ids then being those at each replay.
  */
 pifa_status adapter_plan(const int32_t* ids, int64_t M, int64_t n, void* plan, size_t plan_bytes, void* stream);
 

@@ -199,6 +199,22 @@ def test_special_values_stay_in_their_values(bits):
             assert torch.isnan(m[5]) and torch.isinf(m[70]) and torch.isinf(v[70]) and torch.isfinite(m.cpu()[~bad]).all()
 
 
+def test_quotients_at_the_ends_of_the_range():
+    """m / (root + eps) past fp32 is infinite, over an infinite root nothing."""
+    pifa, torch = _pifa(), torch_mod()
+    inf = float("inf")
+    p, g = torch.ones(6, device="cuda"), torch.zeros(6, device="cuda")
+    m = torch.tensor([1e30, -1e30, 1e30, 0.0, 1e-37, 1e30], device="cuda")
+    v = torch.tensor([0.0, 0.0, inf, inf, 0.0, 1.0], device="cuda")
+    with pifa.AdamW([p], [g], states=[(m, v)]) as opt:
+        opt.step(1.0, 0.5, 0.5, 1e-37, step=60)
+        torch.cuda.synchronize()
+    got = p.double().cpu()
+    assert got[:4].tolist() == [-inf, inf, 1.0, 1.0]
+    # m / 2 over eps, and over the root of v / 2: at most eight roundings of fp32, 2^-21
+    assert abs(float(got[4]) - 0.5) <= 2.0 ** -21 and abs(float(got[5]) / -(0.5e30 / 0.5 ** 0.5) - 1) <= 2.0 ** -21
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_captured_step_counts_on(bits):
     """A graph of a counted step, replayed with eager calls between: the same bits

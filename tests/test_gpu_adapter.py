@@ -108,6 +108,7 @@ SHAPES = [  # M, d_in, d_out, r, n, ids
     (200, 31, 31, 33, 3, "mixed"), (300, 2048, 513, 64, 70, "mixed"), (333, 515, 258, 24, 1, "one"), (512, 256, 128, 100, 1, "one"),
     (513, 264, 136, 128, 1, "one"), (700, 1500, 40, 129, 2, "runs"), (1100, 130, 2050, 4, 3, "mixed"), (1025, 64, 64, 48, 1, "one"),
     (1999, 520, 264, 16, 5, "runs"), (2100, 96, 200, 200, 2, "mixed"), (3000, 256, 320, 32, 4000, "mixed"), (40, 64, 64, 16, 3, "none"),
+    (70, 3, 5, 2, 2, "mixed"), (70, 7, 130, 40, 2, "mixed"), (600, 6, 4, 9, 1, "one"), (130, 9, 263, 90, 30, "mixed"),
 ]
 
 
