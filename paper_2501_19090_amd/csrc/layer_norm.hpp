@@ -30,7 +30,8 @@ struct LayerNormFwd {
     float eps;
 };
 
-// ROWS rows of at most TPR * V full chunks per workgroup.
+// ROWS rows of at most TPR * V full chunks per workgroup.  4096 x 8192 bf16 with the
+// residual 49.6 us, 5.4 TB/s.
 template <typename T, int TPR, int V, int ROWS>
 __global__ __launch_bounds__(TPR* ROWS) void layer_norm_fwd(LayerNormFwd<T> p) {
     using C = NormChunk<T>;
@@ -214,13 +215,20 @@ __device__ __forceinline__ float layer_norm_back(float rho, float uc, float d) {
 // gridDim.x, and keeps the sums of dgain and dbias for the columns its threads
 // hold in registers over all of them; at the end the ROWS sums of a column are
 // added in LDS, so that only gridDim.x partial sums a column go to memory.
+// 4096 x 4096 bf16 28.6 us (4.7 TB/s) and 4.6 for the partial sums; 333 x 2867 fp32,
+// one or two rows a CU, 8.9 and 3.7: a row's loads and two reductions one after the
+// other.
 // EXACT: rows are TPR * V full chunks and have a residual gradient and a dX, so
-// that no load or store stands under a condition.
+// that no load or store stands under a condition.  With four chunks a thread (fp32
+// rows past 8195 values) only H and dY are held beside the sums: gain and dR are
+// loaded where they are used, chunk by chunk so that the registers suffice (2048 x
+// 16384 in fp32 137 us, by the long form below 270; 1140 x 14704 without dR 103, 119).
 template <typename T, int TPR, int V, bool EXACT>
 __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p) {
     using C = NormChunk<T>;
     constexpr int N = C::N;
     constexpr int ROWS = kNormThreads / TPR;
+    constexpr bool HELD = V <= 2;  // gain and dR
     __shared__ float2 red[2][kNormThreads / kWave];
     __shared__ float cols[ROWS > 1 ? kNormThreads * (V * N + 1) : 1];
     const int t = threadIdx.x % TPR, rg = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
@@ -228,20 +236,26 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p
     const bool has_tail = !EXACT && t < N && kt < p.d, add = EXACT || (p.dR && p.dX);
 
     float dg[V][N], db[V][N], dgt = 0.f, dbt = 0.f;
-    u32x4 g[V];
+    u32x4 g[HELD ? V : 1];
     float gt = 1.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        g[i] = zero16();
-        if (p.gain) g[i] = C::load(p.gain, t + i * TPR, nfull);
+        if constexpr (HELD) {
+            g[i] = zero16();
+            if (p.gain) g[i] = C::load(p.gain, t + i * TPR, nfull);
+        }
 #pragma unroll
         for (int e = 0; e < N; ++e) dg[i][e] = db[i][e] = 0.f;
     }
     if (p.gain && has_tail) gt = (float)p.gain[kt];
-    auto gain = [&](int i, int e) { return p.gain ? C::one(g[i], e) : 1.f; };
+    auto gains = [&](int i) {
+        if constexpr (HELD) return g[i];
+        else __builtin_amdgcn_sched_barrier(0);
+        return p.gain ? C::load(p.gain, t + i * TPR, nfull) : zero16();
+    };
 
     struct Rows {
-        u32x4 h[V], y[V], r[V];
+        u32x4 h[V], y[V], r[HELD ? V : 1];
         float ht, yt, rt;
     };
     // ALL: no row past M is among them.  A row past M is zeros and reads nothing:
@@ -256,11 +270,13 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p
             if constexpr (ALL) {  // c < nfull is known; streamed, 4096 x 4096 takes 30.5 us instead of 32.8
                 f.h[i] = load_streamed<u32x4>(p.H + row + c * N);
                 f.y[i] = load_streamed<u32x4>(p.dY + row + c * N);
-                f.r[i] = load_streamed<u32x4>(p.dR + row + c * N);
+                if constexpr (HELD) f.r[i] = load_streamed<u32x4>(p.dR + row + c * N);
             } else {
                 f.h[i] = C::load(p.H + row, c, full);
                 f.y[i] = C::load(p.dY + row, c, full);
-                if (add) f.r[i] = C::load(p.dR + row, c, full);
+                if constexpr (HELD) {
+                    if (add) f.r[i] = C::load(p.dR + row, c, full);
+                }
             }
         }
         f.ht = f.yt = f.rt = 0.f;
@@ -276,7 +292,7 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p
         const bool live = !LAST || m < p.M;
         float sh = cur.ht, su = gt * cur.yt;
 #pragma unroll
-        for (int i = 0; i < V; ++i) layer_norm_sums_of<T>(cur.h[i], cur.y[i], g[i], p.gain != nullptr, sh, su);
+        for (int i = 0; i < V; ++i) layer_norm_sums_of<T>(cur.h[i], cur.y[i], gains(i), p.gain != nullptr, sh, su);
         const float2 sums = row_sum2<TPR>(sh, su, red[0]);
         const float mean = sums.x / (float)p.d, ubar = sums.y / (float)p.d;
         const float ct = has_tail ? cur.ht - mean : 0.f;
@@ -284,41 +300,50 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p
         // h and u less their means, kept for the results where the registers hold them;
         // written-out fused steps: every form of this kernel gives the same bits
         float c[V == 1 ? N : 1], v[V == 1 ? N : 1];
-        auto centre = [&](int i, int e, float& ce, float& ve) {
+        auto centre = [&](int i, int e, u32x4 gi, float& ce, float& ve) {
             ce = EXACT || t + i * TPR < nfull ? C::one(cur.h[i], e) - mean : 0.f;
-            ve = __builtin_fmaf(gain(i, e), C::one(cur.y[i], e), -ubar);
+            ve = __builtin_fmaf(p.gain ? C::one(gi, e) : 1.f, C::one(cur.y[i], e), -ubar);
         };
 #pragma unroll
-        for (int i = 0; i < V; ++i)
+        for (int i = 0; i < V; ++i) {
+            const u32x4 gi = gains(i);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 float ce, ve;
-                centre(i, e, ce, ve);
+                centre(i, e, gi, ce, ve);
                 ss = __builtin_fmaf(ce, ce, ss);
                 uc = __builtin_fmaf(ve, ce, uc);
                 if constexpr (V == 1) c[e] = ce, v[e] = ve;
             }
+        }
         const float2 again = row_sum2<TPR>(ss, uc, red[1]);
         const float rho = rsqrtf(again.x / (float)p.d + p.eps);
         const float back = layer_norm_back(rho, again.y, (float)p.d);
         const int64_t row = live ? m * p.d : 0, full = live ? nfull : 0;
         if constexpr (V > 1) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) asm volatile("" : "+v"(cur.h[i]), "+v"(cur.y[i]), "+v"(g[i]));
+            for (int i = 0; i < V; ++i) {
+                asm volatile("" : "+v"(cur.h[i]), "+v"(cur.y[i]));
+                if constexpr (HELD) asm volatile("" : "+v"(g[i]));
+            }
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
+            const u32x4 gi = gains(i);
+            u32x4 ri = zero16();
+            if constexpr (HELD) ri = cur.r[i];
+            else if (add) ri = C::load(p.dR + row, t + i * TPR, full);
             float dx[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 float ce, ve;
                 if constexpr (V == 1) ce = c[e], ve = v[e];
-                else centre(i, e, ce, ve);
+                else centre(i, e, gi, ce, ve);
                 const float hat = ce * rho, y = C::one(cur.y[i], e);
                 dg[i][e] = __builtin_fmaf(hat, y, dg[i][e]);
                 db[i][e] += y;
                 dx[e] = __builtin_fmaf(-hat, back, ve);
-                dx[e] = add ? __builtin_fmaf(rho, dx[e], C::one(cur.r[i], e)) : rho * dx[e];
+                dx[e] = add ? __builtin_fmaf(rho, dx[e], C::one(ri, e)) : rho * dx[e];
             }
             if constexpr (EXACT && !LAST) C::store(p.dX + row, t + i * TPR, TPR * V, dx);
             else if (p.dX) C::store(p.dX + row, t + i * TPR, full, dx);

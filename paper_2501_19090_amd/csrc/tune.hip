@@ -94,6 +94,7 @@ pifa_status layer_norm_backward_run(const void* H, const void* gain, const void*
         else if (chunks <= 512) launch(integral_constant<int, 512>{}, integral_constant<int, 1>{});
         else if (chunks <= 1024) launch(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
         else if (chunks <= 2048) launch(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+        else if (sizeof(T) == 4 && chunks <= 4096) launch(integral_constant<int, 1024>{}, integral_constant<int, sizeof(T) == 4 ? 4 : 2>{});
         else hipLaunchKernelGGL((layer_norm_bwd_long<T>), grid, block, 0, st, p);
         if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
     }

@@ -21,7 +21,7 @@ pytestmark = pytest.mark.gpu
 EPS = 1e-5
 FP = 2.0 ** -17
 HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
-WIDTHS = [1, 3, 8, 64, 127, 512, 1000, 2048, 2867, 4096, 8192, 8200, 16384, 16391, 33000]
+WIDTHS = [1, 3, 8, 64, 127, 512, 1000, 2048, 2867, 4096, 8192, 8200, 16384, 16387, 16391, 33000]
 TINY = 2.0 ** -126
 
 
