@@ -19,7 +19,7 @@
 // are fp32 and in a fixed order.
 // us of each kernel: 1999 rows of 4096 -> 11008, rank 64: shrink 12, finish 4,
 // expand 21 to 23; gradients of 4096 rows of 4096 x 4096, rank 16: shrink of both
-// jobs 19 (67 MB), finish 4, expand 14 to 17 (67 MB), grads 15 (67 MB), sum 4; of 333
+// jobs 18 (67 MB), finish 4, expand 14 to 17 (67 MB), grads 15 (67 MB), sum 4; of 333
 // rows of 1024 -> 1536, rank 24: 6, 4, 4, 8.  Small calls are chains of launches,
 // each of which waits for the header, then rows, then their data.
 #pragma once
@@ -36,9 +36,7 @@ constexpr int kAdMaxSlots = 4096;
 constexpr int64_t kAdMaxRows = 1 << 20;
 constexpr int kAdMaxSplit = 8;     // of K
 constexpr int kAdThreads = 256;    // of expand
-// Waves of shrink: as many as have room in a CU's LDS twice (ranks of up to 16:
-// 18.7 us with eight, 20.1 with four, 4096 rows of 4096; of 64: 15.8 and 13.2, 1999).
-__host__ __device__ constexpr int adapter_waves(int64_t r) { return r <= 32 ? 8 : 4; }
+constexpr int kAdWaves = 4;        // of shrink
 constexpr int kAdSlice = 64;       // columns that a wave of shrink takes at a time
 
 // ------------------------------------------------------------------ plan
@@ -279,10 +277,10 @@ __device__ __forceinline__ uint32_t adapter_pair(uint32_t even, uint32_t odd, in
 
 // How many workgroups share a tile's K: as many as leave all of them, `target` at
 // most, on the chip at once.
-__host__ __device__ inline int adapter_splits(int tiles, int64_t K, int64_t r, int target) {
+__host__ __device__ inline int adapter_splits(int tiles, int64_t K, int target) {
     int s = tiles > 0 ? target / tiles : 1;
     if (s > kAdMaxSplit) s = kAdMaxSplit;
-    const int64_t most = ceil_div(K, kAdSlice) / adapter_waves(r);  // a slice for every wave
+    const int64_t most = ceil_div(K, kAdSlice) / kAdWaves;  // a slice for every wave
     if (s > most) s = (int)most;
     return s < 1 ? 1 : s;
 }
@@ -316,7 +314,7 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
                                                     int64_t r, int j0, int64_t s0, int64_t s1, int64_t rp, float* out,
                                                     u32x4* lds) {
     constexpr int NX = 2 * RG, NW = 2 * JB;  // loads of a slice: 8 rows each
-    constexpr int WAVES = adapter_waves(16 * JB);
+    constexpr int WAVES = kAdWaves;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int row8 = lane >> 3, c8 = lane & 7;
     const bf16* x[NX];
@@ -432,10 +430,13 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
 }
 
 // Workgroups: x: tiles, y: parts of K, z: blocks of 16 JB columns of t, jobs outermost.
+// Four waves, so that registers (146 for up to 16 columns, 240 for 64) and LDS hold
+// three or two workgroups on a CU (4096 rows of 4096 twice, rank 16: 18.0 us; eight
+// waves, one workgroup a CU, 19.2).
 template <int JB>
-__global__ __launch_bounds__(adapter_waves(16 * JB) * kWave, JB == 4 ? 2 : 1) void adapter_shrink(AdapterShrink j0, AdapterShrink j1, AdapterPlan p, int64_t M,
-                                                             int n, int64_t r, int target) {
-    constexpr int WAVES = adapter_waves(16 * JB), SLICES = WAVES * (8 + 2 * JB) * kWave,
+__global__ __launch_bounds__(kAdWaves * kWave, JB == 1 ? 3 : 2) void adapter_shrink(AdapterShrink j0, AdapterShrink j1, AdapterPlan p,
+                                                                                   int64_t M, int n, int64_t r, int target) {
+    constexpr int WAVES = kAdWaves, SLICES = WAVES * (8 + 2 * JB) * kWave,
                   SUMS = WAVES * kAdTile * (16 * JB + 4) / 4;  // of 16 bytes
     __shared__ u32x4 lds[SLICES > SUMS ? SLICES : SUMS];
     const AdapterHeader h = *p.head;
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(adapter_waves(16 * JB) * kWave, JB == 4 ? 2 : 1) vo
     const int64_t rp = adapter_rp(r);
     const int cols = (int)ceil_div(rp, 16 * JB), job = blockIdx.z / cols, c0 = (blockIdx.z % cols) * 16 * JB;
     const AdapterShrink j = job ? j1 : j0;
-    const int splits = adapter_splits(h.tiles, j.K, r, target);
+    const int splits = adapter_splits(h.tiles, j.K, target);
     if ((int)blockIdx.y >= splits) return;
     const int64_t slices = ceil_div(j.K, kAdSlice);
     const int64_t each = ceil_div(slices, splits), s0 = each * blockIdx.y, s1 = min(s0 + each, slices);
@@ -514,7 +515,7 @@ static __global__ __launch_bounds__(256) void adapter_finish(AdapterFinish j0, A
     const int t = threadIdx.x, y = blockIdx.y;
     {
         const int row = t >> 2, c = (t & 3) * 4;
-        f32x4 v = adapter_t4(j.T + (x * kAdTile + row) * rp + 16 * y + c, adapter_splits(h.tiles, j.K, r, target),
+        f32x4 v = adapter_t4(j.T + (x * kAdTile + row) * rp + 16 * y + c, adapter_splits(h.tiles, j.K, target),
                              (int64_t)h.tiles * kAdTile * rp);
 #pragma unroll
         for (int e = 0; e < 4; ++e) lds[row][c + e] = row < tile.count ? v[e] : 0.f;
@@ -590,7 +591,7 @@ __device__ __forceinline__ void adapter_expand_tile(const AdapterExpand& j, cons
         row[0] = four.x, row[1] = four.y, row[2] = four.z, row[3] = four.w;
     }
     // t's operands
-    const int splits = SUM ? adapter_splits(h.tiles, j.K, r, target) : 1;
+    const int splits = SUM ? adapter_splits(h.tiles, j.K, target) : 1;
     const int64_t group = 4 * (int64_t)blockIdx.y + g;
     u32x4 hi[NB], lo[NB];
     auto operands = [&](int64_t k0) {

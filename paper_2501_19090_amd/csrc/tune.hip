@@ -113,9 +113,10 @@ pifa_status layer_norm_backward_run(const void* H, const void* gain, const void*
 namespace {
 
 constexpr int64_t kAdMaxD = 1 << 19, kAdMaxRank = 1024;
-// Workgroups of a shrink that the chip holds at once, for one or two jobs.
+// Workgroups of shrink that the chip holds at once, three or two a CU, for one or two
+// jobs and by their blocks of columns of t.
 int adapter_target(int64_t r, int jobs) {
-    return (int)((r > 16 && r <= 32 ? 1 : 2) * kCus / (jobs * ceil_div(adapter_rp(r), 64)));
+    return (int)((r <= 16 ? 3 : 2) * kCus / (jobs * ceil_div(adapter_rp(r), 64)));
 }
 
 pifa_status check_plan(int64_t M, int64_t n) {
@@ -164,9 +165,9 @@ hipError_t launch_shrink(const AdapterShrink& a, const AdapterShrink* b, const A
                          int64_t r, int target, hipStream_t st) {
     TimedLaunch timed(kSiteAdapterShrink, st);
     const int64_t rp = adapter_rp(r), jb = std::min<int64_t>(4, rp / 16), most = std::max(a.K, b ? b->K : 0);
-    const dim3 grid((unsigned)adapter_max_tiles(M, n), (unsigned)adapter_splits(1, most, r, target),
+    const dim3 grid((unsigned)adapter_max_tiles(M, n), (unsigned)adapter_splits(1, most, target),
                     (unsigned)(ceil_div(rp, 16 * jb) * (b ? 2 : 1)));
-    const dim3 block((unsigned)adapter_waves(r) * kWave);
+    const dim3 block(kAdWaves * kWave);
     const AdapterShrink& second = b ? *b : a;
     if (jb == 1) hipLaunchKernelGGL((adapter_shrink<1>), grid, block, 0, st, a, second, p, M, (int)n, r, target);
     else if (jb == 2) hipLaunchKernelGGL((adapter_shrink<2>), grid, block, 0, st, a, second, p, M, (int)n, r, target);
@@ -443,7 +444,7 @@ pifa_status adapter_backward(const void* X, const void* A, const void* B, const 
     u32x4* turned_t = (u32x4*)take(adapter_turned_bytes(M, r, n));
     float* part_a = (float*)take(adapter_partial_bytes(M, r, d_in));
     float* part_b = (float*)take(adapter_partial_bytes(M, r, d_out));
-    const int target = adapter_target(r, dB ? 2 : 1);
+    const int target = adapter_target(r, 2);  // also without dB: a gradient has the same bits whichever others are asked for
     const AdapterShrink t{(const bf16*)X, (const bf16*)A, false, scale, T, d_in};
     const AdapterShrink u{(const bf16*)dY, (const bf16*)B, true, scale, U, d_out};
     const AdapterFinish done_u{U, dX ? halves : nullptr, dA ? turned_u : nullptr, d_out}, done_t{T, nullptr, turned_t, d_in};
