@@ -19,7 +19,7 @@
 // are fp32 and in a fixed order.
 // us of each kernel: 1999 rows of 4096 -> 11008, rank 64: shrink 12, finish 4,
 // expand 21 to 23; gradients of 4096 rows of 4096 x 4096, rank 16: shrink of both
-// jobs 18 (67 MB), finish 4, expand 14 to 17 (67 MB), grads 15 (67 MB), sum 4; of 333
+// jobs 17 (67 MB), finish 4, expand 14 to 17 (67 MB), grads 15 (67 MB), sum 4; of 333
 // rows of 1024 -> 1536, rank 24: 6, 4, 4, 8.  Small calls are chains of launches,
 // each of which waits for the header, then rows, then their data.
 #pragma once
@@ -431,8 +431,8 @@ __device__ __forceinline__ void adapter_shrink_tile(const AdapterShrink& j, cons
 
 // Workgroups: x: tiles, y: parts of K, z: blocks of 16 JB columns of t, jobs outermost.
 // Four waves, so that registers (146 for up to 16 columns, 240 for 64) and LDS hold
-// three or two workgroups on a CU (4096 rows of 4096 twice, rank 16: 18.0 us; eight
-// waves, one workgroup a CU, 19.2).
+// three or two workgroups on a CU (4096 rows of 4096 twice, rank 16: 17.2 us; eight
+// waves, one workgroup a CU, 18.4).
 template <int JB>
 __global__ __launch_bounds__(kAdWaves * kWave, JB == 1 ? 3 : 2) void adapter_shrink(AdapterShrink j0, AdapterShrink j1, AdapterPlan p,
                                                                                    int64_t M, int n, int64_t r, int target) {
