@@ -369,3 +369,33 @@ def test_workspaces_of_calls_on_another_stream(as_handle):
     junk = [torch.full((k,), 3.0, device="cuda") for k in (4096, 1 << 18, 1 << 20, 1 << 21) for _ in range(4)]
     torch.cuda.synchronize()
     assert len(junk) == 16 and all(torch.equal(g, w) for g, w in zip(got, want))
+
+
+def test_two_streams_share_a_plan():
+    """Calls that overlap on two streams, with workspaces and outputs of their own."""
+    torch = torch_mod()
+    c = Case(700, 520, 260, 24, 6, "mixed", seed=12)
+    want_y, want = c.forward(Y0=c.y0_dev), c.backward(dX0=c.dx0_dev)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for _ in range(5):
+        for s in streams:
+            got.append((c.forward(Y0=c.y0_dev, stream=s), *c.backward(dX0=c.dx0_dev, stream=s)))
+    torch.cuda.synchronize()
+    for y, dX, dA, dB in got:
+        assert torch.equal(y, want_y) and all(torch.equal(a, b) for a, b in zip((dX, dA, dB), want))
+
+
+def test_a_plan_of_other_numbers_writes_nothing():
+    pifa, torch = _pifa(), torch_mod()
+    c = Case(100, 64, 48, 8, 3, "mixed", seed=13)
+    for M, n in ((200, 3), (100, 5)):
+        other = pifa.AdapterPlan(torch.zeros(M, dtype=torch.int32, device="cuda"), n)
+        assert other.buffer.numel() >= pifa.adapter_plan_bytes(100, 3)
+        other.M, other.n = 100, 3
+        outs = [torch.full(s, 7.0, device="cuda", dtype=t) for s, t in (
+            ((100, 48), torch.bfloat16), ((100, 64), torch.bfloat16), ((3, 8, 64), torch.float32), ((3, 48, 8), torch.float32))]
+        pifa.adapter_forward(c.x_dev, c.a_dev, c.b_dev, other, Y0=c.y0_dev, Y=outs[0])
+        pifa.adapter_backward(c.x_dev, c.a_dev, c.b_dev, other, c.dy_dev, dX0=c.dx0_dev, dX=outs[1], dA=outs[2], dB=outs[3])
+        torch.cuda.synchronize()
+        assert all(bool((t == 7).all()) for t in outs)
