@@ -30,7 +30,9 @@
 namespace pifa {
 
 constexpr int kAdTile = 64;        // rows of a tile
-constexpr int kAdPieceTiles = 8;   // tiles of an adapter that one workgroup of grads sums over
+// Tiles of an adapter that one workgroup of grads sums over (32: 4096 rows of 4 adapters
+// 55.0 us instead of 55.5, 2565 rows of one, 2102 -> 531, 53.3 instead of 39.7).
+constexpr int kAdPieceTiles = 8;
 constexpr int kAdPiece = kAdTile * kAdPieceTiles;
 constexpr int kAdMaxSlots = 4096;
 constexpr int64_t kAdMaxRows = 1 << 20;
@@ -65,7 +67,6 @@ struct AdapterPlan {
     AdapterHeader* head;
     AdapterTile* tiles;    // M / 64 + min(n, M) + 1
     int32_t* rows;         // 64 of each tile, -1 behind the last one
-    int32_t* count;        // n + 1: rows of each bucket
     AdapterPiece* pieces;  // M / 512 + n
     AdapterMulti* multi;   // M / 512
     int32_t* hist;         // for each block of 1024 rows: its rows of each bucket (n + 1)
@@ -86,7 +87,6 @@ __host__ __device__ inline size_t adapter_layout(void* base, int64_t M, int64_t 
     p->head = (AdapterHeader*)take(16);
     p->tiles = (AdapterTile*)take(2 * adapter_max_tiles(M, n));
     p->rows = take(kAdTile * adapter_max_tiles(M, n));
-    p->count = take(n + 1);
     p->pieces = (AdapterPiece*)take(4 * adapter_max_pieces(M, n));
     p->multi = (AdapterMulti*)take(3 * (M / kAdPiece + 1));
     p->hist = take(adapter_blocks(M) > 1 ? adapter_blocks(M) * (n + 1) : 0);
@@ -205,7 +205,6 @@ static __global__ __launch_bounds__(1024) void adapter_place(const int32_t* ids,
         const int64_t last = (int64_t)tile0[a + 1] * kAdTile, end = (int64_t)tile0[a] * kAdTile + total[a];
         if (end + lane < last) p.rows[end + lane] = -1;
     }
-    for (int a = t; a <= n; a += 1024) p.count[a] = total[a];
     __syncthreads();
     auto piece_count = [&](int a) { return max(1, (total[a] + kAdPiece - 1) / kAdPiece); };
     for (int a = t; a < n; a += 1024) at[a] = piece_count(a);
