@@ -460,15 +460,20 @@ __global__ __launch_bounds__(kAdWaves * kWave, JB == 1 ? 3 : 2) void adapter_shr
 }
 
 // ------------------------------------------------------------------ finish
+// What is left over a part; nothing over an infinite one or no number.
+__device__ __forceinline__ float adapter_rest(float v, bf16 part) {
+    const float rest = v - (float)part;
+    return fabsf(rest) <= 3.402823466e38f ? rest : 0.f;
+}
 // The nearest bf16 value, and that nearest to what it leaves.
 __device__ __forceinline__ void adapter_split2(float v, bf16& hi, bf16& lo) {
     hi = (bf16)v;
-    lo = (bf16)(v - (float)hi);
+    lo = (bf16)adapter_rest(v, hi);
 }
 // v as three bf16 values that add up to all its bits.
 __device__ __forceinline__ void adapter_split3(float v, bf16 (&s)[3]) {
     adapter_split2(v, s[0], s[1]);
-    s[2] = (bf16)((v - (float)s[0]) - (float)s[1]);
+    s[2] = (bf16)(adapter_rest(v, s[0]) - (float)s[1]);
 }
 
 // t as operands in the order of a wave's lanes, 16 bytes each:

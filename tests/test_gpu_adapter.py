@@ -254,6 +254,27 @@ def test_special_values_stay_in_their_rows():
     assert torch.equal(got[0][other], dX[other]) and torch.equal(got[1][:3], dA[:3]) and torch.equal(got[2][:3], dB[:3])
 
 
+@pytest.mark.parametrize("M", [100, 300])
+def test_infinite_sums(M):
+    """t and u past fp32 are infinite, and so are the results that take them with one
+    sign, whichever of them; a row's own, and its adapter's gradients."""
+    pifa, torch = _pifa(), torch_mod()
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    X, dY = torch.ones(M, 64, **bf), torch.ones(M, 48, **bf)
+    X[3], X[4], dY[3], dY[4] = 1e38, -1e38, 1e38, -1e38
+    A, B = torch.ones(2, 1, 64, **bf), torch.ones(2, 48, 1, **bf)
+    plan = pifa.AdapterPlan(torch.arange(M, dtype=torch.int32, device="cuda") % 2, 2)  # rows 3 and 4: 1 and 0
+    Y = pifa.adapter_forward(X, A, B, plan)
+    dX, dA, dB = pifa.adapter_backward(X, A, B, plan, dY)
+    torch.cuda.synchronize()
+    inf = float("inf")
+    for out, other in ((Y, 64.0), (dX, 48.0)):
+        assert (out[3] == inf).all() and (out[4] == -inf).all()
+        assert (out[:3] == other).all() and (out[5:] == other).all()
+    # -inf times a negative row is positive: every term of both adapters is, or is finite
+    assert (dA == inf).all() and (dB == inf).all()
+
+
 def test_rows_anywhere_in_a_buffer():
     """Buffers that start at any element, and what lies around them."""
     pifa, torch = _pifa(), torch_mod()
