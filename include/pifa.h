@@ -468,7 +468,9 @@ pifa_status q4_layer_reserve(q4_handle h, int64_t max_M);
  *   Y     device, M x d, dtype.
  * Limits, alignment, stream and M = 0 as for rms_norm_forward.  Sums are fp32, that of the
  * squares taken after the mean is off (a row whose squares of c sum to more than
- * 3.4e38 has rho = 0); H and Y are each rounded once, Y from the unrounded H.
+ * 3.4e38 has rho = 0, one whose own sum does has no number), and what rounding left
+ * of the mean in c is taken off by a second mean, so that rows that hardly vary
+ * keep their digits; H and Y are each rounded once, Y from the unrounded H.
  * H and Y may each be X or R themselves, not each other, and overlap nothing
  * otherwise (PIFA_ERR_INVALID_ARG).
  */

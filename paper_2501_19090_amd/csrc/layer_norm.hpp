@@ -9,14 +9,63 @@
 // the registers of TPR threads, V 16-byte chunks each, between its sums and its
 // results.  The squares are summed after the mean is taken off, in a second
 // reduction: a sum of squares less the squared mean would lose the digits that
-// rows far from zero share.  Sums, mean and rho are fp32; each result is rounded
-// once, from the unrounded h.
+// rows far from zero share.  A rounded mean is itself off by the last bits of the
+// row's size, which rho makes large where a row hardly varies (4096 values of 1000.1:
+// hat up to 0.04 in place of 0).  So the second reduction also sums the c_k, whose
+// mean is what the first one missed: it is taken off c, and its square off the mean
+// of the squares.  Sums, mean and rho are fp32; each result is rounded once, from
+// the unrounded h.
 #pragma once
 
 #include "norm.hpp"
 #include "streamed.hpp"
 
 namespace pifa {
+
+// Of c with a mean of `off` that is still in it; NaN stays NaN.
+__device__ __forceinline__ float layer_norm_rho(float ss, float off, float d, float eps) {
+    const float var = __builtin_fmaf(-off, off, ss / d);
+    return rsqrtf((var < 0.f ? 0.f : var) + eps);
+}
+
+// The value of another lane of the 16 around this one.
+template <int CTRL>
+__device__ __forceinline__ float layer_norm_dpp(float v) {
+    const int i = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, CTRL, 0xF, 0xF, false));
+}
+
+// Sums of up to four values over the TPR threads of each row, in a fixed order.  The
+// four lanes of a quad take a value each, so that adding up over the wave, and
+// then over the row's waves, is adding up one value.  `red` holds four floats a wave;
+// two calls in a row need two arrays.
+template <int TPR>
+__device__ __forceinline__ float4 row_sum4(float a, float b, float c, float d, float* red) {
+    constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kTurn4 = 0x124, kTurn8 = 0x128;  // quad_perm, row_ror
+    constexpr int W = TPR / kWave;
+    const int lane = threadIdx.x & (kWave - 1);
+    const bool odd = lane & 1, high = lane & 2;
+    const float ab = (odd ? b : a) + layer_norm_dpp<kSwap1>(odd ? a : b);
+    const float cd = (odd ? d : c) + layer_norm_dpp<kSwap1>(odd ? c : d);
+    float v = (high ? cd : ab) + layer_norm_dpp<kSwap2>(high ? ab : cd);
+    v += layer_norm_dpp<kTurn4>(v);
+    v += layer_norm_dpp<kTurn8>(v);
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
+    if constexpr (W > 1) {
+        const int wave = threadIdx.x / kWave;
+        if (lane < 4) red[4 * wave + lane] = v;
+        __syncthreads();
+        v = red[4 * (wave / W * W + lane / 4 % W) + lane % 4];
+        v += layer_norm_dpp<kTurn4>(v);
+        if constexpr (W > 2) v += layer_norm_dpp<kTurn8>(v);
+        if constexpr (W > 4) v += __shfl_xor(v, 16);
+        if constexpr (W > 8) v += __shfl_xor(v, 32);
+    }
+    // the first four lanes': the others added up in another order
+    auto of = [&](int k) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), k)); };
+    return float4{of(0), of(1), of(2), of(3)};
+}
 
 template <typename T>
 struct LayerNormFwd {
@@ -36,7 +85,7 @@ template <typename T, int TPR, int V, int ROWS>
 __global__ __launch_bounds__(TPR* ROWS) void layer_norm_fwd(LayerNormFwd<T> p) {
     using C = NormChunk<T>;
     constexpr int N = C::N;
-    __shared__ float red[2][TPR * ROWS / kWave];
+    __shared__ float red[2][4 * TPR * ROWS / kWave];
     const int t = threadIdx.x % TPR;
     const int64_t m = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
     const bool live = m < p.M;
@@ -83,9 +132,9 @@ __global__ __launch_bounds__(TPR* ROWS) void layer_norm_fwd(LayerNormFwd<T> p) {
         for (int i = 0; i < V; ++i) C::store(p.H + row, t + i * TPR, full, h[i]);
         if (tail) p.H[row + kt] = (T)ht;
     }
-    const float mean = row_reduce<TPR>(sum, red[0]) / (float)p.d;
+    const float mean = row_sum4<TPR>(sum, 0.f, 0.f, 0.f, red[0]).x / (float)p.d;
     ht = tail ? ht - mean : 0.f;
-    float ss = ht * ht;
+    float ss = ht * ht, sc = ht;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const bool in = t + i * TPR < full;
@@ -93,20 +142,22 @@ __global__ __launch_bounds__(TPR* ROWS) void layer_norm_fwd(LayerNormFwd<T> p) {
         for (int e = 0; e < N; ++e) {
             h[i][e] = in ? h[i][e] - mean : 0.f;
             ss += h[i][e] * h[i][e];
+            sc += h[i][e];
         }
     }
-    const float rho = rsqrtf(row_reduce<TPR>(ss, red[1]) / (float)p.d + p.eps);
+    const float4 again = row_sum4<TPR>(ss, sc, 0.f, 0.f, red[1]);
+    const float off = again.y / (float)p.d, rho = layer_norm_rho(again.x, off, (float)p.d, p.eps);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            h[i][e] *= rho;
+            h[i][e] = __builtin_fmaf(h[i][e], rho, -off * rho);
             if (p.gain) h[i][e] *= C::one(g[i], e);
             if (p.bias) h[i][e] += C::one(b[i], e);
         }
         C::store(p.Y + row, t + i * TPR, full, h[i]);
     }
-    if (tail) p.Y[row + kt] = (T)(ht * rho * gt + bt);
+    if (tail) p.Y[row + kt] = (T)((ht - off) * rho * gt + bt);
 }
 
 // Rows too long for a workgroup's registers are read again for each sum and for
@@ -116,7 +167,7 @@ template <typename T>
 __global__ __launch_bounds__(kNormThreads) void layer_norm_fwd_long(LayerNormFwd<T> p) {
     using C = NormChunk<T>;
     constexpr int N = C::N;
-    __shared__ float red[2][kNormThreads / kWave];
+    __shared__ float red[2][4 * kNormThreads / kWave];
     const int64_t row = (int64_t)blockIdx.x * p.d;
     const int64_t full = p.d / N, kt = full * N + threadIdx.x;
     const bool tail = threadIdx.x < N && kt < p.d;
@@ -136,16 +187,21 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_fwd_long(LayerNormFwd
 #pragma unroll
         for (int e = 0; e < N; ++e) sum += h[e];
     }
-    const float mean = row_reduce<kNormThreads>(sum, red[0]) / (float)p.d;
+    const float mean = row_sum4<kNormThreads>(sum, 0.f, 0.f, 0.f, red[0]).x / (float)p.d;
     const float ct = tail ? ht - mean : 0.f;
-    float ss = ct * ct;
+    float ss = ct * ct, sc = ct;
     for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
         float h[N];
         load(c, h);
 #pragma unroll
-        for (int e = 0; e < N; ++e) ss += (h[e] - mean) * (h[e] - mean);
+        for (int e = 0; e < N; ++e) {
+            const float k = h[e] - mean;
+            ss += k * k;
+            sc += k;
+        }
     }
-    const float rho = rsqrtf(row_reduce<kNormThreads>(ss, red[1]) / (float)p.d + p.eps);
+    const float4 again = row_sum4<kNormThreads>(ss, sc, 0.f, 0.f, red[1]);
+    const float off = again.y / (float)p.d, rho = layer_norm_rho(again.x, off, (float)p.d, p.eps);
     for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
         float h[N], y[N];
         load(c, h);
@@ -154,7 +210,7 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_fwd_long(LayerNormFwd
         if (p.bias) b = C::load(p.bias, c, full);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            y[e] = (h[e] - mean) * rho;
+            y[e] = (h[e] - mean - off) * rho;
             if (p.gain) y[e] *= C::one(g, e);
             if (p.bias) y[e] += C::one(b, e);
         }
@@ -163,7 +219,7 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_fwd_long(LayerNormFwd
     }
     if (tail) {
         if (p.H) p.H[row + kt] = (T)ht;
-        p.Y[row + kt] = (T)(ct * rho * (p.gain ? (float)p.gain[kt] : 1.f) + (p.bias ? (float)p.bias[kt] : 0.f));
+        p.Y[row + kt] = (T)((ct - off) * rho * (p.gain ? (float)p.gain[kt] : 1.f) + (p.bias ? (float)p.bias[kt] : 0.f));
     }
 }
 
@@ -222,19 +278,23 @@ __device__ __forceinline__ float layer_norm_back(float rho, float uc, float d) {
 // that no load or store stands under a condition.  With four chunks a thread (fp32
 // rows past 8195 values) only H and dY are held beside the sums: gain and dR are
 // loaded where they are used, chunk by chunk so that the registers suffice (2048 x
-// 16384 in fp32 137 us, by the long form below 270; 1140 x 14704 without dR 103, 119).
+// 16384 in fp32 123 us, by the long form below 270; 1140 x 14704 without dR 58, 119;
+// 300 x 10007 26, 40).
 template <typename T, int TPR, int V, bool EXACT>
 __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p) {
     using C = NormChunk<T>;
     constexpr int N = C::N;
     constexpr int ROWS = kNormThreads / TPR;
     constexpr bool HELD = V <= 2;  // gain and dR
-    __shared__ float2 red[2][kNormThreads / kWave];
+    __shared__ float red[2][4 * kNormThreads / kWave];
     __shared__ float cols[ROWS > 1 ? kNormThreads * (V * N + 1) : 1];
     const int t = threadIdx.x % TPR, rg = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
     const int64_t step = (int64_t)gridDim.x * ROWS, nfull = EXACT ? TPR * V : p.d / N, kt = nfull * N + t;
     const bool has_tail = !EXACT && t < N && kt < p.d, add = EXACT || (p.dR && p.dX);
 
+    float mine = has_tail ? 1.f : 0.f;  // values of a row that this thread holds
+#pragma unroll
+    for (int i = 0; i < V; ++i) mine += EXACT || t + i * TPR < nfull ? (float)N : 0.f;
     float dg[V][N], db[V][N], dgt = 0.f, dbt = 0.f;
     u32x4 g[HELD ? V : 1];
     float gt = 1.f;
@@ -293,10 +353,13 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p
         float sh = cur.ht, su = gt * cur.yt;
 #pragma unroll
         for (int i = 0; i < V; ++i) layer_norm_sums_of<T>(cur.h[i], cur.y[i], gains(i), p.gain != nullptr, sh, su);
-        const float2 sums = row_sum2<TPR>(sh, su, red[0]);
+        const float4 sums = row_sum4<TPR>(sh, su, 0.f, 0.f, red[0]);
         const float mean = sums.x / (float)p.d, ubar = sums.y / (float)p.d;
-        const float ct = has_tail ? cur.ht - mean : 0.f;
+        float ct = has_tail ? cur.ht - mean : 0.f;
         float ss = ct * ct, uc = (gt * cur.yt - ubar) * ct;
+        // a thread's sum of bf16 values that lie close together is exact, so what the
+        // mean leaves of it is their c's sum
+        float sc = sizeof(T) == 2 ? __builtin_fmaf(-mine, mean, sh) : ct;
         // h and u less their means, kept for the results where the registers hold them;
         // written-out fused steps: every form of this kernel gives the same bits
         float c[V == 1 ? N : 1], v[V == 1 ? N : 1];
@@ -312,13 +375,15 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p
                 float ce, ve;
                 centre(i, e, gi, ce, ve);
                 ss = __builtin_fmaf(ce, ce, ss);
-                uc = __builtin_fmaf(ve, ce, uc);
+                uc = __builtin_fmaf(ve, ce, uc);  // u - ubar adds up to nothing: c's mean need not be off it
+                if constexpr (sizeof(T) == 4) sc += ce;
                 if constexpr (V == 1) c[e] = ce, v[e] = ve;
             }
         }
-        const float2 again = row_sum2<TPR>(ss, uc, red[1]);
-        const float rho = rsqrtf(again.x / (float)p.d + p.eps);
+        const float4 again = row_sum4<TPR>(ss, uc, sc, 0.f, red[1]);
+        const float off = again.z / (float)p.d, rho = layer_norm_rho(again.x, off, (float)p.d, p.eps), left = -off * rho;
         const float back = layer_norm_back(rho, again.y, (float)p.d);
+        ct -= off;
         const int64_t row = live ? m * p.d : 0, full = live ? nfull : 0;
         if constexpr (V > 1) {
 #pragma unroll
@@ -339,7 +404,7 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd(LayerNormBwd<T> p
                 float ce, ve;
                 if constexpr (V == 1) ce = c[e], ve = v[e];
                 else centre(i, e, gi, ce, ve);
-                const float hat = ce * rho, y = C::one(cur.y[i], e);
+                const float hat = __builtin_fmaf(ce, rho, left), y = C::one(cur.y[i], e);
                 dg[i][e] = __builtin_fmaf(hat, y, dg[i][e]);
                 db[i][e] += y;
                 dx[e] = __builtin_fmaf(-hat, back, ve);
@@ -422,7 +487,7 @@ template <typename T>
 __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd_long(LayerNormBwd<T> p) {
     using C = NormChunk<T>;
     constexpr int N = C::N;
-    __shared__ float2 red[2][kNormThreads / kWave];
+    __shared__ float red[2][4 * kNormThreads / kWave];
     const int64_t full = p.d / N, kt = full * N + threadIdx.x;
     const bool tail = threadIdx.x < N && kt < p.d;
     float* dg = p.dgain ? p.dgain + (int64_t)blockIdx.x * p.stride : nullptr;
@@ -449,10 +514,10 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd_long(LayerNormBwd
                 su += u[e];
             }
         }
-        const float2 sums = row_sum2<kNormThreads>(sh, su, red[0]);
+        const float4 sums = row_sum4<kNormThreads>(sh, su, 0.f, 0.f, red[0]);
         const float mean = sums.x / (float)p.d, ubar = sums.y / (float)p.d;
-        const float ct = tail ? ht - mean : 0.f;
-        float ss = ct * ct, uc = (gt * yt - ubar) * ct;
+        float ct = tail ? ht - mean : 0.f;
+        float ss = ct * ct, uc = (gt * yt - ubar) * ct, sc = ct;
         for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
             float h[N], y[N], u[N];
             load(row, c, h, y, u);
@@ -461,17 +526,19 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd_long(LayerNormBwd
                 const float k = h[e] - mean;
                 ss += k * k;
                 uc += (u[e] - ubar) * k;
+                sc += k;
             }
         }
-        const float2 again = row_sum2<kNormThreads>(ss, uc, red[1]);
-        const float rho = rsqrtf(again.x / (float)p.d + p.eps);
+        const float4 again = row_sum4<kNormThreads>(ss, uc, sc, 0.f, red[1]);
+        const float off = again.z / (float)p.d, rho = layer_norm_rho(again.x, off, (float)p.d, p.eps);
         const float back = layer_norm_back(rho, again.y, (float)p.d);
+        ct -= off;
         const bool begun = m != blockIdx.x;
         for (int64_t c = threadIdx.x; c < full; c += kNormThreads) {
             float h[N], y[N], u[N], dx[N];
             load(row, c, h, y, u);
 #pragma unroll
-            for (int e = 0; e < N; ++e) h[e] = (h[e] - mean) * rho;
+            for (int e = 0; e < N; ++e) h[e] = (h[e] - mean - off) * rho;
             if (dg) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) dg[c * N + e] = (begun ? dg[c * N + e] : 0.f) + h[e] * y[e];

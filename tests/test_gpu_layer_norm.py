@@ -300,3 +300,69 @@ def test_workspace_of_a_call_on_another_stream(as_handle):
     junk = [torch.full((pifa.layer_norm_backward_bytes(M, d) // 4,), 3.0, device="cuda") for _ in range(8)]
     torch.cuda.synchronize()
     assert len(junk) == 8 and all(torch.equal(g, w) for g, w in zip(got, want))
+
+
+def _narrow(h):
+    """rho, hat, and the errors of rho (relative) and of hat, of rows whose mean may be
+    much larger than their deviations.  The first mean is off by dm = FP mean|h|, and
+    so is every c; c's own mean takes that off but for FP of what it sums and the
+    roundings of two subtractions.  The mean of the squares loses FP of itself, dm^2
+    among it, and what is left of the mean squared."""
+    mean = lambda a: a.mean(1, keepdims=True)
+    c = h - mean(h)
+    var = mean(c * c)
+    rho = 1.0 / np.sqrt(var + EPS)
+    dm = FP * mean(np.abs(h))
+    left = 2 * FP * (mean(np.abs(c)) + dm)
+    off = left + 2.0 ** -23 * (np.abs(c) + dm)
+    drho = (2 * FP * (var + dm ** 2) + left ** 2) / (var + EPS) + 2.0 ** -22
+    hat = c * rho
+    return rho, hat, drho, np.abs(hat) * (drho + 2.0 ** -23) + rho * off * (1 + drho), rho * dm
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [2867, 4096, 5000, 16384, 40003])
+def test_rows_that_hardly_vary(d, dtype):
+    """Constant rows, whose centred values are zero, and rows that vary by a hundred
+    thousandth of their size: in fp32, and in bf16 as a sum with a residual that fp32
+    holds exactly; the gradients in bf16 from the rounded sum."""
+    pifa, torch = _pifa(), torch_mod()
+    rng = np.random.default_rng([50, d])
+    base = np.array([100.1, 1000.1, -10000.3, 1e5 + 0.7, 1000.1, -100.1, 1000.1, 12345.6])
+    x = np.repeat(base[:, None], d, 1)
+    x[4:] *= 1 + 1e-5 * rng.standard_normal((4, d))
+    g_dev, g = _vec(d, dtype, 51)
+    b_dev, b = _vec(d, dtype, 52, mean=0.0)
+    dy_dev, dy = _rows(len(base), d, dtype, 53, outliers=False)
+    r, r_dev = None, None
+    if dtype == "bf16":
+        # in steps of 2^-8 of the row's power of two over 2^8: 17 bits in all
+        big = inputs.round_to(x, "bf16")[1]
+        step = 2.0 ** (np.floor(np.log2(np.abs(base)))[:, None] - 16)
+        r_st, r = inputs.round_to(np.clip(np.round((x - big) / step), -256, 256) * step, "bf16")
+        x, r_dev = big, to_dev(r_st)
+    x_st, x = inputs.round_to(x, dtype)
+    h = x if r is None else x + r
+    assert np.array_equal(h, h.astype(np.float32))
+    H = torch.empty_like(to_dev(x_st))
+    Y = pifa.layer_norm_forward(to_dev(x_st), g_dev, b_dev, EPS, R=r_dev, H=H)
+    one = [pifa.layer_norm_backward(H[m:m + 1], g_dev, dy_dev[m:m + 1], EPS) for m in range(len(base))]
+    torch.cuda.synchronize()
+    _, hat, _, eh, _ = _narrow(h)
+    y = hat * g + b
+    _close(from_dev(Y), y, np.abs(y) * HALF[dtype] + np.abs(g) * eh + 2.0 ** -22 * (np.abs(g * hat) + np.abs(b)), "Y")
+    h = from_dev(H)
+    mean = lambda a: a.mean(1, keepdims=True)
+    rho, hat, drho, eh, off = _narrow(h)
+    u = dy * g
+    au, back = np.abs(u), np.abs(mean(u * hat))
+    # u - mean(u) has at most |u| + mean|u|, c before its mean is taken off |c| + dm; what
+    # is left of u's mean, FP of mean|u|, meets the dm
+    eb = 2 * FP * mean((au + mean(au)) * (np.abs(hat) + off)) + 2 * off * FP * mean(au) + back * (drho + FP)
+    want = [o.layer_norm_backward(h[m:m + 1], g, dy[m:m + 1], EPS) for m in range(len(base))]
+    for m, (got, (dx, dg, db)) in enumerate(zip(one, want)):
+        i = slice(m, m + 1)
+        tol = rho[i] * (2 * FP * (au[i] + mean(au[i])) + eh[i] * back[i] + (np.abs(hat[i]) + eh[i]) * eb[i])
+        _close(from_dev(got[0]), dx, tol + np.abs(dx) * (drho[i] + HALF[dtype]) + TINY, "dX %d" % m)
+        _close(from_dev(got[1]), dg, (np.abs(dy[i]) * (eh[i] + 2.0 ** -23 * np.abs(hat[i])))[0] + 1e-30, "dgain %d" % m)
+        _close(from_dev(got[2]), db, FP * np.abs(dy[m]) + 1e-30, "dbias %d" % m)
