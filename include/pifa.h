@@ -576,6 +576,8 @@ size_t adapter_backward_bytes(int64_t M, int64_t d_in, int64_t d_out, int64_t r,
  * AdamW over many tensors in one launch.  Step t, for every value:
  *   g' = g grad_scale,   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2,
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * What p loses, lr weight_decay p and the update, is added up in fp32 and taken off
+ * p with one rounding.
  */
 typedef struct {
     float* p;             /* device, n, fp32: read and written                    */

@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_update(AdamwArgs h) {
     const int left = (int)min((int64_t)kAdamwChunk, T.n - first);
     const AdamwStep step = h.step.t ? h.step : *h.count;
     const float c = h.grad_scale ? *h.grad_scale : 1.f;
-    const float keep = (float)(1.0 - h.lr * T.decay);
+    const float fall = (float)(h.lr * T.decay);
     uint32_t key = 0;
     if constexpr (EIGHT) {
         key = adamw_mix(adamw_mix(h.seed) + (uint32_t)step.t);
@@ -234,8 +234,13 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_update(AdamwArgs h) {
             }
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            p[i][e] = p[i][e] * keep - adamw_quotient(step.rate * m[i][e], __builtin_amdgcn_sqrtf(v[i][e]) * step.root + h.eps);
+        for (int e = 0; e < 4; ++e) {
+            // the decay is added to the update before both meet p: 1 - lr decay, rounded to
+            // fp32 first, would make 1.2e-7 of 1e-7 and nothing of 1e-8 for every value in
+            // every step.  An infinite p stays infinite.
+            const float q = adamw_quotient(step.rate * m[i][e], __builtin_amdgcn_sqrtf(v[i][e]) * step.root + h.eps);
+            p[i][e] -= __builtin_fmaf(fall, __builtin_amdgcn_fmed3f(p[i][e], -0x1.FFFFFEp127f, 0x1.FFFFFEp127f), q);
+        }
         uint32_t mb = 0, vb = 0;
         if constexpr (EIGHT) {
             uint32_t rm[4], rv[4];

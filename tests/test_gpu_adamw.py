@@ -282,3 +282,38 @@ def test_refused_calls():
         opt.step(1e-3)
         opt.step(1e-3)
         assert opt.count() == 2
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("lr", [1e-6, 3e-7, 1.5e-7, 2e-5])
+def test_small_decays_are_right_on_average(lr, bits):
+    """lr * decay of 1.5e-8 to 2e-6, near or below the steps of fp32 at 1: over
+    many values the decay is the formula's.  p is rounded once, by half a step (2^-24
+    of it) at most, up or down as its update falls, which spans many steps: the
+    regression of what p lost beside the update on p has an error of deviation 2^-24
+    (sum p^4)^1/2 / sum p^2 at most, and six of these are allowed.  The update itself,
+    of either sign whatever p is, is good to 8 * 2^-24 of it, likewise."""
+    torch = torch_mod()
+    c = Case([1, 1 << 20], bits, torch.float32, False, 41)
+    g, before = c.g[1].numpy(), c.p[1].astype(np.float64)
+    c.opt.step(lr, 0.9, 0.99, 1e-8, step=9)
+    torch.cuda.synchronize()
+    m, v = o.adamw_moments(g, c.m[1], c.v[1], 0.9, 0.99)
+    upd = lr / (1 - 0.9 ** 9) * m.astype(np.float64) / (np.sqrt(v.astype(np.float64) / (1 - 0.99 ** 9)) + 1e-8)
+    assert np.median(np.abs(upd) / np.abs(before)) > 16 * STEP
+    lost = before - from_dev(c.p_dev[1]) - upd
+    got = (before * lost).sum() / (before ** 2).sum()
+    off = 6 * STEP * (np.sqrt((before ** 4).sum()) + 8 * np.sqrt((before ** 2 * upd ** 2).sum())) / (before ** 2).sum()
+    assert off < 0.05 * lr * c.decay[1] and abs(got - lr * c.decay[1]) <= off, (got, lr * c.decay[1], off)
+    c.opt.close()
+
+
+def test_infinite_parameters_stay_infinite():
+    pifa, torch = _pifa(), torch_mod()
+    inf = float("inf")
+    for decay in (0.0, 0.1):
+        p, g = torch.tensor([inf, -inf, 1.0], device="cuda"), torch.ones(3, device="cuda")
+        with pifa.AdamW([p], [g], decay) as opt:
+            opt.step(1e-3)
+            torch.cuda.synchronize()
+        assert p[:2].tolist() == [inf, -inf] and abs(float(p[2]) - (1 - 1e-3 * (1 + decay))) <= 2.0 ** -22
