@@ -538,8 +538,9 @@ size_t adapter_plan_bytes(int64_t M, int64_t n);
  *   work   device, at least adapter_forward_bytes(...) bytes, 16-byte aligned; it
  *          keeps nothing between calls, and calls that may overlap need one each.
  * No alignment is required of the others.  X A^T is held in fp32 and multiplied
- * as two bf16 values (past their range, 3.39e38, as infinite); Y is rounded once.  A row's sums depend on how many rows
- * the batch has of each adapter (K is cut by their tiles), and are the same in
+ * as two bf16 values (past their range, 3.39e38, as infinite); Y is rounded once.
+ * Infinities give what the formula makes of them.  A row's sums depend on how many
+ * rows the batch has of each adapter (K is cut by their tiles), and are the same in
  * each call on the same batch.  M = 0 returns PIFA_OK without launching.
  * Asynchronous on `stream`.
  */

@@ -15,8 +15,11 @@
 //   grads:  sums over rows; a lane holds 8 rows of 8 columns and turns them round
 //           in its registers, so that the rows become the instruction's K.
 // t and u are fp32 sums; they reach the matrix cores as two bf16 values each (16
-// bits) where the result is bf16, as three (24 bits) where it is fp32.  All sums
-// are fp32 and in a fixed order.
+// bits) where the result is bf16, as three (24 bits) where it is fp32.  The parts
+// behind the first have either sign or none, and beside an infinite operand would
+// make no number of an infinity; so their products are summed first and kept finite,
+// and what the first part, of t's own sign, adds decides.  All sums are fp32 and in a
+// fixed order.
 // us of each kernel: 1999 rows of 4096 -> 11008, rank 64: shrink 12, finish 4,
 // expand 21 to 23; gradients of 4096 rows of 4096 x 4096, rank 16: shrink of both
 // jobs 17 (67 MB), finish 4, expand 14 to 17 (67 MB), grads 15 (67 MB), sum 4; of 333
@@ -269,6 +272,20 @@ __device__ __forceinline__ f32x4 adapter_mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Of 16 columns: a lane has four values of each.
+__device__ __forceinline__ f32x4 adapter_mfma16(uint2 a, uint2 b, f32x4 c) {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), c, 0, 0, 0);
+}
+
+// Infinities and what is no number made finite.
+__device__ __forceinline__ f32x4 adapter_finite(f32x4 v) {
+    constexpr float most = 0x1.FFFFFEp127f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_amdgcn_fmed3f(v[e], -most, most);
+    return v;
+}
+
 // Two rows' values in a register each: the lower or the upper ones of both.
 __device__ __forceinline__ uint32_t adapter_pair(uint32_t even, uint32_t odd, int half) {
     return __builtin_amdgcn_perm(odd, even, half ? 0x07060302u : 0x05040100u);
@@ -478,7 +495,7 @@ __device__ __forceinline__ void adapter_split3(float v, bf16 (&s)[3]) {
 
 // t as operands in the order of a wave's lanes, 16 bytes each:
 //   halves: for each group of 16 rows and 32 columns, the values' and what they
-//           leave (up to 16 columns: both in one, in its two halves of K);
+//           leave (up to 16 columns: four values and four of what they leave in one);
 //   turned: for 32 rows and 16 columns, three parts, K along the rows.
 struct AdapterFinish {
     const float* T;  // splits x 64 tiles x rp
@@ -536,9 +553,15 @@ static __global__ __launch_bounds__(256) void adapter_finish(AdapterFinish j0, A
             lo[e] = b;
         }
         const int64_t group = x * 4 + row / 16;
-        const int q = rp == 16 ? c : 2 * (y & 1) + c;
-        j.halves[adapter_half_at(group, rp, y / 2, 0) + 16 * q + lane] = __builtin_bit_cast(u32x4, hi);
-        j.halves[adapter_half_at(group, rp, y / 2, 1) + 16 * (rp == 16 ? q + 2 : q) + lane] = __builtin_bit_cast(u32x4, lo);
+        const u32x4 h = __builtin_bit_cast(u32x4, hi), l = __builtin_bit_cast(u32x4, lo);
+        u32x4* at = j.halves + adapter_half_at(group, rp, y / 2, 0) + lane;
+        if (rp == 16) {
+            at[16 * (2 * c)] = u32x4{h[0], h[1], l[0], l[1]};
+            at[16 * (2 * c + 1)] = u32x4{h[2], h[3], l[2], l[3]};
+        } else {
+            at[16 * (2 * (y & 1) + c)] = h;
+            j.halves[adapter_half_at(group, rp, y / 2, 1) + lane + 16 * (2 * (y & 1) + c)] = l;
+        }
     }
     if (j.turned && t >= 128) {  // 16 columns x 8 of 8 rows
         const int col = t & 15, r8 = (t >> 4) & 7;
@@ -574,7 +597,7 @@ constexpr int kAdWide = 128;  // columns that a workgroup of expand takes
 // column i is c0 + 8 i + u, so that a lane ends up with 8 columns in a row and 16
 // neighbouring lanes with 256 bytes of each row of Y.  The waves share W's rows of
 // these columns, which go through LDS in the order of the operands, KB blocks of 32
-// columns of t at a time; 0: up to 16 columns, both halves of t in one instruction.
+// columns of t at a time; 0: up to 16 columns, instructions of 16.
 // (W in registers, 64 rows a wave: eight waves a CU instead of twenty, and 1999 rows
 // of 11008 with rank 64 take 30 us.)  ONE: those blocks are all.  SUM: t is still in
 // parts.  COL: W's rows are the columns of t; a thread takes 8 columns of 8 of them
@@ -603,9 +626,11 @@ __device__ __forceinline__ void adapter_expand_tile(const AdapterExpand& j, cons
         for (int b = 0; b < NB; ++b) {
             if constexpr (SUM) {
                 const float* t = j.T + (16 * group + min(i, max(0, tile.count - 1 - 16 * g))) * rp + k0 +
-                                 (KB == 0 ? 8 * (q & 1) : 32 * b + 8 * q);
+                                 (KB == 0 ? 4 * q : 32 * b + 8 * q);
                 const int64_t stride = (int64_t)h.tiles * kAdTile * rp;
-                const f32x4 x = adapter_t4(t, splits, stride), y = adapter_t4(t + 4, splits, stride);
+                const f32x4 x = adapter_t4(t, splits, stride);
+                f32x4 y = x;
+                if constexpr (KB != 0) y = adapter_t4(t + 4, splits, stride);
                 bf16x8 v[2];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -616,7 +641,7 @@ __device__ __forceinline__ void adapter_expand_tile(const AdapterExpand& j, cons
                 }
                 hi[b] = __builtin_bit_cast(u32x4, v[0]);
                 lo[b] = __builtin_bit_cast(u32x4, v[1]);
-                if constexpr (KB == 0) hi[0] = q < 2 ? hi[0] : lo[0];
+                if constexpr (KB == 0) hi[0] = u32x4{hi[0][0], hi[0][1], lo[0][0], lo[0][1]};
             } else {
                 hi[b] = j.halves[adapter_half_at(group, rp, k0 / 32 + b, 0) + lane];
                 if constexpr (KB != 0) lo[b] = j.halves[adapter_half_at(group, rp, k0 / 32 + b, 1) + lane];
@@ -696,13 +721,26 @@ __device__ __forceinline__ void adapter_expand_tile(const AdapterExpand& j, cons
         __syncthreads();
         if (live) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int u = 0; u < 8; ++u) {
+                const u32x4* row = lds + (u * 16 + i) * PITCH;
+                f32x4 left{0.f, 0.f, 0.f, 0.f};
+                if constexpr (KB == 0) {
+                    const uint2 w = reinterpret_cast<const uint2*>(row)[q];
+                    left = adapter_finite(adapter_mfma16(uint2{hi[0][2], hi[0][3]}, w, left));
+                    acc[u] = adapter_mfma16(uint2{hi[0][0], hi[0][1]}, w, left);
+                } else {
+                    u32x4 w[NB];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const u32x4 w = lds[(u * 16 + i) * PITCH + (KB == 0 ? q & 1 : 4 * b + q)];
-                    acc[u] = adapter_mfma(hi[b], w, acc[u]);
-                    if constexpr (KB != 0) acc[u] = adapter_mfma(lo[b], w, acc[u]);
+                    for (int b = 0; b < NB; ++b) {
+                        w[b] = row[4 * b + q];
+                        left = adapter_mfma(lo[b], w[b], left);
+                    }
+                    left = adapter_finite(left);
+                    acc[u] = ONE ? left : acc[u] + left;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) acc[u] = adapter_mfma(hi[b], w[b], acc[u]);
                 }
+            }
         }
         if constexpr (ONE) break;
         k0 += 8 * CH;
@@ -844,9 +882,10 @@ __global__ __launch_bounds__(kAdGradThreads) void adapter_grads(AdapterGrads j0,
 #pragma unroll
             for (int e = 0; e < 4; ++e) turned[e] = adapter_pair(x[2 * e][k / 2], x[2 * e + 1][k / 2], k & 1);
 #pragma unroll
-            for (int u = 0; u < 3; ++u)
-#pragma unroll
-                for (int b = 0; b < JB; ++b) acc[k][b] = adapter_mfma(turned, t[u][b], acc[k][b]);
+            for (int b = 0; b < JB; ++b) {
+                const f32x4 left = adapter_mfma(turned, t[1][b], adapter_mfma(turned, t[2][b], f32x4{0.f, 0.f, 0.f, 0.f}));
+                acc[k][b] = adapter_mfma(turned, t[0][b], acc[k][b]) + adapter_finite(left);
+            }
         }
     }
     if (piece.tiles > 0) {  // the same for all

@@ -419,3 +419,31 @@ def test_a_plan_of_other_numbers_writes_nothing():
         pifa.adapter_backward(c.x_dev, c.a_dev, c.b_dev, other, c.dy_dev, dX0=c.dx0_dev, dX=outs[1], dA=outs[2], dB=outs[3])
         torch.cuda.synchronize()
         assert all(bool((t == 7).all()) for t in outs)
+
+
+@pytest.mark.parametrize("M,d_in,d_out", [(100, 136, 264), (300, 263, 130), (1100, 5, 131)])
+@pytest.mark.parametrize("r", [1, 5, 16, 17, 32, 40, 64, 100, 130])
+def test_infinite_operands(M, d_in, d_out, r):
+    """One infinity in each operand in turn: results that the formula makes infinite
+    have its sign, those that it makes no number are none, the others keep their
+    bounds.  (A few t are as close to zero as they are off, far fewer than are met here.)"""
+    c = Case(M, d_in, d_out, r, 2, "mixed", seed=14)
+    s = c.s.astype(np.float64)
+    row = int(np.flatnonzero(c.ids == 1)[3])
+    for name, at in (("x", (row, d_in - 2)), ("dy", (row, d_out - 1)), ("a", (1, r - 1, 2)), ("b", (1, d_out - 2, r // 2))):
+        for value in (np.inf, -np.inf):
+            host, there = getattr(c, name), getattr(c, name + "_dev")
+            kept = host[at]
+            host[at] = there[at] = value
+            with np.errstate(invalid="ignore"):
+                want = [c._f(c.x, c.a, c.b, c.y0, s), *o.adapter_backward(c.x, c.a, c.b, c.ids, c.dy, s, c.dx0)]
+                size = [c._f(*map(np.abs, (c.x, c.a, c.b, c.y0)), s),
+                        *o.adapter_backward(*map(np.abs, (c.x, c.a, c.b)), c.ids, np.abs(c.dy), s, np.abs(c.dx0))]
+            got = [from_dev(t) for t in (c.forward(Y0=c.y0_dev), *c.backward(dX0=c.dx0_dev))]
+            host[at] = there[at] = kept
+            assert not all(np.isfinite(w).all() for w in want)
+            for g, w, z, half, what in zip(got, want, size, (HALF, HALF, 0, 0), ("Y", "dX", "dA", "dB")):
+                finite, what = np.isfinite(w), (what, name, value)
+                assert np.array_equal(g[~finite], w[~finite], equal_nan=True), what
+                off = np.abs(g[finite] - w[finite]) - (half * np.abs(w[finite]) + 4 * FP * z[finite] + 1e-30)
+                assert np.isfinite(g[finite]).all() and (off <= 0).all(), what
