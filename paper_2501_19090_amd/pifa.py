@@ -1223,24 +1223,26 @@ class AdapterPlan:
 class AdamW:
     """Owns an AdamW handle and the tensors it points to.  Without states they are
     zeros, in 8 bits with bits=8; ``states`` holds them, (m, v) or (m, v, m_scale,
-    v_scale) a tensor."""
+    v_scale) a tensor, and has to be of the ``bits`` that are asked for, if any are."""
 
-    def __init__(self, params, grads, weight_decay=0.0, bits: int = 32, copies=None, states=None, seed: int = 0):
+    def __init__(self, params, grads, weight_decay=0.0, bits: int | None = None, copies=None, states=None, seed: int = 0):
         rt = _rt()
         self.handle = 0
+        if bits not in (None, 8, 32):
+            raise ValueError("bits is %r: 8 or 32" % (bits,))
         self.params, self.grads = list(params), list(grads)
         self.copies = None if copies is None else list(copies)
         if states is None:
-            if bits not in (8, 32):
-                raise ValueError("bits is %r: 8 or 32" % (bits,))
             zeros = lambda p, dtype, n: rt.zeros(n, dtype=dtype, device=p.device)
-            if bits == 32:
+            if bits != 8:
                 states = [(rt.zeros(p.shape, dtype=rt.f32, device=p.device), rt.zeros(p.shape, dtype=rt.f32, device=p.device))
                           for p in self.params]
             else:
                 states = [tuple(rt.zeros(p.shape, dtype=rt.u8, device=p.device).view(rt.e4m3) for _ in range(2)) +
                           tuple(zeros(p, rt.u8, -(-p.numel() // 32)) for _ in range(2)) for p in self.params]
         self.states = [tuple(s) for s in states]
+        if bits and any(len(s) != (4 if bits == 8 else 2) for s in self.states):
+            raise ValueError("states are not those of %d bits" % bits)
         self.handle = adamw_create(self.params, self.grads, self.states, weight_decay, self.copies, seed)
 
     def step(self, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 0,

@@ -305,6 +305,22 @@ def test_adamw_tensors(binding):
     opt.handle = 0
 
 
+def test_states_of_other_bits_are_refused(binding):
+    torch, calls = binding
+    f = lambda: torch.zeros(40)
+    e = lambda: torch.zeros(40, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    u = lambda: torch.zeros(2, dtype=torch.uint8)
+    full, eight = [(f(), f())], [(e(), e(), u(), u())]
+    for bits, states in ((8, full), (32, eight), (16, full), (16, eight), (0, full), (16, None)):
+        with pytest.raises(ValueError):
+            pifa.AdamW([f()], [f()], bits=bits, states=states)
+    assert not calls
+    for bits, states, want in ((None, full, 32), (32, full, 32), (None, eight, 8), (8, eight, 8), (None, None, 32), (8, None, 8)):
+        opt = pifa.AdamW([f()], [f()], bits=bits, states=states)
+        assert calls[-1][0] == "adamw_create" and calls[-1][1][2] == want
+        opt.handle = 0
+
+
 def test_streams_of_another_device_are_refused(binding):
     torch, calls = binding
 
