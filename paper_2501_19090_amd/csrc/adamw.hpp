@@ -142,6 +142,11 @@ __device__ __forceinline__ uint32_t adamw_pack(const float (&x)[4], float top, c
         else c |= __builtin_bit_cast(uint32_t, x[e]) >> 24 & 0x80u;
         out |= c << (8 * e);
     }
+    if (LEAST && k > 9) {  // the units are so large that an a may have vanished
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (x[e] > 0.f && (out >> (8 * e) & 0xFF) == 0) out |= 1u << (8 * e);
+    }
     return bad ? 0x7F7F7F7Fu : out;
 }
 

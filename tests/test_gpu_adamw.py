@@ -317,3 +317,19 @@ def test_infinite_parameters_stay_infinite():
             opt.step(1e-3)
             torch.cuda.synchronize()
         assert p[:2].tolist() == [inf, -inf] and abs(float(p[2]) - (1 - 1e-3 * (1 + decay))) <= 2.0 ** -22
+
+
+def test_a_second_moment_above_zero_stays_above_zero():
+    """Beside one that is 2^220 times larger it is less than fp32 holds of the group's units."""
+    pifa, torch = _pifa(), torch_mod()
+    n = 64
+    p, g = torch.ones(n, device="cuda"), torch.full((n,), 1e-15, device="cuda")
+    g[3], g[40:] = 1e18, 0.0
+    with pifa.AdamW([p], [g], bits=8, seed=5) as opt:
+        opt.step(1e-3, 0.9, 0.999, 1e-8, step=2)
+        torch.cuda.synchronize()
+        _, v = o.adamw_moments(g.cpu().numpy(), np.zeros(n, np.float32), np.zeros(n, np.float32), 0.9, 0.999)
+        codes, scales = o.e4m3_round(v, o.random_bits(5, 2, 0, n)[1], 1)
+        have = opt.states[0][1].view(torch.uint8).cpu().numpy()
+        assert np.array_equal(have, codes) and np.array_equal(opt.states[0][3].cpu().numpy(), scales)
+        assert (have[:40] > 0).all() and (have[40:] == 0).all() and have[4] == 1
