@@ -615,8 +615,11 @@ typedef struct adamw_state* adamw_handle;
  *   mix(x): x = (x ^ x >> 16) 0x6A09E667, x = (x ^ x >> 15) 0xBB67AE85, x ^ x >> 16   (32 bits),
  * the upper 16 for m, the lower for v, i a value's index in its tensor; to the
  * nearest they would not move at all where a step changes them by less than half a
- * unit.  A v above zero becomes the smallest value at least.  The update takes m
- * and v before they are rounded.
+ * unit.  A v above zero becomes the smallest value at least.  So moments are right
+ * on average, with a deviation of about 0.2 of v, where v is not below some units
+ * of its group (a unit is 2^-17 to 2^-18 of the group's largest v); smaller ones stay
+ * at about a unit, which makes their steps too small.  The update takes m and v
+ * before they are rounded.
  */
 pifa_status adamw_create(const adamw_tensor* tensors, int64_t count, int state_bits, pifa_dtype g_dtype,
                          uint32_t seed, adamw_handle* out);

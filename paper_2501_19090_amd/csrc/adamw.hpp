@@ -15,8 +15,13 @@
 // chance instead, up with the probability of what is left over the lower
 // neighbour, which keeps the moment right on average: a step spreads v by about
 // (0.09 (1 - b2))^1/2 of it, and over its memory of 1 / (1 - b2) steps that comes to
-// a deviation of 0.2 v, 0.1 of its root.  The update takes m and v before they
-// are rounded; a v below fp32's normal range counts as zero in it.
+// a deviation of 0.2 v, 0.1 of its root.  That holds for a v of some units or more (a
+// unit: the smallest code of its group, 2^-17 to 2^-18 of the largest v in it).  One
+// of 1.3 units is 15% too large on average, and one below a unit stays at about a
+// unit, because above zero it gets the smallest code at least: a value whose gradients
+// are 5000 times smaller than its group's largest moves by about a tenth of
+// what it should for as long as that one is there.  The update takes m and v before
+// they are rounded; a v below fp32's normal range counts as zero in it.
 #pragma once
 
 #include "common.hpp"

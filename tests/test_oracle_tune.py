@@ -129,3 +129,30 @@ def test_moments_in_8_bits_follow_those_in_64(beta2):
     ratio = o.e4m3_values(codes, scales) / v64
     # deviation 0.2 of v by element; the mean over 2048 of them, 8 deviations of it
     assert abs(ratio.mean() - 1) < 8 * 0.25 / np.sqrt(n) + 0.02 and ratio.std() < 0.4 and ratio.min() > 0.1
+
+
+@pytest.mark.parametrize("beta2,steps", [(0.95, 400), (0.999, 3000)])
+def test_small_second_moments_in_a_group_with_a_large_one(beta2, steps):
+    """v of 1e-2 to 1e-4 of its group's largest is right on average; from about a unit
+    of the group (the smallest code) down it stays at one."""
+    rng = np.random.default_rng(9)
+    groups, share = 128, np.array([1e-2, 1e-3, 1e-4, 1e-6, 1e-8])
+    kind = np.tile(np.concatenate([[-1], np.arange(30) % 5, [-1]]), groups)
+    size = np.where(kind < 0, 1.0, np.sqrt(share[kind]))
+    n = size.size
+    codes, scales, v64 = np.zeros(n, np.uint8), np.zeros(groups, np.uint8), np.zeros(n)
+    got, want, units = np.zeros(n), np.zeros(n), np.zeros(n)
+    for t in range(1, steps + 1):
+        g = rng.standard_normal(n) * size
+        v64 = beta2 * v64 + (1 - beta2) * g * g
+        v = np.float32(beta2) * o.e4m3_values(codes, scales) + np.float32(1 - beta2) * np.float32(g * g)
+        codes, scales = o.e4m3_round(v, o.random_bits(1, t, 0, n)[1], 1)
+        if 2 * t > steps:
+            have = o.e4m3_values(codes, scales).astype(np.float64)
+            got, want = got + have, want + v64
+            units += have / 2.0 ** (np.repeat(scales.astype(float), 32) - 127 - 9) / (steps - steps // 2)
+    for k in range(3):  # 768 values, deviation 0.2 each: six of the mean's
+        assert abs(got[kind == k].sum() / want[kind == k].sum() - 1) < 6 * 0.2 / np.sqrt(768), share[k]
+    for k in (3, 4):
+        assert (units[kind == k] >= 1).all() and units[kind == k].mean() < 2, share[k]
+        assert got[kind == k].sum() > 3 * want[kind == k].sum()
