@@ -447,3 +447,32 @@ def test_infinite_operands(M, d_in, d_out, r):
                 assert np.array_equal(g[~finite], w[~finite], equal_nan=True), what
                 off = np.abs(g[finite] - w[finite]) - (half * np.abs(w[finite]) + 4 * FP * z[finite] + 1e-30)
                 assert np.isfinite(g[finite]).all() and (off <= 0).all(), what
+
+
+@pytest.mark.parametrize("shape", [
+    (130, 100, 9000, 1024, 2, "mixed"), (600, 12001, 64, 300, 1, "one"), (33, 20000, 30001, 201, 2, "mixed"),
+    (20, 1 << 19, 40, 5, 2, "mixed"), (70, 33, 1 << 19, 6, 3, "mixed"), (9, 9001, 1001, 1023, 1, "one"), (9, (1 << 19) - 1, 101, 17, 1, "one"),
+    (257, 72, 40, 65, 4096, "mixed")])
+def test_the_largest_ranks_and_widths(shape):
+    """Up to the limits.  A product's way through a sum over K of d columns: 32 additions
+    in its instruction, one instruction a wave for each 32 * 4 * 8 columns where K is
+    cut into 8 parts (32 * 4 where it is not), 4 waves, 8 parts; over ranks, 32 and two
+    for each 32.  Where that passes 128 the bounds grow with it."""
+    c = Case(*shape, seed=15)
+    M, d_in, d_out, r, n, _ = shape
+    tiles = sum(-(-int((c.ids == a).sum()) // 64) for a in range(n))
+    target = (3 if r <= 16 else 2) * 256 // (2 * -(-r // 64))  # of a launch of two jobs; the forward cuts as much or more
+    split = max(1, min(8, target // tiles))
+    steps = max(44 + max(d_in, d_out) // (128 * split), 32 + 2 * -(-r // 32))
+    more = max(1.0, steps / 128)
+
+    def close(got, want, size, half, what):
+        _close(from_dev(got), want, half * np.abs(want) + 4 * FP * more * size + 1e-30, what)
+
+    s, abs_of = c.s.astype(np.float64), [np.abs(v) for v in (c.x, c.a, c.b)]
+    Y = c.forward(Y0=c.y0_dev)
+    close(Y, c._f(c.x, c.a, c.b, c.y0, s), c._f(*abs_of, np.abs(c.y0), s), HALF, "Y")
+    want = o.adapter_backward(c.x, c.a, c.b, c.ids, c.dy, s, c.dx0)
+    size = o.adapter_backward(*abs_of, c.ids, np.abs(c.dy), s, np.abs(c.dx0))
+    for got, w, z, half, what in zip(c.backward(dX0=c.dx0_dev), want, size, (HALF, 0, 0), ("dX", "dA", "dB")):
+        close(got, w, z, half, what)
