@@ -566,34 +566,4 @@ __global__ __launch_bounds__(kNormThreads) void layer_norm_bwd_long(LayerNormBwd
     }
 }
 
-// dgain and dbias (either may be null) from P <= 256 partial rows of 2 d, in a
-// fixed order: a workgroup of 16 x 64 threads takes 64 columns; a thread's loads
-// are all in flight.
-static __global__ __launch_bounds__(kNormThreads) void layer_norm_sums(const float* __restrict__ part, int P, int64_t d,
-                                                                      float* __restrict__ dgain,
-                                                                      float* __restrict__ dbias) {
-    constexpr int SLICES = kNormThreads / kWave, EACH = kNormMaxGroups / SLICES;
-    __shared__ float red[kNormThreads];
-    const int64_t k = (int64_t)blockIdx.x * kWave + (threadIdx.x & (kWave - 1));
-    float* out = blockIdx.y ? dbias : dgain;
-    if (!out) return;
-    const float* from = part + blockIdx.y * d;
-    const int slice = threadIdx.x / kWave;
-    float v[EACH], s = 0.f;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int q = slice + i * SLICES;
-        v[i] = from[(int64_t)(q < P ? q : 0) * 2 * d + (k < d ? k : 0)];
-    }
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) s += slice + i * SLICES < P ? v[i] : 0.f;
-    red[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x < kWave && k < d) {
-#pragma unroll
-        for (int w = 1; w < SLICES; ++w) s += red[w * kWave + threadIdx.x];
-        out[k] = s;
-    }
-}
-
 }  // namespace pifa

@@ -588,19 +588,26 @@ __global__ __launch_bounds__(kNormThreads) void norm_bwd_long(NormBwd<T> p) {
 }
 
 // dgain = the sum of P <= 256 partial rows of d, in a fixed order: a workgroup
-// of 16 x 64 threads takes 64 columns; a thread's loads are all in flight.
+// of 16 x 64 threads takes 64 columns; a thread's loads are all in flight.  A second
+// row of workgroups (grid y) sums dbias, whose partial rows lie between those of dgain;
+// either may be null then.
 constexpr int kNormMaxGroups = 256;
-[[maybe_unused]] static __global__ __launch_bounds__(kNormThreads) void norm_dgain(const float* __restrict__ part, int P, int64_t d,
-                                                          float* __restrict__ dgain) {
+static __global__ __launch_bounds__(kNormThreads) void norm_dgain(const float* __restrict__ part, int P, int64_t d,
+                                                                 float* __restrict__ dgain,
+                                                                 float* __restrict__ dbias) {
     constexpr int SLICES = kNormThreads / kWave, EACH = kNormMaxGroups / SLICES;
     __shared__ float red[kNormThreads];
     const int64_t k = (int64_t)blockIdx.x * kWave + (threadIdx.x & (kWave - 1));
+    float* out = blockIdx.y ? dbias : dgain;
+    if (!out) return;
+    const float* from = part + blockIdx.y * d;
+    const int64_t stride = gridDim.y * d;
     const int slice = threadIdx.x / kWave;
     float v[EACH], s = 0.f;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int q = slice + i * SLICES;
-        v[i] = part[(int64_t)(q < P ? q : 0) * d + (k < d ? k : 0)];
+        v[i] = from[(q < P ? q : 0) * stride + (k < d ? k : 0)];
     }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) s += slice + i * SLICES < P ? v[i] : 0.f;
@@ -609,7 +616,7 @@ constexpr int kNormMaxGroups = 256;
     if (threadIdx.x < kWave && k < d) {
 #pragma unroll
         for (int w = 1; w < SLICES; ++w) s += red[w * kWave + threadIdx.x];
-        dgain[k] = s;
+        out[k] = s;
     }
 }
 

@@ -2190,7 +2190,7 @@ pifa_status norm_backward_run(const void* H, const void* gain, const void* dY, c
     if (dgain && groups > 1) {
         TimedLaunch timed(kSiteNormDgain, st);
         hipLaunchKernelGGL(norm_dgain, dim3((unsigned)ceil_div(d, kWave)), dim3(kNormThreads), 0, st, work, (int)groups,
-                           d, dgain);
+                           d, dgain, (float*)nullptr);
         if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
     }
     return PIFA_OK;

@@ -100,7 +100,7 @@ pifa_status layer_norm_backward_run(const void* H, const void* gain, const void*
     }
     if (sums) {
         TimedLaunch timed(kSiteLayerNormSums, st);
-        hipLaunchKernelGGL(layer_norm_sums, dim3((unsigned)ceil_div(d, kWave), 2), dim3(kNormThreads), 0, st, work,
+        hipLaunchKernelGGL(norm_dgain, dim3((unsigned)ceil_div(d, kWave), 2), dim3(kNormThreads), 0, st, work,
                            (int)groups, d, dgain, dbias);
         if (hipGetLastError() != hipSuccess) return PIFA_ERR_HIP;
     }
