@@ -153,7 +153,10 @@ __device__ __forceinline__ int adapter_find(const int* v, int len, int x) {
     return lo;
 }
 
-// Bound by its own steps, not by its few bytes: 8 to 14 us, once a batch.
+// Once a batch.  Bound by its own steps, scans of n + 1 places and their barriers:
+// 48 rows 8 us, 4096 rows 13.  Every block adds up the counts of all blocks, which
+// grows with their number squared and with n: both launches of 65536 rows of 16
+// adapters take 27 us, of 2^20 rows 450; of 4096 adapters 125 and 4600.
 // A block of 1024 rows goes to its places: those of its adapter in the blocks
 // before it, then those in the waves before, then in the lanes before.  Block 0
 // also writes the header and the lists.

@@ -80,7 +80,7 @@ struct LayerNormFwd {
 };
 
 // ROWS rows of at most TPR * V full chunks per workgroup.  4096 x 8192 bf16 with the
-// residual 49.6 us, 5.4 TB/s.
+// residual 50.1 us, 5.4 TB/s.
 template <typename T, int TPR, int V, int ROWS>
 __global__ __launch_bounds__(TPR* ROWS) void layer_norm_fwd(LayerNormFwd<T> p) {
     using C = NormChunk<T>;
@@ -271,8 +271,8 @@ __device__ __forceinline__ float layer_norm_back(float rho, float uc, float d) {
 // gridDim.x, and keeps the sums of dgain and dbias for the columns its threads
 // hold in registers over all of them; at the end the ROWS sums of a column are
 // added in LDS, so that only gridDim.x partial sums a column go to memory.
-// 4096 x 4096 bf16 28.6 us (4.7 TB/s) and 4.6 for the partial sums; 333 x 2867 fp32,
-// one or two rows a CU, 8.9 and 3.7: a row's loads and two reductions one after the
+// 4096 x 4096 bf16 27.9 us (4.8 TB/s) and 4.6 for the partial sums; 333 x 2867 fp32,
+// one or two rows a CU, 8.2 and 3.5: a row's loads and two reductions one after the
 // other.
 // EXACT: rows are TPR * V full chunks and have a residual gradient and a dX, so
 // that no load or store stands under a condition.  With four chunks a thread (fp32

@@ -134,7 +134,12 @@ bool aligned(std::initializer_list<const void*> p, uintptr_t to) {
     return true;
 }
 
-// Up to as many rows t stays in parts, which expand adds up itself.
+// Up to as many rows t stays in parts, which each workgroup of expand adds up itself,
+// without finish between.  us of 4096 -> 12288 so, and with finish: 16 rows of rank 16
+// 7.5 and 9.2, of rank 64 11.3 and 11.3, of rank 128 14.7 and 13.2; 256 rows 10.4 and
+// 12.0, 20.7 and 17.0, 35.9 and 20.6; 512 rows of rank 16 13.5 and 14.7, of rank 64
+// 31.5 and 20.3.  So the rows alone decide well up to rank 32, and cost up to 1.8 times
+// the call above.
 constexpr int64_t kAdFewRows = 256;
 
 // Bytes of t (or u): at most 8 parts of K of every tile, and where K is cut at all,
